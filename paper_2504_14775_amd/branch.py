@@ -1,0 +1,179 @@
+"""ctypes binding of the operators for several continuations of one sequence (include/gllm_branch.h): checks of the tensors
+and argument marshalling only.  Every tensor lies on the current GPU; what a call refuses raises GllmError."""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import numpy as np
+
+from .binding import GLLM_OK, GllmError, _stream_ptr, load_library
+
+EXPORTS = [
+    "gllm_op_tree_attention", "gllm_op_tree_attention_workspace_bytes", "gllm_op_tree_commit", "gllm_op_beam_select",
+    "gllm_op_beam_select_workspace_bytes", "gllm_op_copy_pages",
+]
+PAGE = 16
+_INVALID = -1
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        lib = load_library()
+        i32, i64, vp, sz = C.c_int32, C.c_int64, C.c_void_p, C.c_size_t
+        lib.gllm_op_tree_attention.restype = i32
+        lib.gllm_op_tree_attention.argtypes = [vp, i64, vp, vp, i64, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, i32, C.c_float, vp, i64,
+                                               vp, sz, vp]
+        lib.gllm_op_tree_attention_workspace_bytes.restype = sz
+        lib.gllm_op_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        lib.gllm_op_tree_commit.restype = i32
+        lib.gllm_op_tree_commit.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, i32, i64, i32, i32, vp, vp, vp, vp]
+        lib.gllm_op_beam_select.restype = i32
+        lib.gllm_op_beam_select.argtypes = [vp, i64, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        lib.gllm_op_beam_select_workspace_bytes.restype = sz
+        lib.gllm_op_beam_select_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        lib.gllm_op_copy_pages.restype = i32
+        lib.gllm_op_copy_pages.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, i32, vp]
+        _ready = lib
+    return _ready
+
+
+def _refuse(what: str):
+    raise GllmError(_INVALID, what)
+
+
+def _check(call: str, dtype, tensors, rows_only: bool = False) -> None:
+    """tensors: of this type, on the current GPU, contiguous (rows_only: inside a row)."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t.get_device() != dev or t.dtype is not dtype:
+            _refuse(f"{call}: a tensor of {dtype} on the current GPU is wanted, got {t.dtype} on {t.device}")
+        if not (t.dim() == 2 and t.stride(1) == 1 if rows_only else t.is_contiguous()):
+            _refuse(f"{call}: a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not contiguous")
+
+
+def _own_workspace(call: str, size: int, like, stream):
+    """A workspace from torch's allocator, which may give it to somebody else on the call's stream only."""
+    import torch
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=like.device)
+    if isinstance(stream, int):
+        _refuse(f"{call}: a stream given by its handle needs a workspace of the caller's")
+    with torch.cuda.stream(stream):
+        return torch.empty(size, dtype=torch.uint8, device=like.device)
+
+
+def _row_stride(t) -> int:
+    """The row stride of a 2-d tensor (torch gives a tensor of one row any)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _pool_shape(call: str, k_pool, v_pool, dims: int):
+    """(KV heads, head size) of pools [.., n_kv, d/8, 16, 8] and [.., n_kv, d, 16] with `dims` dimensions in front."""
+    k, v = k_pool.shape, v_pool.shape
+    if len(k) != dims + 4 or len(v) != dims + 3 or k[:dims + 1] != v[:dims + 1] or k[-1] != 8 or k[-2] != PAGE or v[-1] != PAGE or v[-2] != 8 * k[-3]:
+        _refuse(f"{call}: pools of shapes {tuple(k)} and {tuple(v)}")
+    return k[dims], v[-2]
+
+
+def gllm_op_tree_attention_workspace_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int, max_nodes: int) -> int:
+    return int(_lib().gllm_op_tree_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, max_nodes))
+
+
+def gllm_op_tree_attention(q, k_pool, v_pool, block_tables, cached_len, row_start, parents, out, max_nodes: int, scale=None,
+                           workspace=None, stream=None) -> None:
+    """q, out: bf16 [R, n_q*d]; k_pool: bf16 [pages, n_kv, d/8, 16, 8], v_pool: bf16 [pages, n_kv, d, 16], one layer; block_tables:
+    int32 [S, entries]; cached_len: int32 [S]; row_start: int32 [S+1]; parents: int32 [R].  scale: 1/sqrt(d) if not given;
+    workspace: uint8, taken from torch's allocator if not given."""
+    import torch
+    call = "gllm_op_tree_attention"
+    n_kv, d = _pool_shape(call, k_pool, v_pool, 1)
+    _check(call, torch.bfloat16, (q, out), rows_only=True)
+    _check(call, torch.bfloat16, (k_pool, v_pool))
+    _check(call, torch.int32, (block_tables, cached_len, row_start, parents))
+    rows, seqs = q.shape[0], cached_len.shape[0]
+    if q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1 or parents.numel() != rows:
+        _refuse(f"{call}: shapes q {tuple(q.shape)}, out {tuple(out.shape)}, block_tables {tuple(block_tables.shape)}, cached_len {tuple(cached_len.shape)}, "
+                f"row_start {tuple(row_start.shape)}, parents {tuple(parents.shape)}")
+    n_q = q.shape[1] // d
+    lib = _lib()
+    if workspace is None:
+        workspace = _own_workspace(call, int(lib.gllm_op_tree_attention_workspace_bytes(n_q, n_kv, d, max_nodes)), q, stream)
+    _check(call, torch.uint8, (workspace,))
+    st = lib.gllm_op_tree_attention(q.data_ptr(), _row_stride(q), k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], block_tables.data_ptr(),
+                                    block_tables.shape[1], cached_len.data_ptr(), row_start.data_ptr(), parents.data_ptr(), seqs, rows,
+                                    max_nodes, n_q, n_kv, d, 1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(), _row_stride(out),
+                                    workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if st != GLLM_OK:
+        raise GllmError(st, call)
+
+
+def gllm_op_tree_commit(tokens, parents, sampled, row_start, cached_len, block_tables, k_pool, v_pool, path, count, next_token,
+                        stream=None) -> None:
+    """tokens, parents, sampled, path: int32 [R]; row_start: int32 [S+1]; cached_len, count, next_token: int32 [S]; block_tables: int32
+    [S, entries]; k_pool: bf16 [layers, pages, n_kv, d/8, 16, 8], v_pool: bf16 [layers, pages, n_kv, d, 16], or both None (no moves)."""
+    import torch
+    call = "gllm_op_tree_commit"
+    _check(call, torch.int32, (tokens, parents, sampled, path, row_start, cached_len, block_tables, count, next_token))
+    rows, seqs = tokens.numel(), cached_len.numel()
+    if parents.numel() != rows or sampled.numel() != rows or path.numel() != rows or row_start.numel() != seqs + 1 or block_tables.dim() != 2 or \
+            block_tables.shape[0] != seqs or count.numel() != seqs or next_token.numel() != seqs or (k_pool is None) != (v_pool is None):
+        _refuse(f"{call}: arrays of {rows} rows and {seqs} sequences do not fit each other")
+    layers = pages = n_kv = d = 0
+    if k_pool is not None:
+        n_kv, d = _pool_shape(call, k_pool, v_pool, 2)
+        _check(call, torch.bfloat16, (k_pool, v_pool))
+        layers, pages = k_pool.shape[:2]
+    st = _lib().gllm_op_tree_commit(tokens.data_ptr(), parents.data_ptr(), sampled.data_ptr(), row_start.data_ptr(), cached_len.data_ptr(),
+                                    block_tables.data_ptr(), block_tables.shape[1], seqs, rows, None if k_pool is None else k_pool.data_ptr(),
+                                    None if v_pool is None else v_pool.data_ptr(), layers, pages, n_kv, d, path.data_ptr(), count.data_ptr(),
+                                    next_token.data_ptr(), _stream_ptr(stream))
+    if st != GLLM_OK:
+        raise GllmError(st, call)
+
+
+def gllm_op_beam_select_workspace_bytes(num_seqs: int, beams: int, vocab: int, keep: int) -> int:
+    return int(_lib().gllm_op_beam_select_workspace_bytes(num_seqs, beams, vocab, keep))
+
+
+def gllm_op_beam_select(logits, vocab: int, scores, out_scores, out_beams, out_tokens, workspace=None, stream=None) -> None:
+    """logits: fp32 [S*W, >= vocab] (row stride taken from the tensor); scores: fp32 [S, W]; out_scores: fp32, out_beams, out_tokens:
+    int32, [S, keep]; workspace: uint8, taken from torch's allocator if not given."""
+    import torch
+    call = "gllm_op_beam_select"
+    _check(call, torch.float32, (logits,), rows_only=True)
+    _check(call, torch.float32, (scores, out_scores))
+    _check(call, torch.int32, (out_beams, out_tokens))
+    if scores.dim() != 2 or out_scores.dim() != 2 or logits.shape[0] != scores.numel() or logits.shape[1] < vocab or out_scores.shape[0] != scores.shape[0] or \
+            out_beams.shape != out_scores.shape or out_tokens.shape != out_scores.shape:
+        _refuse(f"{call}: shapes logits {tuple(logits.shape)}, scores {tuple(scores.shape)}, outputs {tuple(out_scores.shape)}, "
+                f"{tuple(out_beams.shape)}, {tuple(out_tokens.shape)}, vocabulary {vocab}")
+    lib = _lib()
+    seqs, beams, keep = scores.shape[0], scores.shape[1], out_scores.shape[1]
+    if workspace is None:
+        workspace = _own_workspace(call, int(lib.gllm_op_beam_select_workspace_bytes(seqs, beams, vocab, keep)), logits, stream)
+    _check(call, torch.uint8, (workspace,))
+    st = lib.gllm_op_beam_select(logits.data_ptr(), _row_stride(logits), scores.data_ptr(), seqs, beams, vocab, keep, out_scores.data_ptr(),
+                                 out_beams.data_ptr(), out_tokens.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if st != GLLM_OK:
+        raise GllmError(st, call)
+
+
+def gllm_op_copy_pages(k_pool, v_pool, src, dst, stream=None) -> None:
+    """k_pool: bf16 [layers, pages, n_kv, d/8, 16, 8], v_pool: bf16 [layers, pages, n_kv, d, 16]; src, dst: page ids on the host."""
+    import torch
+    call = "gllm_op_copy_pages"
+    n_kv, d = _pool_shape(call, k_pool, v_pool, 2)
+    _check(call, torch.bfloat16, (k_pool, v_pool))
+    s = np.ascontiguousarray(src, dtype=np.int32)
+    t = np.ascontiguousarray(dst, dtype=np.int32)
+    if s.ndim != 1 or s.shape != t.shape:
+        _refuse(f"{call}: {s.shape} sources, {t.shape} destinations")
+    st = _lib().gllm_op_copy_pages(k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pool.shape[1], n_kv, d, s.ctypes.data, t.ctypes.data,
+                                   s.shape[0], _stream_ptr(stream))
+    if st != GLLM_OK:
+        raise GllmError(st, call)

@@ -206,6 +206,30 @@ hipError_t launch_prefill_attention(const AttnArgs& a, const PrefillItem* items,
 bool attention_in_one_launch(int n_q, int n_kv, int64_t num_tiles, bool half, int num_decode_rows);
 hipError_t launch_hybrid_attention(const AttnArgs& a, const PrefillItem* items, int num_items, bool half, const DecodeArgs& dec, hipStream_t stream);
 
+// Trees of drafted tokens (see kernels_tree.hip): device arrays, nothing of which the host reads.
+struct TreeArgs {
+    const bf16_t* q;             // [num_rows][ld_q]
+    int64_t ld_q;
+    const bf16_t* k_pool;        // this layer
+    const bf16_t* v_pool;
+    int32_t num_blocks;
+    const int32_t* block_tables; // sequence s: table_stride ids from s * table_stride, or from bt_off[s]
+    int32_t table_stride;        // most pages of a sequence
+    const int32_t* bt_off;       // or null
+    const int32_t* cached_len;   // [num_seqs]
+    const int32_t* row_begin;    // [num_seqs] the rows of each sequence
+    const int32_t* row_end;
+    const int32_t* parents;      // [num_rows], indices within the sequence
+    int32_t num_seqs, num_rows, max_nodes;
+    bf16_t* out;                 // [num_rows][ld_o]
+    int64_t ld_o;
+    int32_t n_q, n_kv, d;
+    float scale_log2;            // scale * log2(e)
+    void* workspace;             // tree_workspace_bytes()
+};
+size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes);
+hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream);
+
 // Ceiling probes (see kernels_peak.hip).  peak_mfma: workgroups x 4 waves x iters x 16 MFMAs of
 // 2*32*32*16 flop each.  peak_read: reads `bytes` once.
 hipError_t launch_peak_mfma(float* sink, int workgroups, int iters, hipStream_t stream);

@@ -1,0 +1,597 @@
+// Several continuations of one sequence: entry points of include/gllm_branch.h, and the kernels of all of them but tree attention
+// (kernels_tree.hip).
+#include "../../include/gllm_branch.h"
+#include "common.h"
+
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+namespace {
+
+static_assert(GLLM_TREE_MAX_NODES == 256, "a thread per node");
+
+// ---- acceptance and the move of accepted keys and values ---------------------------------------------------------------
+
+struct CommitArgs {
+    const int32_t *tokens, *parents, *sampled, *row_start, *cached_len, *block_tables;
+    int32_t table_stride, num_seqs, num_rows;
+    bf16_t *k_pool, *v_pool;
+    int32_t num_layers, num_blocks, n_kv;
+    int32_t *path, *count, *next_token;
+};
+
+// One workgroup per (sequence, layer, KV head); each of them walks the tree itself (a few steps of one wave over at most 256 nodes in
+// registers), so that one launch does both; the sequence's first one writes the result of the walk.
+// The moves of a (layer, head) are made in order of the path, kMoves at a time, all read before the first is written: position
+// i takes what stands at path[i] >= i, so that no slot is written before it has been read.
+constexpr int kMoves = 16;
+template <int D>
+__global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
+    __shared__ int32_t drawn[GLLM_TREE_MAX_NODES], path[GLLM_TREE_MAX_NODES];
+    __shared__ int accepted, last_drawn;
+    const int per_seq = max(1, a.num_layers * a.n_kv);
+    const int s = blockIdx.x / per_seq, part = blockIdx.x % per_seq, t = threadIdx.x;
+    const int r0 = a.row_start[s], r1 = a.row_start[s + 1], c = a.cached_len[s];
+    const bool rows_ok = r0 >= 0 && r1 >= r0 && r1 <= a.num_rows;
+    const int n = rows_ok ? r1 - r0 : 0;
+    const bool fits = n > 0 && n <= GLLM_TREE_MAX_NODES && c >= 0 && (int64_t)c + n <= (int64_t)a.table_stride * kPage;
+    if (fits) {
+        if (t < n) drawn[t] = a.sampled[r0 + t];
+        __syncthreads();
+        if (t < 64) {
+            int32_t up[4], tok[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = t + 64 * u;
+                up[u] = -2;
+                tok[u] = 0;
+                if (i < n) {
+                    up[u] = a.parents[r0 + i];
+                    tok[u] = a.tokens[r0 + i];
+                    if (up[u] >= i) up[u] = -2;
+                }
+            }
+            int cur = __builtin_amdgcn_readfirstlane(up[0]) == -1 ? 0 : -1, m = 0, last = -1;
+            while (cur >= 0) {  // (a child's index is larger than its parent's)
+                if (t == 0) path[m] = cur;
+                ++m;
+                last = drawn[cur];
+                int next = -1;
+#pragma unroll
+                for (int u = 3; u >= 0; --u) {
+                    const uint64_t hit = __ballot(up[u] == cur && tok[u] == last);
+                    if (hit) next = 64 * u + __builtin_ctzll(hit);
+                }
+                cur = next;
+            }
+            if (t == 0) {
+                accepted = m;
+                last_drawn = last;
+            }
+        }
+        __syncthreads();
+    }
+    const int m = fits ? accepted : 0;
+    if (part == 0) {
+        for (int i = t; i < n; i += 256) a.path[r0 + i] = i < m ? path[i] : -1;
+        if (t == 0) {
+            a.count[s] = m;
+            a.next_token[s] = m > 0 ? last_drawn : -1;
+        }
+    }
+    if (!a.k_pool || m == 0) return;
+    int first = 0;
+    while (first < m && path[first] == first) ++first;  // (the same for all threads)
+    if (first == m) return;
+
+    const int32_t* bt = a.block_tables + (int64_t)s * a.table_stride;
+    const int layer = part / a.n_kv, head = part % a.n_kv;
+    auto page_at = [&](int pos) -> int64_t {  // element offset of the (page, head), -1 for an id outside the pool
+        const int id = bt[pos / kPage];
+        return id >= 0 && id < a.num_blocks ? (((int64_t)layer * a.num_blocks + id) * a.n_kv + head) * (D * kPage) : -1;
+    };
+    constexpr int KP = kMoves * (D / 8) / 256, VP = kMoves * D / 256;  // 16-byte pieces of K, elements of V per thread
+    static_assert(kMoves * (D / 8) % 128 == 0 && kMoves * D % 256 == 0, "whole passes");
+    for (int i0 = first; i0 < m; i0 += kMoves) {
+        u32x4 kv[KP > 0 ? KP : 1];
+        bf16_t vv[VP];
+        auto move = [&](int i, int64_t& from, int64_t& to, int& fs, int& ts) {
+            from = to = -1;
+            if (i >= m) return;
+            const int sp = c + path[i], dp = c + i;
+            if (sp == dp) return;
+            from = page_at(sp);
+            to = page_at(dp);
+            if (from < 0 || to < 0) from = to = -1;
+            fs = sp % kPage;
+            ts = dp % kPage;
+        };
+        auto for_k = [&](auto&& f) {
+#pragma unroll
+            for (int u = 0; u < (KP > 0 ? KP : 1); ++u) {
+                const int x = t + u * 256;
+                if (x >= kMoves * (D / 8)) continue;
+                int64_t from, to;
+                int fs = 0, ts = 0;
+                move(i0 + x / (D / 8), from, to, fs, ts);
+                if (from >= 0) f(u, a.k_pool + from + (x % (D / 8)) * (kPage * 8) + fs * 8, a.k_pool + to + (x % (D / 8)) * (kPage * 8) + ts * 8);
+            }
+        };
+        auto for_v = [&](auto&& f) {
+#pragma unroll
+            for (int u = 0; u < VP; ++u) {
+                const int x = t + u * 256;
+                int64_t from, to;
+                int fs = 0, ts = 0;
+                move(i0 + x / D, from, to, fs, ts);
+                if (from >= 0) f(u, a.v_pool + from + (x % D) * kPage + fs, a.v_pool + to + (x % D) * kPage + ts);
+            }
+        };
+        for_k([&](int u, const bf16_t* src, bf16_t*) { kv[u] = *reinterpret_cast<const u32x4*>(src); });
+        for_v([&](int u, const bf16_t* src, bf16_t*) { vv[u] = *src; });
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (what has been asked for is here before another wave writes)
+        __syncthreads();
+        for_k([&](int u, const bf16_t*, bf16_t* dst) { *reinterpret_cast<u32x4*>(dst) = kv[u]; });
+        for_v([&](int u, const bf16_t*, bf16_t* dst) { *dst = vv[u]; });
+    }
+}
+
+// ---- beam selection -----------------------------------------------------------------------------------------------------
+//
+// Two launches.  beam_rows: a workgroup passes once over a segment of a row of logits and keeps its `keep` largest (no other
+// token of the segment can be among the best of the sequence) beside the segment's largest logit and sum of exponentials.
+// beam_merge: a workgroup per sequence adds up the sums of its rows and picks the best of what the segments kept.
+// The order among beams hangs on the sums: they and the scores are held in 64 bits, so that the order is that of exact
+// arithmetic but where scores agree to some 1e-12.
+
+constexpr int kBeamWaves = 4;
+constexpr int kBeamList = 384;  // places of a wave's list: the 64 kept at most, the 256 of one pass, and a whole number per lane
+
+// Keys in the order of the numbers, 0 for what is no candidate (minus infinity, not a number).
+__device__ __forceinline__ uint32_t order_key(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);  // (one zero)
+    return x > -INFINITY ? b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u) : 0u;
+}
+__device__ __forceinline__ uint64_t order_key(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x + 0.0);
+    return x > -INFINITY ? b ^ (b >> 63 ? ~0ull : 1ull << 63) : 0ull;
+}
+
+// The largest v for which at least k of the wave's U keys per lane are >= v (0 if fewer than k are nonzero): bit by bit.
+template <typename Key, int U>
+__device__ __forceinline__ Key kth_largest(const Key (&key)[U], int k) {
+    Key v = 0;
+    for (int bit = sizeof(Key) * 8 - 1; bit >= 0; --bit) {
+        const Key probe = v | (Key)1 << bit;
+        int above = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) above += __popcll(__ballot(key[u] >= probe));
+        if (above >= k) v = probe;
+    }
+    return v;
+}
+
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The candidates of one wave, in LDS.
+template <typename Key>
+struct WaveList {
+    Key* key;
+    uint32_t* idx;
+    int n;      // the same in all lanes
+    int lane;
+    // Adds the lanes' candidates that `pass`; there has to be room for 64.
+    __device__ __forceinline__ void add(bool pass, Key k, uint32_t i) {
+        const uint64_t who = __ballot(pass);
+        if (pass) {
+            const int at = n + __popcll(who & ((1ull << lane) - 1));
+            key[at] = k;
+            idx[at] = i;
+        }
+        n += __popcll(who);
+    }
+    // Leaves the k best, equal keys by the lower index; returns the k-th key (0: fewer than k).
+    __device__ __forceinline__ Key keep_best(int k) {
+        constexpr int U = kBeamList / 64;
+        wave_fence();
+        Key mine[U];
+        uint32_t at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = lane + 64 * u;
+            mine[u] = i < n ? key[i] : 0;
+            at[u] = i < n ? idx[i] : 0;
+        }
+        const Key v = kth_largest<Key, U>(mine, k);
+        if (v == 0) return 0;
+        int above = 0, same = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            above += __popcll(__ballot(mine[u] > v));
+            same += __popcll(__ballot(mine[u] == v));
+        }
+        uint32_t reach = ~0u;  // of the equal ones the (k - above) lowest indices stay: those whose complement is largest
+        if (same > k - above) {
+            uint32_t rev[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) rev[u] = mine[u] == v ? ~at[u] : 0u;
+            reach = ~kth_largest<uint32_t, U>(rev, k - above);
+        }
+        wave_fence();
+        n = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(mine[u] > v || (mine[u] == v && at[u] <= reach), mine[u], at[u]);
+        wave_fence();
+        return v;
+    }
+};
+
+struct BeamArgs {
+    const float* logits;
+    int64_t ld;
+    const float* scores;
+    int32_t num_seqs, beams, vocab, keep, segs, seg_len;
+    // workspace: per (row, segment) the sum, the largest logit, and `keep` values with their tokens (-1: none)
+    double* sum;
+    float* top;
+    float* value;
+    int32_t* token;
+    float* out_scores;
+    int32_t *out_beams, *out_tokens;
+};
+
+constexpr int kBeamQuads = 4;                        // four-column loads of a lane and pass
+constexpr int kBeamPass = 64 * 4 * kBeamQuads;       // columns of a wave's pass
+constexpr float kBeamSlack = 60.f;
+
+template <bool VEC>
+__global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
+    __shared__ uint32_t keys[kBeamWaves][kBeamList], idxs[kBeamWaves][kBeamList];
+    __shared__ double wave_sum[kBeamWaves];
+    __shared__ float wave_top[kBeamWaves];
+    __shared__ int wave_n[kBeamWaves];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = blockIdx.x / a.segs, seg = blockIdx.x % a.segs;
+    const float* x0 = a.logits + (int64_t)row * a.ld;
+    const int begin = seg * a.seg_len, end = min(a.vocab, begin + a.seg_len);
+    WaveList<uint32_t> list{keys[wave], idxs[wave], 0, lane};
+    uint32_t floor = 0;      // candidates are above it
+    float ref = -INFINITY;   // the sum is of exp(x - ref)
+    double sum = 0.0;        // of this lane
+    // Every wave passes over columns in ascending order, so that behind keep_best an equal key comes with a larger index and loses.
+    for (int at = begin + wave * kBeamPass; at < end; at += kBeamWaves * kBeamPass) {
+        f32x4 x[kBeamQuads];
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kBeamQuads; ++j) {
+            const int col = at + (j * 64 + lane) * 4;
+            if (VEC) {
+                x[j] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (col < end) x[j] = *reinterpret_cast<const f32x4*>(x0 + col);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!VEC) x[j][e] = col + e < end ? x0[col + e] : -INFINITY;
+                else if (col + e >= end) x[j][e] = -INFINITY;
+                if (!(x[j][e] > -INFINITY)) x[j][e] = -INFINITY;  // (not a number)
+                top = fmaxf(top, x[j][e]);
+            }
+        }
+        float wtop = top;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) wtop = fmaxf(wtop, __shfl_xor(wtop, o));
+        if (wtop == -INFINITY) continue;
+        if (wtop > ref + kBeamSlack || ref == -INFINITY) {
+            sum = ref == -INFINITY || wtop == INFINITY ? 0.0 : sum * exp((double)ref - (double)wtop);
+            ref = wtop;
+        }
+#pragma unroll
+        for (int j = 0; j < kBeamQuads; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += x[j][e] == ref ? 1.0 : exp(fmax((double)x[j][e] - (double)ref, -1000.0));
+        if (list.n == 0 && floor == 0) {
+            // the first pass: at least `keep` candidates are not below the keep-th largest of the lanes' maxima
+            const uint32_t lane_top[1] = {order_key(top)};
+            const uint32_t t0 = kth_largest<uint32_t, 1>(lane_top, a.keep);
+            if (t0 > 0) floor = t0 - 1;
+        }
+        if (order_key(wtop) <= floor) continue;
+#pragma unroll
+        for (int j = 0; j < kBeamQuads; ++j) {
+            if (list.n + 256 > kBeamList) floor = max(floor, list.keep_best(a.keep));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t k = order_key(x[j][e]);
+                list.add(k > floor, k, (uint32_t)(at + (j * 64 + lane) * 4 + e));
+            }
+        }
+    }
+    list.keep_best(a.keep);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) {
+        wave_sum[wave] = sum;
+        wave_top[wave] = ref;
+        wave_n[wave] = list.n;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    // the first wave's list takes in the others' (in LDS order: keys and indices decide, not the places)
+    for (int w = 1; w < kBeamWaves; ++w) {
+        if (list.n + 64 > kBeamList) list.keep_best(a.keep);
+        const int n = wave_n[w];
+        list.add(lane < n, lane < n ? keys[w][lane] : 0u, lane < n ? idxs[w][lane] : 0u);
+    }
+    list.keep_best(a.keep);
+    wave_fence();
+    const int64_t place = (int64_t)blockIdx.x;
+    if (lane < a.keep) {
+        const bool there = lane < list.n;
+        const uint32_t i = there ? list.idx[lane] : 0u;
+        a.token[place * a.keep + lane] = there ? (int32_t)i : -1;
+        a.value[place * a.keep + lane] = there ? x0[i] : 0.f;
+    }
+    if (lane == 0) {
+        float m = -INFINITY;
+        for (int w = 0; w < kBeamWaves; ++w) m = fmaxf(m, wave_top[w]);
+        double total = 0.0;
+        for (int w = 0; w < kBeamWaves; ++w)
+            if (wave_top[w] > -INFINITY) total += wave_top[w] == m ? wave_sum[w] : wave_sum[w] * exp((double)wave_top[w] - (double)m);
+        a.top[place] = m;
+        a.sum[place] = total;
+    }
+}
+
+__global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
+    __shared__ uint64_t keys[kBeamWaves][kBeamList];
+    __shared__ uint32_t idxs[kBeamWaves][kBeamList];
+    __shared__ double lse[GLLM_BEAM_MAX_BEAMS];   // log of the sum without the largest logit
+    __shared__ float tops[GLLM_BEAM_MAX_BEAMS];
+    __shared__ int wave_n[kBeamWaves];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int s = blockIdx.x;
+    const int64_t row0 = (int64_t)s * a.beams;
+    for (int b = wave; b < a.beams; b += kBeamWaves) {
+        const int64_t place = (row0 + b) * a.segs;
+        float m = -INFINITY;
+        for (int i = lane; i < a.segs; i += 64) m = fmaxf(m, a.top[place + i]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+        double total = 0.0;
+        for (int i = lane; i < a.segs; i += 64) {
+            const float t = a.top[place + i];
+            if (t > -INFINITY) total += t == m ? a.sum[place + i] : a.sum[place + i] * exp((double)t - (double)m);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+        if (lane == 0) {
+            tops[b] = m;
+            lse[b] = log(total);
+        }
+    }
+    __syncthreads();
+    WaveList<uint64_t> list{keys[wave], idxs[wave], 0, lane};
+    uint64_t floor = 1;
+    const int per_beam = a.segs * a.keep, total = a.beams * per_beam;
+    for (int at = wave * 64; at < total; at += kBeamWaves * 64) {
+        const int i = at + lane;
+        uint64_t k = 0;
+        uint32_t idx = 0;
+        if (i < total) {
+            const int b = i / per_beam;
+            const int64_t place = row0 * per_beam + i;
+            const int32_t token = a.token[place];
+            const float cum = a.scores[row0 + b], x = a.value[place], m = tops[b];
+            if (token >= 0 && cum > -INFINITY && cum < INFINITY) {
+                const double d = x == m ? 0.0 : (double)x - (double)m;
+                k = order_key((double)cum + (d - lse[b]));
+                idx = (uint32_t)b * (uint32_t)a.vocab + (uint32_t)token;
+            }
+        }
+        if (list.n + 64 > kBeamList) floor = max(floor, list.keep_best(a.keep));
+        list.add(k >= floor, k, idx);
+    }
+    list.keep_best(a.keep);
+    if (lane == 0) wave_n[wave] = list.n;
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < kBeamWaves; ++w) {
+        const int n = wave_n[w];
+        list.add(lane < n, lane < n ? keys[w][lane] : 0ull, lane < n ? idxs[w][lane] : 0u);
+    }
+    list.keep_best(a.keep);
+    wave_fence();
+    // the place of each of the at most 64 is the number of those in front of it
+    const bool there = lane < list.n;
+    const uint64_t k = there ? list.key[lane] : 0ull;
+    const uint32_t i = there ? list.idx[lane] : 0u;
+    int rank = 0;
+    for (int j = 0; j < list.n; ++j) {
+        const uint64_t kj = list.key[j];
+        rank += kj > k || (kj == k && list.idx[j] < i);
+    }
+    const int64_t out = (int64_t)s * a.keep;
+    if (there) {
+        const uint64_t bits = k >> 63 ? k ^ (1ull << 63) : ~k;
+        a.out_scores[out + rank] = (float)__builtin_bit_cast(double, bits);
+        a.out_beams[out + rank] = (int32_t)(i / (uint32_t)a.vocab);
+        a.out_tokens[out + rank] = (int32_t)(i % (uint32_t)a.vocab);
+    } else if (lane < a.keep) {
+        a.out_scores[out + lane] = -INFINITY;
+        a.out_beams[out + lane] = -1;
+        a.out_tokens[out + lane] = -1;
+    }
+}
+
+// Segments of a row.
+int beam_segments(int num_seqs, int beams, int vocab) {
+    (void)num_seqs; (void)beams; (void)vocab;
+    return 1;
+}
+
+bool beam_sizes_ok(int num_seqs, int beams, int vocab, int keep) {
+    return num_seqs >= 0 && beams >= 1 && beams <= GLLM_BEAM_MAX_BEAMS && vocab >= 1 && vocab <= 1 << 24 && keep >= 1 && keep <= GLLM_BEAM_MAX_KEEP &&
+           (int64_t)num_seqs * beams <= 1 << 22;
+}
+
+// ---- page copies --------------------------------------------------------------------------------------------------------
+
+constexpr int kCopyPairs = 448;  // pages of a launch: the list travels with the launch, whose arguments may take 4 KiB
+struct CopyArgs {
+    u32x4 *k, *v;
+    int64_t layer_vecs;   // 16-byte pieces of a layer of either pool
+    int32_t page_vecs;    // and of a page
+    int32_t src[kCopyPairs], dst[kCopyPairs];
+};
+static_assert(sizeof(CopyArgs) <= 4096 - 256, "launch arguments");
+
+// grid (pairs, layers, 2)
+__global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs a) {
+    u32x4* pool = (blockIdx.z ? a.v : a.k) + blockIdx.y * a.layer_vecs;
+    const u32x4* src = pool + (int64_t)a.src[blockIdx.x] * a.page_vecs;
+    u32x4* dst = pool + (int64_t)a.dst[blockIdx.x] * a.page_vecs;
+    for (int i = threadIdx.x; i < a.page_vecs; i += 256) dst[i] = src[i];
+}
+
+gllm_status launched() { return hipGetLastError() == hipSuccess ? GLLM_OK : GLLM_E_HIP; }
+
+bool misaligned(const void* p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) != 0; }
+
+bool tree_shape_ok(int n_q, int n_kv, int d, int max_nodes) {
+    return n_q >= 1 && n_kv >= 1 && n_q % n_kv == 0 && n_q / n_kv <= 16 && (d == 64 || d == 128) && max_nodes >= 1 && max_nodes <= GLLM_TREE_MAX_NODES;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gllm_op_tree_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_nodes) {
+    return tree_shape_ok(n_q_heads, n_kv_heads, head_dim, max_nodes) ? tree_workspace_bytes(n_q_heads, n_kv_heads, head_dim, max_nodes) : 0;
+}
+
+gllm_status gllm_op_tree_attention(const void* q, int64_t ld_q, const void* k_pool, const void* v_pool, int64_t num_blocks,
+                                   const int32_t* block_tables, int32_t block_table_stride, const int32_t* cached_len,
+                                   const int32_t* row_start, const int32_t* parents, int32_t num_seqs, int32_t num_rows,
+                                   int32_t max_nodes, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                                   void* out, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (num_seqs < 0 || num_rows < 0 || max_nodes < 1 || num_blocks < 1 || num_blocks > INT32_MAX || block_table_stride < 1 || n_q_heads < 1 || n_kv_heads < 1 ||
+        !(scale > 0.f) || !std::isfinite(scale))
+        return GLLM_E_INVALID;
+    if (!tree_shape_ok(n_q_heads, n_kv_heads, head_dim, max_nodes)) return GLLM_E_UNSUPPORTED;
+    if (num_seqs == 0 || num_rows == 0) return GLLM_OK;
+    if (!q || !k_pool || !v_pool || !block_tables || !cached_len || !row_start || !parents || !out || !workspace) return GLLM_E_INVALID;
+    if (ld_q < (int64_t)n_q_heads * head_dim || ld_out < (int64_t)n_q_heads * head_dim) return GLLM_E_INVALID;
+    if (ld_q % 8 != 0 || ld_out % 4 != 0 || misaligned(q, 16) || misaligned(k_pool, 16) || misaligned(v_pool, 16) || misaligned(out, 8) || misaligned(workspace, 16))
+        return GLLM_E_INVALID;
+    if (workspace_bytes < tree_workspace_bytes(n_q_heads, n_kv_heads, head_dim, max_nodes)) return GLLM_E_CAPACITY;
+    TreeArgs a{};
+    a.q = (const bf16_t*)q; a.ld_q = ld_q;
+    a.k_pool = (const bf16_t*)k_pool; a.v_pool = (const bf16_t*)v_pool; a.num_blocks = (int32_t)num_blocks;
+    a.block_tables = block_tables; a.table_stride = block_table_stride; a.bt_off = nullptr;
+    a.cached_len = cached_len; a.row_begin = row_start; a.row_end = row_start + 1; a.parents = parents;
+    a.num_seqs = num_seqs; a.num_rows = num_rows; a.max_nodes = max_nodes;
+    a.out = (bf16_t*)out; a.ld_o = ld_out;
+    a.n_q = n_q_heads; a.n_kv = n_kv_heads; a.d = head_dim;
+    a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.workspace = workspace;
+    const hipError_t e = launch_tree_attention(a, (hipStream_t)stream);
+    return e == hipSuccess ? GLLM_OK : e == hipErrorInvalidValue ? GLLM_E_CAPACITY : GLLM_E_HIP;
+}
+
+gllm_status gllm_op_tree_commit(const int32_t* tokens, const int32_t* parents, const int32_t* sampled, const int32_t* row_start,
+                                const int32_t* cached_len, const int32_t* block_tables, int32_t block_table_stride,
+                                int32_t num_seqs, int32_t num_rows, void* k_pool, void* v_pool, int32_t num_layers,
+                                int64_t num_blocks, int32_t n_kv_heads, int32_t head_dim, int32_t* path, int32_t* count,
+                                int32_t* next_token, void* stream) {
+    if (num_seqs < 0 || num_rows < 0 || block_table_stride < 1 || !k_pool != !v_pool) return GLLM_E_INVALID;
+    if (k_pool) {
+        if (num_layers < 1 || num_blocks < 1 || num_blocks > INT32_MAX || n_kv_heads < 1 || misaligned(k_pool, 16) || misaligned(v_pool, 16)) return GLLM_E_INVALID;
+        if (head_dim != 64 && head_dim != 128) return GLLM_E_UNSUPPORTED;
+        if ((int64_t)num_layers * n_kv_heads * num_seqs > INT32_MAX) return GLLM_E_CAPACITY;
+    }
+    if (num_seqs == 0) return GLLM_OK;
+    if (!row_start || !cached_len || !block_tables || !count || !next_token) return GLLM_E_INVALID;
+    if (num_rows > 0 && (!tokens || !parents || !sampled || !path)) return GLLM_E_INVALID;
+    const CommitArgs a{tokens, parents, sampled, row_start, cached_len, block_tables, block_table_stride, num_seqs, num_rows,
+                       (bf16_t*)k_pool, (bf16_t*)v_pool, k_pool ? num_layers : 0, (int32_t)(k_pool ? num_blocks : 0), k_pool ? n_kv_heads : 0,
+                       path, count, next_token};
+    const dim3 grid((unsigned)num_seqs * (unsigned)std::max(1, a.num_layers * a.n_kv));
+    if (k_pool && head_dim == 64) tree_commit_kernel<64><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+    else tree_commit_kernel<128><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+    return launched();
+}
+
+size_t gllm_op_beam_select_workspace_bytes(int32_t num_seqs, int32_t beams, int32_t vocab, int32_t keep) {
+    if (!beam_sizes_ok(num_seqs, beams, vocab, keep)) return 0;
+    const size_t places = (size_t)std::max(1, num_seqs) * beams * beam_segments(num_seqs, beams, vocab);
+    return places * (8 + 4 + (size_t)keep * 8);
+}
+
+gllm_status gllm_op_beam_select(const float* logits, int64_t ld_logits, const float* scores, int32_t num_seqs, int32_t beams,
+                                int32_t vocab, int32_t keep, float* out_scores, int32_t* out_beams, int32_t* out_tokens,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+    if (num_seqs < 0 || beams < 1 || vocab < 1 || keep < 1 || ld_logits < vocab) return GLLM_E_INVALID;
+    if (!beam_sizes_ok(num_seqs, beams, vocab, keep)) return GLLM_E_UNSUPPORTED;
+    if (num_seqs == 0) return GLLM_OK;
+    if (!logits || !scores || !out_scores || !out_beams || !out_tokens || !workspace || misaligned(logits, 4) || misaligned(workspace, 16)) return GLLM_E_INVALID;
+    if (workspace_bytes < gllm_op_beam_select_workspace_bytes(num_seqs, beams, vocab, keep)) return GLLM_E_CAPACITY;
+    BeamArgs a{};
+    a.logits = logits; a.ld = ld_logits; a.scores = scores;
+    a.num_seqs = num_seqs; a.beams = beams; a.vocab = vocab; a.keep = keep;
+    a.segs = beam_segments(num_seqs, beams, vocab);
+    a.seg_len = (int32_t)round_up(ceil_div(vocab, a.segs), 4);
+    const int64_t places = (int64_t)num_seqs * beams * a.segs;
+    a.sum = (double*)workspace;
+    a.top = (float*)(a.sum + places);
+    a.value = a.top + places;
+    a.token = (int32_t*)(a.value + places * keep);
+    a.out_scores = out_scores; a.out_beams = out_beams; a.out_tokens = out_tokens;
+    // four logits at a time from rows that all start on a 16-byte boundary (a quad does not pass a row's end then)
+    if (!misaligned(logits, 16) && ld_logits % 4 == 0) beam_rows_kernel<true><<<(unsigned)places, 256, 0, (hipStream_t)stream>>>(a);
+    else beam_rows_kernel<false><<<(unsigned)places, 256, 0, (hipStream_t)stream>>>(a);
+    if (hipGetLastError() != hipSuccess) return GLLM_E_HIP;
+    beam_merge_kernel<<<num_seqs, 256, 0, (hipStream_t)stream>>>(a);
+    return launched();
+}
+
+gllm_status gllm_op_copy_pages(void* k_pool, void* v_pool, int32_t num_layers, int64_t num_blocks, int32_t n_kv_heads,
+                               int32_t head_dim, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
+    if (n < 0 || num_layers < 1 || num_layers > 65535 || num_blocks < 1 || num_blocks > INT32_MAX || n_kv_heads < 1) return GLLM_E_INVALID;
+    if (head_dim != 64 && head_dim != 128) return GLLM_E_UNSUPPORTED;
+    if ((int64_t)n_kv_heads * head_dim * 2 > INT32_MAX) return GLLM_E_UNSUPPORTED;
+    if (n == 0) return GLLM_OK;
+    if (!k_pool || !v_pool || !src || !dst || misaligned(k_pool, 16) || misaligned(v_pool, 16)) return GLLM_E_INVALID;
+    for (int32_t i = 0; i < n; ++i)
+        if (src[i] < 0 || src[i] >= num_blocks || dst[i] < 0 || dst[i] >= num_blocks) return GLLM_E_BLOCK_RANGE;
+    try {
+        std::vector<int32_t> to(dst, dst + n);
+        std::sort(to.begin(), to.end());
+        if (std::adjacent_find(to.begin(), to.end()) != to.end()) return GLLM_E_BLOCK_ALIAS;
+        for (int32_t i = 0; i < n; ++i)
+            if (std::binary_search(to.begin(), to.end(), src[i])) return GLLM_E_BLOCK_ALIAS;
+    } catch (const std::exception&) {
+        return GLLM_E_CAPACITY;
+    }
+    CopyArgs a{};
+    a.k = (u32x4*)k_pool;
+    a.v = (u32x4*)v_pool;
+    a.page_vecs = n_kv_heads * head_dim * 2;
+    a.layer_vecs = num_blocks * a.page_vecs;
+    for (int32_t i0 = 0; i0 < n; i0 += kCopyPairs) {
+        const int32_t m = std::min(n - i0, kCopyPairs);
+        std::copy(src + i0, src + i0 + m, a.src);
+        std::copy(dst + i0, dst + i0 + m, a.dst);
+        copy_pages_kernel<<<dim3((unsigned)m, (unsigned)num_layers, 2), 256, 0, (hipStream_t)stream>>>(a);
+        if (hipGetLastError() != hipSuccess) return GLLM_E_HIP;
+    }
+    return GLLM_OK;
+}
+
+}  // extern "C"
