@@ -16,20 +16,25 @@ constexpr int kTreeNodes = 256;             // most nodes of a tree: one per thr
 constexpr int kTreeWords = kTreeNodes / 32;
 constexpr int kTreeStages = 3;
 
-struct TreeItem {
-    int32_t seq, tile, row0, n, c, pad;
+// A unit of work: the keys of blocks blk_begin .. blk_end - 1 for the columns of one tile of a sequence.
+struct TreeUnit {
+    int32_t seq, tile, row0, n, c;
+    int32_t blk_begin, blk_end;  // equal where the sequence breaks a rule: zeros
+    int32_t parts, part;
+    int32_t slot;                // parts > 1: place of the unit among those with partial results
+    int32_t cut_tile;            // and of its tile among those with such units
 };
 
 // What the closure of a tree takes in LDS: rows of `stride` words per node (odd, so that neighbouring nodes lie in different
 // banks), the parent links, and the words of the nodes that are used.
 __host__ __device__ inline int tree_row_words(int max_nodes) { return (max_nodes / 32 + 2) | 1; }
-__host__ __device__ inline int tree_lds_bytes(int max_nodes) { return (kTreeNodes * tree_row_words(max_nodes) + kTreeNodes + 2 * (kTreeWords + 1) + 16) * 4; }
+__host__ __device__ inline int tree_lds_bytes(int max_nodes) { return (kTreeNodes * tree_row_words(max_nodes) + kTreeNodes + 2 * (kTreeWords + 1) + 2 + 30) * 4; }
 struct TreeLds {
     uint32_t* vis;    // [node][stride]: word w of a node: keys 32w .. 32w+31 behind the first key of block c / 32
     int* up;          // [node]
     uint32_t* used;   // [kTreeWords + 1], as a row of vis: all cached keys and all used nodes
     uint32_t* raw;    // [kTreeWords]
-    int* scratch;     // [16]
+    int* scratch;     // [30], on an 8-byte boundary
     int stride;
     __device__ TreeLds(void* p, int max_nodes) {
         stride = tree_row_words(max_nodes);
@@ -37,7 +42,7 @@ struct TreeLds {
         up = (int*)(vis + kTreeNodes * stride);
         used = (uint32_t*)(up + kTreeNodes);
         raw = used + kTreeWords + 1;
-        scratch = (int*)(raw + kTreeWords + 1);
+        scratch = (int*)(((uintptr_t)(raw + kTreeWords + 1) + 7) & ~(uintptr_t)7);
     }
 };
 
@@ -92,51 +97,201 @@ __device__ __forceinline__ void tree_visibility(const TreeLds& t, const int32_t*
     __syncthreads();
 }
 
-// The workgroup's place in the list of all (sequence, tile of columns): the sequence and tile of place `item`.  Sequences that
-// break a rule keep their place with n or c as found; the caller sees to that.  False behind the last one.  All threads.
-__device__ __forceinline__ bool tree_locate(const TreeArgs& a, int item, int tile_cols, TreeItem& it, int* scratch) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = a.n_q / a.n_kv;
-    int64_t before = 0;
-    for (int s0 = 0; s0 < a.num_seqs; s0 += 256) {
-        const int s = s0 + threadIdx.x;
-        int tiles = 0, r0 = 0, n = 0, c = 0;
-        if (s < a.num_seqs) {
-            r0 = a.row_begin[s];
-            const int r1 = a.row_end[s];
-            c = a.cached_len[s];
-            if (r0 >= 0 && r1 > r0 && r1 <= a.num_rows) n = r1 - r0;
-            tiles = (int)(((int64_t)n * g + tile_cols - 1) / tile_cols);
-        }
-        int sum = tiles;
+// ---- the plan, made by every workgroup for itself -----------------------------------------------------------------------
+//
+// The lengths stand on the device.  The keys of a sequence are cut into parts of at most `share` blocks, equal to within one
+// block, so that all parts of all sequences come to about kTreeTarget workgroups; units are ordered by sequence, part and tile:
+// the tiles of a part, neighbours in the launch but for the KV heads, read the same keys at the same time.
+constexpr int kTreeTarget = 1024;     // workgroups that the keys are cut into, over all KV heads
+constexpr int kTreeMinShare = 4;      // fewest blocks worth a workgroup
+constexpr int tree_target(int n_kv) { return kTreeTarget / n_kv > 0 ? kTreeTarget / n_kv : 1; }
+// Units with partial results: a sequence is cut where it has more blocks than a share, and then into fewer parts than twice its
+// blocks by the share; a share is at least the blocks of all tiles by the target.
+constexpr int tree_max_slots(int n_kv) { return 2 * tree_target(n_kv); }
+// (and their tiles: every one of them has more blocks than a share)
+constexpr int tree_max_cut_tiles(int n_kv) { return tree_target(n_kv); }
+
+struct SeqPlan {
+    int32_t row0, n, c, tiles, blocks;
+};
+__device__ __forceinline__ SeqPlan seq_plan(const TreeArgs& a, int s, int tile_cols) {
+    SeqPlan p{0, 0, 0, 0, 0};
+    if (s >= a.num_seqs) return p;
+    const int r0 = a.row_begin[s], r1 = a.row_end[s];
+    p.c = a.cached_len[s];
+    if (r0 < 0 || r1 <= r0 || r1 > a.num_rows) return p;
+    p.row0 = r0;
+    p.n = r1 - r0;
+    p.tiles = (p.n * (a.n_q / a.n_kv) + tile_cols - 1) / tile_cols;  // (num_rows * group fits 31 bits: the launcher)
+    if (p.n <= a.max_nodes && p.c >= 0 && (int64_t)p.c + p.n <= (int64_t)a.table_stride * kPage) p.blocks = (p.c + p.n + 31) / 32;
+    return p;
+}
+
+struct Two {
+    int64_t x, y;
+};
+// Sums over the 256 threads, of all of them and (`before`) of those in front; scratch: 8 words of 8 bytes.  Two barriers.
+__device__ __forceinline__ Two scan_threads(Two v, Two& before, int64_t* scratch) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Two sum = v;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(sum, o);
-            if (lane >= o) sum += x;
+    for (int o = 1; o < 64; o <<= 1) {
+        const Two up = {__shfl_up(sum.x, o), __shfl_up(sum.y, o)};
+        if (lane >= o) {
+            sum.x += up.x;
+            sum.y += up.y;
         }
-        if (lane == 63) scratch[wave] = sum;
-        if (threadIdx.x == 0) scratch[4] = -1;
-        __syncthreads();
-        int64_t first = before + sum - tiles;
-        for (int w = 0; w < wave; ++w) first += scratch[w];
-        before += (int64_t)scratch[0] + scratch[1] + scratch[2] + scratch[3];
-        if (item >= first && item < first + tiles) {
-            scratch[4] = s;
-            scratch[5] = (int)(item - first);
-            scratch[6] = r0;
-            scratch[7] = n;
-            scratch[8] = c;
+    }
+    __syncthreads();
+    if (lane == 63) {
+        scratch[wave] = sum.x;
+        scratch[4 + wave] = sum.y;
+    }
+    __syncthreads();
+    before = Two{sum.x - v.x, sum.y - v.y};
+    for (int w = 0; w < wave; ++w) {
+        before.x += scratch[w];
+        before.y += scratch[4 + w];
+    }
+    return Two{scratch[0] + scratch[1] + scratch[2] + scratch[3], scratch[4] + scratch[5] + scratch[6] + scratch[7]};
+}
+
+// The unit of place `place`; false behind the last one, with the number of tiles whose keys are cut in `cut_tiles`.
+__device__ __forceinline__ bool tree_unit(const TreeArgs& a, int place, int tile_cols, TreeUnit& u, int& cut_tiles, int64_t* scratch) {
+    Two before, total = {0, 0};  // blocks of all tiles, rows
+    const SeqPlan p = seq_plan(a, threadIdx.x, tile_cols);
+    for (int s0 = 0; s0 < a.num_seqs; s0 += 256) {
+        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + threadIdx.x, tile_cols);
+        const Two t = scan_threads(Two{(int64_t)q.tiles * q.blocks, q.n}, before, scratch);
+        total.x += t.x;
+        total.y += t.y;
+    }
+    cut_tiles = 0;
+    if (total.y > a.num_rows) return false;  // sequences that share rows: the launch has no place for their units
+    const int target = tree_target(a.n_kv);
+    const int share = (int)min(max((total.x + target - 1) / target, (int64_t)kTreeMinShare), (int64_t)INT32_MAX);
+    int64_t units = 0, cut = 0;  // cut: units in the lower half, tiles in the upper one
+    int* found = (int*)(scratch + 8);
+    for (int s0 = 0; s0 < a.num_seqs; s0 += 256) {
+        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + threadIdx.x, tile_cols);
+        const int parts = max(1, (int)(((int64_t)q.blocks + share - 1) / share));
+        const int64_t mine = (int64_t)q.tiles * parts;
+        if (threadIdx.x == 0) found[0] = -1;
+        const Two all = scan_threads(Two{mine, parts > 1 ? mine | (int64_t)q.tiles << 32 : 0}, before, scratch);
+        const int64_t at = place - units - before.x;
+        if (at >= 0 && at < mine) {
+            found[0] = s0 + threadIdx.x;
+            found[1] = (int)at;
+            found[2] = q.row0;
+            found[3] = q.n;
+            found[4] = q.c;
+            found[5] = q.blocks;
+            found[6] = parts;
+            found[7] = (int)(uint32_t)(cut + before.y);
+            found[8] = q.tiles;
+            found[9] = (int)((cut + before.y) >> 32);
         }
         __syncthreads();
-        if (scratch[4] >= 0) {
-            it = TreeItem{scratch[4], scratch[5], scratch[6], scratch[7], scratch[8], 0};
+        if (found[0] >= 0) {
+            const int i = found[1], tiles = found[8], blocks = found[5];
+            u.seq = found[0];
+            u.row0 = found[2];
+            u.n = found[3];
+            u.c = found[4];
+            u.parts = found[6];
+            u.part = i / tiles;
+            u.tile = i % tiles;
+            u.slot = found[7] + i;
+            u.cut_tile = found[9] + u.tile;
+            u.blk_begin = (int)((int64_t)blocks * u.part / u.parts);
+            u.blk_end = (int)((int64_t)blocks * (u.part + 1) / u.parts);
             return true;
         }
+        units += all.x;
+        cut += all.y;
         __syncthreads();
     }
+    cut_tiles = (int)(cut >> 32);
     return false;
 }
 
-// One workgroup of 4 waves per (sequence, tile of 64*NB columns, KV head): a block of 32 keys is brought into LDS once and
+// ---- partial results ------------------------------------------------------------------------------------------------------
+//
+// Workspace: a record per tile whose keys are cut, then per (slot, KV head) the reference and the sum of each column of the tile,
+// then their unnormalised outputs.  A column of a sum below zero is an unused node's.
+struct TreeRecord {
+    int32_t row0, n, tile, parts;
+    int32_t slot, step;  // of the first part, and slots from a part to the next one
+    int32_t pad[2];
+};
+struct TreeParts {
+    int32_t* count;  // records
+    TreeRecord* rec;
+    f32x2* ml;       // [slot][n_kv][tile_cols]
+    float* o;        // [slot][n_kv][tile_cols][d]
+};
+__host__ __device__ inline size_t tree_parts(TreeParts& t, void* base, int n_kv, int d, int tile_cols) {
+    const size_t cols = (size_t)tree_max_slots(n_kv) * n_kv * tile_cols;
+    char* p = (char*)base;
+    t.count = (int32_t*)p;
+    t.rec = (TreeRecord*)(p + 256);
+    size_t off = 256 + (tree_max_cut_tiles(n_kv) * sizeof(TreeRecord) + 255) / 256 * 256;
+    t.ml = (f32x2*)(p + off);
+    off += cols * 8;
+    t.o = (float*)(p + off);
+    return off + cols * d * 4;
+}
+__device__ __forceinline__ void write_record(const TreeParts& parts, const TreeUnit& it, int cols, int tile_cols) {
+    if (it.part == 0) parts.rec[it.cut_tile] = TreeRecord{it.row0, it.n, it.tile, it.parts, it.slot, (cols + tile_cols - 1) / tile_cols, {}};
+}
+
+// ---- the last blocks -------------------------------------------------------------------------------------------------------
+//
+// A lane holds 8 of a block's keys: bit v of `seen` says whether its column sees key v, of `keep` whether any used node does.
+__device__ __forceinline__ void hide_scores(float (&sc)[8], uint32_t seen) {
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+        if (!(seen >> v & 1)) sc[v] = -INFINITY;  // (a column may see nothing of a block: no finite stand-in)
+}
+__device__ __forceinline__ uint32_t pair_mask(uint32_t bits, int w) { return (bits >> (2 * w) & 1 ? 0xFFFFu : 0u) | (bits >> (2 * w + 1) & 1 ? 0xFFFF0000u : 0u); }
+// Bit 15 or 31 of a value that is not finite.
+__device__ __forceinline__ uint32_t not_finite(uint32_t pair) { return ((pair & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+// V operands of the block: 0 * NaN is NaN, so the values that no node sees are emptied, and those of a used node that are not finite too:
+// they may reach the columns that see them only, whose outputs become NaN here.
+template <int D, int NB>
+__device__ __forceinline__ void clean_values(u32x4 (&vf)[D / 16], uint32_t keep, const uint32_t (&seen)[NB], AttnState<D, NB>& st) {
+    uint32_t bad = 0u;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t m = pair_mask(keep, w);
+#pragma unroll
+        for (int b = 0; b < D / 16; ++b) {
+            vf[b][w] &= m;
+            bad |= not_finite(vf[b][w]);
+        }
+    }
+    if (!__any(bad != 0u)) return;
+    for (int b = 0; b < D / 16; ++b) {
+        u32x4 mark, sees;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t off = not_finite(vf[b][w]);
+            mark[w] = (off >> 15 & 1 ? 0x3F80u : 0u) | (off >> 31 ? 0x3F800000u : 0u);  // bf16 ones
+            vf[b][w] &= ~((off >> 15 & 1 ? 0xFFFFu : 0u) | (off >> 31 ? 0xFFFF0000u : 0u));
+        }
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sees[w] = pair_mask(seen[c], w) & 0x3F803F80u;
+            const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (hit[v] > 0.f) st.o[c][b][v] = NAN;
+        }
+    }
+}
+
+// One workgroup of 4 waves per (unit, KV head), of tiles of 64*NB columns: a block of 32 keys is brought into LDS once and
 // read by all waves, each of which has NB groups of 16 columns (the ring and the operand layout are those of prefill attention).
 template <int D, int NB>
 __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
@@ -145,13 +300,18 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     extern __shared__ uint32_t tree_words[];
     const TreeLds tree(tree_words, a.max_nodes);
     const int kvh = blockIdx.x % a.n_kv, g = a.n_q / a.n_kv;
-    TreeItem it;
-    if (!tree_locate(a, blockIdx.x / a.n_kv, TILE, it, tree.scratch)) return;
+    TreeUnit it;
+    TreeParts parts;
+    tree_parts(parts, a.workspace, a.n_kv, D, TILE);
+    int cut_tiles;
+    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles, (int64_t*)tree.scratch)) {
+        if (blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
+        return;
+    }
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, G = lane >> 4;
-    const bool fits = it.n <= a.max_nodes && it.c >= 0 && (int64_t)it.c + it.n <= (int64_t)a.table_stride * kPage;
-    const int cols = it.n * g;  // (n <= num_rows, g <= 16: the launcher sees that it fits)
+    const int cols = it.n * g;
 
     bf16x8 qf[NB][D / 32];
     int node[NB];
@@ -168,8 +328,8 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     AttnState<D, NB> st;
     init_state<D, NB>(st);
     bool used[NB] = {};
-    if (fits) {
-        const int nblk = (it.c + it.n + 31) / 32, n_full = it.c / 32, last_page = (it.c + it.n - 1) / kPage;
+    if (it.blk_begin < it.blk_end) {
+        const int n_full = it.c / 32, last_page = (it.c + it.n - 1) / kPage;
         const int32_t* bt = a.block_tables + (a.bt_off ? (int64_t)a.bt_off[it.seq] : (int64_t)it.seq * a.table_stride);
         // wave w brings in piece w of a block: K page 0, K page 1, V page 0, V page 1
         const bf16_t* pool = wave < 2 ? a.k_pool : a.v_pool;
@@ -197,9 +357,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
                 score_group<D>(sc[c], kf, qf[c]);
                 if (MASKED) {
                     seen[c] = tree.vis[node[c] * tree.stride + blk - n_full] >> (G * 8);
-#pragma unroll
-                    for (int v = 0; v < 8; ++v)
-                        if (!(seen[c] >> v & 1)) sc[c][v] = -INFINITY;  // (a column may see nothing of a block: no finite stand-in)
+                    hide_scores(sc[c], seen[c]);
                 }
             }
             u32x4 vf[D / 16];
@@ -208,78 +366,53 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
                 [&]() -> const u32x4 (&)[D / 16] {
 #pragma unroll
                     for (int b = 0; b < D / 16; ++b) vf[b] = *reinterpret_cast<const u32x4*>(&ring[stage][2 + (G >> 1)][b * 512 + r * 32 + (G & 1) * 16]);
-                    if (MASKED) {
-                        // values of unused nodes and of slots past the last one may be anything: 0 * NaN is NaN
-                        const uint32_t keep = tree.used[blk - n_full] >> (G * 8);
-                        uint32_t bad = 0u;
-#pragma unroll
-                        for (int b = 0; b < D / 16; ++b)
-#pragma unroll
-                            for (int w = 0; w < 4; ++w) {
-                                vf[b][w] &= (keep >> (2 * w) & 1 ? 0xFFFFu : 0u) | (keep >> (2 * w + 1) & 1 ? 0xFFFF0000u : 0u);
-                                bad |= ((vf[b][w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-                            }
-                        if (__any(bad != 0u)) {
-                            // a used node's value is not finite: it may reach the columns that see it only.  Its place is
-                            // emptied here, and the outputs of the columns that see it become NaN
-#pragma unroll
-                            for (int b = 0; b < D / 16; ++b) {
-                                u32x4 mark;
-#pragma unroll
-                                for (int w = 0; w < 4; ++w) {
-                                    const uint32_t off = ((vf[b][w] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;  // bit 15 or 31 of a bad one
-                                    mark[w] = (off >> 15 & 1 ? 0x3F80u : 0u) | (off >> 31 ? 0x3F800000u : 0u);
-                                    vf[b][w] &= (off >> 15 & 1 ? 0u : 0xFFFFu) | (off >> 31 ? 0u : 0xFFFF0000u);
-                                }
-#pragma unroll
-                                for (int c = 0; c < NB; ++c) {
-                                    u32x4 sees;
-#pragma unroll
-                                    for (int w = 0; w < 4; ++w)
-                                        sees[w] = (seen[c] >> (2 * w) & 1 ? 0x3F80u : 0u) | (seen[c] >> (2 * w + 1) & 1 ? 0x3F800000u : 0u);
-                                    const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees),
-                                                                                             f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                                    for (int v = 0; v < 4; ++v)
-                                        if (hit[v] > 0.f) st.o[c][b][v] = NAN;
-                                }
-                            }
-                        }
-                    }
+                    if (MASKED) clean_values<D, NB>(vf, tree.used[blk - n_full] >> (G * 8), seen, st);
                     return vf;
                 });
         };
-        tree_visibility(tree, a.parents + it.row0, it.n, it.c, a.max_nodes);
+        const bool sees_tree = it.blk_end > n_full;  // (one part at least: its last block holds the last node)
+        if (sees_tree) tree_visibility(tree, a.parents + it.row0, it.n, it.c, a.max_nodes);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
+            if (!sees_tree) continue;
             const int at = (it.c & 31) + node[c];
             used[c] = tree.vis[node[c] * tree.stride + (at >> 5)] >> (at & 31) & 1;
         }
         // every wave always issues its piece (indices past the end read the last page again into a stage nobody reads), so the
         // count of outstanding loads is the same in every iteration
 #pragma unroll
-        for (int i = 0; i < NS - 1; ++i) issue_block(page_id(i), i);
-        int pid_next = page_id(NS - 1);
+        for (int i = 0; i < NS - 1; ++i) issue_block(page_id(it.blk_begin + i), i);
+        int pid_next = page_id(it.blk_begin + NS - 1);
         const bool idle = it.tile * TILE + wave * NB * 16 >= cols;  // (the same for the wave)
-        for (int blk = 0; blk < nblk; ++blk) {
+        const int nblk = it.blk_end - it.blk_begin;
+        for (int i = 0; i < nblk; ++i) {
+            const int blk = it.blk_begin + i;
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * IPB) : "memory");
-            __syncthreads();  // block blk has landed; nobody reads stage (blk - 1) % NS any more
-            issue_block(pid_next, (blk + NS - 1) % NS);
+            __syncthreads();  // block blk has landed; nobody reads the stage of the block before it any more
+            issue_block(pid_next, (i + NS - 1) % NS);
             pid_next = page_id(blk + NS);
             if (idle) continue;
-            if (blk < n_full) block_step(blk % NS, blk, std::false_type{});
-            else block_step(blk % NS, blk, std::true_type{});
+            if (blk < n_full) block_step(i % NS, blk, std::false_type{});
+            else block_step(i % NS, blk, std::true_type{});
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no LDS fill may outlive the workgroup
     }
+    if (it.parts > 1 && kvh == 0 && threadIdx.x == 0) write_record(parts, it, cols, TILE);
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
         float l = st.l[c];
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (!stored[c]) continue;
+        const int tcol = (wave * NB + c) * 16 + r, col = it.tile * TILE + tcol;
+        if (it.parts > 1) {
+            const int64_t at = ((int64_t)it.slot * a.n_kv + kvh) * TILE + tcol;
+#pragma unroll
+            for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(parts.o + at * D + b * 16 + G * 4) = st.o[c][b];
+            if (G == 0) parts.ml[at] = f32x2{st.m[c], it.part + 1 == it.parts && !used[c] ? -1.f : l};
+            continue;
+        }
         const float inv = 1.0f / l;
-        const int col = it.tile * TILE + (wave * NB + c) * 16 + r;
         bf16_t* orow = a.out + (int64_t)(it.row0 + node[c]) * a.ld_o + (int64_t)(kvh * g + col - node[c] * g) * D;
 #pragma unroll
         for (int b = 0; b < D / 16; ++b) {
@@ -292,23 +425,84 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     }
 }
 
+// The partial results of a tile joined, in order of the parts: one workgroup per (record, KV head, 16 columns), a thread per four dims
+// of a column and pass.  The kernel is all latency: kMergeBatch parts are asked for at a time.
+constexpr int kMergeBatch = 8;
+template <int D>
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_cols) {
+    TreeParts parts;
+    tree_parts(parts, a.workspace, a.n_kv, D, tile_cols);
+    const int kvh = blockIdx.x % a.n_kv, place = blockIdx.x / a.n_kv, g = a.n_q / a.n_kv;
+    if (place >= *parts.count) return;
+    const TreeRecord rec = parts.rec[place];
+    const int col0 = rec.tile * tile_cols, cols = min(16, rec.n * g - col0 - (int)blockIdx.y * 16);
+    const int64_t step = (int64_t)rec.step * a.n_kv * tile_cols, first = ((int64_t)rec.slot * a.n_kv + kvh) * tile_cols + blockIdx.y * 16;
+    for (int i = threadIdx.x; i < cols * (D / 4); i += 256) {
+        const int tcol = i / (D / 4), e = i % (D / 4) * 4;
+        float m = kNegBig, l = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        bool used = true;
+        for (int p0 = 0; p0 < rec.parts; p0 += kMergeBatch) {
+            f32x2 ml[kMergeBatch];
+            f32x4 o[kMergeBatch];
+#pragma unroll
+            for (int u = 0; u < kMergeBatch; ++u) {
+                const int64_t at = first + tcol + min(p0 + u, rec.parts - 1) * step;
+                ml[u] = parts.ml[at];
+                o[u] = *reinterpret_cast<const f32x4*>(parts.o + at * D + e);
+            }
+            float top = m;
+#pragma unroll
+            for (int u = 0; u < kMergeBatch; ++u) top = fmaxf(top, ml[u][0]);
+            const float down = __builtin_amdgcn_exp2f(m - top);
+            l *= down;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[v] *= down;
+            m = top;
+#pragma unroll
+            for (int u = 0; u < kMergeBatch; ++u) {
+                if (p0 + u >= rec.parts) continue;
+                const float w = __builtin_amdgcn_exp2f(ml[u][0] - m);
+                used = !(ml[u][1] < 0.f);
+                l += ml[u][1] * w;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[v] += o[u][v] * w;
+            }
+        }
+        const float inv = 1.0f / l;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[v] = used ? acc[v] * inv : 0.f;
+        const int col = col0 + blockIdx.y * 16 + tcol;
+        *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) =
+            __builtin_convertvector(acc, bf16x4);
+    }
+}
+
 }  // namespace
 
+// Columns of a tile.
+static int tree_tile_cols(int n_q, int n_kv, int max_nodes) { (void)n_q; (void)n_kv; (void)max_nodes; return 64; }
+
 size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes) {
-    (void)n_q; (void)n_kv; (void)d; (void)max_nodes;
-    return 256;
+    TreeParts t;
+    return tree_parts(t, nullptr, n_kv, d, tree_tile_cols(n_q, n_kv, max_nodes));
 }
 
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
     if (a.num_seqs <= 0 || a.num_rows <= 0) return hipSuccess;
-    const int g = a.n_q / a.n_kv;
-    // no more tiles than whole ones in all rows and a partly filled one per sequence
-    const int64_t items = (int64_t)a.num_rows * g / 64 + a.num_seqs;
-    if (items * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(items * a.n_kv));
+    const int g = a.n_q / a.n_kv, tile_cols = tree_tile_cols(a.n_q, a.n_kv, a.max_nodes);
+    // no more tiles than whole ones in all rows and a partly filled one per sequence; cutting the keys adds no more units than there
+    // are shares; and one place behind the last unit
+    const int64_t units = (int64_t)a.num_rows * g / tile_cols + a.num_seqs + tree_target(a.n_kv) + 1;
+    if (units * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(units * a.n_kv)), merge((unsigned)(tree_max_cut_tiles(a.n_kv) * a.n_kv), (unsigned)(tile_cols / 16));
     const int lds = tree_lds_bytes(a.max_nodes);
-    if (a.d == 128) tree_attention_kernel<128, 1><<<grid, 256, lds, stream>>>(a);
-    else if (a.d == 64) tree_attention_kernel<64, 1><<<grid, 256, lds, stream>>>(a);
-    else return hipErrorInvalidValue;
+    if (a.d == 128) {
+        tree_attention_kernel<128, 1><<<grid, 256, lds, stream>>>(a);
+        tree_merge_kernel<128><<<merge, 256, 0, stream>>>(a, tile_cols);
+    } else if (a.d == 64) {
+        tree_attention_kernel<64, 1><<<grid, 256, lds, stream>>>(a);
+        tree_merge_kernel<64><<<merge, 256, 0, stream>>>(a, tile_cols);
+    } else return hipErrorInvalidValue;
     return hipGetLastError();
 }
