@@ -425,6 +425,149 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     }
 }
 
+// Few columns (tiles of 16*NB): the keys are a stream from HBM, and each wave takes a run of the unit's blocks for all columns, operands
+// straight to registers as in decode attention (load_kv: score tile t is page t, a lane has keys 4G .. 4G+3 of both pages).  The
+// waves' results are joined through LDS, a group of 16 columns at a time.
+template <int D>
+struct StreamLds {
+    float o[4][16][D + 4];
+    float m[4][16], l[4][16];
+};
+template <int D, int NB>
+__global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeArgs a) {
+    constexpr int TILE = 16 * NB;
+    __shared__ StreamLds<D> join;
+    extern __shared__ uint32_t tree_words[];
+    const TreeLds tree(tree_words, a.max_nodes);
+    const int kvh = blockIdx.x % a.n_kv, g = a.n_q / a.n_kv;
+    TreeUnit it;
+    TreeParts parts;
+    tree_parts(parts, a.workspace, a.n_kv, D, TILE);
+    int cut_tiles;
+    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles, (int64_t*)tree.scratch)) {
+        if (blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, G = lane >> 4;
+    const int cols = it.n * g;
+    const int n_full = it.c / 32, last_page = max(it.c + it.n - 1, 0) / kPage;
+    const int run = (it.blk_end - it.blk_begin + 3) / 4;
+    const int b_begin = min(it.blk_begin + wave * run, it.blk_end), b_end = min(b_begin + run, it.blk_end);
+    const int32_t* bt = a.block_tables + (a.bt_off ? (int64_t)a.bt_off[it.seq] : (int64_t)it.seq * a.table_stride);
+    int ids_base = 2 * b_begin, ids = 0;  // page ids, one per lane
+    auto fetch_ids = [&](int base) {
+        ids_base = base;
+        ids = min(max(bt[min(base + lane, last_page)], 0), a.num_blocks - 1);
+    };
+    auto load_block = [&](KvFrag<D>& f, int blk) {
+        const int p0 = min(2 * blk, last_page) - ids_base, p1 = min(2 * blk + 1, last_page) - ids_base;
+        load_kv<D>(f, a.k_pool, a.v_pool, (int64_t)__builtin_amdgcn_readlane(ids, p0), (int64_t)__builtin_amdgcn_readlane(ids, p1), a.n_kv, kvh, lane);
+    };
+    KvFrag<D> fa, fb;
+    if (b_begin < b_end) {
+        fetch_ids(2 * b_begin);
+        load_block(fa, b_begin);
+    }
+    bf16x8 qf[NB][D / 32];
+    int node[NB];
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+        const int cc = min(it.tile * TILE + c * 16 + r, cols - 1);
+        node[c] = cc / g;
+        const bf16_t* qrow = a.q + (int64_t)(it.row0 + node[c]) * a.ld_q + (int64_t)(kvh * g + cc - node[c] * g) * D;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) qf[c][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (s * 4 + G) * 8));
+    }
+    const bool sees_tree = it.blk_begin < it.blk_end && it.blk_end > n_full;
+    if (sees_tree) tree_visibility(tree, a.parents + it.row0, it.n, it.c, a.max_nodes);
+    AttnState<D, NB> st;
+    init_state<D, NB>(st);
+    auto attend = [&](KvFrag<D>& f) {
+        float sc[NB][8];
+#pragma unroll
+        for (int c = 0; c < NB; ++c) score_group<D>(sc[c], f.k, qf[c]);
+        update_groups<D, NB, false>(st, sc, a.scale_log2, []() {}, [&]() -> const u32x4 (&)[D / 16] { return f.v; });
+    };
+    auto next_block = [&](KvFrag<D>& f, int blk) {
+        if (2 * blk + 1 >= ids_base + 64) fetch_ids(2 * blk);
+        load_block(f, blk);
+    };
+    // blocks that all columns see, the next one on its way; then the last ones
+    int blk = b_begin;
+    const int b_full = min(b_end, n_full);
+    while (blk + 1 < b_full) {
+        next_block(fb, blk + 1);
+        attend(fa);
+        if (blk + 2 < b_end) next_block(fa, blk + 2);
+        attend(fb);
+        blk += 2;
+    }
+    if (blk < b_full) {
+        attend(fa);
+        if (++blk < b_end) next_block(fa, blk);
+    }
+    while (blk < b_end) {
+        float sc[NB][8];
+        uint32_t seen[NB];
+        auto mine = [&](uint32_t word) { return (word >> (4 * G) & 15u) | (word >> (16 + 4 * G) & 15u) << 4; };
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+            score_group<D>(sc[c], fa.k, qf[c]);
+            seen[c] = mine(tree.vis[node[c] * tree.stride + blk - n_full]);
+            hide_scores(sc[c], seen[c]);
+        }
+        clean_values<D, NB>(fa.v, mine(tree.used[blk - n_full]), seen, st);
+        update_groups<D, NB, false>(st, sc, a.scale_log2, []() {}, [&]() -> const u32x4 (&)[D / 16] { return fa.v; });
+        if (++blk < b_end) next_block(fa, blk);
+    }
+    if (it.parts > 1 && kvh == 0 && threadIdx.x == 0) write_record(parts, it, cols, TILE);
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+        float l = st.l[c];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (c > 0) __syncthreads();
+        if (G == 0) {
+            join.m[wave][r] = st.m[c];
+            join.l[wave][r] = l;
+        }
+#pragma unroll
+        for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(&join.o[wave][r][b * 16 + G * 4]) = st.o[c][b];
+        __syncthreads();
+        const int col0 = it.tile * TILE + c * 16, here = min(16, cols - col0);
+        for (int i = threadIdx.x; i < here * (D / 4); i += 256) {
+            const int j = i / (D / 4), e = i % (D / 4) * 4, col = col0 + j, nd = col / g;
+            float m = kNegBig, ls = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m = fmaxf(m, join.m[w][j]);
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float x = __builtin_amdgcn_exp2f(join.m[w][j] - m);
+                const f32x4 o = *reinterpret_cast<const f32x4*>(&join.o[w][j][e]);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[v] += o[v] * x;
+                ls += join.l[w][j] * x;
+            }
+            const int at = (it.c & 31) + nd;
+            const bool used = sees_tree && tree.vis[nd * tree.stride + (at >> 5)] >> (at & 31) & 1;
+            if (it.parts > 1) {
+                const int64_t place = ((int64_t)it.slot * a.n_kv + kvh) * TILE + c * 16 + j;
+                *reinterpret_cast<f32x4*>(parts.o + place * D + e) = acc;
+                if (e == 0) parts.ml[place] = f32x2{m, it.part + 1 == it.parts && !used ? -1.f : ls};
+                continue;
+            }
+            const float inv = 1.0f / ls;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[v] = used ? acc[v] * inv : 0.f;
+            *reinterpret_cast<bf16x4*>(a.out + (int64_t)(it.row0 + nd) * a.ld_o + (int64_t)(kvh * g + col - nd * g) * D + e) =
+                __builtin_convertvector(acc, bf16x4);
+        }
+    }
+}
+
 // The partial results of a tile joined, in order of the parts: one workgroup per (record, KV head, 16 columns), a thread per four dims
 // of a column and pass.  The kernel is all latency: kMergeBatch parts are asked for at a time.
 constexpr int kMergeBatch = 8;
@@ -481,11 +624,24 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_co
 }  // namespace
 
 // Columns of a tile.
-static int tree_tile_cols(int n_q, int n_kv, int max_nodes) { (void)n_q; (void)n_kv; (void)max_nodes; return 64; }
+static int tree_tile_cols(int n_q, int n_kv, int max_nodes) {
+    const int64_t cols = (int64_t)max_nodes * (n_q / n_kv);
+    return cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
+}
 
 size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes) {
     TreeParts t;
     return tree_parts(t, nullptr, n_kv, d, tree_tile_cols(n_q, n_kv, max_nodes));
+}
+
+template <int D>
+static void launch_tree(const TreeArgs& a, int tile_cols, int64_t units, hipStream_t stream) {
+    const dim3 grid((unsigned)(units * a.n_kv)), merge((unsigned)(tree_max_cut_tiles(a.n_kv) * a.n_kv), (unsigned)(tile_cols / 16));
+    const int lds = tree_lds_bytes(a.max_nodes);
+    if (tile_cols == 16) tree_stream_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
+    else if (tile_cols == 32) tree_stream_kernel<D, 2><<<grid, 256, lds, stream>>>(a);
+    else tree_attention_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
+    tree_merge_kernel<D><<<merge, 256, 0, stream>>>(a, tile_cols);
 }
 
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
@@ -495,14 +651,8 @@ hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
     // are shares; and one place behind the last unit
     const int64_t units = (int64_t)a.num_rows * g / tile_cols + a.num_seqs + tree_target(a.n_kv) + 1;
     if (units * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(units * a.n_kv)), merge((unsigned)(tree_max_cut_tiles(a.n_kv) * a.n_kv), (unsigned)(tile_cols / 16));
-    const int lds = tree_lds_bytes(a.max_nodes);
-    if (a.d == 128) {
-        tree_attention_kernel<128, 1><<<grid, 256, lds, stream>>>(a);
-        tree_merge_kernel<128><<<merge, 256, 0, stream>>>(a, tile_cols);
-    } else if (a.d == 64) {
-        tree_attention_kernel<64, 1><<<grid, 256, lds, stream>>>(a);
-        tree_merge_kernel<64><<<merge, 256, 0, stream>>>(a, tile_cols);
-    } else return hipErrorInvalidValue;
+    if (a.d == 128) launch_tree<128>(a, tile_cols, units, stream);
+    else if (a.d == 64) launch_tree<64>(a, tile_cols, units, stream);
+    else return hipErrorInvalidValue;
     return hipGetLastError();
 }
