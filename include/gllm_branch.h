@@ -41,8 +41,7 @@ enum { GLLM_TREE_MAX_NODES = 256, GLLM_BEAM_MAX_BEAMS = 32, GLLM_BEAM_MAX_KEEP =
  *   k_pool,v_pool DEVICE bf16, one layer of the pool (layout: gllm_stage_bind_kv_pool), num_blocks pages, 16-byte aligned
  *   block_tables  DEVICE int32 [num_seqs][block_table_stride]; a page id outside [0, num_blocks) is read as the nearest one inside
  *   cached_len    DEVICE int32 [num_seqs]
- *   row_start     DEVICE int32 [num_seqs + 1], ascending, from 0 up to at most num_rows (sequences of more than num_rows rows together: no
- *                 row is written)
+ *   row_start     DEVICE int32 [num_seqs + 1], ascending, from 0 up to at most num_rows (otherwise no row is written)
  *   parents       DEVICE int32 [num_rows]
  *   max_nodes     HOST: most nodes of any tree, 1 .. 256; the kernels are chosen by it
  *   out           DEVICE bf16 [num_rows][ld_out] (ld_out a multiple of 4, 8-byte aligned)

@@ -26,37 +26,63 @@ struct TreeUnit {
 };
 
 // What the closure of a tree takes in LDS: rows of `stride` words per node (odd, so that neighbouring nodes lie in different
-// banks), the parent links, and the words of the nodes that are used.
-__host__ __device__ inline int tree_row_words(int max_nodes) { return (max_nodes / 32 + 2) | 1; }
-__host__ __device__ inline int tree_lds_bytes(int max_nodes) { return (kTreeNodes * tree_row_words(max_nodes) + kTreeNodes + 2 * (kTreeWords + 1) + 2 + 30) * 4; }
+// banks), the words of the nodes that are used, and, above 64 nodes, the parent links.
 struct TreeLds {
-    uint32_t* vis;    // [node][stride]: word w of a node: keys 32w .. 32w+31 behind the first key of block c / 32
-    int* up;          // [node]
+    uint32_t* vis;    // [nodes][stride]: word w of a node: keys 32w .. 32w+31 behind the first key of block c / 32
     uint32_t* used;   // [kTreeWords + 1], as a row of vis: all cached keys and all used nodes
     uint32_t* raw;    // [kTreeWords]
-    int* scratch;     // [30], on an 8-byte boundary
-    int stride;
-    __device__ TreeLds(void* p, int max_nodes) {
-        stride = tree_row_words(max_nodes);
-        vis = (uint32_t*)p;
-        up = (int*)(vis + kTreeNodes * stride);
-        used = (uint32_t*)(up + kTreeNodes);
+    int* up;          // [nodes]
+    int nodes, words, stride;
+    __host__ __device__ TreeLds(void* p, int max_nodes) {
+        nodes = max_nodes <= 64 ? max_nodes : kTreeNodes;
+        words = (max_nodes + 31) / 32 + 1;
+        stride = words | 1;
+        used = (uint32_t*)p;
         raw = used + kTreeWords + 1;
-        scratch = (int*)(((uintptr_t)(raw + kTreeWords + 1) + 7) & ~(uintptr_t)7);
+        vis = raw + kTreeWords;
+        up = (int*)(vis + nodes * stride);
     }
+    __host__ __device__ int bytes(int max_nodes) const { return (2 * kTreeWords + 1 + nodes * stride + (max_nodes > 64 ? nodes : 0)) * 4; }
 };
 
-// The words of all nodes of a tree of n <= max_nodes nodes behind c cached keys.  Every round joins to a node's set that of the
-// node at the end of its link and doubles the link: the depth of the tree is passed in log2 of it rounds.  A link that leads
-// to no root is -2 at the end, and the node's words are zero.  All 256 threads; ends with a barrier.
-__device__ __forceinline__ void tree_visibility(const TreeLds& t, const int32_t* __restrict__ parents, int n, int c, int max_nodes) {
-    const int i = threadIdx.x, words = (max_nodes + 31) / 32, sh = c & 31;
-    uint32_t* mine = t.vis + i * t.stride;
-    int p = -2;
-    if (i < n) {
-        const int given = parents[i];
-        p = given >= -1 && given < i ? given : -2;
+// The words of all nodes of a tree of n nodes behind c cached keys.  Every round joins to a node's set that of the node at the
+// end of its link and doubles the link: a tree is done in log2 of its depth rounds.  A link that leads to no root is -2 at the
+// end, and the node's words are zero.
+//
+// Up to 64 nodes, one per lane: every wave does it for itself, in registers, and all write the same words (no barrier).
+__device__ __forceinline__ void tree_visibility_wave(const TreeLds& t, int given, int n, int c) {
+    const int i = threadIdx.x & 63, sh = c & 31;
+    int p = i < n && given >= -1 && given < i ? given : -2;
+    uint64_t set = 1ull << i;
+    while (__any(p >= 0)) {
+        const int from = max(p, 0);
+        const uint32_t lo = __shfl((int)(uint32_t)set, from), hi = __shfl((int)(uint32_t)(set >> 32), from);
+        const int next = __shfl(p, from);
+        if (p >= 0) {
+            set |= (uint64_t)hi << 32 | lo;
+            p = next;
+        }
     }
+    const uint64_t used = __ballot(p == -1);
+    const uint32_t prefix = (1u << sh) - 1u;  // every used node sees the cached keys of the first block
+    auto words = [&](uint64_t bits, uint32_t* to, bool on) {
+        const uint32_t lo = (uint32_t)bits, hi = (uint32_t)(bits >> 32);
+        to[0] = on ? lo << sh | prefix : 0u;
+        if (t.words > 1) to[1] = on ? (uint32_t)(bits << sh >> 32) : 0u;
+        if (t.words > 2) to[2] = on && sh ? hi >> (32 - sh) : 0u;
+    };
+    if (i < t.nodes) words(set, t.vis + i * t.stride, p == -1);
+    if (i == 0) words(used, t.used, true);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Up to 256 nodes, one per thread; ends with a barrier.
+__device__ __forceinline__ void tree_visibility_group(const TreeLds& t, int given, int n, int c) {
+    const int i = threadIdx.x, words = t.words - 1, sh = c & 31;
+    uint32_t* mine = t.vis + i * t.stride;
+    int p = i < n && given >= -1 && given < i ? given : -2;
     t.up[i] = p;
     for (int w = 0; w < words; ++w) mine[w] = w == i >> 5 ? 1u << (i & 31) : 0u;
     __syncthreads();
@@ -65,10 +91,12 @@ __device__ __forceinline__ void tree_visibility(const TreeLds& t, const int32_t*
         int next = p;
         if (p >= 0) {
             next = t.up[p];
+#pragma unroll
             for (int w = 0; w < kTreeWords; ++w) b[w] = w < words ? t.vis[p * t.stride + w] : 0u;
         }
         if (!__syncthreads_or(p >= 0)) break;
         if (p >= 0) {
+#pragma unroll
             for (int w = 0; w < kTreeWords; ++w)
                 if (w < words) mine[w] |= b[w];
             t.up[i] = next;
@@ -97,13 +125,23 @@ __device__ __forceinline__ void tree_visibility(const TreeLds& t, const int32_t*
     __syncthreads();
 }
 
+// The parent of this thread's node, fetched in front of the rest; all threads call the other with it.
+__device__ __forceinline__ int tree_parent(const TreeArgs& a, int row0, int n) {
+    const int i = a.max_nodes <= 64 ? threadIdx.x & 63 : threadIdx.x;
+    return i < n ? a.parents[row0 + i] : -2;
+}
+__device__ __forceinline__ void tree_visibility(const TreeArgs& a, const TreeLds& t, int given, int n, int c) {
+    if (a.max_nodes <= 64) tree_visibility_wave(t, given, n, c);
+    else tree_visibility_group(t, given, n, c);
+}
+
 // ---- the plan, made by every workgroup for itself -----------------------------------------------------------------------
 //
 // The lengths stand on the device.  The keys of a sequence are cut into parts of at most `share` blocks, equal to within one
 // block, so that all parts of all sequences come to about kTreeTarget workgroups; units are ordered by sequence, part and tile:
 // the tiles of a part, neighbours in the launch but for the KV heads, read the same keys at the same time.
 constexpr int kTreeTarget = 1024;     // workgroups that the keys are cut into, over all KV heads
-constexpr int kTreeMinShare = 4;      // fewest blocks worth a workgroup
+constexpr int kTreeMinShare = 8;      // fewest blocks worth a workgroup
 constexpr int tree_target(int n_kv) { return kTreeTarget / n_kv > 0 ? kTreeTarget / n_kv : 1; }
 // Units with partial results: a sequence is cut where it has more blocks than a share, and then into fewer parts than twice its
 // blocks by the share; a share is at least the blocks of all tiles by the target.
@@ -113,105 +151,88 @@ constexpr int tree_max_cut_tiles(int n_kv) { return tree_target(n_kv); }
 
 struct SeqPlan {
     int32_t row0, n, c, tiles, blocks;
+    bool bad;  // its rows break the order of the rows
 };
 __device__ __forceinline__ SeqPlan seq_plan(const TreeArgs& a, int s, int tile_cols) {
-    SeqPlan p{0, 0, 0, 0, 0};
+    SeqPlan p{0, 0, 0, 0, 0, false};
     if (s >= a.num_seqs) return p;
     const int r0 = a.row_begin[s], r1 = a.row_end[s];
     p.c = a.cached_len[s];
-    if (r0 < 0 || r1 <= r0 || r1 > a.num_rows) return p;
+    p.bad = r0 < 0 || r1 < r0 || r1 > a.num_rows;
     p.row0 = r0;
-    p.n = r1 - r0;
+    p.n = p.bad ? 0 : r1 - r0;
     p.tiles = (p.n * (a.n_q / a.n_kv) + tile_cols - 1) / tile_cols;  // (num_rows * group fits 31 bits: the launcher)
-    if (p.n <= a.max_nodes && p.c >= 0 && (int64_t)p.c + p.n <= (int64_t)a.table_stride * kPage) p.blocks = (p.c + p.n + 31) / 32;
+    if (p.n > 0 && p.n <= a.max_nodes && p.c >= 0 && (int64_t)p.c + p.n <= (int64_t)a.table_stride * kPage) p.blocks = (p.c + p.n + 31) / 32;
     return p;
 }
 
-struct Two {
-    int64_t x, y;
-};
-// Sums over the 256 threads, of all of them and (`before`) of those in front; scratch: 8 words of 8 bytes.  Two barriers.
-__device__ __forceinline__ Two scan_threads(Two v, Two& before, int64_t* scratch) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Two sum = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const Two up = {__shfl_up(sum.x, o), __shfl_up(sum.y, o)};
-        if (lane >= o) {
-            sum.x += up.x;
-            sum.y += up.y;
-        }
-    }
-    __syncthreads();
-    if (lane == 63) {
-        scratch[wave] = sum.x;
-        scratch[4 + wave] = sum.y;
-    }
-    __syncthreads();
-    before = Two{sum.x - v.x, sum.y - v.y};
-    for (int w = 0; w < wave; ++w) {
-        before.x += scratch[w];
-        before.y += scratch[4 + w];
-    }
-    return Two{scratch[0] + scratch[1] + scratch[2] + scratch[3], scratch[4] + scratch[5] + scratch[6] + scratch[7]};
+// Sums over a wave by lane shifts, lane 63 has all of them; x of a lane becomes that of it and the lanes in front.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int lanes_below(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <typename T, int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(T& x) { x += __builtin_bit_cast(T, lanes_below<CTRL, ROWS>(__builtin_bit_cast(int, x))); }
+template <typename T>
+__device__ __forceinline__ void scan_wave(T& x) {
+    scan_step<T, 0x111, 0xf>(x);  // by 1, 2, 4 and 8 lanes in a row of 16
+    scan_step<T, 0x112, 0xf>(x);
+    scan_step<T, 0x114, 0xf>(x);
+    scan_step<T, 0x118, 0xf>(x);
+    scan_step<T, 0x142, 0xa>(x);  // the last lane of a row to the next row, of both to the upper half
+    scan_step<T, 0x143, 0xc>(x);
 }
+__device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// The unit of place `place`; false behind the last one, with the number of tiles whose keys are cut in `cut_tiles`.
-__device__ __forceinline__ bool tree_unit(const TreeArgs& a, int place, int tile_cols, TreeUnit& u, int& cut_tiles, int64_t* scratch) {
-    Two before, total = {0, 0};  // blocks of all tiles, rows
-    const SeqPlan p = seq_plan(a, threadIdx.x, tile_cols);
-    for (int s0 = 0; s0 < a.num_seqs; s0 += 256) {
-        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + threadIdx.x, tile_cols);
-        const Two t = scan_threads(Two{(int64_t)q.tiles * q.blocks, q.n}, before, scratch);
-        total.x += t.x;
-        total.y += t.y;
+// The unit of place `place`; false behind the last one, with the number of tiles whose keys are cut in `cut_tiles`.  Every wave
+// works it out for itself, 64 sequences at a time, without LDS and barriers; all of them with the same arithmetic.
+__device__ __forceinline__ bool tree_unit(const TreeArgs& a, int place, int tile_cols, TreeUnit& u, int& cut_tiles) {
+    const int lane = threadIdx.x & 63;
+    const SeqPlan p = seq_plan(a, lane, tile_cols);
+    float total = 0.f;  // blocks of all tiles
+    bool bad = false;
+    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
+        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + lane, tile_cols);
+        float t = (float)q.tiles * (float)q.blocks;
+        scan_wave(t);
+        total += __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, t), 63));
+        bad |= __any(q.bad);
     }
     cut_tiles = 0;
-    if (total.y > a.num_rows) return false;  // sequences that share rows: the launch has no place for their units
-    const int target = tree_target(a.n_kv);
-    const int share = (int)min(max((total.x + target - 1) / target, (int64_t)kTreeMinShare), (int64_t)INT32_MAX);
-    int64_t units = 0, cut = 0;  // cut: units in the lower half, tiles in the upper one
-    int* found = (int*)(scratch + 8);
-    for (int s0 = 0; s0 < a.num_seqs; s0 += 256) {
-        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + threadIdx.x, tile_cols);
-        const int parts = max(1, (int)(((int64_t)q.blocks + share - 1) / share));
-        const int64_t mine = (int64_t)q.tiles * parts;
-        if (threadIdx.x == 0) found[0] = -1;
-        const Two all = scan_threads(Two{mine, parts > 1 ? mine | (int64_t)q.tiles << 32 : 0}, before, scratch);
-        const int64_t at = place - units - before.x;
-        if (at >= 0 && at < mine) {
-            found[0] = s0 + threadIdx.x;
-            found[1] = (int)at;
-            found[2] = q.row0;
-            found[3] = q.n;
-            found[4] = q.c;
-            found[5] = q.blocks;
-            found[6] = parts;
-            found[7] = (int)(uint32_t)(cut + before.y);
-            found[8] = q.tiles;
-            found[9] = (int)((cut + before.y) >> 32);
-        }
-        __syncthreads();
-        if (found[0] >= 0) {
-            const int i = found[1], tiles = found[8], blocks = found[5];
-            u.seq = found[0];
-            u.row0 = found[2];
-            u.n = found[3];
-            u.c = found[4];
-            u.parts = found[6];
+    if (bad) return false;  // rows in no order may belong to two sequences: the launch would have no place for their units
+    const float target = (float)tree_target(a.n_kv);
+    // (the sum is exact up to 2^24, and more than it by then: a share is never less than the blocks by the target)
+    const float even = total < 16777216.f ? ceilf(total / target) : total / target * 1.0001f + 1.f;
+    const int share = (int)fminf(fmaxf(even, (float)kTreeMinShare), 1e9f);
+    int units = 0, slots = 0;
+    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
+        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + lane, tile_cols);
+        const int parts = max(1, (q.blocks - 1) / share + 1), mine = q.tiles * parts;
+        const bool cut = parts > 1;
+        int upto = mine, cut_upto = cut ? mine : 0, tiles_upto = cut ? q.tiles : 0;
+        scan_wave(upto);
+        scan_wave(cut_upto);
+        scan_wave(tiles_upto);
+        const int at = place - units - (upto - mine);
+        const uint64_t who = __ballot(at >= 0 && at < mine);
+        if (who) {
+            const int l = __builtin_ctzll(who), i = lane_value(at, l), tiles = lane_value(q.tiles, l), blocks = lane_value(q.blocks, l);
+            u.seq = s0 + l;
+            u.row0 = lane_value(q.row0, l);
+            u.n = lane_value(q.n, l);
+            u.c = lane_value(q.c, l);
+            u.parts = lane_value(parts, l);
             u.part = i / tiles;
-            u.tile = i % tiles;
-            u.slot = found[7] + i;
-            u.cut_tile = found[9] + u.tile;
-            u.blk_begin = (int)((int64_t)blocks * u.part / u.parts);
-            u.blk_end = (int)((int64_t)blocks * (u.part + 1) / u.parts);
+            u.tile = i - u.part * tiles;
+            u.slot = slots + lane_value(cut_upto - (cut ? mine : 0), l) + i;
+            u.cut_tile = cut_tiles + lane_value(tiles_upto - (cut ? q.tiles : 0), l) + u.tile;
+            const int each = blocks / u.parts, more = blocks - each * u.parts;  // the first `more` parts have a block more
+            u.blk_begin = u.part * each + min(u.part, more);
+            u.blk_end = u.blk_begin + each + (u.part < more);
             return true;
         }
-        units += all.x;
-        cut += all.y;
-        __syncthreads();
+        units += lane_value(upto, 63);
+        slots += lane_value(cut_upto, 63);
+        cut_tiles += lane_value(tiles_upto, 63);
     }
-    cut_tiles = (int)(cut >> 32);
     return false;
 }
 
@@ -304,7 +325,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     TreeParts parts;
     tree_parts(parts, a.workspace, a.n_kv, D, TILE);
     int cut_tiles;
-    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles, (int64_t*)tree.scratch)) {
+    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles)) {
         if (blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
         return;
     }
@@ -371,7 +392,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
                 });
         };
         const bool sees_tree = it.blk_end > n_full;  // (one part at least: its last block holds the last node)
-        if (sees_tree) tree_visibility(tree, a.parents + it.row0, it.n, it.c, a.max_nodes);
+        if (sees_tree) tree_visibility(a, tree, tree_parent(a, it.row0, it.n), it.n, it.c);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
             if (!sees_tree) continue;
@@ -444,7 +465,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
     TreeParts parts;
     tree_parts(parts, a.workspace, a.n_kv, D, TILE);
     int cut_tiles;
-    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles, (int64_t*)tree.scratch)) {
+    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles)) {
         if (blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
         return;
     }
@@ -481,7 +502,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
         for (int s = 0; s < D / 32; ++s) qf[c][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (s * 4 + G) * 8));
     }
     const bool sees_tree = it.blk_begin < it.blk_end && it.blk_end > n_full;
-    if (sees_tree) tree_visibility(tree, a.parents + it.row0, it.n, it.c, a.max_nodes);
+    if (sees_tree) tree_visibility(a, tree, tree_parent(a, it.row0, it.n), it.n, it.c);
     AttnState<D, NB> st;
     init_state<D, NB>(st);
     auto attend = [&](KvFrag<D>& f) {
@@ -568,57 +589,55 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
     }
 }
 
-// The partial results of a tile joined, in order of the parts: one workgroup per (record, KV head, 16 columns), a thread per four dims
-// of a column and pass.  The kernel is all latency: kMergeBatch parts are asked for at a time.
-constexpr int kMergeBatch = 8;
+// The partial results of a tile joined, in order of the parts: one workgroup per (record, KV head, 1024 / D columns), a thread per four
+// dims of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time.
+constexpr int kMergeBatch = 12;
+constexpr int merge_cols(int d) { return 1024 / d; }
 template <int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_cols) {
     TreeParts parts;
     tree_parts(parts, a.workspace, a.n_kv, D, tile_cols);
     const int kvh = blockIdx.x % a.n_kv, place = blockIdx.x / a.n_kv, g = a.n_q / a.n_kv;
-    if (place >= *parts.count) return;
-    const TreeRecord rec = parts.rec[place];
-    const int col0 = rec.tile * tile_cols, cols = min(16, rec.n * g - col0 - (int)blockIdx.y * 16);
-    const int64_t step = (int64_t)rec.step * a.n_kv * tile_cols, first = ((int64_t)rec.slot * a.n_kv + kvh) * tile_cols + blockIdx.y * 16;
-    for (int i = threadIdx.x; i < cols * (D / 4); i += 256) {
-        const int tcol = i / (D / 4), e = i % (D / 4) * 4;
-        float m = kNegBig, l = 0.f;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        bool used = true;
-        for (int p0 = 0; p0 < rec.parts; p0 += kMergeBatch) {
-            f32x2 ml[kMergeBatch];
-            f32x4 o[kMergeBatch];
+    const int count = *parts.count;
+    const TreeRecord rec = parts.rec[place];  // (behind the last one: anything)
+    if (place >= count) return;
+    const int tcol = blockIdx.y * merge_cols(D) + threadIdx.x / (D / 4), e = threadIdx.x % (D / 4) * 4, col = rec.tile * tile_cols + tcol;
+    if (col >= rec.n * g) return;
+    const int64_t step = (int64_t)rec.step * a.n_kv * tile_cols, first = ((int64_t)rec.slot * a.n_kv + kvh) * tile_cols + tcol;
+    float m = kNegBig, l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    bool used = true;
+    for (int p0 = 0; p0 < rec.parts; p0 += kMergeBatch) {
+        f32x2 ml[kMergeBatch];
+        f32x4 o[kMergeBatch];
 #pragma unroll
-            for (int u = 0; u < kMergeBatch; ++u) {
-                const int64_t at = first + tcol + min(p0 + u, rec.parts - 1) * step;
-                ml[u] = parts.ml[at];
-                o[u] = *reinterpret_cast<const f32x4*>(parts.o + at * D + e);
-            }
-            float top = m;
-#pragma unroll
-            for (int u = 0; u < kMergeBatch; ++u) top = fmaxf(top, ml[u][0]);
-            const float down = __builtin_amdgcn_exp2f(m - top);
-            l *= down;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] *= down;
-            m = top;
-#pragma unroll
-            for (int u = 0; u < kMergeBatch; ++u) {
-                if (p0 + u >= rec.parts) continue;
-                const float w = __builtin_amdgcn_exp2f(ml[u][0] - m);
-                used = !(ml[u][1] < 0.f);
-                l += ml[u][1] * w;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[v] += o[u][v] * w;
-            }
+        for (int u = 0; u < kMergeBatch; ++u) {
+            const int64_t at = first + min(p0 + u, rec.parts - 1) * step;
+            ml[u] = parts.ml[at];
+            o[u] = *reinterpret_cast<const f32x4*>(parts.o + at * D + e);
         }
-        const float inv = 1.0f / l;
+        float top = m;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) acc[v] = used ? acc[v] * inv : 0.f;
-        const int col = col0 + blockIdx.y * 16 + tcol;
-        *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) =
-            __builtin_convertvector(acc, bf16x4);
+        for (int u = 0; u < kMergeBatch; ++u) top = fmaxf(top, ml[u][0]);
+        const float down = __builtin_amdgcn_exp2f(m - top);
+        l *= down;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[v] *= down;
+        m = top;
+#pragma unroll
+        for (int u = 0; u < kMergeBatch; ++u) {
+            if (p0 + u >= rec.parts) continue;
+            const float w = __builtin_amdgcn_exp2f(ml[u][0] - m);
+            used = !(ml[u][1] < 0.f);
+            l += ml[u][1] * w;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[v] += o[u][v] * w;
+        }
     }
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) acc[v] = used ? acc[v] * inv : 0.f;
+    *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) = __builtin_convertvector(acc, bf16x4);
 }
 
 }  // namespace
@@ -636,12 +655,13 @@ size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes) {
 
 template <int D>
 static void launch_tree(const TreeArgs& a, int tile_cols, int64_t units, hipStream_t stream) {
-    const dim3 grid((unsigned)(units * a.n_kv)), merge((unsigned)(tree_max_cut_tiles(a.n_kv) * a.n_kv), (unsigned)(tile_cols / 16));
-    const int lds = tree_lds_bytes(a.max_nodes);
+    const dim3 grid((unsigned)(units * a.n_kv)), merge((unsigned)(tree_max_cut_tiles(a.n_kv) * a.n_kv), (unsigned)ceil_div(tile_cols, merge_cols(D)));
+    const int lds = TreeLds(nullptr, a.max_nodes).bytes(a.max_nodes);
     if (tile_cols == 16) tree_stream_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
     else if (tile_cols == 32) tree_stream_kernel<D, 2><<<grid, 256, lds, stream>>>(a);
     else tree_attention_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
-    tree_merge_kernel<D><<<merge, 256, 0, stream>>>(a, tile_cols);
+    // no sequence can be cut whose table has no more pages than the fewest blocks of a part
+    if (a.table_stride > 2 * kTreeMinShare) tree_merge_kernel<D><<<merge, 256, 0, stream>>>(a, tile_cols);
 }
 
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
