@@ -317,9 +317,10 @@ __device__ __forceinline__ void clean_values(u32x4 (&vf)[D / 16], uint32_t keep,
 template <int D, int NB>
 __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     constexpr int PAGE_BYTES = D * kPage * 2, IPB = PAGE_BYTES / 1024, NS = kTreeStages, TILE = 64 * NB;
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[NS][4][PAGE_BYTES];  // [stage][K0,K1,V0,V1]
-    extern __shared__ uint32_t tree_words[];
-    const TreeLds tree(tree_words, a.max_nodes);
+    // (one LDS object: with a second one the compiler waits for all loads into the ring before it reads from it)
+    extern __shared__ __attribute__((aligned(1024))) unsigned char tree_lds[];
+    auto& ring = *reinterpret_cast<unsigned char(*)[NS][4][PAGE_BYTES]>(tree_lds);  // [stage][K0,K1,V0,V1]
+    const TreeLds tree(tree_lds + NS * 4 * PAGE_BYTES, a.max_nodes);
     const int kvh = blockIdx.x % a.n_kv, g = a.n_q / a.n_kv;
     TreeUnit it;
     TreeParts parts;
@@ -354,7 +355,14 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
         const int32_t* bt = a.block_tables + (a.bt_off ? (int64_t)a.bt_off[it.seq] : (int64_t)it.seq * a.table_stride);
         // wave w brings in piece w of a block: K page 0, K page 1, V page 0, V page 1
         const bf16_t* pool = wave < 2 ? a.k_pool : a.v_pool;
-        auto page_id = [&](int blk) -> int { return min(max(bt[min(blk * 2 + (wave & 1), last_page)], 0), a.num_blocks - 1); };
+        // this wave's pages of 64 blocks, one per lane.  (A load per block would be waited for behind the loads into the ring, which come
+        // back in order: all of them would have to be there)
+        int ids_base = 0, ids = 0;
+        auto fetch_ids = [&](int blk) {
+            ids_base = blk;
+            ids = min(max(bt[min((blk + lane) * 2 + (wave & 1), last_page)], 0), a.num_blocks - 1);
+        };
+        auto page_id = [&](int blk) -> int { return __builtin_amdgcn_readlane(ids, blk - ids_base); };
         auto issue_block = [&](int64_t page, int stage) {
             const int src_lane = wave == 1 ? lane ^ 4 : lane;  // K page 1 lies four slots shifted, against bank conflicts
             const char* src = reinterpret_cast<const char*>(pool + (page * a.n_kv + kvh) * (int64_t)(D * kPage)) + src_lane * 16;
@@ -401,20 +409,27 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
         }
         // every wave always issues its piece (indices past the end read the last page again into a stage nobody reads), so the
         // count of outstanding loads is the same in every iteration
+        fetch_ids(it.blk_begin);
 #pragma unroll
         for (int i = 0; i < NS - 1; ++i) issue_block(page_id(it.blk_begin + i), i);
-        int pid_next = page_id(it.blk_begin + NS - 1);
         const bool idle = it.tile * TILE + wave * NB * 16 >= cols;  // (the same for the wave)
         const int nblk = it.blk_end - it.blk_begin;
-        for (int i = 0; i < nblk; ++i) {
-            const int blk = it.blk_begin + i;
+        auto advance = [&](int i) {
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * IPB) : "memory");
-            __syncthreads();  // block blk has landed; nobody reads the stage of the block before it any more
-            issue_block(pid_next, (i + NS - 1) % NS);
-            pid_next = page_id(blk + NS);
-            if (idle) continue;
-            if (blk < n_full) block_step(i % NS, blk, std::false_type{});
-            else block_step(i % NS, blk, std::true_type{});
+            __syncthreads();  // block i has landed; nobody reads the stage of the block before it any more
+            const int next = it.blk_begin + i + NS - 1;
+            if (next >= ids_base + 64) fetch_ids(next);
+            issue_block(page_id(next), (i + NS - 1) % NS);
+        };
+        // blocks that all columns see, then the last ones
+        const int full = min(nblk, max(n_full - it.blk_begin, 0));
+        for (int i = 0; i < full; ++i) {
+            advance(i);
+            if (!idle) block_step(i % NS, it.blk_begin + i, std::false_type{});
+        }
+        for (int i = full; i < nblk; ++i) {
+            advance(i);
+            if (!idle) block_step(i % NS, it.blk_begin + i, std::true_type{});
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no LDS fill may outlive the workgroup
     }
@@ -645,7 +660,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_co
 // Columns of a tile.
 static int tree_tile_cols(int n_q, int n_kv, int max_nodes) {
     const int64_t cols = (int64_t)max_nodes * (n_q / n_kv);
-    return cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
+    return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
 }
 
 size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes) {
@@ -656,10 +671,11 @@ size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes) {
 template <int D>
 static void launch_tree(const TreeArgs& a, int tile_cols, int64_t units, hipStream_t stream) {
     const dim3 grid((unsigned)(units * a.n_kv)), merge((unsigned)(tree_max_cut_tiles(a.n_kv) * a.n_kv), (unsigned)ceil_div(tile_cols, merge_cols(D)));
-    const int lds = TreeLds(nullptr, a.max_nodes).bytes(a.max_nodes);
+    const int lds = TreeLds(nullptr, a.max_nodes).bytes(a.max_nodes), ring = kTreeStages * 4 * D * kPage * 2;
     if (tile_cols == 16) tree_stream_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
     else if (tile_cols == 32) tree_stream_kernel<D, 2><<<grid, 256, lds, stream>>>(a);
-    else tree_attention_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
+    else if (tile_cols == 64) tree_attention_kernel<D, 1><<<grid, 256, ring + lds, stream>>>(a);
+    else tree_attention_kernel<D, 2><<<grid, 256, ring + lds, stream>>>(a);
     // no sequence can be cut whose table has no more pages than the fewest blocks of a part
     if (a.table_stride > 2 * kTreeMinShare) tree_merge_kernel<D><<<merge, 256, 0, stream>>>(a, tile_cols);
 }
