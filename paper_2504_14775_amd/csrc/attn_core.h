@@ -113,11 +113,9 @@ __device__ __forceinline__ void mask_scores(float (&sc)[8], int key0, int key1, 
 // textbook order): the memory-bound decode kernel, with one group per wave, gains nothing from deferring.
 constexpr float kRefSlack = 64.0f;
 
-// issue_v() is called before the exponentials (a caller that fetches V from LDS starts its reads there),
-// get_v() after them (it returns the fragments, waiting for them if need be).
-template <int D, int NB, bool DEFER, typename IssueV, typename GetV>
-__device__ __forceinline__ void update_groups(AttnState<D, NB>& st, const float (&sc)[NB][8], float scale_log2,
-                                              IssueV&& issue_v, GetV&& get_v) {
+// Moves the references for the scores of a block.
+template <int D, int NB, bool DEFER>
+__device__ __forceinline__ void raise_reference(AttnState<D, NB>& st, const float (&sc)[NB][8], float scale_log2) {
     float lm[NB];
     bool low = false;
 #pragma unroll
@@ -143,8 +141,10 @@ __device__ __forceinline__ void update_groups(AttnState<D, NB>& st, const float 
             st.m[c] = m_new;
         }
     }
-    issue_v();
-    bf16x8 pb[NB];
+}
+// The weights of the block by the present references, the operand of the P.V product, and their sums.
+template <int D, int NB>
+__device__ __forceinline__ void block_weights(AttnState<D, NB>& st, const float (&sc)[NB][8], float scale_log2, bf16x8 (&pb)[NB]) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
         f32x8 p;
@@ -157,6 +157,17 @@ __device__ __forceinline__ void update_groups(AttnState<D, NB>& st, const float 
         st.l[c] += psum;
         pb[c] = __builtin_convertvector(p, bf16x8);
     }
+}
+
+// issue_v() is called before the exponentials (a caller that fetches V from LDS starts its reads there),
+// get_v() after them (it returns the fragments, waiting for them if need be).
+template <int D, int NB, bool DEFER, typename IssueV, typename GetV>
+__device__ __forceinline__ void update_groups(AttnState<D, NB>& st, const float (&sc)[NB][8], float scale_log2,
+                                              IssueV&& issue_v, GetV&& get_v) {
+    raise_reference<D, NB, DEFER>(st, sc, scale_log2);
+    issue_v();
+    bf16x8 pb[NB];
+    block_weights<D, NB>(st, sc, scale_log2, pb);
     const u32x4 (&vf)[D / 16] = get_v();
 #pragma unroll
     for (int b = 0; b < D / 16; ++b)

@@ -10,6 +10,8 @@
 // Everything in front is seen by all columns and goes through a loop without masks.
 #include "attn_core.h"
 
+#include <atomic>
+
 namespace {
 
 constexpr int kTreeNodes = 256;             // most nodes of a tree: one per thread
@@ -138,16 +140,19 @@ __device__ __forceinline__ void tree_visibility(const TreeArgs& a, const TreeLds
 // ---- the plan, made by every workgroup for itself -----------------------------------------------------------------------
 //
 // The lengths stand on the device.  The keys of a sequence are cut into parts of at most `share` blocks, equal to within one
-// block, so that all parts of all sequences come to about kTreeTarget workgroups; units are ordered by sequence, part and tile:
-// the tiles of a part, neighbours in the launch but for the KV heads, read the same keys at the same time.
-constexpr int kTreeTarget = 1024;     // workgroups that the keys are cut into, over all KV heads
+// block, so that all parts of all sequences come to about tree_target workgroups; the tiles of a part, neighbours in the launch but for
+// the KV heads, read the same keys at the same time.
 constexpr int kTreeMinShare = 8;      // fewest blocks worth a workgroup
-constexpr int tree_target(int n_kv) { return kTreeTarget / n_kv > 0 ? kTreeTarget / n_kv : 1; }
+// Workgroups that the keys are cut into, over all KV heads: as many as run at one time.  Every part of a tile writes and reads partial
+// results of (d + 2) floats a column, at 64 columns as much as four blocks of keys.  us at 512 / 768 / 1024 / 2048: one sequence of 30000
+// keys, 64 nodes (8B heads) 58 / 69 / 75 / 98, 64 sequences of 500 to 4000 keys, 8 nodes (70B heads) 108 / 118 / 118 / 131.  Of 16 columns they
+// are small, and shorter parts fill the end of the launch better: 32 single tokens behind 300 to 20000 keys 105 / 102 / 103 / 107.
+constexpr int tree_target(int n_kv, int tile_cols) { return (tile_cols == 16 ? 768 : 512) / n_kv > 0 ? (tile_cols == 16 ? 768 : 512) / n_kv : 1; }
 // Units with partial results: a sequence is cut where it has more blocks than a share, and then into fewer parts than twice its
 // blocks by the share; a share is at least the blocks of all tiles by the target.
-constexpr int tree_max_slots(int n_kv) { return 2 * tree_target(n_kv); }
+constexpr int tree_max_slots(int n_kv, int tile_cols) { return 2 * tree_target(n_kv, tile_cols); }
 // (and their tiles: every one of them has more blocks than a share)
-constexpr int tree_max_cut_tiles(int n_kv) { return tree_target(n_kv); }
+constexpr int tree_max_cut_tiles(int n_kv, int tile_cols) { return tree_target(n_kv, tile_cols); }
 
 struct SeqPlan {
     int32_t row0, n, c, tiles, blocks;
@@ -198,20 +203,49 @@ __device__ __forceinline__ bool tree_unit(const TreeArgs& a, int place, int tile
     }
     cut_tiles = 0;
     if (bad) return false;  // rows in no order may belong to two sequences: the launch would have no place for their units
-    const float target = (float)tree_target(a.n_kv);
+    const float target = (float)tree_target(a.n_kv, tile_cols);
     // (the sum is exact up to 2^24, and more than it by then: a share is never less than the blocks by the target)
     const float even = total < 16777216.f ? ceilf(total / target) : total / target * 1.0001f + 1.f;
     const int share = (int)fminf(fmaxf(even, (float)kTreeMinShare), 1e9f);
-    int units = 0, slots = 0;
+    // Units in order of their size, in quarters of a share, so that the last workgroups to start are short ones; in a quarter by
+    // sequence, part and tile.
+    auto split = [&](const SeqPlan& q, int& parts, int& quarter) {
+        parts = max(1, (q.blocks - 1) / share + 1);
+        const int size = (q.blocks - 1) / parts + 1;
+        quarter = 4 * (int64_t)size > 3 * (int64_t)share ? 0 : 2 * (int64_t)size > share ? 1 : 4 * (int64_t)size > share ? 2 : 3;
+        return q.tiles * parts;
+    };
+    int at_quarter[4] = {0, 0, 0, 0};  // units of the quarters in front, then of the sequences in front too
     for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
         const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + lane, tile_cols);
-        const int parts = max(1, (q.blocks - 1) / share + 1), mine = q.tiles * parts;
+        int parts, quarter;
+        const int mine = split(q, parts, quarter);
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+            int x = quarter == c ? mine : 0;
+            scan_wave(x);
+            at_quarter[c + 1] += lane_value(x, 63);
+        }
+    }
+    at_quarter[2] += at_quarter[1];
+    at_quarter[3] += at_quarter[2];
+    int slots = 0;
+    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
+        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + lane, tile_cols);
+        int parts, quarter, before = 0;
+        const int mine = split(q, parts, quarter);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            int x = quarter == c ? mine : 0;
+            scan_wave(x);
+            if (quarter == c) before = at_quarter[c] + x - mine;
+            at_quarter[c] += lane_value(x, 63);
+        }
         const bool cut = parts > 1;
-        int upto = mine, cut_upto = cut ? mine : 0, tiles_upto = cut ? q.tiles : 0;
-        scan_wave(upto);
+        int cut_upto = cut ? mine : 0, tiles_upto = cut ? q.tiles : 0;
         scan_wave(cut_upto);
         scan_wave(tiles_upto);
-        const int at = place - units - (upto - mine);
+        const int at = place - before;
         const uint64_t who = __ballot(at >= 0 && at < mine);
         if (who) {
             const int l = __builtin_ctzll(who), i = lane_value(at, l), tiles = lane_value(q.tiles, l), blocks = lane_value(q.blocks, l);
@@ -229,7 +263,6 @@ __device__ __forceinline__ bool tree_unit(const TreeArgs& a, int place, int tile
             u.blk_end = u.blk_begin + each + (u.part < more);
             return true;
         }
-        units += lane_value(upto, 63);
         slots += lane_value(cut_upto, 63);
         cut_tiles += lane_value(tiles_upto, 63);
     }
@@ -252,11 +285,11 @@ struct TreeParts {
     float* o;        // [slot][n_kv][tile_cols][d]
 };
 __host__ __device__ inline size_t tree_parts(TreeParts& t, void* base, int n_kv, int d, int tile_cols) {
-    const size_t cols = (size_t)tree_max_slots(n_kv) * n_kv * tile_cols;
+    const size_t cols = (size_t)tree_max_slots(n_kv, tile_cols) * n_kv * tile_cols;
     char* p = (char*)base;
     t.count = (int32_t*)p;
     t.rec = (TreeRecord*)(p + 256);
-    size_t off = 256 + (tree_max_cut_tiles(n_kv) * sizeof(TreeRecord) + 255) / 256 * 256;
+    size_t off = 256 + (tree_max_cut_tiles(n_kv, tile_cols) * sizeof(TreeRecord) + 255) / 256 * 256;
     t.ml = (f32x2*)(p + off);
     off += cols * 8;
     t.o = (float*)(p + off);
@@ -279,20 +312,22 @@ __device__ __forceinline__ uint32_t pair_mask(uint32_t bits, int w) { return (bi
 __device__ __forceinline__ uint32_t not_finite(uint32_t pair) { return ((pair & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 // V operands of the block: 0 * NaN is NaN, so the values that no node sees are emptied, and those of a used node that are not finite too:
 // they may reach the columns that see them only, whose outputs become NaN here.
-template <int D, int NB>
-__device__ __forceinline__ void clean_values(u32x4 (&vf)[D / 16], uint32_t keep, const uint32_t (&seen)[NB], AttnState<D, NB>& st) {
+// (vf: the dims blocks from b0 on.)
+template <int D, int NB, int N>
+__device__ __forceinline__ void clean_values(u32x4 (&vf)[N], int b0, uint32_t keep, const uint32_t (&seen)[NB], AttnState<D, NB>& st) {
     uint32_t bad = 0u;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const uint32_t m = pair_mask(keep, w);
 #pragma unroll
-        for (int b = 0; b < D / 16; ++b) {
+        for (int b = 0; b < N; ++b) {
             vf[b][w] &= m;
             bad |= not_finite(vf[b][w]);
         }
     }
     if (!__any(bad != 0u)) return;
-    for (int b = 0; b < D / 16; ++b) {
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
         u32x4 mark, sees;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -307,7 +342,7 @@ __device__ __forceinline__ void clean_values(u32x4 (&vf)[D / 16], uint32_t keep,
             const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
             for (int v = 0; v < 4; ++v)
-                if (hit[v] > 0.f) st.o[c][b][v] = NAN;
+                if (hit[v] > 0.f) st.o[c][b0 + b][v] = NAN;
         }
     }
 }
@@ -338,20 +373,26 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     bf16x8 qf[NB][D / 32];
     int node[NB];
     bool stored[NB];
+    auto load_q = [&]() {
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+            const bf16_t* qrow = a.q + (int64_t)(it.row0 + node[c]) * a.ld_q + (int64_t)(kvh * g + min(it.tile * TILE + (wave * NB + c) * 16 + r, cols - 1) - node[c] * g) * D;
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) qf[c][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (s * 4 + G) * 8));
+        }
+    };
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
-        const int col = it.tile * TILE + (wave * NB + c) * 16 + r, cc = min(col, cols - 1);
+        const int col = it.tile * TILE + (wave * NB + c) * 16 + r;
         stored[c] = col < cols;
-        node[c] = cc / g;
-        const bf16_t* qrow = a.q + (int64_t)(it.row0 + node[c]) * a.ld_q + (int64_t)(kvh * g + cc - node[c] * g) * D;
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) qf[c][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (s * 4 + G) * 8));
+        node[c] = min(col, cols - 1) / g;
     }
     AttnState<D, NB> st;
     init_state<D, NB>(st);
     bool used[NB] = {};
     if (it.blk_begin < it.blk_end) {
         const int n_full = it.c / 32, last_page = (it.c + it.n - 1) / kPage;
+        const bool sees_tree = it.blk_end > n_full;  // (one part at least: its last block holds the last node)
         const int32_t* bt = a.block_tables + (a.bt_off ? (int64_t)a.bt_off[it.seq] : (int64_t)it.seq * a.table_stride);
         // wave w brings in piece w of a block: K page 0, K page 1, V page 0, V page 1
         const bf16_t* pool = wave < 2 ? a.k_pool : a.v_pool;
@@ -370,50 +411,73 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
             for (int i = 0; i < IPB; ++i)
                 __builtin_amdgcn_global_load_lds((gptr_t)(src + i * 1024), (lptr_t)(&ring[stage][wave][i * 1024]), 16, 0, 0);
         };
+        // The keys are asked for first: they come from HBM, the rest from the caches.
+        const int parent = sees_tree ? tree_parent(a, it.row0, it.n) : -2;
+        fetch_ids(it.blk_begin);
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) issue_block(page_id(it.blk_begin + i), i);
+        load_q();
+        const int kpage = r >> 3, kslot = ((r >> 2) & 1) * 8 + (r & 3);
+        // Raw scores of the block in `stage`.
+        auto scores = [&](int stage, float (&sc)[NB][8]) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                u32x4 kf[D / 32];
+#pragma unroll
+                for (int s = 0; s < D / 32; ++s) kf[s] = *reinterpret_cast<const u32x4*>(&ring[stage][kpage][((s * 4 + G) * 16 + ((kslot + 4 * t) ^ (4 * kpage))) * 16]);
+#pragma unroll
+                for (int c = 0; c < NB; ++c) {
+                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < D / 32; ++s) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[s]), qf[c][s], x, 0, 0, 0);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) sc[c][4 * t + v] = x[v];
+                }
+            }
+        };
         auto block_step = [&](int stage, int blk, auto masked) {
             constexpr bool MASKED = decltype(masked)::value;
             float sc[NB][8];
-            u32x4 kf[2][D / 32];
-            const int kpage = r >> 3, kslot = ((r >> 2) & 1) * 8 + (r & 3);
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int s = 0; s < D / 32; ++s)
-                    kf[t][s] = *reinterpret_cast<const u32x4*>(&ring[stage][kpage][((s * 4 + G) * 16 + ((kslot + 4 * t) ^ (4 * kpage))) * 16]);
+            scores(stage, sc);
             uint32_t seen[NB];
+            if (MASKED)
 #pragma unroll
-            for (int c = 0; c < NB; ++c) {
-                score_group<D>(sc[c], kf, qf[c]);
-                if (MASKED) {
+                for (int c = 0; c < NB; ++c) {
                     seen[c] = tree.vis[node[c] * tree.stride + blk - n_full] >> (G * 8);
                     hide_scores(sc[c], seen[c]);
                 }
-            }
-            u32x4 vf[D / 16];
-            update_groups<D, NB, true>(
-                st, sc, a.scale_log2, []() {},
-                [&]() -> const u32x4 (&)[D / 16] {
+            constexpr int PORTION = 4;  // dims blocks
+            u32x4 vf[PORTION];
+            auto read_v = [&](int b0) {
 #pragma unroll
-                    for (int b = 0; b < D / 16; ++b) vf[b] = *reinterpret_cast<const u32x4*>(&ring[stage][2 + (G >> 1)][b * 512 + r * 32 + (G & 1) * 16]);
-                    if (MASKED) clean_values<D, NB>(vf, tree.used[blk - n_full] >> (G * 8), seen, st);
-                    return vf;
-                });
+                for (int b = 0; b < PORTION; ++b) vf[b] = *reinterpret_cast<const u32x4*>(&ring[stage][2 + (G >> 1)][(b0 + b) * 512 + r * 32 + (G & 1) * 16]);
+            };
+            raise_reference<D, NB, true>(st, sc, a.scale_log2);
+            read_v(0);
+            bf16x8 pb[NB];
+            block_weights<D, NB>(st, sc, a.scale_log2, pb);
+#pragma unroll
+            for (int b0 = 0; b0 < D / 16; b0 += PORTION) {
+                if (b0 > 0) read_v(b0);
+                if (MASKED) clean_values<D, NB, PORTION>(vf, b0, tree.used[blk - n_full] >> (G * 8), seen, st);
+#pragma unroll
+                for (int b = 0; b < PORTION; ++b)
+#pragma unroll
+                    for (int c = 0; c < NB; ++c)
+                        st.o[c][b0 + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[b]), pb[c], st.o[c][b0 + b], 0, 0, 0);
+            }
         };
-        const bool sees_tree = it.blk_end > n_full;  // (one part at least: its last block holds the last node)
-        if (sees_tree) tree_visibility(a, tree, tree_parent(a, it.row0, it.n), it.n, it.c);
+        if (sees_tree) tree_visibility(a, tree, parent, it.n, it.c);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
             if (!sees_tree) continue;
             const int at = (it.c & 31) + node[c];
             used[c] = tree.vis[node[c] * tree.stride + (at >> 5)] >> (at & 31) & 1;
         }
+        const bool idle = it.tile * TILE + wave * NB * 16 >= cols;  // (the same for the wave)
+        const int nblk = it.blk_end - it.blk_begin, full = min(nblk, max(n_full - it.blk_begin, 0));
         // every wave always issues its piece (indices past the end read the last page again into a stage nobody reads), so the
         // count of outstanding loads is the same in every iteration
-        fetch_ids(it.blk_begin);
-#pragma unroll
-        for (int i = 0; i < NS - 1; ++i) issue_block(page_id(it.blk_begin + i), i);
-        const bool idle = it.tile * TILE + wave * NB * 16 >= cols;  // (the same for the wave)
-        const int nblk = it.blk_end - it.blk_begin;
         auto advance = [&](int i) {
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * IPB) : "memory");
             __syncthreads();  // block i has landed; nobody reads the stage of the block before it any more
@@ -422,7 +486,6 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
             issue_block(page_id(next), (i + NS - 1) % NS);
         };
         // blocks that all columns see, then the last ones
-        const int full = min(nblk, max(n_full - it.blk_begin, 0));
         for (int i = 0; i < full; ++i) {
             advance(i);
             if (!idle) block_step(i % NS, it.blk_begin + i, std::false_type{});
@@ -502,6 +565,8 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
         load_kv<D>(f, a.k_pool, a.v_pool, (int64_t)__builtin_amdgcn_readlane(ids, p0), (int64_t)__builtin_amdgcn_readlane(ids, p1), a.n_kv, kvh, lane);
     };
     KvFrag<D> fa, fb;
+    const bool sees_tree = it.blk_begin < it.blk_end && it.blk_end > n_full;
+    const int parent = sees_tree ? tree_parent(a, it.row0, it.n) : -2;
     if (b_begin < b_end) {
         fetch_ids(2 * b_begin);
         load_block(fa, b_begin);
@@ -516,8 +581,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) qf[c][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (s * 4 + G) * 8));
     }
-    const bool sees_tree = it.blk_begin < it.blk_end && it.blk_end > n_full;
-    if (sees_tree) tree_visibility(a, tree, tree_parent(a, it.row0, it.n), it.n, it.c);
+    if (sees_tree) tree_visibility(a, tree, parent, it.n, it.c);
     AttnState<D, NB> st;
     init_state<D, NB>(st);
     auto attend = [&](KvFrag<D>& f) {
@@ -554,7 +618,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
             seen[c] = mine(tree.vis[node[c] * tree.stride + blk - n_full]);
             hide_scores(sc[c], seen[c]);
         }
-        clean_values<D, NB>(fa.v, mine(tree.used[blk - n_full]), seen, st);
+        clean_values<D, NB, D / 16>(fa.v, 0, mine(tree.used[blk - n_full]), seen, st);
         update_groups<D, NB, false>(st, sc, a.scale_log2, []() {}, [&]() -> const u32x4 (&)[D / 16] { return fa.v; });
         if (++blk < b_end) next_block(fa, blk);
     }
@@ -604,19 +668,13 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
     }
 }
 
-// The partial results of a tile joined, in order of the parts: one workgroup per (record, KV head, 1024 / D columns), a thread per four
-// dims of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time.
+// The partial results of all tiles joined, in order of the parts: a work item is (record, KV head, 1024 / D columns), a thread per four dims
+// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time.
 constexpr int kMergeBatch = 12;
-constexpr int merge_cols(int d) { return 1024 / d; }
+constexpr int kMergeGroups = 2048;  // workgroups
 template <int D>
-__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_cols) {
-    TreeParts parts;
-    tree_parts(parts, a.workspace, a.n_kv, D, tile_cols);
-    const int kvh = blockIdx.x % a.n_kv, place = blockIdx.x / a.n_kv, g = a.n_q / a.n_kv;
-    const int count = *parts.count;
-    const TreeRecord rec = parts.rec[place];  // (behind the last one: anything)
-    if (place >= count) return;
-    const int tcol = blockIdx.y * merge_cols(D) + threadIdx.x / (D / 4), e = threadIdx.x % (D / 4) * 4, col = rec.tile * tile_cols + tcol;
+__device__ __forceinline__ void merge_columns(const TreeArgs& a, const TreeParts& parts, const TreeRecord& rec, int kvh, int tcol, int tile_cols) {
+    const int g = a.n_q / a.n_kv, e = threadIdx.x % (D / 4) * 4, col = rec.tile * tile_cols + tcol;
     if (col >= rec.n * g) return;
     const int64_t step = (int64_t)rec.step * a.n_kv * tile_cols, first = ((int64_t)rec.slot * a.n_kv + kvh) * tile_cols + tcol;
     float m = kNegBig, l = 0.f;
@@ -654,13 +712,34 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_co
     for (int v = 0; v < 4; ++v) acc[v] = used ? acc[v] * inv : 0.f;
     *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) = __builtin_convertvector(acc, bf16x4);
 }
+template <int D>
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_cols) {
+    constexpr int COLS = 1024 / D;
+    TreeParts parts;
+    tree_parts(parts, a.workspace, a.n_kv, D, tile_cols);
+    const int groups = (tile_cols + COLS - 1) / COLS, per_record = a.n_kv * groups;
+    int work = blockIdx.x;
+    TreeRecord rec = parts.rec[min(work / per_record, tree_max_cut_tiles(a.n_kv, tile_cols) - 1)];  // (behind the last one: anything)
+    const int total = *parts.count * per_record;
+    while (work < total) {
+        const int rest = work % per_record;
+        work += gridDim.x;
+        const TreeRecord next = parts.rec[min(work / per_record, tree_max_cut_tiles(a.n_kv, tile_cols) - 1)];
+        merge_columns<D>(a, parts, rec, rest % a.n_kv, rest / a.n_kv * COLS + (int)threadIdx.x / (D / 4), tile_cols);
+        rec = next;
+    }
+}
 
 }  // namespace
 
-// Columns of a tile.
+// Columns of a tile.  Up to 32 all columns of a KV head are in one, whose waves stream keys of their own.  Above, tiles of 64 (three
+// workgroups per compute unit, half the partial results) against 128 (two, and half the passes through LDS), us: 26 nodes behind 2500 keys,
+// 104 columns 14.7 / 17.0, 32 x 32 nodes (8B heads) 128 columns 93 / 100, 16 x 64 nodes (8B) 256 columns 108 / 110, 48 ragged trees (14B)
+// up to 300 columns 110 / 114, 16 x 64 nodes (70B) 512 columns 173 / 165, four of 128 nodes (8B) 512 columns 75 / 69, four of 200 nodes (70B) 1600
+// columns 185 / 182.  (16 x 60 nodes of 16 heads on one KV head, 960 columns: 56 / 68.)
 static int tree_tile_cols(int n_q, int n_kv, int max_nodes) {
     const int64_t cols = (int64_t)max_nodes * (n_q / n_kv);
-    return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+    return cols <= 16 ? 16 : cols <= 32 ? 32 : cols < 512 ? 64 : 128;
 }
 
 size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes) {
@@ -668,16 +747,36 @@ size_t tree_workspace_bytes(int n_q, int n_kv, int d, int max_nodes) {
     return tree_parts(t, nullptr, n_kv, d, tree_tile_cols(n_q, n_kv, max_nodes));
 }
 
+template <int D, int NB>
+static hipError_t launch_tiles(const TreeArgs& a, dim3 grid, int lds, hipStream_t stream) {
+    constexpr int ring = kTreeStages * 4 * D * kPage * 2;
+    static std::atomic<uint64_t> allowed{0};  // devices on which this kernel may use the LDS that it asks for
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(tree_attention_kernel<D, NB>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                ring + TreeLds(nullptr, kTreeNodes).bytes(kTreeNodes));
+        if (e != hipSuccess) return e;
+        if (dev < 64) allowed.fetch_or(1ull << dev);
+    }
+    tree_attention_kernel<D, NB><<<grid, 256, ring + lds, stream>>>(a);
+    return hipSuccess;
+}
+
 template <int D>
-static void launch_tree(const TreeArgs& a, int tile_cols, int64_t units, hipStream_t stream) {
-    const dim3 grid((unsigned)(units * a.n_kv)), merge((unsigned)(tree_max_cut_tiles(a.n_kv) * a.n_kv), (unsigned)ceil_div(tile_cols, merge_cols(D)));
-    const int lds = TreeLds(nullptr, a.max_nodes).bytes(a.max_nodes), ring = kTreeStages * 4 * D * kPage * 2;
+static hipError_t launch_tree(const TreeArgs& a, int tile_cols, int64_t units, hipStream_t stream) {
+    const dim3 grid((unsigned)(units * a.n_kv));
+    const int lds = TreeLds(nullptr, a.max_nodes).bytes(a.max_nodes);
+    hipError_t e = hipSuccess;
     if (tile_cols == 16) tree_stream_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
     else if (tile_cols == 32) tree_stream_kernel<D, 2><<<grid, 256, lds, stream>>>(a);
-    else if (tile_cols == 64) tree_attention_kernel<D, 1><<<grid, 256, ring + lds, stream>>>(a);
-    else tree_attention_kernel<D, 2><<<grid, 256, ring + lds, stream>>>(a);
+    else if (tile_cols == 64) e = launch_tiles<D, 1>(a, grid, lds, stream);
+    else e = launch_tiles<D, 2>(a, grid, lds, stream);
+    if (e != hipSuccess) return e;
     // no sequence can be cut whose table has no more pages than the fewest blocks of a part
-    if (a.table_stride > 2 * kTreeMinShare) tree_merge_kernel<D><<<merge, 256, 0, stream>>>(a, tile_cols);
+    if (a.table_stride > 2 * kTreeMinShare) tree_merge_kernel<D><<<kMergeGroups, 256, 0, stream>>>(a, tile_cols);
+    return hipGetLastError();
 }
 
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
@@ -685,10 +784,9 @@ hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
     const int g = a.n_q / a.n_kv, tile_cols = tree_tile_cols(a.n_q, a.n_kv, a.max_nodes);
     // no more tiles than whole ones in all rows and a partly filled one per sequence; cutting the keys adds no more units than there
     // are shares; and one place behind the last unit
-    const int64_t units = (int64_t)a.num_rows * g / tile_cols + a.num_seqs + tree_target(a.n_kv) + 1;
+    const int64_t units = (int64_t)a.num_rows * g / tile_cols + a.num_seqs + tree_target(a.n_kv, tile_cols) + 1;
     if (units * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
-    if (a.d == 128) launch_tree<128>(a, tile_cols, units, stream);
-    else if (a.d == 64) launch_tree<64>(a, tile_cols, units, stream);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    if (a.d == 128) return launch_tree<128>(a, tile_cols, units, stream);
+    if (a.d == 64) return launch_tree<64>(a, tile_cols, units, stream);
+    return hipErrorInvalidValue;
 }
