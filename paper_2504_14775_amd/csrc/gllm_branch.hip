@@ -159,11 +159,11 @@ __device__ __forceinline__ uint64_t order_key(double x) {
 }
 
 // The largest v for which at least k of the wave's U keys per lane are >= v (0 if fewer than k are nonzero): bit by bit.
-template <typename Key, int U>
-__device__ __forceinline__ Key kth_largest(const Key (&key)[U], int k) {
-    Key v = 0;
-    for (int bit = sizeof(Key) * 8 - 1; bit >= 0; --bit) {
-        const Key probe = v | (Key)1 << bit;
+template <int U>
+__device__ __forceinline__ uint32_t kth_largest(const uint32_t (&key)[U], int k) {
+    uint32_t v = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t probe = v | 1u << bit;
         int above = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) above += __popcll(__ballot(key[u] >= probe));
@@ -171,6 +171,41 @@ __device__ __forceinline__ Key kth_largest(const Key (&key)[U], int k) {
     }
     return v;
 }
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void max_step(float& x) {
+    const int b = __builtin_bit_cast(int, x);
+    x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CTRL, ROWS, 0xf, false)));
+}
+// The largest x of the wave, in all lanes: by lane shifts (lane 63 has it).
+__device__ __forceinline__ float wave_max(float x) {
+    max_step<0x111, 0xf>(x);
+    max_step<0x112, 0xf>(x);
+    max_step<0x114, 0xf>(x);
+    max_step<0x118, 0xf>(x);
+    max_step<0x142, 0xa>(x);
+    max_step<0x143, 0xc>(x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// 2^y in 64 bits, off by 7e-12 of itself: y = n + f with |f| <= 1/2, and the Taylor polynomial of 2^f of degree 9, whose next term is
+// (f ln 2)^10 / 10!.  (The library's exp takes three times as long.)
+__device__ __forceinline__ double exp2_wide(double y) {
+    y = fmax(y, -1400.0);
+    const double n = rint(y), f = y - n;
+    double p = 1.0178086009239699e-07;      // ln(2)^9 / 9!
+    p = fma(p, f, 1.3215486790144305e-06);  // ln(2)^8 / 8!
+    p = fma(p, f, 1.5252733804059841e-05);
+    p = fma(p, f, 1.5403530393381609e-04);
+    p = fma(p, f, 1.3333558146428443e-03);
+    p = fma(p, f, 9.6181291076284769e-03);
+    p = fma(p, f, 5.5504108664821580e-02);
+    p = fma(p, f, 2.4022650695910072e-01);
+    p = fma(p, f, 6.9314718055994531e-01);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n);
+}
+constexpr double kLog2E = 1.4426950408889634;
 
 __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -195,9 +230,13 @@ struct WaveList {
         }
         n += __popcll(who);
     }
-    // Leaves the k best, equal keys by the lower index; returns the k-th key (0: fewer than k).
+    // Leaves the k best, equal keys by the lower index; returns the k-th key (0: fewer than k, or nothing to do).
     __device__ __forceinline__ Key keep_best(int k) {
-        constexpr int U = kBeamList / 64;
+        if (n <= k) return 0;
+        return n <= 64 ? best_of<1>(k) : n <= 128 ? best_of<2>(k) : best_of<kBeamList / 64>(k);
+    }
+    template <int U>
+    __device__ __forceinline__ Key best_of(int k) {
         wave_fence();
         Key mine[U];
         uint32_t at[U];
@@ -207,8 +246,7 @@ struct WaveList {
             mine[u] = i < n ? key[i] : 0;
             at[u] = i < n ? idx[i] : 0;
         }
-        const Key v = kth_largest<Key, U>(mine, k);
-        if (v == 0) return 0;
+        const Key v = kth_key(mine, k);
         int above = 0, same = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -220,7 +258,7 @@ struct WaveList {
             uint32_t rev[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) rev[u] = mine[u] == v ? ~at[u] : 0u;
-            reach = ~kth_largest<uint32_t, U>(rev, k - above);
+            reach = ~kth_largest(rev, k - above);
         }
         wave_fence();
         n = 0;
@@ -228,6 +266,22 @@ struct WaveList {
         for (int u = 0; u < U; ++u) add(mine[u] > v || (mine[u] == v && at[u] <= reach), mine[u], at[u]);
         wave_fence();
         return v;
+    }
+    // (64-bit keys by their upper halves first: two of the kept ones seldom agree in these)
+    template <int U>
+    __device__ __forceinline__ uint32_t kth_key(const uint32_t (&x)[U], int k) { return kth_largest(x, k); }
+    template <int U>
+    __device__ __forceinline__ uint64_t kth_key(const uint64_t (&x)[U], int k) {
+        uint32_t half[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) half[u] = (uint32_t)(x[u] >> 32);
+        const uint32_t hi = kth_largest(half, k);
+        int above = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) above += __popcll(__ballot(half[u] > hi));
+#pragma unroll
+        for (int u = 0; u < U; ++u) half[u] = half[u] == hi ? (uint32_t)x[u] : 0u;
+        return (uint64_t)hi << 32 | kth_largest(half, k - above);
     }
 };
 
@@ -249,6 +303,23 @@ constexpr int kBeamQuads = 4;                        // four-column loads of a l
 constexpr int kBeamPass = 64 * 4 * kBeamQuads;       // columns of a wave's pass
 constexpr float kBeamSlack = 60.f;
 
+// Columns `at` .. of a wave's pass; minus infinity behind the end.
+template <bool VEC>
+__device__ __forceinline__ void load_pass(f32x4 (&x)[kBeamQuads], const float* __restrict__ x0, int at, int end, int lane) {
+#pragma unroll
+    for (int j = 0; j < kBeamQuads; ++j) {
+        const int col = at + (j * 64 + lane) * 4;
+        x[j] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (VEC) {
+            if (col < end) x[j] = *reinterpret_cast<const f32x4*>(x0 + col);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < end) x[j][e] = x0[col + e];
+        }
+    }
+}
+
 template <bool VEC>
 __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
     __shared__ uint32_t keys[kBeamWaves][kBeamList], idxs[kBeamWaves][kBeamList];
@@ -264,53 +335,61 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
     uint32_t floor = 0;      // candidates are above it
     float ref = -INFINITY;   // the sum is of exp(x - ref)
     double sum = 0.0;        // of this lane
+    f32x4 x[kBeamQuads], next[kBeamQuads];
+    const int first = begin + wave * kBeamPass, step = kBeamWaves * kBeamPass;
+    if (first < end) load_pass<VEC>(x, x0, first, end, lane);
     // Every wave passes over columns in ascending order, so that behind keep_best an equal key comes with a larger index and loses.
-    for (int at = begin + wave * kBeamPass; at < end; at += kBeamWaves * kBeamPass) {
-        f32x4 x[kBeamQuads];
-        float top = -INFINITY;
+    for (int at = first; at < end; at += step) {
+        if (at + step < end) load_pass<VEC>(next, x0, at + step, end, lane);
+        float quad[kBeamQuads], top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < kBeamQuads; ++j) {
-            const int col = at + (j * 64 + lane) * 4;
-            if (VEC) {
-                x[j] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                if (col < end) x[j] = *reinterpret_cast<const f32x4*>(x0 + col);
-            }
+            quad[j] = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (!VEC) x[j][e] = col + e < end ? x0[col + e] : -INFINITY;
-                else if (col + e >= end) x[j][e] = -INFINITY;
-                if (!(x[j][e] > -INFINITY)) x[j][e] = -INFINITY;  // (not a number)
-                top = fmaxf(top, x[j][e]);
+                if (VEC && at + (j * 64 + lane) * 4 + e >= end) x[j][e] = -INFINITY;
+                x[j][e] = fmaxf(x[j][e], -INFINITY);  // (what is not a number)
+                quad[j] = fmaxf(quad[j], x[j][e]);
             }
+            top = fmaxf(top, quad[j]);
         }
-        float wtop = top;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) wtop = fmaxf(wtop, __shfl_xor(wtop, o));
-        if (wtop == -INFINITY) continue;
-        if (wtop > ref + kBeamSlack || ref == -INFINITY) {
-            sum = ref == -INFINITY || wtop == INFINITY ? 0.0 : sum * exp((double)ref - (double)wtop);
+        const float wtop = wave_max(top);
+        if (wtop > ref + kBeamSlack || (ref == -INFINITY && wtop > ref)) {
+            sum = ref == -INFINITY || wtop == INFINITY ? 0.0 : sum * exp2_wide(((double)ref - (double)wtop) * kLog2E);
             ref = wtop;
         }
+        if (ref == INFINITY) {  // (the same for the wave)
 #pragma unroll
-        for (int j = 0; j < kBeamQuads; ++j)
+            for (int j = 0; j < kBeamQuads; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += x[j][e] == ref ? 1.0 : exp(fmax((double)x[j][e] - (double)ref, -1000.0));
+                for (int e = 0; e < 4; ++e) sum += x[j][e] == ref ? 1.0 : 0.0;
+        } else if (ref > -INFINITY) {
+            const double r = (double)ref;
+#pragma unroll
+            for (int j = 0; j < kBeamQuads; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += exp2_wide(((double)x[j][e] - r) * kLog2E);  // (not x * log2(e) - r * log2(e): logits may be the type's lowest value)
+        }
         if (list.n == 0 && floor == 0) {
             // the first pass: at least `keep` candidates are not below the keep-th largest of the lanes' maxima
             const uint32_t lane_top[1] = {order_key(top)};
-            const uint32_t t0 = kth_largest<uint32_t, 1>(lane_top, a.keep);
+            const uint32_t t0 = kth_largest(lane_top, a.keep);
             if (t0 > 0) floor = t0 - 1;
         }
-        if (order_key(wtop) <= floor) continue;
+        if (order_key(wtop) > floor) {
 #pragma unroll
-        for (int j = 0; j < kBeamQuads; ++j) {
-            if (list.n + 256 > kBeamList) floor = max(floor, list.keep_best(a.keep));
+            for (int j = 0; j < kBeamQuads; ++j) {
+                if (!__any(order_key(quad[j]) > floor)) continue;
+                if (list.n + 256 > kBeamList) floor = max(floor, list.keep_best(a.keep));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t k = order_key(x[j][e]);
-                list.add(k > floor, k, (uint32_t)(at + (j * 64 + lane) * 4 + e));
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t k = order_key(x[j][e]);
+                    list.add(k > floor, k, (uint32_t)(at + (j * 64 + lane) * 4 + e));
+                }
             }
         }
+#pragma unroll
+        for (int j = 0; j < kBeamQuads; ++j) x[j] = next[j];
     }
     list.keep_best(a.keep);
 #pragma unroll
@@ -342,7 +421,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
         for (int w = 0; w < kBeamWaves; ++w) m = fmaxf(m, wave_top[w]);
         double total = 0.0;
         for (int w = 0; w < kBeamWaves; ++w)
-            if (wave_top[w] > -INFINITY) total += wave_top[w] == m ? wave_sum[w] : wave_sum[w] * exp((double)wave_top[w] - (double)m);
+            if (wave_top[w] > -INFINITY) total += wave_top[w] == m ? wave_sum[w] : wave_sum[w] * exp2_wide(((double)wave_top[w] - (double)m) * kLog2E);
         a.top[place] = m;
         a.sum[place] = total;
     }
@@ -362,12 +441,11 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
         const int64_t place = (row0 + b) * a.segs;
         float m = -INFINITY;
         for (int i = lane; i < a.segs; i += 64) m = fmaxf(m, a.top[place + i]);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+        m = wave_max(m);
         double total = 0.0;
         for (int i = lane; i < a.segs; i += 64) {
             const float t = a.top[place + i];
-            if (t > -INFINITY) total += t == m ? a.sum[place + i] : a.sum[place + i] * exp((double)t - (double)m);
+            if (t > -INFINITY) total += t == m ? a.sum[place + i] : a.sum[place + i] * exp2_wide(((double)t - (double)m) * kLog2E);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
@@ -430,10 +508,11 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     }
 }
 
-// Segments of a row.
+// Segments of a row: about kBeamTarget workgroups, each with at least one pass of its four waves.
+constexpr int kBeamTarget = 1024;
 int beam_segments(int num_seqs, int beams, int vocab) {
-    (void)num_seqs; (void)beams; (void)vocab;
-    return 1;
+    const int64_t rows = std::max<int64_t>(1, (int64_t)num_seqs * beams), most = ceil_div(vocab, kBeamWaves * kBeamPass);
+    return (int)std::min(most, ceil_div(kBeamTarget, rows));
 }
 
 bool beam_sizes_ok(int num_seqs, int beams, int vocab, int keep) {
@@ -546,7 +625,7 @@ gllm_status gllm_op_beam_select(const float* logits, int64_t ld_logits, const fl
     a.logits = logits; a.ld = ld_logits; a.scores = scores;
     a.num_seqs = num_seqs; a.beams = beams; a.vocab = vocab; a.keep = keep;
     a.segs = beam_segments(num_seqs, beams, vocab);
-    a.seg_len = (int32_t)round_up(ceil_div(vocab, a.segs), 4);
+    a.seg_len = (int32_t)round_up(ceil_div(vocab, a.segs), kBeamWaves * kBeamPass);  // (the last ones may be short of it, or empty)
     const int64_t places = (int64_t)num_seqs * beams * a.segs;
     a.sum = (double*)workspace;
     a.top = (float*)(a.sum + places);
