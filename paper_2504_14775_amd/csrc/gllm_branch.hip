@@ -143,9 +143,10 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 // token of the segment can be among the best of the sequence) beside the segment's largest logit and sum of exponentials.
 // beam_merge: a workgroup per sequence adds up the sums of its rows and picks the best of what the segments kept.
 // The order among beams hangs on the sums: they and the scores are held in 64 bits, so that the order is that of exact
-// arithmetic but where scores agree to some 1e-12.
+// arithmetic but where scores agree to some 1e-10.
 
 constexpr int kBeamWaves = 4;
+constexpr int kBeamLists = 1280;  // most segments of the rows of a sequence
 constexpr int kBeamList = 384;  // places of a wave's list: the 64 kept at most, the 256 of one pass, and a whole number per lane
 
 // Keys in the order of the numbers, 0 for what is no candidate (minus infinity, not a number).
@@ -153,21 +154,35 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);  // (one zero)
     return x > -INFINITY ? b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u) : 0u;
 }
+// The least number whose key is above `key`, which is a number's, one less, or 0.
+__device__ __forceinline__ float above_key(uint32_t key) {
+    const uint32_t k = key + 1;
+    return key == 0u ? -3.402823466e38f : __builtin_bit_cast(float, k >> 31 ? k ^ 0x80000000u : ~k);  // (above infinity's: not a number, and nothing passes)
+}
 __device__ __forceinline__ uint64_t order_key(double x) {
     const uint64_t b = __builtin_bit_cast(uint64_t, x + 0.0);
     return x > -INFINITY ? b ^ (b >> 63 ? ~0ull : 1ull << 63) : 0ull;
 }
 
-// The largest v for which at least k of the wave's U keys per lane are >= v (0 if fewer than k are nonzero): bit by bit.
+// Bit by bit the largest v with at least `need` of the wave's keys >= v, U per lane, of which those that are `in` count; it stops
+// early at a v that exactly `need` keys reach, most often after the bits in which the need-th key differs from the next one.  count: the keys
+// that reach v.  There have to be `need` of them.
 template <int U>
-__device__ __forceinline__ uint32_t kth_largest(const uint32_t (&key)[U], int k) {
+__device__ __forceinline__ uint32_t reach_of(const uint32_t (&key)[U], const bool (&in)[U], int need, int& count) {
     uint32_t v = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+    count = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) count += __popcll(__ballot(in[u]));
+#pragma unroll 1
+    for (int bit = 31; bit >= 0 && count != need; --bit) {
         const uint32_t probe = v | 1u << bit;
         int above = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) above += __popcll(__ballot(key[u] >= probe));
-        if (above >= k) v = probe;
+        for (int u = 0; u < U; ++u) above += __popcll(__ballot(in[u] && key[u] >= probe));
+        if (above >= need) {
+            v = probe;
+            count = above;
+        }
     }
     return v;
 }
@@ -188,24 +203,34 @@ __device__ __forceinline__ float wave_max(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// 2^y in 64 bits, off by 7e-12 of itself: y = n + f with |f| <= 1/2, and the Taylor polynomial of 2^f of degree 9, whose next term is
-// (f ln 2)^10 / 10!.  (The library's exp takes three times as long.)
+// 2^f for |f| <= 1/2 in 64 bits, off by 4e-11 of itself: the polynomial of degree 7 through 2^f at the Chebyshev nodes.
+__device__ __forceinline__ double exp2_unit(double f) {
+    double p = 1.5303700711365693e-05;
+    p = fma(p, f, 1.5469729214118296e-04);
+    p = fma(p, f, 1.3333478473685416e-03);
+    p = fma(p, f, 9.6180256133180340e-03);
+    p = fma(p, f, 5.5504109063258665e-02);
+    p = fma(p, f, 2.4022651213498092e-01);
+    p = fma(p, f, 6.9314718055683240e-01);
+    return fma(p, f, 9.9999999995956180e-01);
+}
+// 2^y for any y <= 1000.
 __device__ __forceinline__ double exp2_wide(double y) {
     y = fmax(y, -1400.0);
-    const double n = rint(y), f = y - n;
-    double p = 1.0178086009239699e-07;      // ln(2)^9 / 9!
-    p = fma(p, f, 1.3215486790144305e-06);  // ln(2)^8 / 8!
-    p = fma(p, f, 1.5252733804059841e-05);
-    p = fma(p, f, 1.5403530393381609e-04);
-    p = fma(p, f, 1.3333558146428443e-03);
-    p = fma(p, f, 9.6181291076284769e-03);
-    p = fma(p, f, 5.5504108664821580e-02);
-    p = fma(p, f, 2.4022650695910072e-01);
-    p = fma(p, f, 6.9314718055994531e-01);
-    p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
+    const double n = rint(y);
+    return ldexp(exp2_unit(y - n), (int)n);
 }
 constexpr double kLog2E = 1.4426950408889634;
+// 2^(x log2(e) - r) for a whole number r, given kRound - r, where the exponent lies within +-1020: without the instructions on 64 bits that
+// take longer than a multiplication.  The sum with 1.5 * 2^52 rounds x log2(e) to a whole number, which stands, less r, in the low bits,
+// and is added to the exponent of the result.
+constexpr double kRound = 6755399441055744.0;
+__device__ __forceinline__ double exp_near(float x, double round_less_r) {
+    const double t = fma((double)x, kLog2E, round_less_r);
+    u32x2 p = __builtin_bit_cast(u32x2, exp2_unit(fma((double)x, kLog2E, round_less_r - t)));
+    p[1] += __builtin_bit_cast(u32x2, t)[0] << 20;
+    return __builtin_bit_cast(double, p);
+}
 
 __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -230,58 +255,56 @@ struct WaveList {
         }
         n += __popcll(who);
     }
-    // Leaves the k best, equal keys by the lower index; returns the k-th key (0: fewer than k, or nothing to do).
+    // Leaves the k best, equal keys by the lower index.  Returns a key that all of them reach, or 0 where there were no more than k.
     __device__ __forceinline__ Key keep_best(int k) {
         if (n <= k) return 0;
-        return n <= 64 ? best_of<1>(k) : n <= 128 ? best_of<2>(k) : best_of<kBeamList / 64>(k);
+        return n <= 128 ? best_of<2>(k) : n <= 256 ? best_of<4>(k) : best_of<kBeamList / 64>(k);
     }
     template <int U>
     __device__ __forceinline__ Key best_of(int k) {
         wave_fence();
         Key mine[U];
-        uint32_t at[U];
+        uint32_t at[U], part[U];
+        bool tied[U], kept[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = lane + 64 * u;
-            mine[u] = i < n ? key[i] : 0;
-            at[u] = i < n ? idx[i] : 0;
+            tied[u] = i < n;
+            kept[u] = false;
+            mine[u] = tied[u] ? key[i] : 0;
+            at[u] = tied[u] ? idx[i] : 0;
         }
-        const Key v = kth_key(mine, k);
-        int above = 0, same = 0;
+        // by the key's words, upper one first, then by the index: those above the need-th value of a word are kept, those that
+        // agree in it go on
+        Key low = 0;
+        int need = k;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            above += __popcll(__ballot(mine[u] > v));
-            same += __popcll(__ballot(mine[u] == v));
-        }
-        uint32_t reach = ~0u;  // of the equal ones the (k - above) lowest indices stay: those whose complement is largest
-        if (same > k - above) {
-            uint32_t rev[U];
+        for (int word = (int)sizeof(Key) / 4; word >= 0; --word) {
+            if (need == 0) continue;
 #pragma unroll
-            for (int u = 0; u < U; ++u) rev[u] = mine[u] == v ? ~at[u] : 0u;
-            reach = ~kth_largest(rev, k - above);
+            for (int u = 0; u < U; ++u) part[u] = word > 0 ? (uint32_t)(mine[u] >> (32 * (word - 1))) : ~at[u];
+            int count;
+            const uint32_t v = reach_of(part, tied, need, count);
+            if (word > 0) low |= (Key)v << (32 * (word > 0 ? word - 1 : 0));
+            if (count == need) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) kept[u] |= tied[u] && part[u] >= v;
+                need = 0;
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    kept[u] |= tied[u] && part[u] > v;
+                    need -= __popcll(__ballot(tied[u] && part[u] > v));
+                    tied[u] = tied[u] && part[u] == v;
+                }
+            }
         }
         wave_fence();
         n = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) add(mine[u] > v || (mine[u] == v && at[u] <= reach), mine[u], at[u]);
+        for (int u = 0; u < U; ++u) add(kept[u], mine[u], at[u]);
         wave_fence();
-        return v;
-    }
-    // (64-bit keys by their upper halves first: two of the kept ones seldom agree in these)
-    template <int U>
-    __device__ __forceinline__ uint32_t kth_key(const uint32_t (&x)[U], int k) { return kth_largest(x, k); }
-    template <int U>
-    __device__ __forceinline__ uint64_t kth_key(const uint64_t (&x)[U], int k) {
-        uint32_t half[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) half[u] = (uint32_t)(x[u] >> 32);
-        const uint32_t hi = kth_largest(half, k);
-        int above = 0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) above += __popcll(__ballot(half[u] > hi));
-#pragma unroll
-        for (int u = 0; u < U; ++u) half[u] = half[u] == hi ? (uint32_t)x[u] : 0u;
-        return (uint64_t)hi << 32 | kth_largest(half, k - above);
+        return low;
     }
 };
 
@@ -300,7 +323,7 @@ struct BeamArgs {
 };
 
 constexpr int kBeamQuads = 4;                        // four-column loads of a lane and pass
-constexpr int kBeamPass = 64 * 4 * kBeamQuads;       // columns of a wave's pass
+constexpr int kBeamPass = 256 * kBeamQuads;          // columns of a wave's pass
 constexpr float kBeamSlack = 60.f;
 
 // Columns `at` .. of a wave's pass; minus infinity behind the end.
@@ -311,7 +334,7 @@ __device__ __forceinline__ void load_pass(f32x4 (&x)[kBeamQuads], const float* _
         const int col = at + (j * 64 + lane) * 4;
         x[j] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
         if (VEC) {
-            if (col < end) x[j] = *reinterpret_cast<const f32x4*>(x0 + col);
+            if (col < end) x[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(x0 + col));  // (read once)
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -319,9 +342,11 @@ __device__ __forceinline__ void load_pass(f32x4 (&x)[kBeamQuads], const float* _
         }
     }
 }
+// (a bare maximum: fmaxf first makes every loaded value quiet.  Not a number: low.)
+__device__ __forceinline__ float at_least(float x, float low) { return __builtin_amdgcn_fmed3f(x, low, INFINITY); }
 
 template <bool VEC>
-__global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
+__global__ __launch_bounds__(256, 4) void beam_rows_kernel(BeamArgs a) {
     __shared__ uint32_t keys[kBeamWaves][kBeamList], idxs[kBeamWaves][kBeamList];
     __shared__ double wave_sum[kBeamWaves];
     __shared__ float wave_top[kBeamWaves];
@@ -332,66 +357,89 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
     const float* x0 = a.logits + (int64_t)row * a.ld;
     const int begin = seg * a.seg_len, end = min(a.vocab, begin + a.seg_len);
     WaveList<uint32_t> list{keys[wave], idxs[wave], 0, lane};
-    uint32_t floor = 0;      // candidates are above it
-    float ref = -INFINITY;   // the sum is of exp(x - ref)
-    double sum = 0.0;        // of this lane
+    float bar = above_key(0);  // candidates are not below it
+    // The sum of exp(x - ref); where ref is below 1000 in magnitude, of 2^(x log2(e) - r), r = ref log2(e) rounded to a whole number (one
+    // subtraction in 64 bits less per logit, of sixteen operations).
+    float ref = -INFINITY;
+    double sum = 0.0, r = 0.0;  // (sum: of this lane)
+    auto near = [&](float x) { return fabsf(x) < 1000.f; };
+    auto refer_to = [&](float x) {  // (the same for the wave)
+        const double was = near(ref) ? r : (double)ref * kLog2E;
+        r = rint((double)x * kLog2E);
+        sum = ref == -INFINITY || x == INFINITY ? 0.0 : sum * exp2_wide(was - (near(x) ? r : (double)x * kLog2E));
+        ref = x;
+    };
+    auto raise = [&]() {
+        const uint32_t floor = list.keep_best(a.keep);
+        if (floor > 0) bar = fmaxf(bar, above_key(floor));
+    };
     f32x4 x[kBeamQuads], next[kBeamQuads];
     const int first = begin + wave * kBeamPass, step = kBeamWaves * kBeamPass;
     if (first < end) load_pass<VEC>(x, x0, first, end, lane);
     // Every wave passes over columns in ascending order, so that behind keep_best an equal key comes with a larger index and loses.
+#pragma unroll 1
     for (int at = first; at < end; at += step) {
         if (at + step < end) load_pass<VEC>(next, x0, at + step, end, lane);
-        float quad[kBeamQuads], top = -INFINITY;
+        if (VEC && at + kBeamPass > end) {  // (the same for the wave)
+#pragma unroll
+            for (int j = 0; j < kBeamQuads; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at + (j * 64 + lane) * 4 + e >= end) x[j][e] = -INFINITY;
+        }
+        if (at == first) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < kBeamQuads; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, x[j][e]);
+            const float now = wave_max(top);
+            if (now > -INFINITY) refer_to(now);
+            // at least `keep` candidates are not below the keep-th largest of the lanes' maxima
+            const uint32_t lane_top[1] = {order_key(top)};
+            const bool in[1] = {lane_top[0] > 0};
+            int count;
+            if (__popcll(__ballot(in[0])) >= a.keep) bar = above_key(max(reach_of(lane_top, in, a.keep, count), 1u) - 1);
+        }
+        // what is lower weighs 1e-304; a quad's maximum is exact where it is higher
+        const float low = near(ref) ? ref - 700.f : -INFINITY;
+        float quad[kBeamQuads], top = low;
 #pragma unroll
         for (int j = 0; j < kBeamQuads; ++j) {
-            quad[j] = -INFINITY;
+            quad[j] = low;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (VEC && at + (j * 64 + lane) * 4 + e >= end) x[j][e] = -INFINITY;
-                x[j][e] = fmaxf(x[j][e], -INFINITY);  // (what is not a number)
-                quad[j] = fmaxf(quad[j], x[j][e]);
-            }
+            for (int e = 0; e < 4; ++e) quad[j] = fmaxf(quad[j], at_least(x[j][e], low));
             top = fmaxf(top, quad[j]);
         }
-        const float wtop = wave_max(top);
-        if (wtop > ref + kBeamSlack || (ref == -INFINITY && wtop > ref)) {
-            sum = ref == -INFINITY || wtop == INFINITY ? 0.0 : sum * exp2_wide(((double)ref - (double)wtop) * kLog2E);
-            ref = wtop;
-        }
-        if (ref == INFINITY) {  // (the same for the wave)
+        if (__any(top > ref + kBeamSlack || (top > ref && ref == -INFINITY))) refer_to(wave_max(top));
+        if (near(ref)) {
+            const double c = kRound - r;
 #pragma unroll
             for (int j = 0; j < kBeamQuads; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += x[j][e] == ref ? 1.0 : 0.0;
+                for (int e = 0; e < 4; ++e) sum += exp_near(at_least(x[j][e], ref - 700.f), c);
         } else if (ref > -INFINITY) {
-            const double r = (double)ref;
 #pragma unroll
             for (int j = 0; j < kBeamQuads; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += exp2_wide(((double)x[j][e] - r) * kLog2E);  // (not x * log2(e) - r * log2(e): logits may be the type's lowest value)
+                for (int e = 0; e < 4; ++e)  // (not x * log2(e) - ref * log2(e): logits may be the type's lowest value)
+                    sum += x[j][e] == ref ? 1.0 : ref < INFINITY ? exp2_wide(((double)x[j][e] - (double)ref) * kLog2E) : 0.0;
         }
-        if (list.n == 0 && floor == 0) {
-            // the first pass: at least `keep` candidates are not below the keep-th largest of the lanes' maxima
-            const uint32_t lane_top[1] = {order_key(top)};
-            const uint32_t t0 = kth_largest(lane_top, a.keep);
-            if (t0 > 0) floor = t0 - 1;
-        }
-        if (order_key(wtop) > floor) {
+        if (__any(top >= bar)) {
 #pragma unroll
             for (int j = 0; j < kBeamQuads; ++j) {
-                if (!__any(order_key(quad[j]) > floor)) continue;
-                if (list.n + 256 > kBeamList) floor = max(floor, list.keep_best(a.keep));
+                if (!__any(quad[j] >= bar)) continue;
+                if (list.n + 256 > kBeamList) raise();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t k = order_key(x[j][e]);
-                    list.add(k > floor, k, (uint32_t)(at + (j * 64 + lane) * 4 + e));
-                }
+                for (int e = 0; e < 4; ++e) list.add(x[j][e] >= bar, order_key(x[j][e]), (uint32_t)(at + (j * 64 + lane) * 4 + e));
             }
+            if (list.n >= 2 * a.keep) raise();  // (the sooner the bar is high the fewer candidates come: in pass p about keep / p)
         }
 #pragma unroll
         for (int j = 0; j < kBeamQuads; ++j) x[j] = next[j];
     }
-    list.keep_best(a.keep);
+    if (near(ref)) sum *= exp2_wide(r - (double)ref * kLog2E);
+    if (list.n > 64) list.keep_best(a.keep);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if (lane == 0) {
@@ -401,9 +449,8 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
     }
     __syncthreads();
     if (wave > 0) return;
-    // the first wave's list takes in the others' (in LDS order: keys and indices decide, not the places)
+    // the first wave's list takes in the others', of at most 64 each (keys and indices decide, not the places)
     for (int w = 1; w < kBeamWaves; ++w) {
-        if (list.n + 64 > kBeamList) list.keep_best(a.keep);
         const int n = wave_n[w];
         list.add(lane < n, lane < n ? keys[w][lane] : 0u, lane < n ? idxs[w][lane] : 0u);
     }
@@ -432,51 +479,155 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     __shared__ uint32_t idxs[kBeamWaves][kBeamList];
     __shared__ double lse[GLLM_BEAM_MAX_BEAMS];   // log of the sum without the largest logit
     __shared__ float tops[GLLM_BEAM_MAX_BEAMS];
+    __shared__ float list_top[kBeamLists];
+    __shared__ double list_sum[kBeamLists];
     __shared__ int wave_n[kBeamWaves];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int s = blockIdx.x;
     const int64_t row0 = (int64_t)s * a.beams;
+    const int lists = a.beams * a.segs;
+    for (int i = threadIdx.x; i < lists; i += 256) {
+        list_top[i] = a.top[row0 * a.segs + i];
+        list_sum[i] = a.sum[row0 * a.segs + i];
+    }
+    // (few candidates are all asked for at once, without a look at the lists' first ones)
+    constexpr int FEW = 4;
+    const bool few = lists * a.keep <= FEW * 256;
+    int32_t few_token[FEW];
+    float few_value[FEW];
+#pragma unroll
+    for (int t = 0; t < FEW; ++t) {
+        const int i = (t * kBeamWaves + wave) * 64 + lane;
+        few_token[t] = -1;
+        few_value[t] = 0.f;
+        if (few && i < lists * a.keep) {
+            few_token[t] = a.token[row0 * a.segs * a.keep + i];
+            few_value[t] = a.value[row0 * a.segs * a.keep + i];
+        }
+    }
+    __syncthreads();
     for (int b = wave; b < a.beams; b += kBeamWaves) {
-        const int64_t place = (row0 + b) * a.segs;
+        const int at = b * a.segs;
         float m = -INFINITY;
-        for (int i = lane; i < a.segs; i += 64) m = fmaxf(m, a.top[place + i]);
+        for (int i = lane; i < a.segs; i += 64) m = fmaxf(m, list_top[at + i]);
         m = wave_max(m);
         double total = 0.0;
         for (int i = lane; i < a.segs; i += 64) {
-            const float t = a.top[place + i];
-            if (t > -INFINITY) total += t == m ? a.sum[place + i] : a.sum[place + i] * exp2_wide(((double)t - (double)m) * kLog2E);
+            const float t = list_top[at + i];
+            if (t > -INFINITY) total += t == m ? list_sum[at + i] : list_sum[at + i] * exp2_wide(((double)t - (double)m) * kLog2E);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
         if (lane == 0) {
             tops[b] = m;
-            lse[b] = log(total);
+            // the logarithm in 32 bits and a step of Newton's method, whose error is half the square of the first one's
+            const double y = (double)__logf((float)total);
+            lse[b] = total > 0.0 ? y + (total * exp2_wide(-y * kLog2E) - 1.0) : 0.0;
         }
     }
     __syncthreads();
+    auto score = [&](float x, int b) {  // of a logit of beam b; 0: no candidate
+        const float cum = a.scores[row0 + b], m = tops[b];
+        if (!(cum > -INFINITY && cum < INFINITY)) return (uint64_t)0;
+        return order_key((double)cum + ((x == m ? 0.0 : (double)x - (double)m) - lse[b]));
+    };
     WaveList<uint64_t> list{keys[wave], idxs[wave], 0, lane};
-    uint64_t floor = 1;
-    const int per_beam = a.segs * a.keep, total = a.beams * per_beam;
-    for (int at = wave * 64; at < total; at += kBeamWaves * 64) {
-        const int i = at + lane;
-        uint64_t k = 0;
-        uint32_t idx = 0;
-        if (i < total) {
-            const int b = i / per_beam;
-            const int64_t place = row0 * per_beam + i;
-            const int32_t token = a.token[place];
-            const float cum = a.scores[row0 + b], x = a.value[place], m = tops[b];
-            if (token >= 0 && cum > -INFINITY && cum < INFINITY) {
-                const double d = x == m ? 0.0 : (double)x - (double)m;
-                k = order_key((double)cum + (d - lse[b]));
-                idx = (uint32_t)b * (uint32_t)a.vocab + (uint32_t)token;
+    if (few) {
+#pragma unroll
+        for (int t = 0; t < FEW; ++t) {
+            const int b = ((t * kBeamWaves + wave) * 64 + lane) / (a.segs * a.keep);
+            const uint64_t k = few_token[t] >= 0 ? score(few_value[t], b) : 0;
+            list.add(k > 0, k, (uint32_t)b * (uint32_t)a.vocab + (uint32_t)few_token[t]);
+        }
+    } else {
+        // What the segments kept is a list each.  At least `keep` candidates are not below the keep-th best of the lists' largest ones: of a
+        // wave's lists first, then of those that all waves have found, and few lists are left to be looked into.
+        constexpr int U = kBeamLists / 256;
+        uint64_t best[U];
+        uint32_t high[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = (u * 64 + lane) * kBeamWaves + wave;
+            best[u] = 0;
+            if (i < lists) best[u] = score(list_top[i], i / a.segs);
+            high[u] = (uint32_t)(best[u] >> 32);
+        }
+        bool in[U];
+        int found = 0, count;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            in[u] = best[u] > 0;
+            found += __popcll(__ballot(in[u]));
+        }
+        const uint32_t own = found >= a.keep ? reach_of(high, in, a.keep, count) : 0u;
+        uint32_t* const heads = &idxs[0][0];  // [kBeamWaves][64]: of each wave's lists the first keep that reach its bound
+        {
+            heads[wave * 64 + lane] = 0;
+            wave_fence();
+            int at = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool take = in[u] && high[u] >= own;
+                const uint64_t who = __ballot(take);
+                const int to = at + __popcll(who & ((1ull << lane) - 1));
+                if (take && to < 64) heads[wave * 64 + to] = high[u];
+                at += __popcll(who);
             }
         }
-        if (list.n + 64 > kBeamList) floor = max(floor, list.keep_best(a.keep));
-        list.add(k >= floor, k, idx);
+        __syncthreads();
+        uint64_t floor = 1;
+        {
+            uint32_t every[kBeamWaves];
+            bool of[kBeamWaves];
+            int there = 0;
+#pragma unroll
+            for (int w = 0; w < kBeamWaves; ++w) {
+                every[w] = heads[w * 64 + lane];
+                of[w] = every[w] > 0;
+                there += __popcll(__ballot(of[w]));
+            }
+            if (there >= a.keep) floor = max(floor, (uint64_t)reach_of(every, of, a.keep, count) << 32);
+        }
+        __syncthreads();  // (the heads have been read)
+        int room = 1;  // lanes to a list
+        while (room < a.keep) room *= 2;
+        const int at_once = 64 / room, mine = lane / room, e = lane % room;
+        for (int u = 0; u < U; ++u) {
+            uint64_t left = __ballot(best[u] >= floor);
+            while (left) {
+                constexpr int STEPS = 4;  // on their way at one time
+                int32_t token[STEPS];
+                float value[STEPS];
+                int beam[STEPS];
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    int l = -1;  // this lane's list: the mine-th of those left
+                    for (int q = 0; q < at_once && left; ++q) {
+                        if (q == mine) l = __builtin_ctzll(left);
+                        left &= left - 1;
+                    }
+                    token[t] = -1;
+                    value[t] = 0.f;
+                    beam[t] = 0;
+                    if (l >= 0 && e < a.keep) {
+                        const int i = (u * 64 + l) * kBeamWaves + wave;
+                        const int64_t place = (row0 * a.segs + i) * a.keep + e;
+                        beam[t] = i / a.segs;
+                        token[t] = a.token[place];
+                        value[t] = a.value[place];
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) {
+                    const uint64_t k = token[t] >= 0 ? score(value[t], beam[t]) : 0;
+                    if (list.n + 64 > kBeamList) floor = max(floor, list.keep_best(a.keep));
+                    list.add(k >= floor, k, (uint32_t)beam[t] * (uint32_t)a.vocab + (uint32_t)token[t]);
+                }
+            }
+        }
     }
-    list.keep_best(a.keep);
+    if (list.n > 64) list.keep_best(a.keep);
     if (lane == 0) wave_n[wave] = list.n;
     __syncthreads();
     if (wave > 0) return;
@@ -512,7 +663,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
 constexpr int kBeamTarget = 1024;
 int beam_segments(int num_seqs, int beams, int vocab) {
     const int64_t rows = std::max<int64_t>(1, (int64_t)num_seqs * beams), most = ceil_div(vocab, kBeamWaves * kBeamPass);
-    return (int)std::min(most, ceil_div(kBeamTarget, rows));
+    return (int)std::min({most, ceil_div(kBeamTarget, rows), (int64_t)kBeamLists / beams});
 }
 
 bool beam_sizes_ok(int num_seqs, int beams, int vocab, int keep) {
