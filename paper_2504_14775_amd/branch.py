@@ -6,6 +6,7 @@ import ctypes as C
 import math
 
 import numpy as np
+import torch
 
 from .binding import GLLM_OK, GllmError, _stream_ptr, load_library
 
@@ -45,20 +46,33 @@ def _refuse(what: str):
     raise GllmError(_INVALID, what)
 
 
-def _check(call: str, dtype, tensors, rows_only: bool = False) -> None:
-    """tensors: of this type, on the current GPU, contiguous (rows_only: inside a row)."""
-    import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+
+
+def _check(call: str, tensors, rows_only=()) -> int:
+    """tensors: pairs of a tensor and its type, all on the current GPU and contiguous (those of rows_only: inside a row).  Returns the
+    GPU's index."""
+    dev = tensors[0][0].get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():           # (what torch.cuda.current_device() asks, behind a look at the environment)
+        _refuse(f"{call}: tensors on the current GPU are wanted, got one on {tensors[0][0].device}")
+    for t, dtype in tensors:
         if t.get_device() != dev or t.dtype is not dtype:
-            _refuse(f"{call}: a tensor of {dtype} on the current GPU is wanted, got {t.dtype} on {t.device}")
-        if not (t.dim() == 2 and t.stride(1) == 1 if rows_only else t.is_contiguous()):
-            _refuse(f"{call}: a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not contiguous")
+            _refuse(f"{call}: a tensor of {dtype} on cuda:{dev} is wanted, got {t.dtype} on {t.device}")
+        if not t.is_contiguous():
+            for r in rows_only:
+                if r is t and t.dim() == 2 and t.stride(1) == 1:
+                    break
+            else:
+                _refuse(f"{call}: a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not contiguous")
+    return dev
+
+
+def _stream(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream_ptr(stream)
 
 
 def _own_workspace(call: str, size: int, like, stream):
     """A workspace from torch's allocator, which may give it to somebody else on the call's stream only."""
-    import torch
     if stream is None:
         return torch.empty(size, dtype=torch.uint8, device=like.device)
     if isinstance(stream, int):
@@ -89,25 +103,23 @@ def gllm_op_tree_attention(q, k_pool, v_pool, block_tables, cached_len, row_star
     """q, out: bf16 [R, n_q*d]; k_pool: bf16 [pages, n_kv, d/8, 16, 8], v_pool: bf16 [pages, n_kv, d, 16], one layer; block_tables:
     int32 [S, entries]; cached_len: int32 [S]; row_start: int32 [S+1]; parents: int32 [R].  scale: 1/sqrt(d) if not given;
     workspace: uint8, taken from torch's allocator if not given."""
-    import torch
     call = "gllm_op_tree_attention"
     n_kv, d = _pool_shape(call, k_pool, v_pool, 1)
-    _check(call, torch.bfloat16, (q, out), rows_only=True)
-    _check(call, torch.bfloat16, (k_pool, v_pool))
-    _check(call, torch.int32, (block_tables, cached_len, row_start, parents))
+    dev = _check(call, ((q, _BF16), (out, _BF16), (k_pool, _BF16), (v_pool, _BF16), (block_tables, _I32), (cached_len, _I32), (row_start, _I32),
+                        (parents, _I32)), rows_only=(q, out))
     rows, seqs = q.shape[0], cached_len.shape[0]
-    if q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1 or parents.numel() != rows:
+    if q.dim() != 2 or q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1 or parents.numel() != rows:
         _refuse(f"{call}: shapes q {tuple(q.shape)}, out {tuple(out.shape)}, block_tables {tuple(block_tables.shape)}, cached_len {tuple(cached_len.shape)}, "
                 f"row_start {tuple(row_start.shape)}, parents {tuple(parents.shape)}")
     n_q = q.shape[1] // d
     lib = _lib()
     if workspace is None:
         workspace = _own_workspace(call, int(lib.gllm_op_tree_attention_workspace_bytes(n_q, n_kv, d, max_nodes)), q, stream)
-    _check(call, torch.uint8, (workspace,))
+    _check(call, ((workspace, _U8),))
     st = lib.gllm_op_tree_attention(q.data_ptr(), _row_stride(q), k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], block_tables.data_ptr(),
                                     block_tables.shape[1], cached_len.data_ptr(), row_start.data_ptr(), parents.data_ptr(), seqs, rows,
                                     max_nodes, n_q, n_kv, d, 1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(), _row_stride(out),
-                                    workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+                                    workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
     if st != GLLM_OK:
         raise GllmError(st, call)
 
@@ -116,9 +128,9 @@ def gllm_op_tree_commit(tokens, parents, sampled, row_start, cached_len, block_t
                         stream=None) -> None:
     """tokens, parents, sampled, path: int32 [R]; row_start: int32 [S+1]; cached_len, count, next_token: int32 [S]; block_tables: int32
     [S, entries]; k_pool: bf16 [layers, pages, n_kv, d/8, 16, 8], v_pool: bf16 [layers, pages, n_kv, d, 16], or both None (no moves)."""
-    import torch
     call = "gllm_op_tree_commit"
-    _check(call, torch.int32, (tokens, parents, sampled, path, row_start, cached_len, block_tables, count, next_token))
+    dev = _check(call, ((tokens, _I32), (parents, _I32), (sampled, _I32), (path, _I32), (row_start, _I32), (cached_len, _I32), (block_tables, _I32),
+                        (count, _I32), (next_token, _I32)))
     rows, seqs = tokens.numel(), cached_len.numel()
     if parents.numel() != rows or sampled.numel() != rows or path.numel() != rows or row_start.numel() != seqs + 1 or block_tables.dim() != 2 or \
             block_tables.shape[0] != seqs or count.numel() != seqs or next_token.numel() != seqs or (k_pool is None) != (v_pool is None):
@@ -126,12 +138,12 @@ def gllm_op_tree_commit(tokens, parents, sampled, row_start, cached_len, block_t
     layers = pages = n_kv = d = 0
     if k_pool is not None:
         n_kv, d = _pool_shape(call, k_pool, v_pool, 2)
-        _check(call, torch.bfloat16, (k_pool, v_pool))
+        _check(call, ((k_pool, _BF16), (v_pool, _BF16)))
         layers, pages = k_pool.shape[:2]
     st = _lib().gllm_op_tree_commit(tokens.data_ptr(), parents.data_ptr(), sampled.data_ptr(), row_start.data_ptr(), cached_len.data_ptr(),
                                     block_tables.data_ptr(), block_tables.shape[1], seqs, rows, None if k_pool is None else k_pool.data_ptr(),
                                     None if v_pool is None else v_pool.data_ptr(), layers, pages, n_kv, d, path.data_ptr(), count.data_ptr(),
-                                    next_token.data_ptr(), _stream_ptr(stream))
+                                    next_token.data_ptr(), _stream(stream, dev))
     if st != GLLM_OK:
         raise GllmError(st, call)
 
@@ -143,12 +155,9 @@ def gllm_op_beam_select_workspace_bytes(num_seqs: int, beams: int, vocab: int, k
 def gllm_op_beam_select(logits, vocab: int, scores, out_scores, out_beams, out_tokens, workspace=None, stream=None) -> None:
     """logits: fp32 [S*W, >= vocab] (row stride taken from the tensor); scores: fp32 [S, W]; out_scores: fp32, out_beams, out_tokens:
     int32, [S, keep]; workspace: uint8, taken from torch's allocator if not given."""
-    import torch
     call = "gllm_op_beam_select"
-    _check(call, torch.float32, (logits,), rows_only=True)
-    _check(call, torch.float32, (scores, out_scores))
-    _check(call, torch.int32, (out_beams, out_tokens))
-    if scores.dim() != 2 or out_scores.dim() != 2 or logits.shape[0] != scores.numel() or logits.shape[1] < vocab or out_scores.shape[0] != scores.shape[0] or \
+    dev = _check(call, ((logits, _F32), (scores, _F32), (out_scores, _F32), (out_beams, _I32), (out_tokens, _I32)), rows_only=(logits,))
+    if logits.dim() != 2 or scores.dim() != 2 or out_scores.dim() != 2 or logits.shape[0] != scores.numel() or logits.shape[1] < vocab or out_scores.shape[0] != scores.shape[0] or \
             out_beams.shape != out_scores.shape or out_tokens.shape != out_scores.shape:
         _refuse(f"{call}: shapes logits {tuple(logits.shape)}, scores {tuple(scores.shape)}, outputs {tuple(out_scores.shape)}, "
                 f"{tuple(out_beams.shape)}, {tuple(out_tokens.shape)}, vocabulary {vocab}")
@@ -156,24 +165,23 @@ def gllm_op_beam_select(logits, vocab: int, scores, out_scores, out_beams, out_t
     seqs, beams, keep = scores.shape[0], scores.shape[1], out_scores.shape[1]
     if workspace is None:
         workspace = _own_workspace(call, int(lib.gllm_op_beam_select_workspace_bytes(seqs, beams, vocab, keep)), logits, stream)
-    _check(call, torch.uint8, (workspace,))
+    _check(call, ((workspace, _U8),))
     st = lib.gllm_op_beam_select(logits.data_ptr(), _row_stride(logits), scores.data_ptr(), seqs, beams, vocab, keep, out_scores.data_ptr(),
-                                 out_beams.data_ptr(), out_tokens.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+                                 out_beams.data_ptr(), out_tokens.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream, dev))
     if st != GLLM_OK:
         raise GllmError(st, call)
 
 
 def gllm_op_copy_pages(k_pool, v_pool, src, dst, stream=None) -> None:
     """k_pool: bf16 [layers, pages, n_kv, d/8, 16, 8], v_pool: bf16 [layers, pages, n_kv, d, 16]; src, dst: page ids on the host."""
-    import torch
     call = "gllm_op_copy_pages"
     n_kv, d = _pool_shape(call, k_pool, v_pool, 2)
-    _check(call, torch.bfloat16, (k_pool, v_pool))
+    dev = _check(call, ((k_pool, _BF16), (v_pool, _BF16)))
     s = np.ascontiguousarray(src, dtype=np.int32)
     t = np.ascontiguousarray(dst, dtype=np.int32)
     if s.ndim != 1 or s.shape != t.shape:
         _refuse(f"{call}: {s.shape} sources, {t.shape} destinations")
     st = _lib().gllm_op_copy_pages(k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pool.shape[1], n_kv, d, s.ctypes.data, t.ctypes.data,
-                                   s.shape[0], _stream_ptr(stream))
+                                   s.shape[0], _stream(stream, dev))
     if st != GLLM_OK:
         raise GllmError(st, call)
