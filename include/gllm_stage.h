@@ -176,6 +176,16 @@ gllm_status gllm_stage_set_option(gllm_stage* stage, const char* name /*HOST*/, 
 gllm_status gllm_stage_forward(gllm_stage* stage, const gllm_batch* batch /*HOST*/, const void* hidden_in,
                                void* hidden_out, float* hidden_out_f32, void* stream);
 
+/* The same for batches whose sequences may be trees of drafted tokens (speculative decoding; the operators around it are in
+ * gllm_branch.h).
+ *   parents  HOST [T]: for every row the index of its parent among the rows of its sequence, smaller than its own, or -1 for a root
+ *            (GLLM_E_INVALID otherwise)
+ * A sequence with parents -1, 0, 1, ..., new_tokens - 2 is a chunk or a decode row as in gllm_stage_forward, with the same results.
+ * Any other is a tree of at most 256 nodes (GLLM_E_CAPACITY): row i sees positions 0 .. cached_len-1, its ancestors and itself, is
+ * rotated for position cached_len + depth (a root's depth is 0), and its keys and values are written to position cached_len + i. */
+gllm_status gllm_stage_forward_tree(gllm_stage* stage, const gllm_batch* batch /*HOST*/, const int32_t* parents /*HOST*/,
+                                    const void* hidden_in, void* hidden_out, float* hidden_out_f32, void* stream);
+
 /* Per-kernel timing.  With profiling on, forward() brackets every kernel with HIP events on
  * the caller's stream; gllm_stage_read_profile() synchronises those events and adds their
  * durations to per-class totals.  Classes are listed by gllm_profile_class_name(i) for

@@ -23,7 +23,7 @@ GEMM_STORE_F32, GEMM_ADD_F32, GEMM_SWIGLU_BF16 = 0, 1, 2
 EXPORTS = [
     "gllm_stage_create", "gllm_stage_destroy", "gllm_last_error", "gllm_status_name",
     "gllm_stage_workspace_bytes", "gllm_stage_bind_workspace", "gllm_stage_load_layer",
-    "gllm_stage_bind_kv_pool", "gllm_stage_share_weights", "gllm_stage_set_alias_check", "gllm_stage_set_option", "gllm_stage_forward",
+    "gllm_stage_bind_kv_pool", "gllm_stage_share_weights", "gllm_stage_set_alias_check", "gllm_stage_set_option", "gllm_stage_forward", "gllm_stage_forward_tree",
     "gllm_stage_set_profiling", "gllm_stage_read_profile", "gllm_profile_num_classes",
     "gllm_profile_class_name", "gllm_op_pack_weight", "gllm_op_gemm_bf16", "gllm_op_gemm_bf16_splitk", "gllm_op_gemm_plan", "gllm_op_gemm_tile_columns", "gllm_op_rmsnorm", "gllm_op_peak_mfma", "gllm_op_peak_read", "gllm_op_peak_read_nt",
 ]
@@ -111,6 +111,8 @@ def load_library():
     lib.gllm_stage_set_option.argtypes = [vp, C.c_char_p, i64]
     lib.gllm_stage_forward.restype = i32
     lib.gllm_stage_forward.argtypes = [vp, C.POINTER(gllm_batch), vp, vp, vp, vp]
+    lib.gllm_stage_forward_tree.restype = i32
+    lib.gllm_stage_forward_tree.argtypes = [vp, C.POINTER(gllm_batch), C.POINTER(i32), vp, vp, vp, vp]
     lib.gllm_stage_set_profiling.restype = i32
     lib.gllm_stage_set_profiling.argtypes = [vp, i32]
     lib.gllm_stage_read_profile.restype = i32
@@ -226,6 +228,21 @@ class Stage:
         f32 = None if hidden_out_f32 is None else hidden_out_f32.data_ptr()
         self._check(self.lib.gllm_stage_forward(self.handle, C.byref(b), hidden_in.data_ptr(), hidden_out.data_ptr(),
                                                 f32, _stream_ptr(stream)))
+
+    def forward_tree(self, new_tokens, cached_len, block_tables, parents, hidden_in, hidden_out, hidden_out_f32=None,
+                     stream=None) -> None:
+        """forward() of a batch whose sequences may be trees: parents, one per row, index within the sequence, -1 for a root."""
+        nt = np.ascontiguousarray(new_tokens, dtype=np.int32)
+        cl = np.ascontiguousarray(cached_len, dtype=np.int32)
+        bt = np.ascontiguousarray(block_tables, dtype=np.int32)
+        up = np.ascontiguousarray(parents, dtype=np.int32)
+        assert bt.ndim == 2 and bt.shape[0] == nt.shape[0] == cl.shape[0] and up.shape == (int(nt.sum()),)
+        ip = C.POINTER(C.c_int32)
+        b = gllm_batch(int(nt.shape[0]), int(bt.shape[1]), nt.ctypes.data_as(ip), cl.ctypes.data_as(ip),
+                       bt.ctypes.data_as(ip))
+        f32 = None if hidden_out_f32 is None else hidden_out_f32.data_ptr()
+        self._check(self.lib.gllm_stage_forward_tree(self.handle, C.byref(b), up.ctypes.data_as(ip), hidden_in.data_ptr(), hidden_out.data_ptr(),
+                                                     f32, _stream_ptr(stream)))
 
     def forward_raw(self, batch: gllm_batch, hidden_in_ptr, hidden_out_ptr, hidden_out_f32_ptr, stream_ptr) -> int:
         """Unchecked call (returns the status), for tests of the error paths."""

@@ -105,6 +105,7 @@ struct RopeKvArgs {
     const float* rope_cs;    // [max_position][d/2][2] (cos, sin)
     const int32_t* tok_pos;  // [T]
     const int32_t* tok_page; // [T] physical page of the token's own position
+    const int32_t* tok_rope; // [T] rotary position where that is not tok_pos (nodes of trees), or null
     bf16_t* q_out;           // [T][n_q*d] bf16, rotated
     int64_t ld_q;
     bf16_t* k_pool;          // this layer's K pool
@@ -206,6 +207,7 @@ hipError_t launch_prefill_attention(const AttnArgs& a, const PrefillItem* items,
 bool attention_in_one_launch(int n_q, int n_kv, int64_t num_tiles, bool half, int num_decode_rows);
 hipError_t launch_hybrid_attention(const AttnArgs& a, const PrefillItem* items, int num_items, bool half, const DecodeArgs& dec, hipStream_t stream);
 
+constexpr int kMaxTreeNodes = 256;
 // Trees of drafted tokens (see kernels_tree.hip): device arrays, nothing of which the host reads.
 struct TreeArgs {
     const bf16_t* q;             // [num_rows][ld_q]

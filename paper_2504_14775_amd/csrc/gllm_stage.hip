@@ -27,10 +27,10 @@ namespace {
 
 enum ProfClass {
     PC_RMSNORM = 0, PC_GEMM_QKV, PC_ROPE_KV, PC_ATTN_PREFILL, PC_ATTN_DECODE, PC_ATTN_MERGE, PC_GEMM_O,
-    PC_GEMM_GATEUP, PC_GEMM_DOWN, PC_CAST, PC_COUNT
+    PC_GEMM_GATEUP, PC_GEMM_DOWN, PC_CAST, PC_ATTN_TREE, PC_COUNT
 };
 const char* kProfNames[PC_COUNT] = {"rmsnorm", "gemm_qkv", "rope_kv_write", "attn_prefill", "attn_decode",
-                                    "attn_decode_merge", "gemm_o", "gemm_gate_up_swiglu", "gemm_down", "cast_out"};
+                                    "attn_decode_merge", "gemm_o", "gemm_gate_up_swiglu", "gemm_down", "cast_out", "attn_tree"};
 
 thread_local std::string g_create_error;
 
@@ -50,7 +50,9 @@ constexpr int kDecodeSlots = 512;  // decode attention workgroups that run at on
 constexpr int kMaxSplits = kMaxPlanes;
 
 struct MetaLayout {  // offsets in bytes inside the metadata block (host staging and device copy alike)
-    size_t tok_pos, tok_page, tok_own_v, bt_flat, dec_items, dec_rows, pre_items, v_tiles, total;
+    size_t tok_pos, tok_page, tok_own_v, bt_flat, dec_items, dec_rows, pre_items, v_tiles;
+    size_t tok_rope, parents, trees;  // of batches with trees
+    size_t total;
 };
 
 }  // namespace
@@ -109,6 +111,7 @@ struct gllm_stage {
     // scratch for the decode work items, max_items each: as they come, and the order they are launched in
     std::vector<DecodeItem> item_list;
     std::vector<int32_t> item_order;
+    std::vector<uint8_t> tree_seq;      // per sequence of a batch with trees: whether it is one
     std::vector<uint8_t> page_writers;  // per page of the pool, 0 between calls (see own_pages)
 };
 
@@ -121,6 +124,13 @@ gllm_status fail(gllm_stage* s, gllm_status code, const std::string& msg) {
 
 gllm_status hip_fail(gllm_stage* s, hipError_t e, const char* what) {
     return fail(s, GLLM_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+// Whether the parents of a sequence's n rows make it a tree, not a chain.
+bool is_tree(const int32_t* parents, int n) {
+    for (int t = 0; t < n; ++t)
+        if (parents[t] != t - 1) return true;
+    return false;
 }
 
 void free_layer(LayerBuffers& L) {
@@ -173,7 +183,10 @@ size_t workspace_layout(gllm_stage* s, unsigned char* base) {
     s->act = (bf16_t*)take((size_t)s->m_pad * s->inter_pad * 2);
     s->part_o = (float*)take((size_t)s->max_items * c.n_q_heads * c.head_dim * 4);
     s->part_ml = (float*)take((size_t)s->max_items * c.n_q_heads * 2 * 4);
-    s->y = (float*)take((size_t)kMaxSplits * c.max_tokens * c.hidden * 4);
+    // (the attention of trees keeps its partial results where those of the projections lie before and after it)
+    size_t tree_bytes = 0;
+    for (int n = 1; n <= kMaxTreeNodes; ++n) tree_bytes = std::max(tree_bytes, tree_workspace_bytes(c.n_q_heads, c.n_kv_heads, c.head_dim, n));
+    s->y = (float*)take(std::max((size_t)kMaxSplits * c.max_tokens * c.hidden * 4, tree_bytes));
     return off;
 }
 
@@ -378,6 +391,9 @@ gllm_status gllm_stage_create(const gllm_stage_config* cfg, gllm_stage** out) {
         m.dec_rows = take(((size_t)c.max_seqs + s->max_items / 2) * sizeof(DecodeRow));
         m.pre_items = take((size_t)s->max_pre_items * sizeof(PrefillItem));
         m.v_tiles = take((size_t)s->max_v_tiles * sizeof(VTile));
+        m.tok_rope = take((size_t)c.max_tokens * 4);
+        m.parents = take((size_t)c.max_tokens * 4);
+        m.trees = take((size_t)c.max_seqs * 16);
         m.total = off;
         if ((e = hipMalloc((void**)&s->meta_dev, m.total)) != hipSuccess) return bail(e, "hipMalloc(metadata)");
         for (int i = 0; i < kStagingSlots; ++i) {
@@ -565,8 +581,9 @@ static bool worth_cutting(const gllm_stage_config& c, int64_t rows, int64_t wg_b
     return scale * std::max(block * longest_part, block_of_all * wg_blocks) + merge < 0.9 * scale * block * longest;
 }
 
-gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* hidden_in, void* hidden_out,
-                               float* hidden_out_f32, void* stream_) {
+// parents: null, or the parent of every token row within its sequence (gllm_stage_forward_tree).
+static gllm_status forward(gllm_stage* s, const gllm_batch* b, const int32_t* parents, const void* hidden_in, void* hidden_out,
+                           float* hidden_out_f32, void* stream_) {
     if (!s) return GLLM_E_INVALID;
     const gllm_stage_config& c = s->cfg;
     if (!b || !hidden_in || !hidden_out) return fail(s, GLLM_E_INVALID, "null argument");
@@ -580,7 +597,8 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
     if (S > c.max_seqs) return fail(s, GLLM_E_INVALID, "num_seqs exceeds max_seqs");
 
     // ---- validation (no side effects before it has passed) ----
-    int64_t T = 0, total_pages = 0;
+    int64_t T = 0, total_pages = 0, tree_rows = 0;
+    int n_trees = 0, most_nodes = 0, most_pages = 0;
     for (int i = 0; i < S; ++i) {
         const int n = b->new_tokens[i], cl = b->cached_len[i];
         if (n < 1) return fail(s, GLLM_E_INVALID, "new_tokens < 1 for sequence " + std::to_string(i));
@@ -593,6 +611,17 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
         T += n;
         total_pages += pages;
         if (T > c.max_tokens) return fail(s, GLLM_E_CAPACITY, "batch exceeds max_tokens");
+        const int64_t row0 = T - n;
+        if (parents && is_tree(parents + row0, n)) {
+            if (n > kMaxTreeNodes) return fail(s, GLLM_E_CAPACITY, "sequence " + std::to_string(i) + " has a tree of more than 256 nodes");
+            for (int t = 0; t < n; ++t)
+                if (parents[row0 + t] < -1 || parents[row0 + t] >= t)
+                    return fail(s, GLLM_E_INVALID, "sequence " + std::to_string(i) + " node " + std::to_string(t) + " has parent " + std::to_string(parents[row0 + t]));
+            ++n_trees;
+            tree_rows += n;
+            most_nodes = std::max(most_nodes, n);
+            most_pages = std::max(most_pages, (int)pages);
+        }
         const int32_t* row = b->block_tables + (int64_t)i * b->block_table_stride;
         for (int64_t p = 0; p < pages; ++p)
             if (row[p] < 0 || row[p] >= s->num_blocks)
@@ -611,6 +640,17 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
             return fail(s, GLLM_E_BLOCK_ALIAS, "two (sequence, logical page) pairs receiving new tokens share a physical page");
     }
     if (T == 0) return GLLM_OK;
+
+    // A sequence is a decode row, a chunk or a tree.  (The lists exist where there are trees.)
+    try {
+        s->tree_seq.assign(n_trees > 0 ? (size_t)S : 0, 0);
+    } catch (const std::bad_alloc&) {
+        return fail(s, GLLM_E_CAPACITY, "no memory for the list of trees");
+    }
+    if (n_trees > 0)
+        for (int64_t i = 0, row0 = 0; i < S; row0 += b->new_tokens[i++]) s->tree_seq[i] = is_tree(parents + row0, b->new_tokens[i]);
+    auto tree = [&](int i) { return n_trees > 0 && s->tree_seq[i] != 0; };
+    auto chunk = [&](int i) { return b->new_tokens[i] > 1 && !tree(i); };
 
     // ---- decode partitioning ----
     int n_dec = 0;
@@ -662,13 +702,13 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
     // keys and values pass through LDS once per item: 2048 rows 8975, halves 9047).
     int64_t whole_wgs = 0;
     for (int i = 0; i < S; ++i)
-        if (b->new_tokens[i] > 1) whole_wgs += ceil_div(b->new_tokens[i], prefill_item_rows(c.n_q_heads, c.n_kv_heads, false));
+        if (chunk(i)) whole_wgs += ceil_div(b->new_tokens[i], prefill_item_rows(c.n_q_heads, c.n_kv_heads, false));
     whole_wgs *= c.n_q_heads / prefill_heads_per_workgroup(c.n_q_heads, c.n_kv_heads, false);
     const bool half_items = whole_wgs <= kHalfItemsMax;
     const int pre_rows = prefill_item_rows(c.n_q_heads, c.n_kv_heads, half_items);
     int64_t n_tiles = 0;
     for (int i = 0; i < S; ++i)
-        if (b->new_tokens[i] > 1) n_tiles += ceil_div(b->new_tokens[i], pre_rows);
+        if (chunk(i)) n_tiles += ceil_div(b->new_tokens[i], pre_rows);
     const bool one_launch = attention_in_one_launch(c.n_q_heads, c.n_kv_heads, n_tiles, half_items, n_dec);
     // f(first row, rows, key blocks, those of them that every row of it sees) for each prefill tile of sequence i
     auto for_tiles = [&](int i, auto&& f) {
@@ -701,7 +741,7 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
             if (b->new_tokens[i] == 1) {
                 room -= ceil_div((int64_t)b->cached_len[i] + 1, part);
                 dec_keys += (int64_t)b->cached_len[i] + 1;
-            } else for_tiles(i, [&](int, int, int all, int full) {
+            } else if (chunk(i)) for_tiles(i, [&](int, int, int all, int full) {
                 blocks += all;
                 longest = std::max<int64_t>(longest, all);
                 most_full = std::max<int64_t>(most_full, full);
@@ -712,7 +752,7 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
             int64_t items = 0, longest_part = 0;
             cut_slots = cut_rows = 0;
             for (int i = 0; i < S; ++i)
-                if (b->new_tokens[i] > 1) for_tiles(i, [&](int, int rows, int all, int full) {
+                if (chunk(i)) for_tiles(i, [&](int, int rows, int all, int full) {
                     const int parts = parts_of(full, len);
                     items += parts;
                     longest_part = std::max<int64_t>(longest_part, all - full + ceil_div(full, parts));
@@ -720,7 +760,7 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
                     cut_rows += parts > 1 ? rows : 0;
                 });
             if (items * groups > kPrefillSlots || cut_slots > room) continue;
-            if (worth_cutting(c, T - n_dec, blocks * groups, longest, longest_part, cut_slots)) part_blocks = len;
+            if (worth_cutting(c, T - n_dec - tree_rows, blocks * groups, longest, longest_part, cut_slots)) part_blocks = len;
             break;
         }
         if (part_blocks == INT32_MAX) cut_slots = cut_rows = 0;
@@ -728,7 +768,7 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
     for (int i = 0; i < S; ++i) {
         if (b->new_tokens[i] == 1) cnt_items += ceil_div((int64_t)b->cached_len[i] + 1, part);
         else {
-            for_tiles(i, [&](int, int, int, int full) { cnt_pre += parts_of(full, part_blocks); });
+            if (chunk(i)) for_tiles(i, [&](int, int, int, int full) { cnt_pre += parts_of(full, part_blocks); });
             cnt_vt += ((int64_t)b->cached_len[i] + b->new_tokens[i] - 1) / kPage - b->cached_len[i] / kPage + 1;
         }
     }
@@ -746,6 +786,9 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
         ml.dec_rows = take((size_t)(n_dec + cut_rows) * sizeof(DecodeRow));
         ml.pre_items = take((size_t)cnt_pre * sizeof(PrefillItem));
         ml.v_tiles = take((size_t)cnt_vt * sizeof(VTile));
+        ml.tok_rope = take(n_trees > 0 ? (size_t)T * 4 : 0);
+        ml.parents = take(n_trees > 0 ? (size_t)T * 4 : 0);
+        ml.trees = take((size_t)n_trees * 16);
         ml.total = off;
     }
     int32_t* tok_pos = (int32_t*)(st_base + ml.tok_pos);
@@ -756,7 +799,10 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
     DecodeItem* dec_items = (DecodeItem*)(st_base + ml.dec_items);
     DecodeRow* dec_rows = (DecodeRow*)(st_base + ml.dec_rows);
     PrefillItem* pre_items = (PrefillItem*)(st_base + ml.pre_items);
-    int n_items = 0, n_rows = 0, n_pre = 0, n_vt = 0;
+    // of each tree: cached length, first row, row behind the last one, offset of its first page id
+    int32_t *tree_cached = (int32_t*)(st_base + ml.trees), *tree_begin = tree_cached + n_trees, *tree_end = tree_begin + n_trees, *tree_bt = tree_end + n_trees;
+    if (n_trees > 0) std::memcpy(st_base + ml.parents, parents, (size_t)T * 4);
+    int n_items = 0, n_rows = 0, n_pre = 0, n_vt = 0, at_tree = 0;
     int64_t bt_off = 0, row = 0, cut_at = 0;
     for (int i = 0; i < S; ++i) {
         const int n = b->new_tokens[i], cl = b->cached_len[i];
@@ -767,6 +813,10 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
             tok_pos[row + t] = cl + t;
             tok_page[row + t] = tab[(cl + t) / kPage];
             tok_own_v[row + t] = n == 1;
+        }
+        if (n_trees > 0) {  // a node's rotary position is its depth behind the cached tokens, not its slot's
+            int32_t* rope = (int32_t*)(st_base + ml.tok_rope) + row;
+            for (int t = 0; t < n; ++t) rope[t] = !tree(i) ? cl + t : parents[row + t] < 0 ? cl : rope[parents[row + t]] + 1;
         }
         if (n > 1)  // the V of a chunk is written run by run: the tokens that share a page
             for (int p0 = cl; p0 < cl + n;) {
@@ -790,6 +840,11 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
             // a row with a single item is finished by the attention kernel; the others are merged afterwards
             if (n_items - first == 1) s->item_list[first].single = 1;
             else dec_rows[n_rows++] = DecodeRow{(int32_t)row, first, n_items - first, 0};
+        } else if (tree(i)) {
+            tree_cached[at_tree] = cl;
+            tree_begin[at_tree] = (int32_t)row;
+            tree_end[at_tree] = (int32_t)(row + n);
+            tree_bt[at_tree++] = (int32_t)bt_off;
         } else {
             for_tiles(i, [&](int t0, int rows, int all, int full) {
                 const int parts = parts_of(full, part_blocks);
@@ -858,7 +913,7 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
         }
         // (found out here, while the first kernels already run)
         if (l == s->layer_begin)
-            from_qkv = n_pre == 0 && worth_looking_through(s, total_pages, T) && own_pages(s, b);
+            from_qkv = n_pre == 0 && n_trees == 0 && worth_looking_through(s, total_pages, T) && own_pages(s, b);
         RopeKvArgs ra{};
         ra.qkv = s->qkv; ra.ld_qkv = s->n_qkv_pad; ra.planes = plan_qkv.splits; ra.plane_stride = qkv_plane;
         ra.bias = c.has_qkv_bias ? L.bias : nullptr;
@@ -867,6 +922,7 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
         ra.k_pool = s->k_pool + (int64_t)l * pool_layer; ra.v_pool = s->v_pool + (int64_t)l * pool_layer;
         ra.T = Ti; ra.n_q = c.n_q_heads; ra.n_kv = c.n_kv_heads; ra.d = d;
         ra.v_tiles = d_v_tiles; ra.n_vtiles = n_vt; ra.tok_own_v = d_tok_own_v;
+        ra.tok_rope = n_trees > 0 ? (const int32_t*)(s->meta_dev + ml.tok_rope) : nullptr;
         if (!from_qkv) {
             ProfScope ps(s, st, PC_ROPE_KV);
             HIP_TRY(s, launch_rope_kv_write(ra, st));
@@ -891,6 +947,22 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
                 ProfScope ps(s, st, PC_ATTN_DECODE);
                 HIP_TRY(s, launch_decode_attention(aa, da, st));
             }
+        }
+        if (n_trees > 0) {
+            ProfScope ps(s, st, PC_ATTN_TREE);
+            const int32_t* d_trees = (const int32_t*)(s->meta_dev + ml.trees);
+            TreeArgs ta{};
+            ta.q = s->q; ta.ld_q = s->q_dim;
+            ta.k_pool = aa.k_pool; ta.v_pool = aa.v_pool; ta.num_blocks = (int32_t)s->num_blocks;
+            ta.block_tables = d_bt; ta.table_stride = most_pages; ta.bt_off = d_trees + 3 * n_trees;
+            ta.cached_len = d_trees; ta.row_begin = d_trees + n_trees; ta.row_end = d_trees + 2 * n_trees;
+            ta.parents = (const int32_t*)(s->meta_dev + ml.parents);
+            ta.num_seqs = n_trees; ta.num_rows = Ti; ta.max_nodes = most_nodes;
+            ta.out = s->attn; ta.ld_o = s->q_dim;
+            ta.n_q = c.n_q_heads; ta.n_kv = c.n_kv_heads; ta.d = d;
+            ta.scale_log2 = aa.scale_log2;
+            ta.workspace = s->y;
+            HIP_TRY(s, launch_tree_attention(ta, st));
         }
         if (n_items > 0 || n_rows > 0) {
             ProfScope ps(s, st, PC_ATTN_MERGE);
@@ -923,6 +995,18 @@ gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* h
         HIP_TRY(s, launch_add_cast_out(s->x, s->y, pending, y_plane, (bf16_t*)hidden_out, hidden_out_f32, (int64_t)Ti * H, st));
     }
     return GLLM_OK;
+}
+
+gllm_status gllm_stage_forward(gllm_stage* s, const gllm_batch* b, const void* hidden_in, void* hidden_out,
+                               float* hidden_out_f32, void* stream) {
+    return forward(s, b, nullptr, hidden_in, hidden_out, hidden_out_f32, stream);
+}
+
+gllm_status gllm_stage_forward_tree(gllm_stage* s, const gllm_batch* b, const int32_t* parents, const void* hidden_in, void* hidden_out,
+                                    float* hidden_out_f32, void* stream) {
+    if (!s) return GLLM_E_INVALID;
+    if (!parents && b && b->num_seqs > 0) return fail(s, GLLM_E_INVALID, "null parents");
+    return forward(s, b, parents, hidden_in, hidden_out, hidden_out_f32, stream);
 }
 
 gllm_status gllm_op_gemm_bf16(const void* a, int64_t lda, const void* w, int64_t ldw, void* out, int64_t ldc,

@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256) void rope_kv_write_kernel(RopeKvArgs a, int pa
     const int64_t page = a.tok_page[t];
     const int slot = pos & (kPage - 1);
     const float* row = a.qkv + (int64_t)t * a.ld_qkv;
-    const f32x4* cs = reinterpret_cast<const f32x4*>(a.rope_cs + (int64_t)pos * half * 2);
+    const f32x4* cs = reinterpret_cast<const f32x4*>(a.rope_cs + (int64_t)(a.tok_rope ? a.tok_rope[t] : pos) * half * 2);
     const int q_quads = a.n_q * hq, k_quads = a.n_kv * hq;
     const int k_col0 = a.n_q * d, v_col0 = k_col0 + a.n_kv * d;
     auto gather = [&](int col) {  // sum of the partial planes (+ bias) of 4 consecutive columns
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256) void rope_kv_write_batched_kernel(RopeKvArgs a
     const int64_t page = a.tok_page[t];
     const int slot = pos & (kPage - 1);
     const float* row = a.qkv + (int64_t)t * a.ld_qkv;
-    const f32x4* cs = reinterpret_cast<const f32x4*>(a.rope_cs + (int64_t)pos * half * 2);
+    const f32x4* cs = reinterpret_cast<const f32x4*>(a.rope_cs + (int64_t)(a.tok_rope ? a.tok_rope[t] : pos) * half * 2);
     const bool own_v = !a.tok_own_v || a.tok_own_v[t];
     const int q_quads = a.n_q * hq, rope_units = (a.n_q + a.n_kv) * hq, units = rope_units + (own_v ? a.n_kv * d / 4 : 0);
     const int k_col0 = a.n_q * d, v_col0 = k_col0 + a.n_kv * d;

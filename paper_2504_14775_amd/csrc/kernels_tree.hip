@@ -14,7 +14,8 @@
 
 namespace {
 
-constexpr int kTreeNodes = 256;             // most nodes of a tree: one per thread
+constexpr int kTreeNodes = kMaxTreeNodes;   // one per thread
+static_assert(kTreeNodes == 256, "a node per thread of a workgroup");
 constexpr int kTreeWords = kTreeNodes / 32;
 constexpr int kTreeStages = 3;
 
