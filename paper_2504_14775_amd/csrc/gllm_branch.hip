@@ -362,6 +362,7 @@ __global__ __launch_bounds__(256, 4) void beam_rows_kernel(BeamArgs a) {
     // subtraction in 64 bits less per logit, of sixteen operations).
     float ref = -INFINITY;
     double sum = 0.0, r = 0.0;  // (sum: of this lane)
+    float most = -INFINITY;     // this lane's largest
     auto near = [&](float x) { return fabsf(x) < 1000.f; };
     auto refer_to = [&](float x) {  // (the same for the wave)
         const double was = near(ref) ? r : (double)ref * kLog2E;
@@ -411,6 +412,7 @@ __global__ __launch_bounds__(256, 4) void beam_rows_kernel(BeamArgs a) {
             for (int e = 0; e < 4; ++e) quad[j] = fmaxf(quad[j], at_least(x[j][e], low));
             top = fmaxf(top, quad[j]);
         }
+        most = fmaxf(most, top);
         if (__any(top > ref + kBeamSlack || (top > ref && ref == -INFINITY))) refer_to(wave_max(top));
         if (near(ref)) {
             const double c = kRound - r;
@@ -438,13 +440,16 @@ __global__ __launch_bounds__(256, 4) void beam_rows_kernel(BeamArgs a) {
 #pragma unroll
         for (int j = 0; j < kBeamQuads; ++j) x[j] = next[j];
     }
-    if (near(ref)) sum *= exp2_wide(r - (double)ref * kLog2E);
+    // what goes out is the sum by the largest logit: the merge takes it for that of the best candidate too
+    const float largest = wave_max(most);
+    if (near(ref)) sum *= exp2_wide(r - (double)largest * kLog2E);
+    else if (largest > ref) sum *= exp2_wide(((double)ref - (double)largest) * kLog2E);
     if (list.n > 64) list.keep_best(a.keep);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if (lane == 0) {
         wave_sum[wave] = sum;
-        wave_top[wave] = ref;
+        wave_top[wave] = largest;
         wave_n[wave] = list.n;
     }
     __syncthreads();

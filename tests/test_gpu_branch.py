@@ -387,7 +387,8 @@ def check_beams(x, scores, keep, vocab=None, label="", dev=None, **kw):
 
 
 @pytest.mark.parametrize("seqs,beams,vocab,keep", [(1, 1, 1, 1), (1, 1, 5, 8), (2, 3, 63, 6), (3, 4, 1000, 8), (1, 32, 4097, 64), (5, 2, 5003, 4), (16, 5, 50261, 10),
-                                                   (1, 4, 128256, 8), (3, 8, 152064, 16), (1, 1, 300001, 64), (40, 1, 777, 2)])
+                                                   (1, 4, 128256, 8), (3, 8, 152064, 16), (1, 1, 300001, 64), (40, 1, 777, 2),
+                                                   (2, 16, 197294, 26), (8, 32, 20000, 64), (6, 32, 33333, 40), (300, 1, 9001, 5)])
 def test_beam_select(seqs, beams, vocab, keep):
     print(f"beams {seqs} x {beams}, {vocab}, {keep}", flush=True)
     rng = np.random.default_rng(vocab)
