@@ -512,19 +512,21 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
         }
     }
     __syncthreads();
-    for (int b = wave; b < a.beams; b += kBeamWaves) {
-        const int at = b * a.segs;
+    // sixteen lanes to a beam
+    for (int b0 = 0; b0 < a.beams; b0 += 4 * kBeamWaves) {
+        const int b = b0 + wave * 4 + lane / 16, at = min(b, a.beams - 1) * a.segs;
         float m = -INFINITY;
-        for (int i = lane; i < a.segs; i += 64) m = fmaxf(m, list_top[at + i]);
-        m = wave_max(m);
+        for (int i = lane % 16; i < a.segs; i += 16) m = fmaxf(m, list_top[at + i]);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
         double total = 0.0;
-        for (int i = lane; i < a.segs; i += 64) {
+        for (int i = lane % 16; i < a.segs; i += 16) {
             const float t = list_top[at + i];
             if (t > -INFINITY) total += t == m ? list_sum[at + i] : list_sum[at + i] * exp2_wide(((double)t - (double)m) * kLog2E);
         }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-        if (lane == 0) {
+        for (int o = 8; o > 0; o >>= 1) total += __shfl_xor(total, o);
+        if (lane % 16 == 0 && b < a.beams) {
             tops[b] = m;
             // the logarithm in 32 bits and a step of Newton's method, whose error is half the square of the first one's
             const double y = (double)__logf((float)total);
@@ -664,11 +666,12 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     }
 }
 
-// Segments of a row: about kBeamTarget workgroups, each with at least one pass of its four waves.
+// Segments of a row: no more workgroups than run at one time (four per compute unit), unless there are more rows, each with at least one
+// pass of its four waves.
 constexpr int kBeamTarget = 1024;
 int beam_segments(int num_seqs, int beams, int vocab) {
     const int64_t rows = std::max<int64_t>(1, (int64_t)num_seqs * beams), most = ceil_div(vocab, kBeamWaves * kBeamPass);
-    return (int)std::min({most, ceil_div(kBeamTarget, rows), (int64_t)kBeamLists / beams});
+    return (int)std::min({most, std::max<int64_t>(1, kBeamTarget / rows), (int64_t)kBeamLists / beams});
 }
 
 bool beam_sizes_ok(int num_seqs, int beams, int vocab, int keep) {
@@ -781,7 +784,7 @@ gllm_status gllm_op_beam_select(const float* logits, int64_t ld_logits, const fl
     a.logits = logits; a.ld = ld_logits; a.scores = scores;
     a.num_seqs = num_seqs; a.beams = beams; a.vocab = vocab; a.keep = keep;
     a.segs = beam_segments(num_seqs, beams, vocab);
-    a.seg_len = (int32_t)round_up(ceil_div(vocab, a.segs), kBeamWaves * kBeamPass);  // (the last ones may be short of it, or empty)
+    a.seg_len = (int32_t)round_up(ceil_div(vocab, a.segs), kBeamPass);  // (the last ones may be short of it, or empty)
     const int64_t places = (int64_t)num_seqs * beams * a.segs;
     a.sum = (double*)workspace;
     a.top = (float*)(a.sum + places);
