@@ -283,6 +283,35 @@ def test_tree_attention_replayed_from_a_graph():
         t.check(label=f"replayed, {cached}")
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 64), (16, 4, 128)], ids=str)
+def test_any_bound_on_the_nodes_of_a_tree_and_two_calls_at_once(heads):
+    """Trees of 1 to 4 nodes under bounds from 4 to 256: every kernel, with tiles that are mostly empty, over more sequences than a wave has
+    lanes, a few of them cut; then two such calls on streams of their own."""
+    rng = np.random.default_rng(21)
+    cached = [int(rng.integers(0, 90)) for _ in range(80)] + [9000, 5001, 0, 2600]
+    t = Trees(heads, cached, [random_tree(rng, int(rng.integers(1, 5)), "tree") for _ in cached], seed=21, tail_rows=2)
+    whole = {}
+    for most in (4, 8, 9, 64, 65, 127, 128, 256):
+        print(f"{heads}, at most {most} nodes", flush=True)
+        t.out.fill_(7.0)
+        t.run(max_nodes=most)
+        t.check(max_nodes=most, label=f"{heads}, at most {most} nodes")
+        whole[most] = t.out.clone()
+    torch.cuda.synchronize()
+    pairs = []
+    for most in (4, 128):
+        s = torch.cuda.Stream()
+        ws = torch.empty(BR.gllm_op_tree_attention_workspace_bytes(*heads, most), dtype=torch.uint8, device=DEV)
+        pairs.append((most, s, ws, torch.full_like(t.out, 7.0)))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for most, s, ws, out in pairs:
+            BR.gllm_op_tree_attention(t.q, t.k, t.v, *t.dev, out, most, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    for most, _, _, out in pairs:
+        assert torch.equal(out, whole[most])
+
+
 # ---- commit -----------------------------------------------------------------------------------------------------------------
 
 class Commit:
@@ -365,6 +394,40 @@ def test_commit_where_a_rule_is_broken():
     c.cached = np.array([-1, 3, 2 ** 31 - 1, 41, 16 * c.tables.shape[1] - 3], dtype=np.int32)
     _, count, follow = c.check()
     assert count[[0, 1, 2, 4]].tolist() == [0] * 4 and follow[[0, 1, 2, 4]].tolist() == [-1] * 4
+
+
+def test_commit_on_a_stream_and_replayed_from_a_graph():
+    print("commit from a graph", flush=True)
+    rng = np.random.default_rng(31)
+    c = Commit((2, 128), 2, [13, 40, 0], [random_tree(rng, n, "tree") for n in (60, 7, 200)], seed=31, accept=0.9)
+    pools = c.k.clone(), c.v.clone()
+    ints = [dev_ints(x) for x in (c.tokens, c.parents, c.sampled, c.starts, c.cached, c.tables)]
+    out = [torch.empty(n, dtype=torch.int32, device=DEV) for n in (len(c.parents), 3, 3)]
+    call = lambda stream=None: BR.gllm_op_tree_commit(*ints, c.k, c.v, *out, stream=stream)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    call(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    bits = lambda t: t.view(torch.int16).cpu().numpy()
+    for i in range(3):
+        if i:
+            c.sampled = rng.permutation(c.sampled)                               # other tokens at every replay
+        ints[2].copy_(dev_ints(c.sampled))
+        for x, y in zip((c.k, c.v), pools):
+            x.copy_(y)
+        k, v = bits(c.k).copy(), bits(c.v).copy()
+        want = O.tree_commit(c.tokens, c.parents, c.sampled, c.starts, c.cached, c.tables, k, v)
+        for x in out:
+            x.fill_(-7)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(out, want))
+        assert np.array_equal(bits(c.k), k) and np.array_equal(bits(c.v), v)
+        print(f"replay {i}: {want[1].tolist()} accepted", flush=True)
 
 
 # ---- beams --------------------------------------------------------------------------------------------------------------------
@@ -497,3 +560,27 @@ def test_copy_pages(heads, layers, n):
     torch.cuda.synchronize()
     for w, x in zip(want, (k, v)):
         assert torch.equal(w, x.view(torch.int16))
+
+
+def test_copies_on_a_stream_and_replayed_from_a_graph():
+    print("copies from a graph", flush=True)
+    k = torch.arange(2 * 9 * 2 * 8 * PAGE * 8, device=DEV).remainder(251).bfloat16().reshape(2, 9, 2, 8, PAGE, 8)
+    v = torch.arange(2 * 9 * 2 * 64 * PAGE, device=DEV).remainder(241).bfloat16().reshape(2, 9, 2, 64, PAGE)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    BR.gllm_op_copy_pages(k, v, [0, 0], [1, 2], stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(k[:, 1], k[:, 0]) and torch.equal(v[:, 2], v[:, 0])
+    ids = [np.array([3, 4], dtype=np.int32), np.array([5, 6], dtype=np.int32)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        BR.gllm_op_copy_pages(k, v, *ids)
+    ids[0][:], ids[1][:] = 7, 8                                                  # (the pages of the graph are those of the call)
+    for i in range(3):
+        k[:, 3] += 1
+        want = [x.clone() for x in (k, v)]
+        for w in want:
+            w[:, [5, 6]] = w[:, [3, 4]]
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])

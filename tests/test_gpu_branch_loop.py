@@ -149,6 +149,42 @@ def test_stage_over_trees_is_the_stage_over_each_of_their_paths(n_q, n_kv, d, hi
     stage.destroy()
 
 
+def test_a_pass_over_trees_replayed_from_a_graph():
+    print("stage over trees from a graph", flush=True)
+    m = Model(17, 40)
+    rng = np.random.default_rng(17)
+    trees = [[-1, 0, 0, 1, 1, 2, 5, 5], [-1], list(range(-1, 20)), [-1, -1, 0, 1, 3]]
+    new, cached = [len(t) for t in trees], [50, 33, 10, 0]
+    T, tables = sum(new), np.arange(32).reshape(4, 8)[:, ::-1].copy()
+    m.k.normal_(generator=torch.Generator(device=DEV).manual_seed(1))
+    m.v.normal_(generator=torch.Generator(device=DEV).manual_seed(2))
+    pools = m.k.clone(), m.v.clone()
+    x = torch.empty(T, m.shape.hidden, dtype=torch.bfloat16, device=DEV)
+    out, again = torch.empty_like(x), torch.empty_like(x)
+    call = lambda o: m.stage.forward_tree(new, cached, tables, np.concatenate(trees), x, o)
+    x.normal_()
+    call(out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(again)
+    for i in range(3):
+        x.copy_(torch.tensor(rng.standard_normal((T, m.shape.hidden)), device=DEV))
+        for a, b in zip((m.k, m.v), pools):
+            a.copy_(b)
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = again.clone(), m.k.clone(), m.v.clone()
+        for a, b in zip((m.k, m.v), pools):
+            a.copy_(b)
+        call(out)
+        torch.cuda.synchronize()
+        assert torch.isfinite(out.float()).all()
+        for a, b in zip(replayed, (out, m.k, m.v)):
+            assert torch.equal(a, b)
+    m.close()
+
+
 def test_trees_of_too_many_nodes_are_refused_by_the_stage():
     m = Model(3, 64, layers=1, max_tokens=300, context=512)
     x = torch.zeros(257, m.shape.hidden, dtype=torch.bfloat16, device=DEV)
