@@ -8,6 +8,11 @@
 // Which keys a column sees differs in the last blocks only (blocks of 32 keys; the tree starts in block c / 32): there a
 // node has one 32-bit word per block, bit k for key k of the block, from the closure of the parent links (tree_visibility).
 // Everything in front is seen by all columns and goes through a loop without masks.
+//
+// Work: 4 * d * columns multiplications and additions per key and KV head against 4 * d bytes of keys and values, so the kernels go with
+// the keys' stream from HBM up to some 200 columns, and with the inner step (matrix and vector instructions) above.  Measured (one layer;
+// keys in HBM): 32 single tokens behind 300 to 20000 keys (32 heads on 8, 615 MB) 97 + 4 us, 6.3 TB/s; 16 trees of 64 nodes behind 1000 to
+// 8000 (64 on 8) 160 + 16 us, the second figure the joining of the parts; both in a row behind one another take 102 and 168.
 #include "attn_core.h"
 
 #include <atomic>
@@ -350,6 +355,13 @@ __device__ __forceinline__ void clean_values(u32x4 (&vf)[N], int b0, uint32_t ke
 
 // One workgroup of 4 waves per (unit, KV head), of tiles of 64*NB columns: a block of 32 keys is brought into LDS once and
 // read by all waves, each of which has NB groups of 16 columns (the ring and the operand layout are those of prefill attention).
+//
+// What bounds it: of a block a wave takes 16*NB matrix instructions of 16 cycles and some 56*NB vector ones (per score a maximum, a
+// multiplication and addition, a sum, half a conversion, and an exponential of four times their length), and its workgroup passes 64 KiB
+// through LDS (at NB = 1 as much for half the columns).  At NB = 2 the matrix cores are busy for 0.39 of the time, the vector units for 0.50; a block takes 1.18 us with two
+// workgroups on a compute unit, 0.92 PFLOP/s, and 16 trees of 64 nodes (64 heads on 8, 1000 to 8000 keys) come to 0.7 with the start of
+// the units and their last, masked blocks.  Tried without gain: the scores of the next block between the exponentials of this one (a ring
+// of four), raised wave priority in either part (169 -> 167 to 173 us with the joining), three workgroups a compute unit at NB = 2 (spills).
 template <int D, int NB>
 __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     constexpr int PAGE_BYTES = D * kPage * 2, IPB = PAGE_BYTES / 1024, NS = kTreeStages, TILE = 64 * NB;
@@ -527,7 +539,8 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
 
 // Few columns (tiles of 16*NB): the keys are a stream from HBM, and each wave takes a run of the unit's blocks for all columns, operands
 // straight to registers as in decode attention (load_kv: score tile t is page t, a lane has keys 4G .. 4G+3 of both pages).  The
-// waves' results are joined through LDS, a group of 16 columns at a time.
+// waves' results are joined through LDS, a group of 16 columns at a time.  Bound by HBM: 6.3 TB/s at 32 single tokens behind 300 to 20000
+// keys (a bare read in this way reaches 6.2); one short sequence is all latency (5.7 us at 64 keys and less).
 template <int D>
 struct StreamLds {
     float o[4][16][D + 4];
@@ -670,7 +683,8 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
 }
 
 // The partial results of all tiles joined, in order of the parts: a work item is (record, KV head, 1024 / D columns), a thread per four dims
-// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time.
+// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time (16 us at 512 workgroups' results of 128 columns, 34 MB;
+// 4 at those of 32 single tokens).
 constexpr int kMergeBatch = 12;
 constexpr int kMergeGroups = 2048;  // workgroups
 template <int D>
