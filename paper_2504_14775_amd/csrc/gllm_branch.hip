@@ -18,12 +18,13 @@ struct CommitArgs {
     int32_t table_stride, num_seqs, num_rows;
     bf16_t *k_pool, *v_pool;
     int32_t num_layers, num_blocks, n_kv;
+    int32_t per_group, groups;  // (layer, head)s of a workgroup, workgroups of a sequence
     int32_t *path, *count, *next_token;
 };
 
-// One workgroup per (sequence, layer, KV head); each of them walks the tree itself (a few steps of one wave over at most 256 nodes in
+// A workgroup has a sequence and per_group of its (layer, KV head)s; each of them walks the tree itself (a few steps of one wave over at most 256 nodes in
 // registers), so that one launch does both; the sequence's first one writes the result of the walk.
-// The moves of a (layer, head) are made in order of the path, kMoves at a time, all read before the first is written: position
+// The moves of the (layer, head)s, those of one in order of the path, are made kMoves at a time, all read before the first is written: position
 // i takes what stands at path[i] >= i, so that no slot is written before it has been read.
 //
 // Bound by HBM where there is much to move, and by how V lies there: a token's values are 2 bytes of every 32, so that its 256 bytes of a
@@ -31,12 +32,14 @@ struct CommitArgs {
 // 128): 31 MB of keys and values moved, 73 MB read and 33 MB written, 35 us; one tree of 26 nodes 6.1 us, a launch and the walk.
 // (A thread has a 16-byte piece of K, and V elements of neighbouring dims.)
 constexpr int kMoves = 16;
+// Workgroups that the (layer, head)s are spread over: two rounds of those that run at one time.  (us at 1024 / 2048 / 4096 / one for each, 64 trees
+// of 60 nodes: 12 layers, 6144 of them, 45 / 35 / 35 / 38; 20 layers, 10240, 81 / 66 / 64 / 65.)
+constexpr int kCommitGroups = 4096;
 template <int D>
 __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
     __shared__ int32_t drawn[GLLM_TREE_MAX_NODES], path[GLLM_TREE_MAX_NODES];
     __shared__ int accepted, last_drawn;
-    const int per_seq = max(1, a.num_layers * a.n_kv);
-    const int s = blockIdx.x / per_seq, part = blockIdx.x % per_seq, t = threadIdx.x;
+    const int s = blockIdx.x / a.groups, part0 = blockIdx.x % a.groups * a.per_group, t = threadIdx.x;
     const int r0 = a.row_start[s], r1 = a.row_start[s + 1], c = a.cached_len[s];
     const bool rows_ok = r0 >= 0 && r1 >= r0 && r1 <= a.num_rows;
     const int n = rows_ok ? r1 - r0 : 0;
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
         __syncthreads();
     }
     const int m = fits ? accepted : 0;
-    if (part == 0) {
+    if (part0 == 0) {
         for (int i = t; i < n; i += 256) a.path[r0 + i] = i < m ? path[i] : -1;
         if (t == 0) {
             a.count[s] = m;
@@ -91,23 +94,23 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
     if (first == m) return;
 
     const int32_t* bt = a.block_tables + (int64_t)s * a.table_stride;
-    const int layer = part / a.n_kv, head = part % a.n_kv;
-    auto page_at = [&](int pos) -> int64_t {  // element offset of the (page, head), -1 for an id outside the pool
-        const int id = bt[pos / kPage];
-        return id >= 0 && id < a.num_blocks ? (((int64_t)layer * a.num_blocks + id) * a.n_kv + head) * (D * kPage) : -1;
+    const int moves = m - first, todo = min(a.per_group, a.num_layers * a.n_kv - part0) * moves;  // (behind the first, all nodes move)
+    auto page_at = [&](int part, int pos) -> int64_t {  // element offset of the (page, head), -1 for an id outside the pool
+        const int id = bt[pos / kPage], layer = part / a.n_kv;
+        return id >= 0 && id < a.num_blocks ? (((int64_t)layer * a.num_blocks + id) * a.n_kv + part - layer * a.n_kv) * (D * kPage) : -1;
     };
     constexpr int KP = kMoves * (D / 8) / 256, VP = kMoves * D / 256;  // 16-byte pieces of K, elements of V per thread
     static_assert(kMoves * (D / 8) % 128 == 0 && kMoves * D % 256 == 0, "whole passes");
-    for (int i0 = first; i0 < m; i0 += kMoves) {
+    for (int j0 = 0; j0 < todo; j0 += kMoves) {
         u32x4 kv[KP > 0 ? KP : 1];
         bf16_t vv[VP];
-        auto move = [&](int i, int64_t& from, int64_t& to, int& fs, int& ts) {
+        auto move = [&](int j, int64_t& from, int64_t& to, int& fs, int& ts) {
             from = to = -1;
-            if (i >= m) return;
+            if (j >= todo) return;
+            const int part = part0 + j / moves, i = first + j % moves;
             const int sp = c + path[i], dp = c + i;
-            if (sp == dp) return;
-            from = page_at(sp);
-            to = page_at(dp);
+            from = page_at(part, sp);
+            to = page_at(part, dp);
             if (from < 0 || to < 0) from = to = -1;
             fs = sp % kPage;
             ts = dp % kPage;
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
                 if (x >= kMoves * (D / 8)) continue;
                 int64_t from, to;
                 int fs = 0, ts = 0;
-                move(i0 + x / (D / 8), from, to, fs, ts);
+                move(j0 + x / (D / 8), from, to, fs, ts);
                 if (from >= 0) f(u, a.k_pool + from + (x % (D / 8)) * (kPage * 8) + fs * 8, a.k_pool + to + (x % (D / 8)) * (kPage * 8) + ts * 8);
             }
         };
@@ -129,7 +132,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
                 const int x = t + u * 256;
                 int64_t from, to;
                 int fs = 0, ts = 0;
-                move(i0 + x / D, from, to, fs, ts);
+                move(j0 + x / D, from, to, fs, ts);
                 if (from >= 0) f(u, a.v_pool + from + (x % D) * kPage + fs, a.v_pool + to + (x % D) * kPage + ts);
             }
         };
@@ -769,10 +772,13 @@ gllm_status gllm_op_tree_commit(const int32_t* tokens, const int32_t* parents, c
     if (num_seqs == 0) return GLLM_OK;
     if (!row_start || !cached_len || !block_tables || !count || !next_token) return GLLM_E_INVALID;
     if (num_rows > 0 && (!tokens || !parents || !sampled || !path)) return GLLM_E_INVALID;
+    const int64_t parts = k_pool ? (int64_t)num_layers * n_kv_heads : 1;
+    const int32_t per_group = (int32_t)std::max<int64_t>(1, ceil_div(parts * num_seqs, kCommitGroups));
     const CommitArgs a{tokens, parents, sampled, row_start, cached_len, block_tables, block_table_stride, num_seqs, num_rows,
                        (bf16_t*)k_pool, (bf16_t*)v_pool, k_pool ? num_layers : 0, (int32_t)(k_pool ? num_blocks : 0), k_pool ? n_kv_heads : 0,
+                       per_group, (int32_t)ceil_div(parts, per_group),
                        path, count, next_token};
-    const dim3 grid((unsigned)num_seqs * (unsigned)std::max(1, a.num_layers * a.n_kv));
+    const dim3 grid((unsigned)num_seqs * (unsigned)a.groups);
     if (k_pool && head_dim == 64) tree_commit_kernel<64><<<grid, 256, 0, (hipStream_t)stream>>>(a);
     else tree_commit_kernel<128><<<grid, 256, 0, (hipStream_t)stream>>>(a);
     return launched();

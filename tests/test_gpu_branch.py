@@ -386,6 +386,17 @@ def test_commit_moves_long_paths_in_order():
     assert count.tolist() == [255, 255]
 
 
+@pytest.mark.parametrize("heads,layers,seqs", [((16, 64), 37, 9), ((7, 128), 61, 20)])
+def test_commit_of_many_layers_and_sequences(heads, layers, seqs):
+    """More (sequence, layer, head)s than one workgroup each, and not a whole number of them to a workgroup."""
+    print(f"commit {heads} {layers} layers {seqs} sequences", flush=True)
+    rng = np.random.default_rng(layers)
+    c = Commit(heads, layers, [int(rng.integers(0, 60)) for _ in range(seqs)], [random_tree(rng, int(rng.integers(1, 30)), "tree") for _ in range(seqs)],
+               seed=layers, accept=0.95)
+    _, count, _ = c.check()
+    print(f"accepted {count.tolist()}", flush=True)
+
+
 def test_commit_where_a_rule_is_broken():
     print("commit out of the rules", flush=True)
     c = Commit((2, 64), 2, [5, 3, 0, 40, 7], [[-1, 0, 0, 1], [0, 0, 1], [-1, 5, 1, -3, 0], [-1, 0, 0, 2, 3], [-1, 0, 0, 2]], seed=13, accept=1.0)
