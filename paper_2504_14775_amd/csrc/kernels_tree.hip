@@ -143,7 +143,7 @@ __device__ __forceinline__ void tree_visibility(const TreeArgs& a, const TreeLds
     else tree_visibility_group(t, given, n, c);
 }
 
-// ---- the plan, made by every workgroup for itself -----------------------------------------------------------------------
+// ---- the plan --------------------------------------------------------------------------------------------------------------
 //
 // The lengths stand on the device.  The keys of a sequence are cut into parts of at most `share` blocks, equal to within one
 // block, so that all parts of all sequences come to about tree_target workgroups; the tiles of a part, neighbours in the launch but for
@@ -193,91 +193,179 @@ __device__ __forceinline__ void scan_wave(T& x) {
 }
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// The unit of place `place`; false behind the last one, with the number of tiles whose keys are cut in `cut_tiles`.  Every wave
-// works it out for itself, 64 sequences at a time, without LDS and barriers; all of them with the same arithmetic.
-__device__ __forceinline__ bool tree_unit(const TreeArgs& a, int place, int tile_cols, TreeUnit& u, int& cut_tiles) {
-    const int lane = threadIdx.x & 63;
-    const SeqPlan p = seq_plan(a, lane, tile_cols);
-    float total = 0.f;  // blocks of all tiles
-    bool bad = false;
-    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
-        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + lane, tile_cols);
-        float t = (float)q.tiles * (float)q.blocks;
-        scan_wave(t);
-        total += __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, t), 63));
-        bad |= __any(q.bad);
-    }
-    cut_tiles = 0;
-    if (bad) return false;  // rows in no order may belong to two sequences: the launch would have no place for their units
-    const float target = (float)tree_target(a.n_kv, tile_cols);
-    // (the sum is exact up to 2^24, and more than it by then: a share is never less than the blocks by the target)
+// Blocks of a share, from those of all tiles.  (The sum is exact up to 2^24, and more than it by then: a share is never less than the blocks by
+// the target.)
+__device__ __forceinline__ int share_of(float total, int n_kv, int tile_cols) {
+    const float target = (float)tree_target(n_kv, tile_cols);
     const float even = total < 16777216.f ? ceilf(total / target) : total / target * 1.0001f + 1.f;
-    const int share = (int)fminf(fmaxf(even, (float)kTreeMinShare), 1e9f);
-    // Units in order of their size, in quarters of a share, so that the last workgroups to start are short ones; in a quarter by
-    // sequence, part and tile.
-    auto split = [&](const SeqPlan& q, int& parts, int& quarter) {
-        parts = max(1, (q.blocks - 1) / share + 1);
-        const int size = (q.blocks - 1) / parts + 1;
-        quarter = 4 * (int64_t)size > 3 * (int64_t)share ? 0 : 2 * (int64_t)size > share ? 1 : 4 * (int64_t)size > share ? 2 : 3;
-        return q.tiles * parts;
-    };
-    int at_quarter[4] = {0, 0, 0, 0};  // units of the quarters in front, then of the sequences in front too
-    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
-        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + lane, tile_cols);
-        int parts, quarter;
-        const int mine = split(q, parts, quarter);
-#pragma unroll
-        for (int c = 0; c < 3; ++c) {
-            int x = quarter == c ? mine : 0;
-            scan_wave(x);
-            at_quarter[c + 1] += lane_value(x, 63);
-        }
+    return (int)fminf(fmaxf(even, (float)kTreeMinShare), 1e9f);
+}
+// The units of a sequence.  They are in order of their size, in quarters of a share, so that the last workgroups to start are short ones;
+// in a quarter by sequence, part and tile.
+__device__ __forceinline__ int split_seq(const SeqPlan& q, int share, int& parts, int& quarter) {
+    parts = max(1, (q.blocks - 1) / share + 1);
+    const int size = (q.blocks - 1) / parts + 1;
+    quarter = 4 * (int64_t)size > 3 * (int64_t)share ? 0 : 2 * (int64_t)size > share ? 1 : 4 * (int64_t)size > share ? 2 : 3;
+    return q.tiles * parts;
+}
+// The unit of place `place`, if it is one of the 64 sequences from s0 on, one per lane, of whose `mine` units (0: not looked at) the first is
+// at place `before`.  slots, cut_tiles: those of the sequences in front, on return of these too.
+__device__ __forceinline__ bool unit_of(const SeqPlan& q, int parts, int units, int mine, int before, int place, int s0, int& slots, int& cut_tiles, TreeUnit& u) {
+    const bool cut = parts > 1;
+    int cut_upto = cut ? units : 0, tiles_upto = cut ? q.tiles : 0;
+    scan_wave(cut_upto);
+    scan_wave(tiles_upto);
+    const int at = place - before;
+    const uint64_t who = __ballot(at >= 0 && at < mine);
+    if (who) {
+        const int l = __builtin_ctzll(who), i = lane_value(at, l), tiles = lane_value(q.tiles, l), blocks = lane_value(q.blocks, l);
+        u.seq = s0 + l;
+        u.row0 = lane_value(q.row0, l);
+        u.n = lane_value(q.n, l);
+        u.c = lane_value(q.c, l);
+        u.parts = lane_value(parts, l);
+        u.part = i / tiles;
+        u.tile = i - u.part * tiles;
+        u.slot = slots + lane_value(cut_upto - (cut ? units : 0), l) + i;
+        u.cut_tile = cut_tiles + lane_value(tiles_upto - (cut ? q.tiles : 0), l) + u.tile;
+        const int each = blocks / u.parts, more = blocks - each * u.parts;  // the first `more` parts have a block more
+        u.blk_begin = u.part * each + min(u.part, more);
+        u.blk_end = u.blk_begin + each + (u.part < more);
+        return true;
     }
-    at_quarter[2] += at_quarter[1];
-    at_quarter[3] += at_quarter[2];
-    int slots = 0;
-    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
-        const SeqPlan q = s0 == 0 ? p : seq_plan(a, s0 + lane, tile_cols);
-        int parts, quarter, before = 0;
-        const int mine = split(q, parts, quarter);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            int x = quarter == c ? mine : 0;
-            scan_wave(x);
-            if (quarter == c) before = at_quarter[c] + x - mine;
-            at_quarter[c] += lane_value(x, 63);
-        }
-        const bool cut = parts > 1;
-        int cut_upto = cut ? mine : 0, tiles_upto = cut ? q.tiles : 0;
-        scan_wave(cut_upto);
-        scan_wave(tiles_upto);
-        const int at = place - before;
-        const uint64_t who = __ballot(at >= 0 && at < mine);
-        if (who) {
-            const int l = __builtin_ctzll(who), i = lane_value(at, l), tiles = lane_value(q.tiles, l), blocks = lane_value(q.blocks, l);
-            u.seq = s0 + l;
-            u.row0 = lane_value(q.row0, l);
-            u.n = lane_value(q.n, l);
-            u.c = lane_value(q.c, l);
-            u.parts = lane_value(parts, l);
-            u.part = i / tiles;
-            u.tile = i - u.part * tiles;
-            u.slot = slots + lane_value(cut_upto - (cut ? mine : 0), l) + i;
-            u.cut_tile = cut_tiles + lane_value(tiles_upto - (cut ? q.tiles : 0), l) + u.tile;
-            const int each = blocks / u.parts, more = blocks - each * u.parts;  // the first `more` parts have a block more
-            u.blk_begin = u.part * each + min(u.part, more);
-            u.blk_end = u.blk_begin + each + (u.part < more);
-            return true;
-        }
-        slots += lane_value(cut_upto, 63);
-        cut_tiles += lane_value(tiles_upto, 63);
-    }
+    slots += lane_value(cut_upto, 63);
+    cut_tiles += lane_value(tiles_upto, 63);
     return false;
+}
+
+// Up to 64 sequences every wave works the plan out for itself, all of them with the same arithmetic, without LDS and barriers.  More are
+// planned by a launch of their own, which cuts them into up to 64 runs of whole waves and leaves what stands in front of each; a wave then looks
+// at the runs and at one of them.  us of single tokens behind 300 to 700 keys (8B heads), for itself / by
+// the launch: 128 sequences of 500 to 4000 keys 149 / 152, 256 105 / 86, 1024 668 / 330, 4096 7531 / 1306 (6.1 TB/s): a square law against 3 us.
+constexpr int kPlanRuns = 64;
+struct TreePlan {
+    int32_t share, units;               // units: none where the rows break their order
+    int32_t start[4];                   // place of the first unit of a quarter
+    int32_t before[4][kPlanRuns];       // place of a run's first unit in a quarter
+    int32_t slots[kPlanRuns], cut_tiles[kPlanRuns];  // in front of a run
+};
+__host__ __device__ inline int plan_run(int num_seqs) { return (num_seqs + 64 * kPlanRuns - 1) / (64 * kPlanRuns) * 64; }  // sequences
+
+// false behind the last unit.  cut_tiles: behind it the number of tiles whose keys are cut, or -1 where the plan's launch has written it.
+__device__ __forceinline__ bool tree_unit(const TreeArgs& a, const TreePlan* plan, int place, int tile_cols, TreeUnit& u, int& cut_tiles) {
+    const int lane = threadIdx.x & 63;
+    int slots = 0;
+    if (a.num_seqs > 64) {
+        cut_tiles = -1;
+        if (place >= plan->units) return false;
+        const int share = plan->share;
+        const int quarter = (place >= plan->start[1]) + (place >= plan->start[2]) + (place >= plan->start[3]);
+        const int first = plan->before[quarter][lane];
+        const int run = __popcll(__ballot(first <= place)) - 1, begin = run * plan_run(a.num_seqs), end = min(begin + plan_run(a.num_seqs), a.num_seqs);
+        int at = lane_value(first, run), cut = plan->cut_tiles[run];
+        slots = plan->slots[run];
+        for (int s0 = begin; s0 < end; s0 += 64) {
+            const SeqPlan q = seq_plan(a, s0 + lane, tile_cols);
+            int parts, its;
+            const int units = split_seq(q, share, parts, its), mine = its == quarter ? units : 0;
+            int x = mine;
+            scan_wave(x);
+            if (unit_of(q, parts, units, mine, at + x - mine, place, s0, slots, cut, u)) return true;
+            at += lane_value(x, 63);
+        }
+        return false;
+    }
+    const SeqPlan p = seq_plan(a, lane, tile_cols);
+    cut_tiles = 0;
+    if (__any(p.bad)) return false;  // rows in no order may belong to two sequences: the launch would have no place for their units
+    float total = (float)p.tiles * (float)p.blocks;
+    scan_wave(total);
+    total = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63));
+    int parts, quarter, before = 0, start = 0;
+    const int units = split_seq(p, share_of(total, a.n_kv, tile_cols), parts, quarter);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        int x = quarter == c ? units : 0;
+        scan_wave(x);
+        if (quarter == c) before = start + x - units;
+        start += lane_value(x, 63);
+    }
+    return unit_of(p, parts, units, units, before, place, 0, slots, cut_tiles, u);
+}
+
+// One workgroup; wave w has the runs w, w + 16, ...
+__global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs a, TreePlan* plan, int32_t* count, int tile_cols) {
+    __shared__ float totals[kPlanRuns];
+    __shared__ int sums[6][kPlanRuns];  // of a run: units of each quarter, slots, tiles that are cut
+    __shared__ int any_bad;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int len = plan_run(a.num_seqs);
+    if (threadIdx.x < kPlanRuns) {
+        totals[threadIdx.x] = 0.f;
+        for (int k = 0; k < 6; ++k) sums[k][threadIdx.x] = 0;
+    }
+    if (threadIdx.x == 0) any_bad = 0;
+    __syncthreads();
+    for (int run = wave; run < kPlanRuns && run * len < a.num_seqs; run += 16) {
+        float total = 0.f;
+        bool bad = false;
+        for (int s0 = run * len; s0 < min((run + 1) * len, a.num_seqs); s0 += 64) {
+            const SeqPlan q = seq_plan(a, s0 + lane, tile_cols);
+            total += (float)q.tiles * (float)q.blocks;
+            bad |= q.bad;
+        }
+        scan_wave(total);
+        if (lane == 63) totals[run] = total;
+        if (bad) any_bad = 1;
+    }
+    __syncthreads();
+    float total = totals[lane];
+    scan_wave(total);
+    const int share = share_of(__builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63)), a.n_kv, tile_cols);
+    for (int run = wave; run < kPlanRuns && run * len < a.num_seqs; run += 16) {
+        int sum[6] = {0, 0, 0, 0, 0, 0};
+        for (int s0 = run * len; s0 < min((run + 1) * len, a.num_seqs); s0 += 64) {
+            const SeqPlan q = seq_plan(a, s0 + lane, tile_cols);
+            int parts, quarter;
+            const int units = split_seq(q, share, parts, quarter);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[c] += quarter == c ? units : 0;
+            sum[4] += parts > 1 ? units : 0;
+            sum[5] += parts > 1 ? q.tiles : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < 6; ++k) {
+            scan_wave(sum[k]);
+            if (lane == 63) sums[k][run] = sum[k];
+        }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    int start = 0;
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+        const int own = sums[k][lane];
+        int upto = own;
+        scan_wave(upto);
+        const int all = lane_value(upto, 63);
+        if (k < 4) {
+            if (lane == 0) plan->start[k] = start;
+            plan->before[k][lane] = lane * len < a.num_seqs ? start + upto - own : INT32_MAX;
+            start += all;
+        } else {
+            (k == 4 ? plan->slots : plan->cut_tiles)[lane] = upto - own;
+            if (k == 5 && lane == 0) *count = any_bad ? 0 : all;
+        }
+    }
+    if (lane == 0) {
+        plan->share = share;
+        plan->units = any_bad ? 0 : start;
+    }
 }
 
 // ---- partial results ------------------------------------------------------------------------------------------------------
 //
-// Workspace: a record per tile whose keys are cut, then per (slot, KV head) the reference and the sum of each column of the tile,
+// Workspace: the plan of many sequences, a record per tile whose keys are cut, then per (slot, KV head) the reference and the sum of each column of the tile,
 // then their unnormalised outputs.  A column of a sum below zero is an unused node's.
 struct TreeRecord {
     int32_t row0, n, tile, parts;
@@ -286,6 +374,7 @@ struct TreeRecord {
 };
 struct TreeParts {
     int32_t* count;  // records
+    TreePlan* plan;
     TreeRecord* rec;
     f32x2* ml;       // [slot][n_kv][tile_cols]
     float* o;        // [slot][n_kv][tile_cols][d]
@@ -294,8 +383,10 @@ __host__ __device__ inline size_t tree_parts(TreeParts& t, void* base, int n_kv,
     const size_t cols = (size_t)tree_max_slots(n_kv, tile_cols) * n_kv * tile_cols;
     char* p = (char*)base;
     t.count = (int32_t*)p;
-    t.rec = (TreeRecord*)(p + 256);
-    size_t off = 256 + (tree_max_cut_tiles(n_kv, tile_cols) * sizeof(TreeRecord) + 255) / 256 * 256;
+    t.plan = (TreePlan*)(p + 256);
+    constexpr size_t head = 256 + (sizeof(TreePlan) + 255) / 256 * 256;
+    t.rec = (TreeRecord*)(p + head);
+    size_t off = head + (tree_max_cut_tiles(n_kv, tile_cols) * sizeof(TreeRecord) + 255) / 256 * 256;
     t.ml = (f32x2*)(p + off);
     off += cols * 8;
     t.o = (float*)(p + off);
@@ -374,8 +465,8 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
     TreeParts parts;
     tree_parts(parts, a.workspace, a.n_kv, D, TILE);
     int cut_tiles;
-    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles)) {
-        if (blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
+    if (!tree_unit(a, parts.plan, blockIdx.x / a.n_kv, TILE, it, cut_tiles)) {
+        if (cut_tiles >= 0 && blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
         return;
     }
     const int lane = threadIdx.x & 63;
@@ -557,8 +648,8 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
     TreeParts parts;
     tree_parts(parts, a.workspace, a.n_kv, D, TILE);
     int cut_tiles;
-    if (!tree_unit(a, blockIdx.x / a.n_kv, TILE, it, cut_tiles)) {
-        if (blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
+    if (!tree_unit(a, parts.plan, blockIdx.x / a.n_kv, TILE, it, cut_tiles)) {
+        if (cut_tiles >= 0 && blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
         return;
     }
     const int lane = threadIdx.x & 63;
@@ -784,6 +875,11 @@ static hipError_t launch_tree(const TreeArgs& a, int tile_cols, int64_t units, h
     const dim3 grid((unsigned)(units * a.n_kv));
     const int lds = TreeLds(nullptr, a.max_nodes).bytes(a.max_nodes);
     hipError_t e = hipSuccess;
+    if (a.num_seqs > 64) {
+        TreeParts parts;
+        tree_parts(parts, a.workspace, a.n_kv, D, tile_cols);
+        tree_plan_kernel<<<1, 1024, 0, stream>>>(a, parts.plan, parts.count, tile_cols);
+    }
     if (tile_cols == 16) tree_stream_kernel<D, 1><<<grid, 256, lds, stream>>>(a);
     else if (tile_cols == 32) tree_stream_kernel<D, 2><<<grid, 256, lds, stream>>>(a);
     else if (tile_cols == 64) e = launch_tiles<D, 1>(a, grid, lds, stream);
@@ -800,7 +896,7 @@ hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
     // no more tiles than whole ones in all rows and a partly filled one per sequence; cutting the keys adds no more units than there
     // are shares; and one place behind the last unit
     const int64_t units = (int64_t)a.num_rows * g / tile_cols + a.num_seqs + tree_target(a.n_kv, tile_cols) + 1;
-    if (units * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
+    if (a.num_seqs > 1 << 30 || units * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
     if (a.d == 128) return launch_tree<128>(a, tile_cols, units, stream);
     if (a.d == 64) return launch_tree<64>(a, tile_cols, units, stream);
     return hipErrorInvalidValue;

@@ -283,6 +283,32 @@ def test_tree_attention_replayed_from_a_graph():
         t.check(label=f"replayed, {cached}")
 
 
+@pytest.mark.parametrize("seqs,heads,most", [(65, (4, 2, 64), 2), (129, (16, 1, 128), 3), (1000, (2, 1, 64), 40), (4500, (2, 1, 64), 2)])
+def test_more_sequences_than_a_wave_plans_for_itself(seqs, heads, most):
+    """Some of them cut, some without rows, some that break a rule (zeros); and rows in no order (nothing written)."""
+    print(f"{seqs} sequences, {heads}, at most {most} nodes", flush=True)
+    rng = np.random.default_rng(seqs)
+    cached = [int(rng.integers(0, 40)) for _ in range(seqs)]
+    for s in rng.integers(0, seqs, 12):
+        cached[s] = int(rng.integers(500, 5000))
+    trees = [random_tree(rng, int(rng.integers(0, most + 1)) or 1, "tree") if rng.random() < 0.9 else [] for _ in range(seqs)]
+    t = Trees(heads, cached, trees, seed=seqs, tail_rows=3)
+    broken = [s for s in rng.integers(0, seqs, 5) if trees[s]]
+    for s in broken:
+        t.cached[s] = -1
+    t.dev[1].copy_(dev_ints(t.cached))
+    t.run(max_nodes=most)
+    ref, got = t.check(max_nodes=most, label=f"{seqs} sequences")
+    for s in broken:
+        assert not got[t.starts[s]:t.starts[s + 1]].any()
+    swapped = t.starts.copy()
+    swapped[seqs // 2] = t.starts[-1]
+    t.dev[2].copy_(dev_ints(swapped))
+    t.out.fill_(7.0)
+    t.run(max_nodes=most)
+    assert bool((t.out == 7.0).all())
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 64), (16, 4, 128)], ids=str)
 def test_any_bound_on_the_nodes_of_a_tree_and_two_calls_at_once(heads):
     """Trees of 1 to 4 nodes under bounds from 4 to 256: every kernel, with tiles that are mostly empty, over more sequences than a wave has
