@@ -579,7 +579,10 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
             used[c] = tree.vis[node[c] * tree.stride + (at >> 5)] >> (at & 31) & 1;
         }
         const bool idle = it.tile * TILE + wave * NB * 16 >= cols;  // (the same for the wave)
-        const int nblk = it.blk_end - it.blk_begin, full = min(nblk, max(n_full - it.blk_begin, 0));
+        // No node sees a later one: the last block of the tile, and of the wave, is that of its last node.  (A part may be left without blocks.
+        // 64 trees of 256 nodes behind 10 to 500 keys, 8B heads: 252 -> 220 us.)
+        auto stop = [&](int columns) { return (it.c + (min(it.tile * TILE + columns, cols) - 1) / g) / 32 + 1; };
+        const int nblk = min(it.blk_end, stop(TILE)) - it.blk_begin, full = min(nblk, max(n_full - it.blk_begin, 0)), mine = stop((wave + 1) * NB * 16) - it.blk_begin;
         // every wave always issues its piece (indices past the end read the last page again into a stage nobody reads), so the
         // count of outstanding loads is the same in every iteration
         auto advance = [&](int i) {
@@ -596,7 +599,7 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
         }
         for (int i = full; i < nblk; ++i) {
             advance(i);
-            if (!idle) block_step(i % NS, it.blk_begin + i, std::true_type{});
+            if (!idle && i < mine) block_step(i % NS, it.blk_begin + i, std::true_type{});
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no LDS fill may outlive the workgroup
     }
