@@ -156,7 +156,8 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 // Measured (64 sequences of 8 beams over a vocabulary of 152064, keep 16: 311 MB): 87 + 8 us, of which HBM would take 50.  What bounds
 // beam_rows are vector instructions and their latency, some 20 a logit, 12 of them in 64 bits (the exponential), with one pass on its way
 // while the last one is worked on: at 128 rows it takes 30 us, without exponentials and without lists behind the first pass 16.  Reading
-// past the caches takes 94 us where a plain load takes 96.  beam_merge is latency: four dependent steps (sums, logarithms, the bound, the lists above it).
+// past the caches takes 94 us where a plain load takes 96.  beam_merge is latency: four dependent steps (sums, logarithms, the bound, the lists above
+// it, all in one queue so that up to 8 loads are on their way: 32 beams that keep 64 53 -> 47 us).
 
 constexpr int kBeamWaves = 4;
 constexpr int kBeamLists = 1280;  // most segments of the rows of a sequence
@@ -496,15 +497,17 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     __shared__ uint64_t keys[kBeamWaves][kBeamList];
     __shared__ uint32_t idxs[kBeamWaves][kBeamList];
     __shared__ double lse[GLLM_BEAM_MAX_BEAMS];   // log of the sum without the largest logit
-    __shared__ float tops[GLLM_BEAM_MAX_BEAMS];
+    __shared__ float tops[GLLM_BEAM_MAX_BEAMS], so_far[GLLM_BEAM_MAX_BEAMS];
     __shared__ float list_top[kBeamLists];
     __shared__ double list_sum[kBeamLists];
+    __shared__ uint16_t queue[kBeamWaves][kBeamLists / kBeamWaves];  // a wave's lists that are looked into
     __shared__ int wave_n[kBeamWaves];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int s = blockIdx.x;
     const int64_t row0 = (int64_t)s * a.beams;
     const int lists = a.beams * a.segs;
+    if ((int)threadIdx.x < a.beams) so_far[threadIdx.x] = a.scores[row0 + threadIdx.x];
     for (int i = threadIdx.x; i < lists; i += 256) {
         list_top[i] = a.top[row0 * a.segs + i];
         list_sum[i] = a.sum[row0 * a.segs + i];
@@ -548,7 +551,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     }
     __syncthreads();
     auto score = [&](float x, int b) {  // of a logit of beam b; 0: no candidate
-        const float cum = a.scores[row0 + b], m = tops[b];
+        const float cum = so_far[b], m = tops[b];
         if (!(cum > -INFINITY && cum < INFINITY)) return (uint64_t)0;
         return order_key((double)cum + ((x == m ? 0.0 : (double)x - (double)m) - lse[b]));
     };
@@ -613,37 +616,40 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
         int room = 1;  // lanes to a list
         while (room < a.keep) room *= 2;
         const int at_once = 64 / room, mine = lane / room, e = lane % room;
+        int queued = 0;
+#pragma unroll
         for (int u = 0; u < U; ++u) {
-            uint64_t left = __ballot(best[u] >= floor);
-            while (left) {
-                constexpr int STEPS = 4;  // on their way at one time
-                int32_t token[STEPS];
-                float value[STEPS];
-                int beam[STEPS];
+            const bool take = best[u] >= floor;
+            const uint64_t who = __ballot(take);
+            if (take) queue[wave][queued + __popcll(who & ((1ull << lane) - 1))] = (uint16_t)((u * 64 + lane) * kBeamWaves + wave);
+            queued += __popcll(who);
+        }
+        wave_fence();
+        constexpr int STEPS = 8;  // on their way at one time
+        for (int q0 = 0; q0 < queued; q0 += STEPS * at_once) {
+            int32_t token[STEPS];
+            float value[STEPS];
+            int beam[STEPS];
 #pragma unroll
-                for (int t = 0; t < STEPS; ++t) {
-                    int l = -1;  // this lane's list: the mine-th of those left
-                    for (int q = 0; q < at_once && left; ++q) {
-                        if (q == mine) l = __builtin_ctzll(left);
-                        left &= left - 1;
-                    }
-                    token[t] = -1;
-                    value[t] = 0.f;
-                    beam[t] = 0;
-                    if (l >= 0 && e < a.keep) {
-                        const int i = (u * 64 + l) * kBeamWaves + wave;
-                        const int64_t place = (row0 * a.segs + i) * a.keep + e;
-                        beam[t] = i / a.segs;
-                        token[t] = a.token[place];
-                        value[t] = a.value[place];
-                    }
+            for (int t = 0; t < STEPS; ++t) {
+                const int q = q0 + t * at_once + mine;
+                token[t] = -1;
+                value[t] = 0.f;
+                beam[t] = 0;
+                if (q < queued && e < a.keep) {
+                    const int i = queue[wave][q];
+                    const int64_t place = (row0 * a.segs + i) * a.keep + e;
+                    beam[t] = i / a.segs;
+                    token[t] = a.token[place];
+                    value[t] = a.value[place];
                 }
+            }
 #pragma unroll
-                for (int t = 0; t < STEPS; ++t) {
-                    const uint64_t k = token[t] >= 0 ? score(value[t], beam[t]) : 0;
-                    if (list.n + 64 > kBeamList) floor = max(floor, list.keep_best(a.keep));
-                    list.add(k >= floor, k, (uint32_t)beam[t] * (uint32_t)a.vocab + (uint32_t)token[t]);
-                }
+            for (int t = 0; t < STEPS; ++t) {
+                if (q0 + t * at_once >= queued) continue;
+                const uint64_t k = token[t] >= 0 ? score(value[t], beam[t]) : 0;
+                if (list.n + 64 > kBeamList) floor = max(floor, list.keep_best(a.keep));
+                list.add(k >= floor, k, (uint32_t)beam[t] * (uint32_t)a.vocab + (uint32_t)token[t]);
             }
         }
     }
@@ -663,8 +669,8 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     const uint32_t i = there ? list.idx[lane] : 0u;
     int rank = 0;
     for (int j = 0; j < list.n; ++j) {
-        const uint64_t kj = list.key[j];
-        rank += kj > k || (kj == k && list.idx[j] < i);
+        const uint64_t kj = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, j);
+        rank += kj > k || (kj == k && (uint32_t)__builtin_amdgcn_readlane((int)i, j) < i);
     }
     const int64_t out = (int64_t)s * a.keep;
     if (there) {
