@@ -552,7 +552,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     __syncthreads();
     auto score = [&](float x, int b) {  // of a logit of beam b; 0: no candidate
         const float cum = so_far[b], m = tops[b];
-        if (!(cum > -INFINITY && cum < INFINITY)) return (uint64_t)0;
+        if (!(cum > -INFINITY && cum < INFINITY) || x == -INFINITY) return (uint64_t)0;  // (x: the largest logit of a list that is empty)
         return order_key((double)cum + ((x == m ? 0.0 : (double)x - (double)m) - lse[b]));
     };
     WaveList<uint64_t> list{keys[wave], idxs[wave], 0, lane};

@@ -1,0 +1,52 @@
+"""GPU tests of the operators for several continuations of one sequence (include/gllm_branch.h) where their sizes send them through other
+kernels and paths than tests/test_gpu_branch.py does with the same contents; helpers and bounds are that file's."""
+import numpy as np
+import pytest
+
+from test_gpu_branch import check_beams
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("what", ["-inf", "nan", "both"])
+@pytest.mark.parametrize("beams,vocab,keep", [(8, 128256, 16), (4, 152064, 8), (32, 33333, 64), (2, 700001, 64)])
+def test_beams_without_any_continuation_among_many_candidates(beams, vocab, keep, what):
+    """Whole rows of logits that are no continuations, of beams whose score is the best: the first, a middle one, several, all but one, all.
+    More than 1024 places of kept logits a sequence."""
+    rng = np.random.default_rng(vocab + keep)
+    x = (rng.standard_normal((beams, vocab)) * 4.5).astype(np.float32)
+    rows = [[0], [beams // 2], sorted({0, beams // 2, beams - 1}), list(range(1, beams)), list(range(beams))]
+    for empty in rows:
+        print(f"{beams} beams, {vocab}, keep {keep}: {what} in rows {empty}", flush=True)
+        y, scores = x.copy(), (-rng.random((1, beams)) * 3 - 20).astype(np.float32)
+        for i, r in enumerate(empty):
+            y[r] = -np.inf if what == "-inf" or (what == "both" and i % 2) else np.nan
+            scores[0, r] = -1.0
+        if what == "both" and len(empty) == 1:
+            y[empty[0], ::2] = -np.inf
+        got = check_beams(y, scores, keep, label=f"{what} in rows {empty}")
+        assert len(empty) < beams or got[1].max() == -1
+
+
+@pytest.mark.parametrize("beams,vocab,keep", [(8, 128256, 16), (32, 33333, 64)])
+def test_odd_logits_among_many_candidates(beams, vocab, keep):
+    """Rows with continuations in one segment only, with fewer than are kept, with +infinity, with the type's lowest value, far apart."""
+    rng = np.random.default_rng(keep)
+    x = (rng.standard_normal((3 * beams, vocab)) * 4.5).astype(np.float32)
+    scores = (-rng.random((3, beams)) * 3 - 2).astype(np.float32)
+    print(f"odd logits, {beams} beams, {vocab}, keep {keep}", flush=True)
+    x[0, :-7] = -np.inf
+    x[1, 5:] = np.nan
+    x[2, [17, vocab // 2, vocab - 1]] = np.inf
+    x[3, 100:] = np.finfo(np.float32).min
+    x[beams:2 * beams, 3:] = -np.inf                # fewer in the whole sequence than are kept
+    x[beams + 1] = np.nan
+    x[2 * beams] *= 1e30
+    x[2 * beams + 1, vocab - 2] = 3e38
+    scores[2, 2] = -np.inf
+    scores[2, 3] = np.nan
+    check_beams(x, scores, keep, label="odd logits")
+    first = np.full((3, beams), -np.inf, dtype=np.float32)
+    first[:, beams - 1] = 0.0                       # one beam
+    got = check_beams(x, first, keep, label="one beam")
+    assert set(got[1].flatten()) <= {beams - 1, -1}
