@@ -2,8 +2,11 @@
 kernels and paths than tests/test_gpu_branch.py does with the same contents; helpers and bounds are that file's."""
 import numpy as np
 import pytest
+import torch
 
-from test_gpu_branch import check_beams
+from gpu_util import DEV
+from paper_2504_14775_amd import branch as BR
+from test_gpu_branch import check_beams, dev_ints
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +53,19 @@ def test_odd_logits_among_many_candidates(beams, vocab, keep):
     first[:, beams - 1] = 0.0                       # one beam
     got = check_beams(x, first, keep, label="one beam")
     assert set(got[1].flatten()) <= {beams - 1, -1}
+
+
+@pytest.mark.parametrize("beams,vocab", [(4, 20000), (8, 152064), (32, 60000)])
+def test_beams_of_equal_sums_tie_wherever_their_largest_logit_stands(beams, vocab):
+    """Every row's weights are ones (its logits 0 but for one of 1e-20, at another place in each), so all continuations tie in 64 bits."""
+    print(f"equal sums, {beams} beams, {vocab}", flush=True)
+    x = torch.zeros(beams, vocab, device=DEV)
+    for b in range(beams):
+        x[b, (b + 1) * vocab // beams - 1] = 1e-20
+    scores = torch.full((1, beams), -2.0, device=DEV)
+    out = torch.empty(1, 8, device=DEV), dev_ints(np.zeros((1, 8))), dev_ints(np.zeros((1, 8)))
+    BR.gllm_op_beam_select(x, vocab, scores, *out)
+    torch.cuda.synchronize()
+    assert (out[1] == 0).all()
+    want = -2.0 - np.log(vocab)
+    assert np.all(np.abs(out[0].cpu().numpy() - want) <= 2.0 ** -24 * 1.001 * abs(want) + 1e-9)
