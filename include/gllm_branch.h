@@ -83,7 +83,8 @@ gllm_status gllm_op_tree_commit(const int32_t* tokens, const int32_t* parents, c
 
 /* Beam search: for every sequence the `keep` best continuations (beam b, token v) by
  *   scores[s][b] + logits[s*beams + b][v] - log sum_u exp logits[s*beams + b][u],
- * best first, equal ones in order of the beam, then of the token.  They are compared, and the sum is taken, in 64 bits.
+ * best first.  They are compared, and the sum is taken, in 64 bits (log sum exp is good to some 1e-10); those that agree there are in order of
+ * the beam, in a beam of the logit, the largest first, and equal logits in order of the token.
  *   logits  DEVICE float [num_seqs*beams][ld_logits]; scores DEVICE float [num_seqs][beams]: log probability of each beam so far
  *   out_scores DEVICE float, out_beams, out_tokens DEVICE int32, [num_seqs][keep]
  * A beam whose score is not finite has no continuations (fewer beams than room: -infinity).  A logit that is not a number counts as

@@ -111,7 +111,8 @@ def log_softmax(x):
 
 
 def beam_select(logits, scores, keep):
-    """logits [S*W][V], scores [S][W].  Returns scores, beams, tokens [S][keep]."""
+    """logits [S*W][V], scores [S][W].  Returns scores, beams, tokens [S][keep]: by the sum in 64 bits, equal ones by the beam, in a beam by
+    the logit, then by the token."""
     seqs, beams = scores.shape
     vocab = logits.shape[1]
     out = np.full((seqs, keep), -np.inf), np.full((seqs, keep), -1, np.int32), np.full((seqs, keep), -1, np.int32)
@@ -120,9 +121,11 @@ def beam_select(logits, scores, keep):
         for b in range(beams):
             if np.isfinite(scores[s, b]):
                 total[b] = np.float64(scores[s, b]) + log_softmax(logits[s * beams + b])
-        flat = total.reshape(-1)
-        order = np.argsort(-flat, kind="stable")[:keep]
-        order = order[flat[order] > -np.inf]
+        flat, x = total.reshape(-1), logits[s * beams:(s + 1) * beams].reshape(-1)
+        there = np.flatnonzero(flat > -np.inf)
+        if len(there) > keep:                                                    # those that reach the keep-th best sum
+            there = there[flat[there] >= np.partition(flat[there], -keep)[-keep]]
+        order = there[np.lexsort((there % vocab, -x[there].astype(np.float64), there // vocab, -flat[there]))][:keep]
         out[0][s, :len(order)] = flat[order]
         out[1][s, :len(order)] = order // vocab
         out[2][s, :len(order)] = order % vocab

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 // token of the segment can be among the best of the sequence) beside the segment's largest logit and sum of exponentials.
 // beam_merge: a workgroup per sequence adds up the sums of its rows and picks the best of what the segments kept.
 // The order among beams hangs on the sums: they and the scores are held in 64 bits, so that the order is that of exact
-// arithmetic but where scores agree to some 1e-10.
+// arithmetic but where scores of two beams agree to some 1e-10; in a beam it is that of the logits.
 //
 // Measured (64 sequences of 8 beams over a vocabulary of 152064, keep 16: 311 MB): 87 + 8 us, of which HBM would take 50.  What bounds
 // beam_rows are vector instructions and their latency, some 20 a logit, 12 of them in 64 bits (the exponential), with one pass on its way
@@ -160,6 +160,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 // it, all in one queue so that up to 8 loads are on their way: 32 beams that keep 64 53 -> 47 us).
 
 constexpr int kBeamWaves = 4;
+constexpr int kBeamTokenBits = 24, kBeamMaxVocab = 1 << kBeamTokenBits;
 constexpr int kBeamLists = 1280;  // most segments of the rows of a sequence
 constexpr int kBeamList = 384;  // places of a wave's list: the 64 kept at most, the 256 of one pass, and a whole number per lane
 
@@ -253,15 +254,15 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// The candidates of one wave, in LDS.
-template <typename Key>
+// The candidates of one wave, in LDS: by the key, the highest first, equal keys by the index, the lowest first.
+template <typename Key, typename Idx>
 struct WaveList {
     Key* key;
-    uint32_t* idx;
+    Idx* idx;
     int n;      // the same in all lanes
     int lane;
     // Adds the lanes' candidates that `pass`; there has to be room for 64.
-    __device__ __forceinline__ void add(bool pass, Key k, uint32_t i) {
+    __device__ __forceinline__ void add(bool pass, Key k, Idx i) {
         const uint64_t who = __ballot(pass);
         if (pass) {
             const int at = n + __popcll(who & ((1ull << lane) - 1));
@@ -270,7 +271,7 @@ struct WaveList {
         }
         n += __popcll(who);
     }
-    // Leaves the k best, equal keys by the lower index.  Returns a key that all of them reach, or 0 where there were no more than k.
+    // Leaves the k best.  Returns a key that all of them reach, or 0 where there were no more than k.
     __device__ __forceinline__ Key keep_best(int k) {
         if (n <= k) return 0;
         return n <= 128 ? best_of<2>(k) : n <= 256 ? best_of<4>(k) : best_of<kBeamList / 64>(k);
@@ -279,7 +280,8 @@ struct WaveList {
     __device__ __forceinline__ Key best_of(int k) {
         wave_fence();
         Key mine[U];
-        uint32_t at[U], part[U];
+        Idx at[U];
+        uint32_t part[U];
         bool tied[U], kept[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -294,13 +296,14 @@ struct WaveList {
         Key low = 0;
         int need = k;
 #pragma unroll
-        for (int word = (int)sizeof(Key) / 4; word >= 0; --word) {
+        for (int word = 0; word < (int)(sizeof(Key) + sizeof(Idx)) / 4; ++word) {
             if (need == 0) continue;
+            const int down = (int)sizeof(Key) * 8 - 32 * (word + 1);  // of the key, below zero behind its last word
 #pragma unroll
-            for (int u = 0; u < U; ++u) part[u] = word > 0 ? (uint32_t)(mine[u] >> (32 * (word - 1))) : ~at[u];
+            for (int u = 0; u < U; ++u) part[u] = down >= 0 ? (uint32_t)(mine[u] >> (down & 63)) : ~(uint32_t)(at[u] >> (down + (int)sizeof(Idx) * 8 & 63));
             int count;
             const uint32_t v = reach_of(part, tied, need, count);
-            if (word > 0) low |= (Key)v << (32 * (word > 0 ? word - 1 : 0));
+            if (down >= 0) low |= (Key)v << (down & 63);
             if (count == need) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) kept[u] |= tied[u] && part[u] >= v;
@@ -371,7 +374,7 @@ __global__ __launch_bounds__(256, 4) void beam_rows_kernel(BeamArgs a) {
     const int row = blockIdx.x / a.segs, seg = blockIdx.x % a.segs;
     const float* x0 = a.logits + (int64_t)row * a.ld;
     const int begin = seg * a.seg_len, end = min(a.vocab, begin + a.seg_len);
-    WaveList<uint32_t> list{keys[wave], idxs[wave], 0, lane};
+    WaveList<uint32_t, uint32_t> list{keys[wave], idxs[wave], 0, lane};
     float bar = above_key(0);  // candidates are not below it
     // The sum of exp(x - ref); where ref is below 1000 in magnitude, of 2^(x log2(e) - r), r = ref log2(e) rounded to a whole number (one
     // subtraction in 64 bits less per logit, of sixteen operations).
@@ -495,8 +498,7 @@ __global__ __launch_bounds__(256, 4) void beam_rows_kernel(BeamArgs a) {
 }
 
 __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
-    __shared__ uint64_t keys[kBeamWaves][kBeamList];
-    __shared__ uint32_t idxs[kBeamWaves][kBeamList];
+    __shared__ uint64_t keys[kBeamWaves][kBeamList], idxs[kBeamWaves][kBeamList];
     __shared__ double lse[GLLM_BEAM_MAX_BEAMS];   // log of the sum without the largest logit
     __shared__ float tops[GLLM_BEAM_MAX_BEAMS], so_far[GLLM_BEAM_MAX_BEAMS];
     __shared__ float list_top[kBeamLists];
@@ -556,13 +558,18 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
         if (!(cum > -INFINITY && cum < INFINITY) || x == -INFINITY) return (uint64_t)0;  // (x: the largest logit of a list that is empty)
         return order_key((double)cum + ((x == m ? 0.0 : (double)x - (double)m) - lse[b]));
     };
-    WaveList<uint64_t> list{keys[wave], idxs[wave], 0, lane};
+    // What orders equal scores: the beam, then the logit, whose differences the score may have swallowed, then the token.  The segments kept the
+    // best of their row by the last two, so that nothing they left out comes in front of what they kept.
+    constexpr int kBeamAt = kBeamTokenBits + 32;
+    static_assert(GLLM_BEAM_MAX_BEAMS <= 1 << (64 - kBeamAt), "a beam has room");
+    auto place_of = [](int b, float x, int token) { return (uint64_t)b << kBeamAt | (uint64_t)~order_key(x) << kBeamTokenBits | (uint32_t)token; };
+    WaveList<uint64_t, uint64_t> list{keys[wave], idxs[wave], 0, lane};
     if (few) {
 #pragma unroll
         for (int t = 0; t < FEW; ++t) {
             const int b = ((t * kBeamWaves + wave) * 64 + lane) / (a.segs * a.keep);
             const uint64_t k = few_token[t] >= 0 ? score(few_value[t], b) : 0;
-            list.add(k > 0, k, (uint32_t)b * (uint32_t)a.vocab + (uint32_t)few_token[t]);
+            list.add(k > 0, k, place_of(b, few_value[t], few_token[t]));
         }
     } else {
         // What the segments kept is a list each.  At least `keep` candidates are not below the keep-th best of the lists' largest ones: of a
@@ -585,7 +592,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
             found += __popcll(__ballot(in[u]));
         }
         const uint32_t own = found >= a.keep ? reach_of(high, in, a.keep, count) : 0u;
-        uint32_t* const heads = &idxs[0][0];  // [kBeamWaves][64]: of each wave's lists the first keep that reach its bound
+        uint32_t* const heads = reinterpret_cast<uint32_t*>(&idxs[0][0]);  // [kBeamWaves][64]: of each wave's lists the first keep that reach its bound
         {
             heads[wave * 64 + lane] = 0;
             wave_fence();
@@ -650,7 +657,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
                 if (q0 + t * at_once >= queued) continue;
                 const uint64_t k = token[t] >= 0 ? score(value[t], beam[t]) : 0;
                 if (list.n + 64 > kBeamList) floor = max(floor, list.keep_best(a.keep));
-                list.add(k >= floor, k, (uint32_t)beam[t] * (uint32_t)a.vocab + (uint32_t)token[t]);
+                list.add(k >= floor, k, place_of(beam[t], value[t], token[t]));
             }
         }
     }
@@ -660,25 +667,26 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     if (wave > 0) return;
     for (int w = 1; w < kBeamWaves; ++w) {
         const int n = wave_n[w];
-        list.add(lane < n, lane < n ? keys[w][lane] : 0ull, lane < n ? idxs[w][lane] : 0u);
+        list.add(lane < n, lane < n ? keys[w][lane] : 0ull, lane < n ? idxs[w][lane] : 0ull);
     }
     list.keep_best(a.keep);
     wave_fence();
     // the place of each of the at most 64 is the number of those in front of it
     const bool there = lane < list.n;
     const uint64_t k = there ? list.key[lane] : 0ull;
-    const uint32_t i = there ? list.idx[lane] : 0u;
+    const uint64_t i = there ? list.idx[lane] : 0ull;
+    auto of_lane = [](uint64_t x, int l) { return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l); };
     int rank = 0;
     for (int j = 0; j < list.n; ++j) {
-        const uint64_t kj = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, j);
-        rank += kj > k || (kj == k && (uint32_t)__builtin_amdgcn_readlane((int)i, j) < i);
+        const uint64_t kj = of_lane(k, j);
+        rank += kj > k || (kj == k && of_lane(i, j) < i);
     }
     const int64_t out = (int64_t)s * a.keep;
     if (there) {
         const uint64_t bits = k >> 63 ? k ^ (1ull << 63) : ~k;
         a.out_scores[out + rank] = (float)__builtin_bit_cast(double, bits);
-        a.out_beams[out + rank] = (int32_t)(i / (uint32_t)a.vocab);
-        a.out_tokens[out + rank] = (int32_t)(i % (uint32_t)a.vocab);
+        a.out_beams[out + rank] = (int32_t)(i >> kBeamAt);
+        a.out_tokens[out + rank] = (int32_t)i & (kBeamMaxVocab - 1);
     } else if (lane < a.keep) {
         a.out_scores[out + lane] = -INFINITY;
         a.out_beams[out + lane] = -1;
@@ -696,7 +704,7 @@ int beam_segments(int num_seqs, int beams, int vocab) {
 }
 
 bool beam_sizes_ok(int num_seqs, int beams, int vocab, int keep) {
-    return num_seqs >= 0 && beams >= 1 && beams <= GLLM_BEAM_MAX_BEAMS && vocab >= 1 && vocab <= 1 << 24 && keep >= 1 && keep <= GLLM_BEAM_MAX_KEEP &&
+    return num_seqs >= 0 && beams >= 1 && beams <= GLLM_BEAM_MAX_BEAMS && vocab >= 1 && vocab <= kBeamMaxVocab && keep >= 1 && keep <= GLLM_BEAM_MAX_KEEP &&
            (int64_t)num_seqs * beams <= 1 << 22;
 }
 

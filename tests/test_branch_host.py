@@ -146,3 +146,12 @@ def test_oracle_beams_by_brute_force():
         every.sort(key=lambda e: (-e[0], e[1], e[2]))
         assert [(b, t) for _, b, t in every[:5]] == list(zip(beam[i], token[i]))
         assert np.allclose(score[i], [e[0] for e in every[:5]])
+
+
+def test_oracle_beams_of_equal_sums():
+    """Differences of the logits that the sum in 64 bits swallows still order the continuations of a beam, and not those of two."""
+    x = np.array([[1e-20, 3e-20, 2e-20, 3e-20], [9e-20, 0.0, 5e-20, 0.0]], dtype=np.float32)
+    score, beam, token = O.beam_select(x, np.zeros((1, 2), dtype=np.float32), 6)
+    assert beam[0].tolist() == [0, 0, 0, 0, 1, 1] and token[0].tolist() == [1, 3, 2, 0, 0, 2] and len(set(score[0])) == 1
+    score, beam, token = O.beam_select(x * 1e20, np.full((1, 2), -1e18, dtype=np.float32), 6)
+    assert beam[0].tolist() == [0, 0, 0, 0, 1, 1] and token[0].tolist() == [1, 3, 2, 0, 0, 2]

@@ -69,3 +69,18 @@ def test_beams_of_equal_sums_tie_wherever_their_largest_logit_stands(beams, voca
     assert (out[1] == 0).all()
     want = -2.0 - np.log(vocab)
     assert np.all(np.abs(out[0].cpu().numpy() - want) <= 2.0 ** -24 * 1.001 * abs(want) + 1e-9)
+
+
+@pytest.mark.parametrize("seqs,beams,vocab,keep", [(2, 3, 700, 8), (1, 4, 60000, 8), (1, 8, 128256, 16), (2, 32, 33333, 64), (1, 1, 300001, 64)])
+def test_sums_that_agree_in_64_bits_go_by_beam_logit_and_token(seqs, beams, vocab, keep):
+    """Logits whose differences the sum swallows: next to nothing beside log(vocabulary), or behind a score of -1e18 (64 bits there are 128 apart)."""
+    print(f"equal sums, {seqs} x {beams} beams, {vocab}, keep {keep}", flush=True)
+    rng = np.random.default_rng(vocab)
+    x = rng.standard_normal((seqs * beams, vocab)).astype(np.float32)
+    x[:, ::7] = x[:, :1]                            # equal ones among them
+    check_beams(x * np.float32(1e-20), np.full((seqs, beams), -1.0, dtype=np.float32), keep, label="small logits")
+    scores = np.full((seqs, beams), -1e18, dtype=np.float32)
+    check_beams(x, scores, keep, label="large scores")
+    scores[:, beams // 2] = -1e17
+    got = check_beams(x, scores, keep, label="one beam ahead")
+    assert (got[1] == beams // 2).all()
