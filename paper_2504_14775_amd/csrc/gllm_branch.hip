@@ -169,10 +169,12 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);  // (one zero)
     return x > -INFINITY ? b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u) : 0u;
 }
-// The least number whose key is above `key`, which is a number's, one less, or 0.
+// The least number whose key is above `key`, which is a number's, one less, or 0; infinity for infinity's own (candidates of the same key
+// are sorted out by their index).
 __device__ __forceinline__ float above_key(uint32_t key) {
-    const uint32_t k = key + 1;
-    return key == 0u ? -3.402823466e38f : __builtin_bit_cast(float, k >> 31 ? k ^ 0x80000000u : ~k);  // (above infinity's: not a number, and nothing passes)
+    constexpr uint32_t kInfinity = 0xFF800000u;
+    const uint32_t k = min(key + 1, kInfinity);
+    return key == 0u ? -3.402823466e38f : __builtin_bit_cast(float, k >> 31 ? k ^ 0x80000000u : ~k);
 }
 __device__ __forceinline__ uint64_t order_key(double x) {
     const uint64_t b = __builtin_bit_cast(uint64_t, x + 0.0);

@@ -84,3 +84,16 @@ def test_sums_that_agree_in_64_bits_go_by_beam_logit_and_token(seqs, beams, voca
     scores[:, beams // 2] = -1e17
     got = check_beams(x, scores, keep, label="one beam ahead")
     assert (got[1] == beams // 2).all()
+
+
+@pytest.mark.parametrize("beams,vocab,keep", [(3, 9000, 4), (8, 128256, 16), (2, 300001, 64)])
+def test_more_logits_of_infinity_than_are_kept(beams, vocab, keep):
+    """Infinities that fill the lists at once or bit by bit, among numbers of any size: they share the probability, the lowest tokens come first."""
+    print(f"infinities, {beams} beams, {vocab}, keep {keep}", flush=True)
+    rng = np.random.default_rng(vocab)
+    for step in (1, 3, vocab // (keep + 1)):
+        x = (rng.standard_normal((beams, vocab)) * 4.5).astype(np.float32)
+        x[:, ::step] = np.inf
+        x[beams - 1] = np.sort(rng.standard_normal(vocab) * 1e37)
+        x[beams - 1, vocab // 2:] = np.finfo(np.float32).max
+        check_beams(x, (-rng.random((1, beams)) * 3 - 2).astype(np.float32), keep, label=f"every {step}th")
