@@ -48,7 +48,7 @@ enum { GLLM_TREE_MAX_NODES = 256, GLLM_BEAM_MAX_BEAMS = 32, GLLM_BEAM_MAX_KEEP =
  *   workspace     DEVICE, 16-byte aligned, at least gllm_op_tree_attention_workspace_bytes() of it; contents need not survive
  *                 between calls, and calls that may overlap in time need one each
  * Unused nodes, and all nodes of a sequence with more than max_nodes, with cached_len < 0 or with more positions than its table row
- * has entries for, receive zeros.  Rows outside every sequence are left as they are.  The keys and values of unused nodes and of slots
+ * has entries for (or than 2^31 - 64), receive zeros.  Rows outside every sequence are left as they are.  The keys and values of unused nodes and of slots
  * past the last node may hold anything; those of the prefix and of used nodes have to be finite for every row that sees them, and a value
  * that is not finite spoils the rows that see it only.
  * Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads with at most 16 query heads per KV head (else
@@ -65,7 +65,7 @@ size_t gllm_op_tree_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_he
  * none.  The nodes passed are accepted (node 0 always is), path[row_start[s] ..] receives their indices in order and -1 behind
  * them, count[s] their number, next_token[s] the token sampled at the last of them; count 0, next_token -1 and a path of -1 for a
  * sequence without rows, with more than 256, whose node 0 is no root, or whose positions do not fit its table row (cached_len < 0
- * among them).
+ * and more than 2^31 - 64 positions among them).
  * Then, in all layers, the keys and values of the i-th accepted node move to position cached_len[s] + i: the sequence goes on with
  * cached_len[s] + count[s] positions and next_token[s] as its next root.  Other slots are left as they are; a move from or to a page id
  * outside [0, num_blocks) is left out.  No page that holds a node may belong to two sequences of the call.

@@ -208,6 +208,7 @@ bool attention_in_one_launch(int n_q, int n_kv, int64_t num_tiles, bool half, in
 hipError_t launch_hybrid_attention(const AttnArgs& a, const PrefillItem* items, int num_items, bool half, const DecodeArgs& dec, hipStream_t stream);
 
 constexpr int kMaxTreeNodes = 256;
+constexpr int kMaxPositions = INT32_MAX - 63;  // of a sequence with a tree, so that a position, and one of the blocks behind it, fits 32 bits
 // Trees of drafted tokens (see kernels_tree.hip): device arrays, nothing of which the host reads.
 struct TreeArgs {
     const bf16_t* q;             // [num_rows][ld_q]

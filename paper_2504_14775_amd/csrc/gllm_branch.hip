@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
     const int r0 = a.row_start[s], r1 = a.row_start[s + 1], c = a.cached_len[s];
     const bool rows_ok = r0 >= 0 && r1 >= r0 && r1 <= a.num_rows;
     const int n = rows_ok ? r1 - r0 : 0;
-    const bool fits = n > 0 && n <= GLLM_TREE_MAX_NODES && c >= 0 && (int64_t)c + n <= (int64_t)a.table_stride * kPage;
+    const bool fits = n > 0 && n <= GLLM_TREE_MAX_NODES && c >= 0 && (int64_t)c + n <= min((int64_t)a.table_stride * kPage, (int64_t)kMaxPositions);
     if (fits) {
         if (t < n) drawn[t] = a.sampled[r0 + t];
         __syncthreads();

@@ -173,7 +173,7 @@ __device__ __forceinline__ SeqPlan seq_plan(const TreeArgs& a, int s, int tile_c
     p.row0 = r0;
     p.n = p.bad ? 0 : r1 - r0;
     p.tiles = (p.n * (a.n_q / a.n_kv) + tile_cols - 1) / tile_cols;  // (num_rows * group fits 31 bits: the launcher)
-    if (p.n > 0 && p.n <= a.max_nodes && p.c >= 0 && (int64_t)p.c + p.n <= (int64_t)a.table_stride * kPage) p.blocks = (p.c + p.n + 31) / 32;
+    if (p.n > 0 && p.n <= a.max_nodes && p.c >= 0 && (int64_t)p.c + p.n <= min((int64_t)a.table_stride * kPage, (int64_t)kMaxPositions)) p.blocks = (p.c + p.n + 31) / 32;
     return p;
 }
 

@@ -97,3 +97,43 @@ def test_more_logits_of_infinity_than_are_kept(beams, vocab, keep):
         x[beams - 1] = np.sort(rng.standard_normal(vocab) * 1e37)
         x[beams - 1, vocab // 2:] = np.finfo(np.float32).max
         check_beams(x, (-rng.random((1, beams)) * 3 - 2).astype(np.float32), keep, label=f"every {step}th")
+
+
+def test_positions_up_to_where_32_bits_end():
+    """One sequence of nearly 2^31 positions, every page of it the same one, and one that goes past: its rows receive zeros, its walk is empty.
+    The sums of a column are of 2^26 / 512 blocks at most in a wave, of 2^-24 each, in numerator and denominator."""
+    print("2^31 positions", flush=True)
+    limit, n, d = 2 ** 31 - 64, 3, 64
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k = torch.randn(2, 1, d // 8, 16, 8, generator=g, device=DEV).bfloat16()
+    v = torch.randn(2, 1, d, 16, generator=g, device=DEV).bfloat16()
+    q = torch.randn(n, 2 * d, generator=g, device=DEV).bfloat16()
+    tables = torch.zeros(1, 2 ** 27, dtype=torch.int32, device=DEV)
+    starts, parents, out = dev_ints([0, n]), dev_ints([-1, 0, 0]), torch.full((n, 2 * d), 7.0, dtype=torch.bfloat16, device=DEV)
+    BR.gllm_op_tree_attention(q, k, v, tables, dev_ints([limit - n]), starts, parents, out, n)
+    torch.cuda.synchronize()
+    kk, vv, qq = k[0, 0].double().permute(1, 0, 2).reshape(16, d), v[0, 0].double().t(), q.double().view(n, 2, d)
+    x = torch.einsum("rhd,kd->rhk", qq.cpu(), kk.cpu()) * d ** -0.5
+    p = torch.softmax(x, -1)
+    ref, weight = (torch.einsum("rhk,kd->rhd", p, y.cpu()) for y in (vv, vv.abs()))
+    mass = torch.einsum("rhd,kd->rhk", qq.cpu().abs(), kk.cpu().abs()).amax(-1, keepdim=True) * d ** -0.5
+    tol = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * mass * (d + 8) * 2.0 ** -24 + 2.0 ** -18 + 2 * 2.0 ** 17 / 2 ** 24) * weight
+    off = (out.double().cpu().view(n, 2, d) - ref).abs()
+    print(f"[parity] 2^31 positions: max abs {off.max():.3g}, of the bound {(off / tol).max():.2f}", flush=True)
+    assert (off <= tol).all()
+    BR.gllm_op_tree_attention(q, k, v, tables, dev_ints([limit - n + 1]), starts, parents, out, n)
+    torch.cuda.synchronize()
+    assert not out.any()
+    # the walk: the second child is accepted, from the last slots there are
+    page, slot = (limit - n) // 16, (limit - n) % 16
+    assert slot + n == 16
+    tables[0, page] = 1
+    pools = torch.randn(1, 2, 1, d // 8, 16, 8, generator=g, device=DEV).bfloat16(), torch.randn(1, 2, 1, d, 16, generator=g, device=DEV).bfloat16()
+    want = [x.clone() for x in pools]
+    want[0][:, 1, :, :, slot + 1], want[1][:, 1, :, :, slot + 1] = want[0][:, 1, :, :, slot + 2], want[1][:, 1, :, :, slot + 2]
+    for cached, result in ((limit - n, [0, 2, -1, 2, 8]), (limit - n + 1, [-1, -1, -1, 0, -1]), (2 ** 31 - 1, [-1, -1, -1, 0, -1])):
+        path, count, follow = dev_ints([-7] * n), dev_ints([-7]), dev_ints([-7])
+        BR.gllm_op_tree_commit(dev_ints([5, 6, 7]), parents, dev_ints([7, 9, 8]), starts, dev_ints([cached]), tables, *pools, path, count, follow)
+        torch.cuda.synchronize()
+        assert path.tolist() + count.tolist() + follow.tolist() == result
+        assert torch.equal(pools[0], want[0]) and torch.equal(pools[1], want[1])
