@@ -193,8 +193,11 @@ __device__ __forceinline__ void scan_wave(T& x) {
 }
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// Blocks of a share, from those of all tiles.  (The sum is exact up to 2^24, and more than it by then: a share is never less than the blocks by
-// the target.)
+// Blocks of a share, from those of all tiles.  (The sum is exact up to 2^24, and by 1e-4 of itself more from there on, which is more than the
+// roundings of its additions, 2^-24 of it each, take away: kTreeMaxSeqs / 4096 of a lane and 15 over lanes and runs.  A share is never less
+// than the blocks by the target: the units with partial results would outgrow their places.)
+constexpr int kTreeMaxSeqs = 1 << 22;
+static_assert(kTreeMaxSeqs / (64 * 64) + 15 < 16777216 / 10000, "the sum of all blocks");
 __device__ __forceinline__ int share_of(float total, int n_kv, int tile_cols) {
     const float target = (float)tree_target(n_kv, tile_cols);
     const float even = total < 16777216.f ? ceilf(total / target) : total / target * 1.0001f + 1.f;
@@ -899,7 +902,7 @@ hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t stream) {
     // no more tiles than whole ones in all rows and a partly filled one per sequence; cutting the keys adds no more units than there
     // are shares; and one place behind the last unit
     const int64_t units = (int64_t)a.num_rows * g / tile_cols + a.num_seqs + tree_target(a.n_kv, tile_cols) + 1;
-    if (a.num_seqs > 1 << 30 || units * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
+    if (a.num_seqs > kTreeMaxSeqs || units * a.n_kv > INT32_MAX || (int64_t)a.num_rows * g > INT32_MAX) return hipErrorInvalidValue;
     if (a.d == 128) return launch_tree<128>(a, tile_cols, units, stream);
     if (a.d == 64) return launch_tree<64>(a, tile_cols, units, stream);
     return hipErrorInvalidValue;

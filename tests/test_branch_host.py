@@ -155,3 +155,8 @@ def test_oracle_beams_of_equal_sums():
     assert beam[0].tolist() == [0, 0, 0, 0, 1, 1] and token[0].tolist() == [1, 3, 2, 0, 0, 2] and len(set(score[0])) == 1
     score, beam, token = O.beam_select(x * 1e20, np.full((1, 2), -1e18, dtype=np.float32), 6)
     assert beam[0].tolist() == [0, 0, 0, 0, 1, 1] and token[0].tolist() == [1, 3, 2, 0, 0, 2]
+
+
+def test_tree_attention_refuses_more_sequences_than_the_plan_adds_up():
+    for seqs in ((1 << 22) + 1, 1 << 30):
+        assert BR._lib().gllm_op_tree_attention(*{**ATTENTION, "seqs": seqs}.values()) == CAPACITY
