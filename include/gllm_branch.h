@@ -52,7 +52,8 @@ enum { GLLM_TREE_MAX_NODES = 256, GLLM_BEAM_MAX_BEAMS = 32, GLLM_BEAM_MAX_KEEP =
  * past the last node may hold anything; those of the prefix and of used nodes have to be finite for every row that sees them, and a value
  * that is not finite spoils the rows that see it only.
  * Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads with at most 16 query heads per KV head (else
- * GLLM_E_UNSUPPORTED); scale > 0 and finite.  GLLM_E_CAPACITY for a workspace that is too small and for more than 2^22 sequences. */
+ * GLLM_E_UNSUPPORTED); scale > 0 and at most 2.3e38 (else GLLM_E_INVALID), q . k finite in float, and q . k * scale between -5e29 and 2e38.
+ * GLLM_E_CAPACITY for a workspace that is too small and for more than 2^22 sequences. */
 gllm_status gllm_op_tree_attention(const void* q, int64_t ld_q, const void* k_pool, const void* v_pool, int64_t num_blocks,
                                    const int32_t* block_tables, int32_t block_table_stride, const int32_t* cached_len,
                                    const int32_t* row_start, const int32_t* parents, int32_t num_seqs, int32_t num_rows,

@@ -734,6 +734,8 @@ gllm_status launched() { return hipGetLastError() == hipSuccess ? GLLM_OK : GLLM
 
 bool misaligned(const void* p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) != 0; }
 
+float base2(float scale) { return (float)(scale * 1.4426950408889634); }  // of scores whose exponentials are taken in base 2
+
 bool tree_shape_ok(int n_q, int n_kv, int d, int max_nodes) {
     return n_q >= 1 && n_kv >= 1 && n_q % n_kv == 0 && n_q / n_kv <= 16 && (d == 64 || d == 128) && max_nodes >= 1 && max_nodes <= GLLM_TREE_MAX_NODES;
 }
@@ -752,7 +754,7 @@ gllm_status gllm_op_tree_attention(const void* q, int64_t ld_q, const void* k_po
                                    int32_t max_nodes, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
                                    void* out, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
     if (num_seqs < 0 || num_rows < 0 || max_nodes < 1 || num_blocks < 1 || num_blocks > INT32_MAX || block_table_stride < 1 || n_q_heads < 1 || n_kv_heads < 1 ||
-        !(scale > 0.f) || !std::isfinite(scale))
+        !(scale > 0.f) || !std::isfinite(base2(scale)))
         return GLLM_E_INVALID;
     if (!tree_shape_ok(n_q_heads, n_kv_heads, head_dim, max_nodes)) return GLLM_E_UNSUPPORTED;
     if (num_seqs == 0 || num_rows == 0) return GLLM_OK;
@@ -769,7 +771,7 @@ gllm_status gllm_op_tree_attention(const void* q, int64_t ld_q, const void* k_po
     a.num_seqs = num_seqs; a.num_rows = num_rows; a.max_nodes = max_nodes;
     a.out = (bf16_t*)out; a.ld_o = ld_out;
     a.n_q = n_q_heads; a.n_kv = n_kv_heads; a.d = head_dim;
-    a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.scale_log2 = base2(scale);
     a.workspace = workspace;
     const hipError_t e = launch_tree_attention(a, (hipStream_t)stream);
     return e == hipSuccess ? GLLM_OK : e == hipErrorInvalidValue ? GLLM_E_CAPACITY : GLLM_E_HIP;

@@ -160,3 +160,8 @@ def test_oracle_beams_of_equal_sums():
 def test_tree_attention_refuses_more_sequences_than_the_plan_adds_up():
     for seqs in ((1 << 22) + 1, 1 << 30):
         assert BR._lib().gllm_op_tree_attention(*{**ATTENTION, "seqs": seqs}.values()) == CAPACITY
+
+
+@pytest.mark.parametrize("scale,status", [(2.4e38, INVALID), (3.4e38, INVALID), (2.3e38, CAPACITY)])
+def test_tree_attention_refuses_a_scale_that_is_not_finite_in_base_2(scale, status):
+    assert BR._lib().gllm_op_tree_attention(*{**ATTENTION, "scale": scale, "ws_bytes": 0}.values()) == status
