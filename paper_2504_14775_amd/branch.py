@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+from array import array
 
 import numpy as np
 import torch
@@ -15,7 +16,7 @@ EXPORTS = [
     "gllm_op_beam_select_workspace_bytes", "gllm_op_copy_pages",
 ]
 PAGE = 16
-_INVALID = -1
+_INVALID, _BLOCK_RANGE = -1, -3
 
 _ready = None
 
@@ -172,16 +173,40 @@ def gllm_op_beam_select(logits, vocab: int, scores, out_scores, out_beams, out_t
         raise GllmError(st, call)
 
 
+def _page_ids(call: str, ids):
+    """(address, number, owner of the memory) of int32 page ids; what is no whole number of 32 bits is refused, not cut to one."""
+    if type(ids) is list:
+        try:
+            a = array("i", ids)
+            return *a.buffer_info(), a
+        except (TypeError, OverflowError):
+            pass
+    given = np.asarray(ids)
+    if given.dtype.kind in "iu":
+        a = np.ascontiguousarray(given, dtype=np.int32)
+        if a is not given and not (a == given).all():
+            raise GllmError(_BLOCK_RANGE, f"{call}: page ids outside the pool")
+    else:
+        if given.size > 0 and given.dtype.kind != "f" and not all(isinstance(x, int) for x in given.flat):
+            _refuse(f"{call}: page ids are whole numbers, got an array of {given.dtype}")
+        if given.dtype.kind == "f" and not (given == np.floor(given)).all():
+            _refuse(f"{call}: page ids are whole numbers")
+        if given.size > 0 and not -2 ** 31 <= given.min() <= given.max() < 2 ** 31:
+            raise GllmError(_BLOCK_RANGE, f"{call}: page ids outside the pool")
+        a = np.ascontiguousarray(given, dtype=np.int32)
+    if given.ndim != 1:
+        _refuse(f"{call}: page ids of shape {given.shape}")
+    return a.ctypes.data, a.shape[0], a
+
+
 def gllm_op_copy_pages(k_pool, v_pool, src, dst, stream=None) -> None:
     """k_pool: bf16 [layers, pages, n_kv, d/8, 16, 8], v_pool: bf16 [layers, pages, n_kv, d, 16]; src, dst: page ids on the host."""
     call = "gllm_op_copy_pages"
     n_kv, d = _pool_shape(call, k_pool, v_pool, 2)
+    (s, n, _s), (t, n_dst, _t) = _page_ids(call, src), _page_ids(call, dst)
     dev = _check(call, ((k_pool, _BF16), (v_pool, _BF16)))
-    s = np.ascontiguousarray(src, dtype=np.int32)
-    t = np.ascontiguousarray(dst, dtype=np.int32)
-    if s.ndim != 1 or s.shape != t.shape:
-        _refuse(f"{call}: {s.shape} sources, {t.shape} destinations")
-    st = _lib().gllm_op_copy_pages(k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pool.shape[1], n_kv, d, s.ctypes.data, t.ctypes.data,
-                                   s.shape[0], _stream(stream, dev))
+    if n != n_dst:
+        _refuse(f"{call}: {n} sources, {n_dst} destinations")
+    st = _lib().gllm_op_copy_pages(k_pool.data_ptr(), v_pool.data_ptr(), k_pool.shape[0], k_pool.shape[1], n_kv, d, s, t, n, _stream(stream, dev))
     if st != GLLM_OK:
         raise GllmError(st, call)

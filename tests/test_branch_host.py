@@ -165,3 +165,13 @@ def test_tree_attention_refuses_more_sequences_than_the_plan_adds_up():
 @pytest.mark.parametrize("scale,status", [(2.4e38, INVALID), (3.4e38, INVALID), (2.3e38, CAPACITY)])
 def test_tree_attention_refuses_a_scale_that_is_not_finite_in_base_2(scale, status):
     assert BR._lib().gllm_op_tree_attention(*{**ATTENTION, "scale": scale, "ws_bytes": 0}.values()) == status
+
+
+@pytest.mark.parametrize("src,dst,status", [([1 << 32], [1], RANGE), ([0], [(1 << 32) + 1], RANGE), ([0], [-(1 << 32) + 1], RANGE), ([0], [1 << 70], RANGE),
+                                            ([0.5], [1], INVALID), ([0], [float("nan")], INVALID), ([0], [[1]], INVALID), ([0], ["1"], INVALID), ([0], [None], INVALID)])
+def test_page_ids_that_are_no_32_bit_numbers_are_refused(src, dst, status):
+    """Not taken modulo 2^32, not rounded (and before a look at the pools, which lie on the host here)."""
+    k, v = torch.zeros(2, 3, 2, 8, 16, 8, dtype=torch.bfloat16), torch.zeros(2, 3, 2, 64, 16, dtype=torch.bfloat16)
+    with pytest.raises(B.GllmError) as e:
+        BR.gllm_op_copy_pages(k, v, src, dst)
+    assert e.value.status == status and "cpu" not in e.value.message
