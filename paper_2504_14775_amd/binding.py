@@ -152,6 +152,20 @@ def _stream_ptr(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _int32_of(x, what: str):
+    """x as int32 numbers on the host; one that is no whole number of 32 bits is refused, not cut to one."""
+    given = np.asarray(x)
+    try:
+        with np.errstate(invalid="ignore"):
+            a = np.ascontiguousarray(given, dtype=np.int32)
+        fits = a is given or given.size == 0 or (given.dtype.kind in "iufO" and bool((a == given).all()))
+    except (TypeError, ValueError, OverflowError):
+        fits = False
+    if not fits:
+        raise GllmError(-1, f"{what}: a number is no whole one of 32 bits")
+    return a
+
+
 def make_config(shape, max_tokens: int, max_seqs: int, max_blocks_per_seq: int, max_position: int) -> gllm_stage_config:
     return gllm_stage_config(shape.num_layers, shape.hidden, shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
                              shape.intermediate, shape.page_size, int(bool(shape.has_qkv_bias)), max_tokens,
@@ -235,7 +249,7 @@ class Stage:
         nt = np.ascontiguousarray(new_tokens, dtype=np.int32)
         cl = np.ascontiguousarray(cached_len, dtype=np.int32)
         bt = np.ascontiguousarray(block_tables, dtype=np.int32)
-        up = np.ascontiguousarray(parents, dtype=np.int32)
+        up = _int32_of(parents, "parents")
         assert bt.ndim == 2 and bt.shape[0] == nt.shape[0] == cl.shape[0] and up.shape == (int(nt.sum()),)
         ip = C.POINTER(C.c_int32)
         b = gllm_batch(int(nt.shape[0]), int(bt.shape[1]), nt.ctypes.data_as(ip), cl.ctypes.data_as(ip),

@@ -5,8 +5,10 @@ import pytest
 import torch
 
 from gpu_util import DEV
+from paper_2504_14775_amd import binding as B
 from paper_2504_14775_amd import branch as BR
 from test_gpu_branch import check_beams, dev_ints
+from test_gpu_branch_loop import Model
 
 pytestmark = pytest.mark.gpu
 
@@ -137,3 +139,15 @@ def test_positions_up_to_where_32_bits_end():
         torch.cuda.synchronize()
         assert path.tolist() + count.tolist() + follow.tolist() == result
         assert torch.equal(pools[0], want[0]) and torch.equal(pools[1], want[1])
+
+
+def test_parents_that_are_no_32_bit_numbers_are_refused():
+    print("parents modulo 2^32", flush=True)
+    m = Model(5, 8, layers=1)
+    x = torch.zeros(3, m.shape.hidden, dtype=torch.bfloat16, device=DEV)
+    for bad in ([-1, 1 << 32, 0], [-1, 0, (1 << 32) + 1], [(1 << 32) - 1, 0, 0], [-1, 0.5, 1], [-1, 0, 1 << 70]):
+        with pytest.raises(B.GllmError) as e:
+            m.stage.forward_tree([3], [0], np.zeros((1, 1)), bad, x, torch.empty_like(x))
+        assert e.value.status == -1
+    m.stage.forward_tree([3], [0], np.zeros((1, 1)), np.array([-1, 0, 0]), x, torch.empty_like(x))
+    m.close()
