@@ -611,22 +611,24 @@ static gllm_status forward(gllm_stage* s, const gllm_batch* b, const int32_t* pa
         T += n;
         total_pages += pages;
         if (T > c.max_tokens) return fail(s, GLLM_E_CAPACITY, "batch exceeds max_tokens");
-        const int64_t row0 = T - n;
-        if (parents && is_tree(parents + row0, n)) {
-            if (n > kMaxTreeNodes) return fail(s, GLLM_E_CAPACITY, "sequence " + std::to_string(i) + " has a tree of more than 256 nodes");
-            for (int t = 0; t < n; ++t)
-                if (parents[row0 + t] < -1 || parents[row0 + t] >= t)
-                    return fail(s, GLLM_E_INVALID, "sequence " + std::to_string(i) + " node " + std::to_string(t) + " has parent " + std::to_string(parents[row0 + t]));
-            ++n_trees;
-            tree_rows += n;
-            most_nodes = std::max(most_nodes, n);
-            most_pages = std::max(most_pages, (int)pages);
-        }
         const int32_t* row = b->block_tables + (int64_t)i * b->block_table_stride;
         for (int64_t p = 0; p < pages; ++p)
             if (row[p] < 0 || row[p] >= s->num_blocks)
                 return fail(s, GLLM_E_BLOCK_RANGE, "sequence " + std::to_string(i) + " logical page " + std::to_string(p) +
                                                        " names page " + std::to_string(row[p]) + " outside the pool");
+    }
+    int64_t row0 = 0;
+    for (int i = 0; parents && i < S; row0 += b->new_tokens[i++]) {  // (of T rows: the lengths hold)
+        const int n = b->new_tokens[i];
+        if (!is_tree(parents + row0, n)) continue;
+        if (n > kMaxTreeNodes) return fail(s, GLLM_E_CAPACITY, "sequence " + std::to_string(i) + " has a tree of more than 256 nodes");
+        for (int t = 0; t < n; ++t)
+            if (parents[row0 + t] < -1 || parents[row0 + t] >= t)
+                return fail(s, GLLM_E_INVALID, "sequence " + std::to_string(i) + " node " + std::to_string(t) + " has parent " + std::to_string(parents[row0 + t]));
+        ++n_trees;
+        tree_rows += n;
+        most_nodes = std::max(most_nodes, n);
+        most_pages = std::max(most_pages, (int)ceil_div((int64_t)b->cached_len[i] + n, kPage));
     }
     if (s->alias_check) {
         s->written_pages.clear();

@@ -151,3 +151,15 @@ def test_parents_that_are_no_32_bit_numbers_are_refused():
         assert e.value.status == -1
     m.stage.forward_tree([3], [0], np.zeros((1, 1)), np.array([-1, 0, 0]), x, torch.empty_like(x))
     m.close()
+
+
+def test_the_stage_reads_parents_only_behind_lengths_that_hold():
+    """How many parents there are goes by the lengths: one that is refused is named, not the parents in front of it."""
+    print("parents and lengths", flush=True)
+    m = Model(6, 8, layers=1)
+    x = torch.zeros(4, m.shape.hidden, dtype=torch.bfloat16, device=DEV)
+    for new, cached, status in (([3, -1], [0, 0], -1), ([1, 1, 0], [0, 0, 0], -1), ([1, 1], [0, -1], -1), ([1, 1], [0, 1 << 20], -2)):
+        with pytest.raises(B.GllmError) as e:
+            m.stage.forward_tree(new, cached, np.zeros((len(new), 1)), [5] * sum(new), x, torch.empty_like(x))
+        assert e.value.status == status and "parent" not in e.value.message, e.value.message
+    m.close()
