@@ -90,7 +90,7 @@ def _row_stride(t) -> int:
 def _pool_shape(call: str, k_pool, v_pool, dims: int):
     """(KV heads, head size) of pools [.., n_kv, d/8, 16, 8] and [.., n_kv, d, 16] with `dims` dimensions in front."""
     k, v = k_pool.shape, v_pool.shape
-    if len(k) != dims + 4 or len(v) != dims + 3 or k[:dims + 1] != v[:dims + 1] or k[-1] != 8 or k[-2] != PAGE or v[-1] != PAGE or v[-2] != 8 * k[-3]:
+    if len(k) != dims + 4 or len(v) != dims + 3 or k[:dims + 1] != v[:dims + 1] or k[-1] != 8 or k[-2] != PAGE or v[-1] != PAGE or v[-2] != 8 * k[-3] or v[-2] == 0:
         _refuse(f"{call}: pools of shapes {tuple(k)} and {tuple(v)}")
     return k[dims], v[-2]
 
@@ -108,8 +108,8 @@ def gllm_op_tree_attention(q, k_pool, v_pool, block_tables, cached_len, row_star
     n_kv, d = _pool_shape(call, k_pool, v_pool, 1)
     dev = _check(call, ((q, _BF16), (out, _BF16), (k_pool, _BF16), (v_pool, _BF16), (block_tables, _I32), (cached_len, _I32), (row_start, _I32),
                         (parents, _I32)), rows_only=(q, out))
-    rows, seqs = q.shape[0], cached_len.shape[0]
-    if q.dim() != 2 or q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1 or parents.numel() != rows:
+    rows, seqs = parents.numel(), cached_len.numel()
+    if q.dim() != 2 or q.shape[0] != rows or cached_len.dim() < 1 or q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1:
         _refuse(f"{call}: shapes q {tuple(q.shape)}, out {tuple(out.shape)}, block_tables {tuple(block_tables.shape)}, cached_len {tuple(cached_len.shape)}, "
                 f"row_start {tuple(row_start.shape)}, parents {tuple(parents.shape)}")
     n_q = q.shape[1] // d

@@ -175,3 +175,12 @@ def test_page_ids_that_are_no_32_bit_numbers_are_refused(src, dst, status):
     with pytest.raises(B.GllmError) as e:
         BR.gllm_op_copy_pages(k, v, src, dst)
     assert e.value.status == status and "cpu" not in e.value.message
+
+
+def test_pools_without_a_head_dimension_are_refused():
+    b, i = torch.zeros(4, 128, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    k, v = torch.zeros(2, 3, 2, 0, 16, 8, dtype=torch.bfloat16), torch.zeros(2, 3, 2, 0, 16, dtype=torch.bfloat16)
+    for call in (lambda: BR.gllm_op_tree_attention(b, k[0], v[0], i.view(1, 4), i[:1], i[:2], i, b, 4), lambda: BR.gllm_op_copy_pages(k, v, [0], [1])):
+        with pytest.raises(B.GllmError) as e:
+            call()
+        assert e.value.status == INVALID and "shapes" in e.value.message

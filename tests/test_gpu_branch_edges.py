@@ -163,3 +163,24 @@ def test_the_stage_reads_parents_only_behind_lengths_that_hold():
             m.stage.forward_tree(new, cached, np.zeros((len(new), 1)), [5] * sum(new), x, torch.empty_like(x))
         assert e.value.status == status and "parent" not in e.value.message, e.value.message
     m.close()
+
+
+def test_tensors_of_other_dimensions_are_refused():
+    print("dimensions", flush=True)
+    i, b = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(4, 128, dtype=torch.bfloat16, device=DEV)
+    k, v = torch.zeros(1, 3, 2, 8, 16, 8, dtype=torch.bfloat16, device=DEV), torch.zeros(1, 3, 2, 64, 16, dtype=torch.bfloat16, device=DEV)
+    x, f = torch.zeros(8, 100, device=DEV), torch.zeros(2, 4, device=DEV)
+    attention = dict(q=b, k_pool=k[0], v_pool=v[0], block_tables=i.view(1, 4), cached_len=i[:1], row_start=i[:2], parents=i, out=b.clone(), max_nodes=4)
+    commit = dict(tokens=i, parents=i, sampled=i, row_start=i[:2], cached_len=i[:1], block_tables=i.view(1, 4), k_pool=k, v_pool=v, path=i.clone(), count=i[:1], next_token=i[:1])
+    beams = dict(logits=x, vocab=100, scores=f, out_scores=f.clone(), out_beams=f.int(), out_tokens=f.int())
+    for call, args, names in ((BR.gllm_op_tree_attention, attention, ("q", "out", "block_tables")), (BR.gllm_op_tree_commit, commit, ("block_tables",)),
+                              (BR.gllm_op_beam_select, beams, ("logits", "scores", "out_scores", "out_beams", "out_tokens"))):
+        for name in names:
+            for other in (args[name].reshape(-1)[0], args[name].reshape(-1), args[name][None]):
+                with pytest.raises(B.GllmError) as e:
+                    call(**{**args, name: other})
+                assert e.value.status == -1, name
+    for name in ("cached_len", "row_start", "parents"):
+        with pytest.raises(B.GllmError) as e:
+            BR.gllm_op_tree_attention(**{**attention, name: i[0]})
+        assert e.value.status == -1, name
