@@ -5,9 +5,10 @@ import pytest
 import torch
 
 from gpu_util import DEV
+from oracle import branch_oracle as O
 from paper_2504_14775_amd import binding as B
 from paper_2504_14775_amd import branch as BR
-from test_gpu_branch import check_beams, dev_ints
+from test_gpu_branch import Trees, check_beams, dev_ints, f64
 from test_gpu_branch_loop import Model
 
 pytestmark = pytest.mark.gpu
@@ -184,3 +185,34 @@ def test_tensors_of_other_dimensions_are_refused():
         with pytest.raises(B.GllmError) as e:
             BR.gllm_op_tree_attention(**{**attention, name: i[0]})
         assert e.value.status == -1, name
+
+
+@pytest.mark.parametrize("cached", [58, 3003])
+@pytest.mark.parametrize("heads,most", [((2, 2, 64), 8), ((2, 2, 128), 8), ((8, 2, 128), 8), ((8, 2, 64), 16), ((8, 2, 128), 16), ((8, 2, 128), 65), ((8, 2, 64), 128),
+                                        ((8, 2, 128), 128), ((32, 2, 128), 256)], ids=str)
+def test_values_that_are_not_finite_in_every_kernel(heads, most, cached):
+    """Tiles of 16, 32, 64 and 128 columns, uncut and cut keys, nodes in two blocks: keys and values of nodes, and a value of the prefix in the
+    tree's first block, that are not finite change the rows and dims that see them only, the others not by a bit."""
+    print(f"not finite, {heads}, at most {most} nodes, {cached} cached", flush=True)
+    n_q, n_kv, d = heads
+    g = n_q // n_kv
+    tree = [-1, 0, 0, 1, 2, 2, 3, 4]
+    t = Trees(heads, [cached], [tree], seed=most)
+    clean = f64(t.run(max_nodes=most)).reshape(8, n_q, d).copy()
+    assert np.isfinite(clean).all()
+    nan, inf = float("nan"), float("inf")
+    hit = np.zeros(clean.shape, dtype=bool)
+    for node, what, dim in ((2, nan, 9), (6, inf, d - 3), (1, -inf, d // 2 + 1)):
+        page, slot = t.slot(0, cached + node)
+        t.v[page, 0, dim, slot] = what
+        see = [i for i in range(8) if node in O.chain(tree, i)]
+        hit[see, :g, dim] = True
+    page, slot = t.slot(0, cached - 3)
+    t.v[page, 1, d - 1, slot] = nan
+    hit[:, g:2 * g, d - 1] = True
+    page, slot = t.slot(0, cached + 5)
+    t.k[page, 1, :, slot, 3] = nan
+    hit[5, g:2 * g] = True
+    got = f64(t.run(max_nodes=most)).reshape(8, n_q, d)
+    assert not np.isfinite(got[hit]).any()
+    assert np.array_equal(got[~hit], clean[~hit])
