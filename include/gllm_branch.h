@@ -75,7 +75,7 @@ size_t gllm_op_tree_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_he
  *   k_pool, v_pool  DEVICE bf16, num_layers layers of num_blocks pages (16-byte aligned); both NULL: nothing is moved, and
  *            num_layers, num_blocks, n_kv_heads, head_dim are not looked at
  *   path DEVICE int32 [num_rows], count, next_token DEVICE int32 [num_seqs]
- * head_dim 64 or 128, else GLLM_E_UNSUPPORTED. */
+ * head_dim 64 or 128, else GLLM_E_UNSUPPORTED; num_layers * n_kv_heads * num_seqs below 2^31, else GLLM_E_CAPACITY. */
 gllm_status gllm_op_tree_commit(const int32_t* tokens, const int32_t* parents, const int32_t* sampled, const int32_t* row_start,
                                 const int32_t* cached_len, const int32_t* block_tables, int32_t block_table_stride,
                                 int32_t num_seqs, int32_t num_rows, void* k_pool, void* v_pool, int32_t num_layers,

@@ -786,7 +786,7 @@ gllm_status gllm_op_tree_commit(const int32_t* tokens, const int32_t* parents, c
     if (k_pool) {
         if (num_layers < 1 || num_blocks < 1 || num_blocks > INT32_MAX || n_kv_heads < 1 || misaligned(k_pool, 16) || misaligned(v_pool, 16)) return GLLM_E_INVALID;
         if (head_dim != 64 && head_dim != 128) return GLLM_E_UNSUPPORTED;
-        if ((int64_t)num_layers * n_kv_heads * num_seqs > INT32_MAX) return GLLM_E_CAPACITY;
+        if ((int64_t)num_layers * n_kv_heads > INT32_MAX / std::max(1, num_seqs)) return GLLM_E_CAPACITY;
     }
     if (num_seqs == 0) return GLLM_OK;
     if (!row_start || !cached_len || !block_tables || !count || !next_token) return GLLM_E_INVALID;

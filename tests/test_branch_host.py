@@ -184,3 +184,9 @@ def test_pools_without_a_head_dimension_are_refused():
         with pytest.raises(B.GllmError) as e:
             call()
         assert e.value.status == INVALID and "shapes" in e.value.message
+
+
+@pytest.mark.parametrize("change", [dict(layers=(1 << 31) - 1, n_kv=(1 << 31) - 1, seqs=4), dict(layers=1 << 30, n_kv=1 << 30, seqs=16), dict(layers=1 << 16, n_kv=1 << 15, seqs=1),
+                                    dict(layers=1 << 15, n_kv=1 << 10, seqs=1 << 6)], ids=str)
+def test_tree_commit_refuses_more_moves_than_a_launch_has_places(change):
+    assert BR._lib().gllm_op_tree_commit(*{**COMMIT, **change}.values()) == CAPACITY
