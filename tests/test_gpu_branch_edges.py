@@ -1,13 +1,18 @@
 """GPU tests of the operators for several continuations of one sequence (include/gllm_branch.h) where their sizes send them through other
 kernels and paths than tests/test_gpu_branch.py does with the same contents; helpers and bounds are that file's."""
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
 
-from gpu_util import DEV
+import oracle
+from gpu_util import DEV, to_dev_bits
+from helpers import layer_weights_np
 from oracle import branch_oracle as O
 from paper_2504_14775_amd import binding as B
 from paper_2504_14775_amd import branch as BR
+from paper_2504_14775_amd import synth
 from test_gpu_branch import Trees, check_beams, dev_ints, f64
 from test_gpu_branch_loop import Model
 
@@ -216,3 +221,87 @@ def test_values_that_are_not_finite_in_every_kernel(heads, most, cached):
     got = f64(t.run(max_nodes=most)).reshape(8, n_q, d)
     assert not np.isfinite(got[hit]).any()
     assert np.array_equal(got[~hit], clean[~hit])
+
+
+def test_many_candidates_from_a_graph_and_two_calls_at_once():
+    """The path of many kept logits: a workspace that holds anything, replays with other logits, two calls on streams of their own."""
+    print("many candidates: graph, streams", flush=True)
+    rng = np.random.default_rng(41)
+    vocab, keep = 128256, 16
+    x = (rng.standard_normal((16, vocab)) * 4.5).astype(np.float32)
+    x[3] = -np.inf
+    scores = -rng.random((2, 8)).astype(np.float32)
+    size = BR.gllm_op_beam_select_workspace_bytes(2, 8, vocab, keep)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV).fill_(255)
+    check_beams(x, scores, keep, workspace=ws)
+    lg, sc = torch.from_numpy(x).to(DEV), torch.from_numpy(scores).to(DEV)
+    new = lambda: (torch.full((2, keep), 7.0, device=DEV), dev_ints(np.full((2, keep), -9)), dev_ints(np.full((2, keep), -9)))
+    out = new()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        BR.gllm_op_beam_select(lg, vocab, sc, *out, workspace=ws)
+    for shift in (0, 77, 9001):
+        y = np.roll(x, shift, axis=1)
+        if shift:
+            y[3], y[12] = rng.standard_normal(vocab), np.nan
+        lg.copy_(torch.from_numpy(y))
+        ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        ref = check_beams(y, scores, keep, label=f"replayed, {shift}")
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(out, ref))
+    calls = [(torch.cuda.Stream(), torch.from_numpy(z).to(DEV), torch.empty(size, dtype=torch.uint8, device=DEV).fill_(255), new()) for z in (x, np.roll(x, 5, axis=1))]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for stream, z, w, o in calls:
+            BR.gllm_op_beam_select(z, vocab, sc, *o, workspace=w, stream=stream)
+    torch.cuda.synchronize()
+    for _, z, _, o in calls:
+        ref = check_beams(z.cpu().numpy(), scores, keep)
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(o, ref))
+
+
+def test_the_stage_over_more_trees_than_a_wave_plans_for_itself():
+    """70 trees and a few decode rows, some of the trees behind keys that are cut: every path from a root to a leaf against the oracle, within
+    the tolerance of tests/test_gpu_branch_loop.py."""
+    print("stage over 70 trees", flush=True)
+    rng = np.random.default_rng(70)
+    shape = dataclasses.replace(synth.SHAPES["tiny"], num_layers=1, name="trees")
+    weights = layer_weights_np(shape, 9)
+    trees = [[-1] if s % 12 == 5 else [-1, 0, 0] + [int(rng.integers(0, i)) for i in range(3, int(rng.integers(3, 8)))] for s in range(76)]
+    cached = [int(rng.integers(400, 700)) if s % 15 == 3 else int(rng.integers(0, 50)) for s in range(76)]
+    new = [len(t) for t in trees]
+    assert sum(n > 1 for n in new) >= 65
+    pages = [-(-(c + n) // 16) for c, n in zip(cached, new)]
+    order = rng.permutation(sum(pages) + 2)
+    tables, at = np.zeros((76, max(pages)), dtype=np.int32), 0
+    for s, p in enumerate(pages):
+        tables[s, :p] = order[at:at + p]
+        at += p
+    k0, v0 = (synth.bf16_bits(x).copy() for x in synth.make_pool(shape, 9, len(order)))
+    hidden = synth.bf16_bits(synth.make_hidden(shape, 9, sum(new)))
+    stage = B.Stage(B.make_config(shape, sum(new), 76, max(pages), max(pages) * 16))
+    stage.bind_workspace(torch.empty(stage.workspace_bytes(), dtype=torch.uint8, device=DEV))
+    stage.load_layer(0, {k: to_dev_bits(v) for k, v in weights[0].items()})
+    dk, dv, x = to_dev_bits(k0), to_dev_bits(v0), to_dev_bits(hidden)
+    stage.bind_kv_pool(dk, dv, len(order))
+    out, out32 = torch.empty(sum(new), shape.hidden, dtype=torch.bfloat16, device=DEV), torch.empty(sum(new), shape.hidden, device=DEV)
+    stage.forward_tree(new, cached, tables, np.concatenate(trees), x, out, out32)
+    torch.cuda.synchronize()
+    starts = np.concatenate([[0], np.cumsum(new)])
+    paths = [(s, O.chain(t, i)) for s, t in enumerate(trees) for i in range(len(t)) if i not in t]
+    per = synth.pool_elems_per_layer(shape, len(order)) // len(order)
+    K, V = (z.reshape(len(order), per) for z in (k0, v0))
+    ptab, ids = np.zeros((len(paths), max(pages)), dtype=np.int32), []
+    for i, (s, path) in enumerate(paths):
+        p = -(-(cached[s] + len(path)) // 16)
+        ptab[i, :p] = np.arange(len(ids), len(ids) + p)
+        ids += tables[s, :p].tolist()
+    rows = np.concatenate([starts[s] + np.array(path) for s, path in paths])
+    ref, _ = oracle.stage_forward(shape, weights, np.array([len(p) for _, p in paths], dtype=np.int32), np.array([cached[s] for s, _ in paths], dtype=np.int32),
+                                  ptab, len(ids), K[ids].reshape(-1), V[ids].reshape(-1), hidden[rows])
+    off = np.abs(out32.cpu().numpy().astype(np.float64)[rows] - ref)
+    print(f"[parity] 70 trees: max_abs={off.max():.4g} mean_rel={off.sum() / np.abs(ref).sum():.4g} over {len(rows)} rows", flush=True)
+    assert set(rows) == set(range(sum(new)))
+    assert off.max() <= 2e-2 * max(1.0, np.sqrt((ref ** 2).mean())) and off.sum() / np.abs(ref).sum() <= 5e-3
+    stage.destroy()
