@@ -142,7 +142,10 @@ __device__ __forceinline__ void raise_reference(AttnState<D, NB>& st, const floa
         }
     }
 }
-// The weights of the block by the present references, the operand of the P.V product, and their sums.
+// The weights of the block by the present references, the operand of the P.V product, and their sums.  The operand is rounded to bf16, since the
+// matrix instruction takes both operands in the type of V: each weight is off by at most 2^-8 of itself, independently, on top of an output that
+// is rounded to bf16 anyway (error of an output against 64 bits 0.0018 to 0.0023 of its size, 0.0017 with weights of 32 bits).  The sums take the
+// weights as they were.
 template <int D, int NB>
 __device__ __forceinline__ void block_weights(AttnState<D, NB>& st, const float (&sc)[NB][8], float scale_log2, bf16x8 (&pb)[NB]) {
 #pragma unroll

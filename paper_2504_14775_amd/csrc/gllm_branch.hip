@@ -29,7 +29,8 @@ struct CommitArgs {
 //
 // Bound by HBM where there is much to move, and by how V lies there: a token's values are 2 bytes of every 32, so that its 256 bytes of a
 // head are in all 32 128-byte lines of a (page, head), which a move reads and writes.  64 trees of 60 nodes in 12 layers (8 KV heads of
-// 128): 31 MB of keys and values moved, 73 MB read and 33 MB written, 35 us; one tree of 26 nodes 6.1 us, a launch and the walk.
+// 128): 31 MB of keys and values moved, 73 MB read and 33 MB written, 36 us (mean of thirty launches, 34 the fastest); one tree of 26 nodes
+// 6.4 us, a launch and the walk.
 // (A thread has a 16-byte piece of K, and V elements of neighbouring dims.)
 constexpr int kMoves = 16;
 // Workgroups that the (layer, head)s are spread over: two rounds of those that run at one time.  (us at 1024 / 2048 / 4096 / one for each, 64 trees
@@ -153,11 +154,12 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 // The order among beams hangs on the sums: they and the scores are held in 64 bits, so that the order is that of exact
 // arithmetic but where scores of two beams agree to some 1e-10; in a beam it is that of the logits.
 //
-// Measured (64 sequences of 8 beams over a vocabulary of 152064, keep 16: 311 MB): 87 + 8 us, of which HBM would take 50.  What bounds
-// beam_rows are vector instructions and their latency, some 20 a logit, 12 of them in 64 bits (the exponential), with one pass on its way
-// while the last one is worked on: at 128 rows it takes 30 us, without exponentials and without lists behind the first pass 16.  Reading
-// past the caches takes 94 us where a plain load takes 96.  beam_merge is latency: four dependent steps (sums, logarithms, the bound, the lists above
-// it, all in one queue so that up to 8 loads are on their way: 32 beams that keep 64 53 -> 47 us).
+// Measured (64 sequences of 8 beams over a vocabulary of 152064, keep 16: 311 MB): 91 + 8.5 us, means of thirty launches (87.5 + 8 the fastest), of
+// which HBM would take 50.  What bounds beam_rows are vector instructions and their latency, 27 a logit, 12 of them in 64 bits (the exponential),
+// with one pass on its way while the last one is worked on: at 128 rows it takes 30 us, without exponentials and without lists behind the first
+// pass 16.  Reading past the caches takes 94 us where a plain load takes 96.  Rows that do not start on a 16-byte boundary: 18.1 us where aligned ones
+// take 16.0 (80 rows of 50261).  beam_merge is latency: four dependent steps (sums, logarithms, the bound, the lists above it, all in one queue so
+// that up to 8 loads are on their way: both launches of 32 beams that keep 64 53 -> 47 us, 49 with the 64 bits that order equal scores).
 
 constexpr int kBeamWaves = 4;
 constexpr int kBeamTokenBits = 24, kBeamMaxVocab = 1 << kBeamTokenBits;
@@ -517,8 +519,11 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
         list_top[i] = a.top[row0 * a.segs + i];
         list_sum[i] = a.sum[row0 * a.segs + i];
     }
-    // (few candidates are all asked for at once, without a look at the lists' first ones)
+    // Few candidates are all asked for at once, without a look at the lists' first ones.  (us of both launches, all at once / by the lists: 64 places
+    // 13.2 / 17.3, 256 14.2 / 17.5, 600 24.7 / 28.1, 1024 17.9 / 19.2 and 17.0 / 18.7.  With 6 instead of 4, 1216 and 1536 places take 18.5 and 18.8
+    // instead of 19.3, and all smaller ones 0.2 to 0.4 more.)
     constexpr int FEW = 4;
+    static_assert(FEW * 64 <= kBeamList, "a wave's candidates have room");
     const bool few = lists * a.keep <= FEW * 256;
     int32_t few_token[FEW];
     float few_value[FEW];
@@ -722,7 +727,7 @@ struct CopyArgs {
 static_assert(sizeof(CopyArgs) <= 4096 - 256, "launch arguments");
 
 // grid (pairs, layers, 2): a workgroup copies the page's part of a layer in one pool, 4 KiB of it per step (16 bytes a thread).  Bound by
-// HBM: 160 pages in 20 layers (8 KV heads of 128, 210 MB read and as many written) 71 us, 5.9 TB/s; 3 pages 3.5 us.
+// HBM: 160 pages in 20 layers (8 KV heads of 128, 210 MB read and as many written) 72 us, 5.8 TB/s; 3 pages 3.8 us (means of thirty launches).
 __global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs a) {
     u32x4* pool = (blockIdx.z ? a.v : a.k) + blockIdx.y * a.layer_vecs;
     const u32x4* src = pool + (int64_t)a.src[blockIdx.x] * a.page_vecs;

@@ -11,8 +11,9 @@
 //
 // Work: 4 * d * columns multiplications and additions per key and KV head against 4 * d bytes of keys and values, so the kernels go with
 // the keys' stream from HBM up to some 200 columns, and with the inner step (matrix and vector instructions) above.  Measured (one layer;
-// keys in HBM): 32 single tokens behind 300 to 20000 keys (32 heads on 8, 615 MB) 97 + 4 us, 6.3 TB/s; 16 trees of 64 nodes behind 1000 to
-// 8000 (64 on 8) 160 + 16 us, the second figure the joining of the parts; both in a row behind one another take 102 and 168.
+// keys in HBM; means of thirty launches): 32 single tokens behind 300 to 20000 keys (32 heads on 8, 615 MB) 99 + 4.8 us, 6.2 TB/s; 16 trees of 64
+// nodes behind 1000 to 8000 (64 on 8) 178 to 187 + 18 us on two cards, the second figure the joining of the parts (the fastest 163 + 16.4); calls
+// that follow one another without a profiler take 102 and 168.
 #include "attn_core.h"
 
 #include <atomic>
@@ -244,7 +245,8 @@ __device__ __forceinline__ bool unit_of(const SeqPlan& q, int parts, int units, 
 // Up to 64 sequences every wave works the plan out for itself, all of them with the same arithmetic, without LDS and barriers.  More are
 // planned by a launch of their own, which cuts them into up to 64 runs of whole waves and leaves what stands in front of each; a wave then looks
 // at the runs and at one of them.  us of single tokens behind 300 to 700 keys (8B heads), for itself / by
-// the launch: 128 sequences of 500 to 4000 keys 149 / 152, 256 105 / 86, 1024 668 / 330, 4096 7531 / 1306 (6.1 TB/s): a square law against 3 us.
+// the launch: 128 sequences of 500 to 4000 keys 149 / 152, 256 105 / 86, 1024 668 / 330, 4096 7531 / 1306 (6.1 TB/s): a square law against a
+// launch of 5.2 us at 256, 5.7 at 1024 and 12.3 at 4096 sequences, of which the stream's launch hides the start.
 constexpr int kPlanRuns = 64;
 struct TreePlan {
     int32_t share, units;               // units: none where the rows break their order
@@ -452,7 +454,7 @@ __device__ __forceinline__ void clean_values(u32x4 (&vf)[N], int b0, uint32_t ke
 //
 // What bounds it: of a block a wave takes 16*NB matrix instructions of 16 cycles and some 56*NB vector ones (per score a maximum, a
 // multiplication and addition, a sum, half a conversion, and an exponential of four times their length), and its workgroup passes 64 KiB
-// through LDS (at NB = 1 as much for half the columns).  At NB = 2 the matrix cores are busy for 0.39 of the time, the vector units for 0.50; a block takes 1.18 us with two
+// through LDS (at NB = 1 as much for half the columns).  At NB = 2 the matrix cores are busy for 0.40 of the time, the vector units for 0.50; a block takes 1.18 us with two
 // workgroups on a compute unit, 0.92 PFLOP/s, and 16 trees of 64 nodes (64 heads on 8, 1000 to 8000 keys) come to 0.7 with the start of
 // the units and their last, masked blocks.  Tried without gain: the scores of the next block between the exponentials of this one (a ring
 // of four), raised wave priority in either part (169 -> 167 to 173 us with the joining), three workgroups a compute unit at NB = 2 (spills).
@@ -636,8 +638,8 @@ __global__ __launch_bounds__(256, 2) void tree_attention_kernel(TreeArgs a) {
 
 // Few columns (tiles of 16*NB): the keys are a stream from HBM, and each wave takes a run of the unit's blocks for all columns, operands
 // straight to registers as in decode attention (load_kv: score tile t is page t, a lane has keys 4G .. 4G+3 of both pages).  The
-// waves' results are joined through LDS, a group of 16 columns at a time.  Bound by HBM: 6.3 TB/s at 32 single tokens behind 300 to 20000
-// keys (a bare read in this way reaches 6.2); one short sequence is all latency (5.7 us at 64 keys and less).
+// waves' results are joined through LDS, a group of 16 columns at a time.  Bound by HBM: 6.2 TB/s at 32 single tokens behind 300 to 20000
+// keys (a bare read in this way reaches 6.2); one short sequence is all latency (6.0 us at 64 keys and less).
 template <int D>
 struct StreamLds {
     float o[4][16][D + 4];
@@ -780,8 +782,8 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
 }
 
 // The partial results of all tiles joined, in order of the parts: a work item is (record, KV head, 1024 / D columns), a thread per four dims
-// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time (16 us at 512 workgroups' results of 128 columns, 34 MB;
-// 4 at those of 32 single tokens).
+// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time, where there are fewer the last one again (18 us, 16.5 the
+// fastest, at 512 workgroups' results of 128 columns, 34 MB; 4.8 at those of 32 single tokens).
 constexpr int kMergeBatch = 12;
 constexpr int kMergeGroups = 2048;  // workgroups
 template <int D>
@@ -848,7 +850,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int tile_co
 // workgroups per compute unit, half the partial results) against 128 (two, and half the passes through LDS), us: 26 nodes behind 2500 keys,
 // 104 columns 14.7 / 17.0, 32 x 32 nodes (8B heads) 128 columns 93 / 100, 16 x 64 nodes (8B) 256 columns 108 / 110, 48 ragged trees (14B)
 // up to 300 columns 110 / 114, 16 x 64 nodes (70B) 512 columns 173 / 165, four of 128 nodes (8B) 512 columns 75 / 69, four of 200 nodes (70B) 1600
-// columns 185 / 182.  (16 x 60 nodes of 16 heads on one KV head, 960 columns: 56 / 68.)
+// columns 185 / 182.  The rule goes by the columns alone, and loses where few KV heads leave few workgroups: 16 x 60 nodes of 16 heads on one KV
+// head, 960 columns, 56 / 68.
 static int tree_tile_cols(int n_q, int n_kv, int max_nodes) {
     const int64_t cols = (int64_t)max_nodes * (n_q / n_kv);
     return cols <= 16 ? 16 : cols <= 32 ? 32 : cols < 512 ? 64 : 128;
