@@ -154,8 +154,8 @@ def _stream_ptr(stream) -> Optional[int]:
 
 def _int32_of(x, what: str):
     """x as int32 numbers on the host; one that is no whole number of 32 bits is refused, not cut to one."""
-    given = np.asarray(x)
     try:
+        given = np.asarray(x)
         with np.errstate(invalid="ignore"):
             a = np.ascontiguousarray(given, dtype=np.int32)
         fits = a is given or given.size == 0 or (given.dtype.kind in "iufO" and bool((a == given).all()))

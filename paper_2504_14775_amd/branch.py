@@ -181,7 +181,10 @@ def _page_ids(call: str, ids):
             return *a.buffer_info(), a
         except (TypeError, OverflowError):
             pass
-    given = np.asarray(ids)
+    try:
+        given = np.asarray(ids)
+    except (TypeError, ValueError):
+        _refuse(f"{call}: page ids are whole numbers on the host, got {type(ids).__name__}")
     if given.dtype.kind in "iu":
         a = np.ascontiguousarray(given, dtype=np.int32)
         if a is not given and not (a == given).all():

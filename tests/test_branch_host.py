@@ -190,3 +190,11 @@ def test_pools_without_a_head_dimension_are_refused():
                                     dict(layers=1 << 15, n_kv=1 << 10, seqs=1 << 6)], ids=str)
 def test_tree_commit_refuses_more_moves_than_a_launch_has_places(change):
     assert BR._lib().gllm_op_tree_commit(*{**COMMIT, **change}.values()) == CAPACITY
+
+
+@pytest.mark.parametrize("ids", [[[1], [1, 2]], torch.zeros(2, device="meta", dtype=torch.int32)], ids=["ragged", "meta"])
+def test_page_ids_that_are_no_array_of_the_host_are_refused(ids):
+    k, v = torch.zeros(2, 3, 2, 8, 16, 8, dtype=torch.bfloat16), torch.zeros(2, 3, 2, 64, 16, dtype=torch.bfloat16)
+    with pytest.raises(B.GllmError) as e:
+        BR.gllm_op_copy_pages(k, v, ids, [1])
+    assert e.value.status == INVALID and "page ids" in e.value.message
