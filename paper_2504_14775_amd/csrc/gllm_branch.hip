@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 // with one pass on its way while the last one is worked on: at 128 rows it takes 30 us, without exponentials and without lists behind the first
 // pass 16.  Reading past the caches takes 94 us where a plain load takes 96.  Rows that do not start on a 16-byte boundary: 18.1 us where aligned ones
 // take 16.0 (80 rows of 50261).  beam_merge is latency: four dependent steps (sums, logarithms, the bound, the lists above it, all in one queue so
-// that up to 8 loads are on their way: both launches of 32 beams that keep 64 53 -> 47 us, 49 with the 64 bits that order equal scores).
+// that up to 8 loads are on their way: both launches of 32 beams that keep 64 53 -> 47 us).
 
 constexpr int kBeamWaves = 4;
 constexpr int kBeamTokenBits = 24, kBeamMaxVocab = 1 << kBeamTokenBits;
@@ -678,16 +678,20 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamArgs a) {
     }
     list.keep_best(a.keep);
     wave_fence();
-    // the place of each of the at most 64 is the number of those in front of it
+    // the place of each of the at most 64 is the number of those in front of it (the index is looked at where keys are equal only)
     const bool there = lane < list.n;
     const uint64_t k = there ? list.key[lane] : 0ull;
     const uint64_t i = there ? list.idx[lane] : 0ull;
     auto of_lane = [](uint64_t x, int l) { return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l); };
     int rank = 0;
+    bool ties = false;
     for (int j = 0; j < list.n; ++j) {
         const uint64_t kj = of_lane(k, j);
-        rank += kj > k || (kj == k && of_lane(i, j) < i);
+        rank += kj > k;
+        ties |= kj == k && j != lane;
     }
+    if (__any(there && ties))
+        for (int j = 0; j < list.n; ++j) rank += of_lane(k, j) == k && of_lane(i, j) < i;
     const int64_t out = (int64_t)s * a.keep;
     if (there) {
         const uint64_t bits = k >> 63 ? k ^ (1ull << 63) : ~k;
