@@ -154,11 +154,11 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 // The order among beams hangs on the sums: they and the scores are held in 64 bits, so that the order is that of exact
 // arithmetic but where scores of two beams agree to some 1e-10; in a beam it is that of the logits.
 //
-// Measured (64 sequences of 8 beams over a vocabulary of 152064, keep 16: 311 MB): 91 + 8.5 us, means of thirty launches (87.5 + 8 the fastest), of
+// Measured (64 sequences of 8 beams over a vocabulary of 152064, keep 16: 311 MB): 91 + 8.1 us, means of thirty launches (88 + 7.6 the fastest), of
 // which HBM would take 50.  What bounds beam_rows are vector instructions and their latency, 27 a logit, 12 of them in 64 bits (the exponential),
 // with one pass on its way while the last one is worked on: at 128 rows it takes 30 us, without exponentials and without lists behind the first
-// pass 16.  Reading past the caches takes 94 us where a plain load takes 96.  Rows that do not start on a 16-byte boundary: 18.1 us where aligned ones
-// take 16.0 (80 rows of 50261).  beam_merge is latency: four dependent steps (sums, logarithms, the bound, the lists above it, all in one queue so
+// pass 16.  Reading past the caches takes 94 us where a plain load takes 96.  Rows that do not start on a 16-byte boundary: 18.3 us where aligned ones
+// take 16.6 (80 rows of 50261).  beam_merge is latency: four dependent steps (sums, logarithms, the bound, the lists above it, all in one queue so
 // that up to 8 loads are on their way: both launches of 32 beams that keep 64 53 -> 47 us).
 
 constexpr int kBeamWaves = 4;

@@ -12,7 +12,7 @@
 // Work: 4 * d * columns multiplications and additions per key and KV head against 4 * d bytes of keys and values, so the kernels go with
 // the keys' stream from HBM up to some 200 columns, and with the inner step (matrix and vector instructions) above.  Measured (one layer;
 // keys in HBM; means of thirty launches): 32 single tokens behind 300 to 20000 keys (32 heads on 8, 615 MB) 99 + 4.8 us, 6.2 TB/s; 16 trees of 64
-// nodes behind 1000 to 8000 (64 on 8) 178 to 187 + 18 us on two cards, the second figure the joining of the parts (the fastest 163 + 16.4); calls
+// nodes behind 1000 to 8000 (64 on 8) 178 to 187 + 18.5 us on three cards, the second figure the joining of the parts (the fastest 163 + 16.4); calls
 // that follow one another without a profiler take 102 and 168.
 #include "attn_core.h"
 
@@ -246,7 +246,7 @@ __device__ __forceinline__ bool unit_of(const SeqPlan& q, int parts, int units, 
 // planned by a launch of their own, which cuts them into up to 64 runs of whole waves and leaves what stands in front of each; a wave then looks
 // at the runs and at one of them.  us of single tokens behind 300 to 700 keys (8B heads), for itself / by
 // the launch: 128 sequences of 500 to 4000 keys 149 / 152, 256 105 / 86, 1024 668 / 330, 4096 7531 / 1306 (6.1 TB/s): a square law against a
-// launch of 5.2 us at 256, 5.7 at 1024 and 12.3 at 4096 sequences, of which the stream's launch hides the start.
+// launch of 5.4 us at 256, 5.7 at 1024 and 12.3 at 4096 sequences, of which the stream's launch hides the start.
 constexpr int kPlanRuns = 64;
 struct TreePlan {
     int32_t share, units;               // units: none where the rows break their order
@@ -782,7 +782,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeA
 }
 
 // The partial results of all tiles joined, in order of the parts: a work item is (record, KV head, 1024 / D columns), a thread per four dims
-// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time, where there are fewer the last one again (18 us, 16.5 the
+// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time, where there are fewer the last one again (18.5 us, 16.5 the
 // fastest, at 512 workgroups' results of 128 columns, 34 MB; 4.8 at those of 32 single tokens).
 constexpr int kMergeBatch = 12;
 constexpr int kMergeGroups = 2048;  // workgroups
