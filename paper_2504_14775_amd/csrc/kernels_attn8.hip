@@ -315,6 +315,14 @@ __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d
 
 // ---- common to both kinds of units -------------------------------------------------------------------------------------
 
+// A barrier that waits for this wave's reads and writes of LDS only: __syncthreads() would wait for the loads into the ring too.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Says in which half of the register file a value stands at this point: that of the matrix instructions' accumulators, or the other, where the
+// vector instructions read.
+__device__ __forceinline__ void in_accumulators(f32x16& x) { asm("" : "+a"(x)); }
+__device__ __forceinline__ void in_vectors(f32x16& x) { asm("" : "+v"(x)); }
+
 // Four codes as bf16, without rounding.
 __device__ __forceinline__ u32x2 widen(uint32_t codes) {
     return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false)),
@@ -441,8 +449,8 @@ __device__ __forceinline__ void stream_unit(const Attn8Args& a, const Unit& it, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int key = key0 + G * kPage + 4 * t + i;
-                    if (bad[t] >> (8 * i + 7) & 1) s[t][i] = NAN;
-                    if (key > pos || (key <= low && key >= a.sinks)) s[t][i] = -INFINITY;
+                    const bool hidden = (key > pos) | ((key <= low) & (key >= a.sinks));
+                    s[t][i] = hidden ? -INFINITY : bad[t] >> (8 * i + 7) & 1 ? NAN : s[t][i];
                 }
         }
         float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
@@ -665,6 +673,8 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
 #pragma unroll
                 for (int c = 0; c < CG; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c][k], s[c], 0, 0, 0);
             }
+#pragma unroll
+            for (int c = 0; c < CG; ++c) in_vectors(s[c]);
         };
         float factor = 0.f, log_values = 0.f, per_value = 0.f;  // of the page of this lane's keys in the step to come
         // Masks, and the references that step i needs.
@@ -683,8 +693,8 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const int key = key0 + h * kPage + v;
-                        if (bad >> v & 1) s[c][v] = NAN;
-                        if (key > pos[c] || (key <= low[c] && key >= a.sinks)) s[c][v] = -INFINITY;
+                        const bool hidden = (key > pos[c]) | ((key <= low[c]) & (key >= a.sinks));
+                        s[c][v] = hidden ? -INFINITY : bad >> v & 1 ? NAN : s[c][v];
                     }
             }
             float top[CG];
@@ -704,9 +714,12 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                     m[c] = up;
                     l[c] *= down;
 #pragma unroll
-                    for (int t = 0; t < D / 32; ++t)
+                    for (int t = 0; t < D / 32; ++t) {
+                        in_accumulators(o[c][t]);  // (or they are copied in front of the branch in every round)
 #pragma unroll
                         for (int v = 0; v < 16; ++v) o[c][t][v] *= down;
+                        in_accumulators(o[c][t]);
+                    }
                 }
             }
         };
@@ -748,7 +761,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 3) * LOADS) : "memory");
         convert(0);
         convert(1);
-        __syncthreads();
+        lds_barrier();
         f32x16 s[CG];
         scores(0, s);
         settle(0, s);
@@ -766,7 +779,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             }
             convert(i + 2);
             if (threadIdx.x == 0) lds.bad[(i + 3) % 4] = 0u;
-            __syncthreads();
+            lds_barrier();
             if (!idle && i + 1 < steps) {
                 settle(i + 1, next);
 #pragma unroll
