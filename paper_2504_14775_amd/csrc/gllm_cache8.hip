@@ -20,13 +20,18 @@ constexpr int kMapsThreads = 256, kMapsPer = 4, kMapsTile = kMapsThreads * kMaps
 constexpr int kMapsGroups = 256;                                                      // workgroups at most
 
 // Sums over a wave by lane shifts: x of a lane becomes that of it and the lanes in front.
-__device__ __forceinline__ int64_t scan_wave64(int64_t x) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) {
-        const int64_t y = __shfl_up(x, by);
-        if (lane >= by) x += y;
-    }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(int64_t& x) {
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false);
+    x += (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+}
+__device__ __forceinline__ int64_t scan_wave(int64_t x) {
+    scan_step<0x111, 0xf>(x);  // by 1, 2, 4 and 8 lanes in a row of 16
+    scan_step<0x112, 0xf>(x);
+    scan_step<0x114, 0xf>(x);
+    scan_step<0x118, 0xf>(x);
+    scan_step<0x142, 0xa>(x);  // the last lane of a row to the next row, of both to the upper half
+    scan_step<0x143, 0xc>(x);
     return x;
 }
 
@@ -43,6 +48,12 @@ __global__ __launch_bounds__(kMapsThreads) void step_maps_kernel(MapsArgs a) {
     if (t == 0) fit = 0;
     if (t == 0 && blockIdx.x == 0) a.row_start[0] = 0;
     const int64_t most = min((int64_t)a.table_stride * kPage, (int64_t)kMaxPositions);
+    // the runs of 256 rows are dealt to the workgroups in turn: this thread's row of the first run of its own that reaches behind row r0
+    const int64_t step = (int64_t)gridDim.x * kMapsThreads;
+    auto my_row = [&](int r0) {
+        const uint32_t run = (uint32_t)r0 / kMapsThreads, turn = run % gridDim.x;
+        return (int64_t)(run - turn + blockIdx.x + (blockIdx.x < turn ? gridDim.x : 0)) * kMapsThreads + t;
+    };
     for (int s0 = 0; s0 < a.num_seqs; s0 += kMapsTile) {
         int32_t n[kMapsPer], c[kMapsPer], need[kMapsPer];
         int64_t rows = 0, pages = 0;
@@ -60,7 +71,7 @@ __global__ __launch_bounds__(kMapsThreads) void step_maps_kernel(MapsArgs a) {
             rows += n[i];
             pages += need[i];
         }
-        const int64_t rows_upto = scan_wave64(rows), pages_upto = scan_wave64(pages);
+        const int64_t rows_upto = scan_wave(rows), pages_upto = scan_wave(pages);
         if (lane == 63) {
             wave_rows[wave] = rows_upto;
             wave_pages[wave] = pages_upto;
@@ -98,9 +109,8 @@ __global__ __launch_bounds__(kMapsThreads) void step_maps_kernel(MapsArgs a) {
             if (s < a.num_seqs && (s0 / kMapsTile) % gridDim.x == blockIdx.x) a.row_start[s + 1] = e;
         }
         __syncthreads();
-        for (int64_t r0 = (int64_t)(first / kMapsThreads) * kMapsThreads; r0 < all; r0 += kMapsThreads) {
-            const int64_t r = r0 + t;
-            if ((r0 / kMapsThreads) % gridDim.x != blockIdx.x || r < first || r >= all) continue;
+        for (int64_t r = my_row(first); r < all; r += step) {
+            if (r < first) continue;
             int lo = 0, hi = kMapsTile;  // the sequence with start[lo] <= r < start[lo + 1]: the last one that starts at r or in front
             while (hi - lo > 1) {
                 const int mid = (lo + hi) / 2;
@@ -132,9 +142,8 @@ __global__ __launch_bounds__(kMapsThreads) void step_maps_kernel(MapsArgs a) {
         a.needed[0] = (int32_t)min(rows_before, (int64_t)INT32_MAX);
         a.needed[1] = (int32_t)min(pages_before, (int64_t)INT32_MAX);
     }
-    for (int64_t r0 = (int64_t)(fit / kMapsThreads) * kMapsThreads; r0 < a.num_rows; r0 += kMapsThreads) {
-        const int64_t r = r0 + t;
-        if ((r0 / kMapsThreads) % gridDim.x != blockIdx.x || r < fit || r >= a.num_rows) continue;
+    for (int64_t r = my_row(fit); r < a.num_rows; r += step) {
+        if (r < fit) continue;
         a.positions[r] = 0;
         a.slots[r] = -1;
     }
@@ -236,136 +245,200 @@ __device__ __forceinline__ void norm_rotate(f32x4& lo, f32x4& hi, const bf16_t* 
     hi = b;
 }
 
-// A workgroup has a row: its query heads, and, where it is the first row of a page, the keys and values of all rows of the page; a wave takes a page's keys (or values) of one KV head, so that their largest magnitude needs no more than a wave.
+// A wave has kQueryPasses passes over query heads of a row, all asked for at one time, or the keys, or the values, of one KV head of the pages whose first rows are among
+// `per` rows: a page's largest magnitude then needs no more than a wave, and there is one pass over the projection.
+constexpr int kQueryPasses = 4;
+
+// The rows of a page and their slots in it, in order of the rows.
+struct PageRows {
+    const u32x2* run;  // LDS
+    int n, first;      // first: the lowest slot
+    bool whole;        // all slots, in order
+    __device__ __forceinline__ int row(int t) const { return (int)run[t][0]; }
+    __device__ __forceinline__ int slot(int t) const { return (int)run[t][1]; }
+};
+
 template <int D, typename T>
-__global__ __launch_bounds__(256) void norm_rope_store8_kernel(Store8Args a) {
-    constexpr int LANES = D / 8, PER = 64 / LANES;  // lanes of a head, heads (or tokens) of a wave
-    __shared__ u32x2 run[4][kPage];                 // rows and slots of a page
-    const int r = blockIdx.x, lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ void store_queries(const Store8Args& a, int r, int part) {
+    constexpr int LANES = D / 8, PER = 64 / LANES;  // lanes of a head, heads of a pass
+    const int lane = threadIdx.x & 63, sub = lane / LANES, e = lane % LANES * 4;
+    const T* x = static_cast<const T*>(a.qkv) + (int64_t)r * a.ld_qkv + e;
+    f32x4 lo[kQueryPasses], hi[kQueryPasses];
+    const int head0 = part * kQueryPasses * PER;
+#pragma unroll
+    for (int i = 0; i < kQueryPasses; ++i) {
+        if (head0 + i * PER >= a.n_q) break;
+        const T* at = x + (int64_t)min(head0 + i * PER + sub, a.n_q - 1) * D;
+        lo[i] = load4<T>(at);
+        hi[i] = load4<T>(at + D / 2);
+    }
     const int64_t slot = a.slots[r];
+    const float* rope = a.rope + (int64_t)min(max(a.positions[r], 0), a.max_position - 1) * D;
     if (slot < 0 || slot >= a.num_slots) return;
-    const T* qkv = static_cast<const T*>(a.qkv);
-    const int sub = lane / LANES, e = lane % LANES * 4;
-    auto rope_of = [&](int row) { return a.rope + (int64_t)min(max(a.positions[row], 0), a.max_position - 1) * D; };
-    const int q_tasks = (a.n_q + PER - 1) / PER;
-    for (int task = wave; task < q_tasks; task += 4) {
-        const int h = task * PER + sub, hh = min(h, a.n_q - 1);
-        const T* x = qkv + (int64_t)r * a.ld_qkv + (int64_t)hh * D + e;
-        f32x4 lo = load4<T>(x), hi = load4<T>(x + D / 2);
-        norm_rotate<D>(lo, hi, a.q_gain, a.eps, rope_of(r), e);
+#pragma unroll
+    for (int i = 0; i < kQueryPasses; ++i) {
+        if (head0 + i * PER >= a.n_q) break;
+        norm_rotate<D>(lo[i], hi[i], a.q_gain, a.eps, rope, e);
+        const int h = head0 + i * PER + sub;
         if (h < a.n_q) {
             bf16_t* o = a.q_out + (int64_t)r * a.ld_q + (int64_t)h * D + e;
-            *reinterpret_cast<bf16x4*>(o) = __builtin_convertvector(lo, bf16x4);
-            *reinterpret_cast<bf16x4*>(o + D / 2) = __builtin_convertvector(hi, bf16x4);
+            *reinterpret_cast<bf16x4*>(o) = __builtin_convertvector(lo[i], bf16x4);
+            *reinterpret_cast<bf16x4*>(o + D / 2) = __builtin_convertvector(hi[i], bf16x4);
         }
     }
-    // the rows of the page: lane 15 is this row, lanes 15 .. 30 those of the page that this workgroup stores, if none in front is one
-    const int at = r - (kPage - 1) + lane;
-    const int64_t other = lane < 2 * kPage - 1 && at >= 0 && at < a.num_rows ? a.slots[at] : -1;
-    const uint64_t same = __ballot(other >= 0 && other / kPage == slot / kPage);
-    if (same & ((1ull << (kPage - 1)) - 1)) return;
-    const int n = __popcll(same);
-    if (same >> lane & 1) run[wave][__popcll(same & ((1ull << lane) - 1))] = u32x2{(uint32_t)at, (uint32_t)(other % kPage)};
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    int first = same >> lane & 1 ? (int)(other % kPage) : kPage;  // the lowest slot
+}
+
+template <int D, typename T>
+__device__ __forceinline__ void store_keys(const Store8Args& a, const PageRows& p, int64_t page, int h) {
+    constexpr int LANES = D / 8, PER = 64 / LANES, IT = kPage / PER;  // lanes of a head, tokens of a pass, passes
+    const int lane = threadIdx.x & 63, sub = lane / LANES, e = lane % LANES * 4;
+    float* scale_at = a.scales + (page * a.n_kv + h) * 2;
+    const float old = p.first > 0 ? *scale_at : 0.f;
+    f32x4 lo[IT], hi[IT];
+    int pos[IT];
 #pragma unroll
-    for (int by = 1; by < 64; by *= 2) first = min(first, __shfl_xor(first, by));
-    const bool whole = n == kPage && __all(!(same >> lane & 1) || other % kPage == lane - (kPage - 1));  // all slots, in order
-    auto row_of = [&](int t) { return (int)run[wave][t][0]; };
-    auto slot_of = [&](int t) { return (int)run[wave][t][1]; };
-    const int64_t page = slot / kPage;
-    for (int task = wave; task < 2 * a.n_kv; task += 4) {
-        const int h = task >> 1;
-        float* scale_at = a.scales + (page * a.n_kv + h) * 2 + (task & 1);
-        const float old = first > 0 ? *scale_at : 0.f;
-        int halvings;
-        if (task % 2 == 0) {
-            constexpr int IT = kPage / PER;
-            f32x4 lo[IT], hi[IT];
-            float m = 0.f;
+    for (int i = 0; i < IT; ++i) {
+        if (i * PER >= p.n) break;
+        const int row = p.row(min(i * PER + sub, p.n - 1));  // (lanes past the page's rows repeat the last one)
+        const T* x = static_cast<const T*>(a.qkv) + (int64_t)row * a.ld_qkv + (int64_t)(a.n_q + h) * D + e;
+        lo[i] = load4<T>(x);
+        hi[i] = load4<T>(x + D / 2);
+        pos[i] = a.positions[row];
+    }
+    float m = 0.f;
 #pragma unroll
-            for (int i = 0; i < IT; ++i) {
-                const int t = min(i * PER + sub, n - 1);  // (lanes past the page's rows repeat the last one)
-                const T* x = qkv + (int64_t)row_of(t) * a.ld_qkv + (int64_t)(a.n_q + h) * D + e;
-                lo[i] = load4<T>(x);
-                hi[i] = load4<T>(x + D / 2);
-            }
+    for (int i = 0; i < IT; ++i) {
+        if (i * PER >= p.n) break;
+        norm_rotate<D>(lo[i], hi[i], a.k_gain, a.eps, a.rope + (int64_t)min(max(pos[i], 0), a.max_position - 1) * D, e);
 #pragma unroll
-            for (int i = 0; i < IT; ++i) {
-                norm_rotate<D>(lo[i], hi[i], a.k_gain, a.eps, rope_of(row_of(min(i * PER + sub, n - 1))), e);
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, fmaxf(finite_abs(lo[i][v]), finite_abs(hi[i][v])));
+    }
+    int halvings;
+    const float scale = page_scale(max_wave(m), p.first == 0, old, halvings), inv = 1.0f / scale;
+    uint8_t* base = a.k_pool + (page * a.n_kv + h) * (D * kPage);
+    if (halvings > 0) {
+        const float by = __builtin_ldexpf(1.0f, -halvings);
+        for (int x = lane; x < D; x += 64) {  // 16-byte pieces: 16 dims of one slot
+            if (x / (D / 4) * 4 + x % 4 >= p.first) continue;
+            u32x4* at = reinterpret_cast<u32x4*>(base + x * 16);
+            u32x4 c = *at;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) m = fmaxf(m, fmaxf(finite_abs(lo[i][v]), finite_abs(hi[i][v])));
-            }
-            const float scale = page_scale(max_wave(m), first == 0, old, halvings), inv = 1.0f / scale;
-            uint8_t* base = a.k_pool + (page * a.n_kv + h) * (D * kPage);
-            if (halvings > 0) {
-                const float by = __builtin_ldexpf(1.0f, -halvings);
-                for (int p = lane; p < D; p += 64) {  // 16-byte pieces: 16 dims of one slot
-                    if (p / (D / 4) * 4 + p % 4 >= first) continue;
-                    u32x4* at = reinterpret_cast<u32x4*>(base + p * 16);
-                    u32x4 c = *at;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) c[v] = scaled_codes(c[v], by);
-                    *at = c;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < IT; ++i) {
-                const int t = i * PER + sub;
-                if (t >= n) continue;
-                const int s = slot_of(t);
-                uint8_t* at = base + s / 4 * (4 * D) + s % 4 * 16 + e % 16;
-                *reinterpret_cast<uint32_t*>(at + e / 16 * 64) = codes4(lo[i], scale, inv);
-                *reinterpret_cast<uint32_t*>(at + (e + D / 2) / 16 * 64) = codes4(hi[i], scale, inv);
-            }
-            if (lane == 0) *scale_at = scale;
-        } else {
-            constexpr int DIMS = D / 64;  // of a lane, next to each other
-            float x[kPage][DIMS], m = 0.f;
-#pragma unroll
-            for (int t = 0; t < kPage; ++t)
-#pragma unroll
-                for (int j = 0; j < DIMS; ++j) x[t][j] = t < n ? (float)qkv[(int64_t)row_of(t) * a.ld_qkv + (int64_t)(a.n_q + a.n_kv + h) * D + lane * DIMS + j] : 0.f;
-#pragma unroll
-            for (int t = 0; t < kPage; ++t)
-#pragma unroll
-                for (int j = 0; j < DIMS; ++j) m = fmaxf(m, finite_abs(x[t][j]));
-            const float scale = page_scale(max_wave(m), first == 0, old, halvings), inv = 1.0f / scale;
-            uint8_t* base = a.v_pool + (page * a.n_kv + h) * (D * kPage) + lane * DIMS * kPage;
-            const float by = __builtin_ldexpf(1.0f, -halvings);
-#pragma unroll
-            for (int j = 0; j < DIMS; ++j) {
-                u32x4* at = reinterpret_cast<u32x4*>(base + j * kPage);
-                u32x4 c;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) c[v] = codes4(f32x4{x[4 * v][j], x[4 * v + 1][j], x[4 * v + 2][j], x[4 * v + 3][j]}, scale, inv);
-                if (whole) {
-                    *at = c;
-                    continue;
-                }
-                // the bytes of the slots written are new, those in front of the first are kept, the others stay
-                u32x4 was = *at;
-                uint8_t* b = reinterpret_cast<uint8_t*>(at);
-                if (halvings > 0) {
-                    u32x4 kept;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        kept[v] = scaled_codes(was[v], by);
-                        const int mine = min(max(first - 4 * v, 0), 4);
-                        const uint32_t mask = mine == 4 ? 0xFFFFFFFFu : (1u << (8 * mine)) - 1u;
-                        was[v] = (was[v] & ~mask) | (kept[v] & mask);
-                    }
-                    *at = was;
-                }
-#pragma unroll
-                for (int t = 0; t < kPage; ++t)
-                    if (t < n) b[slot_of(t)] = (uint8_t)(c[t / 4] >> (8 * (t % 4)));
-            }
-            if (lane == 0) *scale_at = scale;
+            for (int v = 0; v < 4; ++v) c[v] = scaled_codes(c[v], by);
+            *at = c;
         }
+    }
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        const int t = i * PER + sub;
+        if (t >= p.n) continue;
+        const int s = p.slot(t);
+        uint8_t* at = base + s / 4 * (4 * D) + s % 4 * 16 + e % 16;
+        *reinterpret_cast<uint32_t*>(at + e / 16 * 64) = codes4(lo[i], scale, inv);
+        *reinterpret_cast<uint32_t*>(at + (e + D / 2) / 16 * 64) = codes4(hi[i], scale, inv);
+    }
+    if (lane == 0) *scale_at = scale;
+}
+
+template <int D, typename T>
+__device__ __forceinline__ void store_values(const Store8Args& a, const PageRows& p, int64_t page, int h) {
+    constexpr int DIMS = D / 64;  // of a lane, next to each other
+    typedef T pair_t __attribute__((ext_vector_type(DIMS)));
+    const int lane = threadIdx.x & 63;
+    float* scale_at = a.scales + (page * a.n_kv + h) * 2 + 1;
+    const float old = p.first > 0 ? *scale_at : 0.f;
+    float x[kPage][DIMS], m = 0.f;
+#pragma unroll
+    for (int t = 0; t < kPage; ++t) {
+#pragma unroll
+        for (int j = 0; j < DIMS; ++j) x[t][j] = 0.f;
+        if (t >= p.n) continue;
+        const T* at = static_cast<const T*>(a.qkv) + (int64_t)p.row(t) * a.ld_qkv + (int64_t)(a.n_q + a.n_kv + h) * D + lane * DIMS;
+        const pair_t y = *reinterpret_cast<const pair_t*>(at);
+#pragma unroll
+        for (int j = 0; j < DIMS; ++j) x[t][j] = (float)y[j];
+    }
+#pragma unroll
+    for (int t = 0; t < kPage; ++t)
+#pragma unroll
+        for (int j = 0; j < DIMS; ++j) m = fmaxf(m, finite_abs(x[t][j]));
+    int halvings;
+    const float scale = page_scale(max_wave(m), p.first == 0, old, halvings), inv = 1.0f / scale;
+    uint8_t* base = a.v_pool + (page * a.n_kv + h) * (D * kPage) + lane * DIMS * kPage;
+    const float by = __builtin_ldexpf(1.0f, -halvings);
+#pragma unroll
+    for (int j = 0; j < DIMS; ++j) {
+        u32x4* at = reinterpret_cast<u32x4*>(base + j * kPage);
+        u32x4 c;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) c[v] = codes4(f32x4{x[4 * v][j], x[4 * v + 1][j], x[4 * v + 2][j], x[4 * v + 3][j]}, scale, inv);
+        if (p.whole) {
+            *at = c;
+            continue;
+        }
+        if (halvings > 0) {  // the codes in front of the first slot are kept
+            u32x4 was = *at;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int mine = min(max(p.first - 4 * v, 0), 4);
+                const uint32_t mask = mine == 4 ? 0xFFFFFFFFu : (1u << (8 * mine)) - 1u;
+                was[v] = (was[v] & ~mask) | (scaled_codes(was[v], by) & mask);
+            }
+            *at = was;
+        }
+        uint8_t* b = reinterpret_cast<uint8_t*>(at);
+#pragma unroll
+        for (int t = 0; t < kPage; ++t)
+            if (t < p.n) b[p.slot(t)] = (uint8_t)(c[t / 4] >> (8 * (t % 4)));
+    }
+    if (lane == 0) *scale_at = scale;
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(256) void norm_rope_store8_kernel(Store8Args a, int query_groups, int query_parts, int per) {
+    __shared__ u32x2 runs[4][kPage];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x < query_groups) {
+        const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+        const int r = (int)(id / query_parts);
+        if (r < a.num_rows) store_queries<D, T>(a, r, (int)(id - (int64_t)r * query_parts));
+        return;
+    }
+    const int64_t id = (int64_t)((int)blockIdx.x - query_groups) * 4 + wave;
+    const int64_t block = id / (2 * a.n_kv), r0 = block * per;
+    const int task = (int)(id - block * (2 * a.n_kv));
+    if (r0 >= a.num_rows) return;
+    // lanes 15 .. 14 + per have the rows among which first ones are looked for, the 15 lanes on either side those that may be of the same page
+    const int64_t at = r0 - (kPage - 1) + lane;
+    int64_t slot = lane < per + 2 * (kPage - 1) && at >= 0 && at < a.num_rows ? a.slots[at] : -1;
+    if (slot >= a.num_slots) slot = -1;
+    const int page = slot < 0 ? -1 : (int)(slot / kPage);
+    const int above = __shfl_up(page, 1);
+    uint64_t firsts = __ballot(page >= 0 && page != above) & (((1ull << per) - 1) << (kPage - 1));
+    while (firsts) {
+        const int l = __builtin_ctzll(firsts);
+        firsts &= firsts - 1;
+        const int of = __builtin_amdgcn_readlane(page, l);
+        const uint64_t same = __ballot(page == of) & (((1ull << (2 * kPage - 1)) - 1) << (l - (kPage - 1)));
+        if (same & ((1ull << l) - 1)) continue;  // a row further up is of this page
+        const bool mine = same >> lane & 1;
+        PageRows p;
+        p.run = runs[wave];
+        p.n = __popcll(same);
+        const int s = (int)slot % kPage;
+        __builtin_amdgcn_wave_barrier();
+        if (mine) runs[wave][__popcll(same & ((1ull << lane) - 1))] = u32x2{(uint32_t)at, (uint32_t)s};
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        uint32_t held = 0u;  // the slots that are written
+        held = mine ? 1u << s : 0u;
+#pragma unroll
+        for (int by = 1; by < 64; by *= 2) held |= (uint32_t)__shfl_xor((int)held, by);
+        p.first = __builtin_ctz(held);
+        p.whole = p.n == kPage && __all(!mine || s == lane - l);
+        if (task % 2 == 0) store_keys<D, T>(a, p, of, task / 2);
+        else store_values<D, T>(a, p, of, task / 2);
     }
 }
 
@@ -415,11 +488,19 @@ gllm_status gllm_op_norm_rope_store8(const void* qkv, int64_t ld_qkv, int32_t ro
         return GLLM_E_INVALID;
     const Store8Args a{qkv, ld_qkv, (const bf16_t*)q_gain, (const bf16_t*)k_gain, (float)eps, rope, max_position, positions, slots, num_rows,
                        n_q_heads, n_kv_heads, (bf16_t*)q_out, ld_q, (uint8_t*)k_pool, (uint8_t*)v_pool, scales, num_blocks * kPage};
-    const dim3 grid((unsigned)num_rows);
-    if (head_dim == 128 && rows_type == GLLM_ROWS_F32) norm_rope_store8_kernel<128, float><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-    else if (head_dim == 128) norm_rope_store8_kernel<128, bf16_t><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-    else if (rows_type == GLLM_ROWS_F32) norm_rope_store8_kernel<64, float><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-    else norm_rope_store8_kernel<64, bf16_t><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+    // Few rows: a wave looks for a page at one row only, so that no wave does several after another; many, most of them of the same page as their
+    // neighbours: at 16, so that not most waves find none.
+    const int per = num_rows >= 4096 ? 16 : num_rows >= 1024 ? 4 : 1;
+    const int64_t parts = ceil_div(n_q_heads, kQueryPasses * (512 / head_dim));
+    const int64_t queries = ceil_div(num_rows * parts, 4), pages = ceil_div(ceil_div(num_rows, per) * 2 * n_kv_heads, 4);
+    if (queries + pages > INT32_MAX) return GLLM_E_CAPACITY;
+    const dim3 grid((unsigned)(queries + pages));
+#define GLLM_STORE8(D_, T_) norm_rope_store8_kernel<D_, T_><<<grid, 256, 0, (hipStream_t)stream>>>(a, (int)queries, (int)parts, per)
+    if (head_dim == 128 && rows_type == GLLM_ROWS_F32) GLLM_STORE8(128, float);
+    else if (head_dim == 128) GLLM_STORE8(128, bf16_t);
+    else if (rows_type == GLLM_ROWS_F32) GLLM_STORE8(64, float);
+    else GLLM_STORE8(64, bf16_t);
+#undef GLLM_STORE8
     return launched();
 }
 

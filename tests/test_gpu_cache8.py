@@ -232,6 +232,23 @@ def test_store_rows_left_out_strides_and_many_rows():
     Store((2, 1, 64), [(0, 16)] * 200, seed=5).check("whole pages")
 
 
+@pytest.mark.parametrize("pages", [10, 150, 520])
+def test_store_of_rows_in_any_order_within_their_page(pages):
+    """A page's rows in another order than their slots, with slots between them that nobody writes, and rows without slots between them.  Few rows, more
+    than 1024, more than 4096."""
+    print(f"store: rows in any order, {pages} pages", flush=True)
+    rng = np.random.default_rng(pages)
+    s = Store((2, 1, 64), [(0, int(rng.integers(5, 13))) for _ in range(pages)], seed=6)
+    at = 0
+    for p in range(pages):
+        n = int((s.slots[at:] // PAGE == s.slots[at] // PAGE).sum())
+        s.slots[at:at + n] = s.slots[at] // PAGE * PAGE + rng.permutation(PAGE)[:n]
+        if p % 3 == 0:
+            s.slots[at + n // 2] = -1
+        at += n
+    s.check("any order")
+
+
 @pytest.mark.parametrize("norm", [True, False])
 def test_store_takes_one_gain_without_the_other(norm):
     s = Store((4, 2, 128), RUNS, seed=6)
