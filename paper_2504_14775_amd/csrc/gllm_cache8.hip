@@ -245,8 +245,9 @@ __device__ __forceinline__ void norm_rotate(f32x4& lo, f32x4& hi, const bf16_t* 
     hi = b;
 }
 
-// A wave has kQueryPasses passes over query heads of a row, all asked for at one time, or the keys, or the values, of one KV head of the pages whose first rows are among
-// `per` rows: a page's largest magnitude then needs no more than a wave, and there is one pass over the projection.
+// A wave has kQueryPasses passes over query heads of a row, all asked for at one time, or the keys, or the values, of one KV head of the pages whose
+// first rows are among 16 rows: a page's largest magnitude then needs no more than a wave, and there is one pass over the projection.  The pages
+// among these that receive one row only (decode rows) are done together, D/8 lanes to each, the others one after another.
 constexpr int kQueryPasses = 4;
 
 // The rows of a page and their slots in it, in order of the rows.
@@ -339,6 +340,19 @@ __device__ __forceinline__ void store_keys(const Store8Args& a, const PageRows& 
     if (lane == 0) *scale_at = scale;
 }
 
+// The values of a dim in the slots in front of `first` times `by`.
+__device__ __forceinline__ void keep_scaled(void* values, int first, float by) {
+    u32x4* at = static_cast<u32x4*>(values);
+    u32x4 was = *at;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const int mine = min(max(first - 4 * v, 0), 4);
+        const uint32_t mask = mine == 4 ? 0xFFFFFFFFu : (1u << (8 * mine)) - 1u;
+        was[v] = (was[v] & ~mask) | (scaled_codes(was[v], by) & mask);
+    }
+    *at = was;
+}
+
 template <int D, typename T>
 __device__ __forceinline__ void store_values(const Store8Args& a, const PageRows& p, int64_t page, int h) {
     constexpr int DIMS = D / 64;  // of a lane, next to each other
@@ -375,16 +389,7 @@ __device__ __forceinline__ void store_values(const Store8Args& a, const PageRows
             *at = c;
             continue;
         }
-        if (halvings > 0) {  // the codes in front of the first slot are kept
-            u32x4 was = *at;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int mine = min(max(p.first - 4 * v, 0), 4);
-                const uint32_t mask = mine == 4 ? 0xFFFFFFFFu : (1u << (8 * mine)) - 1u;
-                was[v] = (was[v] & ~mask) | (scaled_codes(was[v], by) & mask);
-            }
-            *at = was;
-        }
+        if (halvings > 0) keep_scaled(at, p.first, by);
         uint8_t* b = reinterpret_cast<uint8_t*>(at);
 #pragma unroll
         for (int t = 0; t < kPage; ++t)
@@ -393,9 +398,71 @@ __device__ __forceinline__ void store_values(const Store8Args& a, const PageRows
     if (lane == 0) *scale_at = scale;
 }
 
+// Keys (or values) of a KV head for n rows that are the only ones of their pages; list: row and slot of each.
+template <int D, bool KEYS, typename T>
+__device__ __forceinline__ void store_singles(const Store8Args& a, const u32x2* list, int n, int h) {
+    constexpr int LANES = D / 8, PER = 64 / LANES, IT = kPage / PER;
+    const int lane = threadIdx.x & 63, sub = lane / LANES, e = lane % LANES * 4;
+    f32x4 lo[IT], hi[IT];
+    float old[IT];
+    int pos[IT], slot[IT];
+    uint8_t* const pool = KEYS ? a.k_pool : a.v_pool;
+    auto scale_of = [&](int i) { return a.scales + ((int64_t)(slot[i] / kPage) * a.n_kv + h) * 2 + (KEYS ? 0 : 1); };
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        if (i * PER >= n) break;
+        const u32x2 of = list[min(i * PER + sub, n - 1)];
+        const T* x = static_cast<const T*>(a.qkv) + (int64_t)of[0] * a.ld_qkv + (int64_t)(a.n_q + (KEYS ? 0 : a.n_kv) + h) * D + e;
+        lo[i] = load4<T>(x);
+        hi[i] = load4<T>(x + D / 2);
+        slot[i] = (int)of[1];
+        old[i] = *scale_of(i);
+        pos[i] = KEYS ? a.positions[of[0]] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        if (i * PER >= n) break;
+        if (KEYS) norm_rotate<D>(lo[i], hi[i], a.k_gain, a.eps, a.rope + (int64_t)min(max(pos[i], 0), a.max_position - 1) * D, e);
+        float m = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, fmaxf(finite_abs(lo[i][v]), finite_abs(hi[i][v])));
+#pragma unroll
+        for (int by = 1; by < LANES; by *= 2) m = fmaxf(m, __shfl_xor(m, by));
+        if (i * PER + sub >= n) continue;
+        const int first = slot[i] % kPage;
+        int halvings;
+        const float scale = page_scale(m, first == 0, old[i], halvings), inv = 1.0f / scale, by = __builtin_ldexpf(1.0f, -halvings);
+        uint8_t* base = pool + ((int64_t)(slot[i] / kPage) * a.n_kv + h) * (D * kPage);
+        const uint32_t cl = codes4(lo[i], scale, inv), ch = codes4(hi[i], scale, inv);
+        if (KEYS) {
+            if (halvings > 0) {
+                for (int x = lane % LANES; x < D; x += LANES) {  // 16-byte pieces: 16 dims of one slot
+                    if (x / (D / 4) * 4 + x % 4 >= first) continue;
+                    u32x4* at = reinterpret_cast<u32x4*>(base + x * 16);
+                    u32x4 c = *at;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) c[v] = scaled_codes(c[v], by);
+                    *at = c;
+                }
+            }
+            uint8_t* at = base + first / 4 * (4 * D) + first % 4 * 16 + e % 16;
+            *reinterpret_cast<uint32_t*>(at + e / 16 * 64) = cl;
+            *reinterpret_cast<uint32_t*>(at + (e + D / 2) / 16 * 64) = ch;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint8_t* at = base + (e + j % 4 + (j < 4 ? 0 : D / 2)) * kPage;
+                if (halvings > 0) keep_scaled(at, first, by);
+                at[first] = (uint8_t)((j < 4 ? cl : ch) >> (8 * (j % 4)));
+            }
+        }
+        if (lane % LANES == 0) *scale_of(i) = scale;
+    }
+}
+
 template <int D, typename T>
-__global__ __launch_bounds__(256) void norm_rope_store8_kernel(Store8Args a, int query_groups, int query_parts, int per) {
-    __shared__ u32x2 runs[4][kPage];
+__global__ __launch_bounds__(256) void norm_rope_store8_kernel(Store8Args a, int query_groups, int query_parts) {
+    __shared__ u32x2 lists[4][kPage];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if ((int)blockIdx.x < query_groups) {
@@ -405,40 +472,50 @@ __global__ __launch_bounds__(256) void norm_rope_store8_kernel(Store8Args a, int
         return;
     }
     const int64_t id = (int64_t)((int)blockIdx.x - query_groups) * 4 + wave;
-    const int64_t block = id / (2 * a.n_kv), r0 = block * per;
-    const int task = (int)(id - block * (2 * a.n_kv));
+    const int64_t block = id / (2 * a.n_kv), r0 = block * kPage;
+    const int task = (int)(id - block * (2 * a.n_kv)), h = task / 2;
     if (r0 >= a.num_rows) return;
-    // lanes 15 .. 14 + per have the rows among which first ones are looked for, the 15 lanes on either side those that may be of the same page
+    // lanes 15 .. 30 have the rows among which first ones are looked for, the 15 lanes on either side those that may be of the same page
     const int64_t at = r0 - (kPage - 1) + lane;
-    int64_t slot = lane < per + 2 * (kPage - 1) && at >= 0 && at < a.num_rows ? a.slots[at] : -1;
+    int slot = lane < 3 * kPage - 2 && at >= 0 && at < a.num_rows ? a.slots[at] : -1;
     if (slot >= a.num_slots) slot = -1;
-    const int page = slot < 0 ? -1 : (int)(slot / kPage);
-    const int above = __shfl_up(page, 1);
-    uint64_t firsts = __ballot(page >= 0 && page != above) & (((1ull << per) - 1) << (kPage - 1));
-    while (firsts) {
-        const int l = __builtin_ctzll(firsts);
-        firsts &= firsts - 1;
-        const int of = __builtin_amdgcn_readlane(page, l);
-        const uint64_t same = __ballot(page == of) & (((1ull << (2 * kPage - 1)) - 1) << (l - (kPage - 1)));
-        if (same & ((1ull << l) - 1)) continue;  // a row further up is of this page
-        const bool mine = same >> lane & 1;
-        PageRows p;
-        p.run = runs[wave];
-        p.n = __popcll(same);
-        const int s = (int)slot % kPage;
+    const int page = slot < 0 ? -1 : slot / kPage, s = slot % kPage;
+    u32x2* const list = lists[wave];
+    auto write_list = [&](uint64_t who, int what) {
         __builtin_amdgcn_wave_barrier();
-        if (mine) runs[wave][__popcll(same & ((1ull << lane) - 1))] = u32x2{(uint32_t)at, (uint32_t)s};
+        if (who >> lane & 1) list[__popcll(who & ((1ull << lane) - 1))] = u32x2{(uint32_t)at, (uint32_t)what};
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        uint32_t held = 0u;  // the slots that are written
-        held = mine ? 1u << s : 0u;
+    };
+    const int above = __shfl_up(page, 1);  // (by all lanes, also those without a page)
+    uint64_t firsts = __ballot(page >= 0 && page != above) & (((1ull << kPage) - 1) << (kPage - 1)), singles = 0;
+    for (uint64_t todo = firsts; todo; todo &= todo - 1) {
+        const int l = __builtin_ctzll(todo), of = __builtin_amdgcn_readlane(page, l);
+        const uint64_t same = __ballot(page == of) & (((1ull << (2 * kPage - 1)) - 1) << (l - (kPage - 1))), this_one = 1ull << l;
+        if (same & (this_one - 1)) firsts &= ~this_one;  // a row further up is of this page
+        else if (same == this_one) singles |= this_one;
+    }
+    if (singles) {
+        write_list(singles, slot);
+        if (task % 2 == 0) store_singles<D, true, T>(a, list, __popcll(singles), h);
+        else store_singles<D, false, T>(a, list, __popcll(singles), h);
+    }
+    for (uint64_t todo = firsts & ~singles; todo; todo &= todo - 1) {
+        const int l = __builtin_ctzll(todo), of = __builtin_amdgcn_readlane(page, l);
+        const uint64_t same = __ballot(page == of) & (((1ull << kPage) - 1) << l);
+        const bool mine = same >> lane & 1;
+        PageRows p;
+        p.run = list;
+        p.n = __popcll(same);
+        write_list(same, s);
+        uint32_t held = mine ? 1u << s : 0u;  // the slots that are written
 #pragma unroll
         for (int by = 1; by < 64; by *= 2) held |= (uint32_t)__shfl_xor((int)held, by);
         p.first = __builtin_ctz(held);
         p.whole = p.n == kPage && __all(!mine || s == lane - l);
-        if (task % 2 == 0) store_keys<D, T>(a, p, of, task / 2);
-        else store_values<D, T>(a, p, of, task / 2);
+        if (task % 2 == 0) store_keys<D, T>(a, p, of, h);
+        else store_values<D, T>(a, p, of, h);
     }
 }
 
@@ -488,14 +565,11 @@ gllm_status gllm_op_norm_rope_store8(const void* qkv, int64_t ld_qkv, int32_t ro
         return GLLM_E_INVALID;
     const Store8Args a{qkv, ld_qkv, (const bf16_t*)q_gain, (const bf16_t*)k_gain, (float)eps, rope, max_position, positions, slots, num_rows,
                        n_q_heads, n_kv_heads, (bf16_t*)q_out, ld_q, (uint8_t*)k_pool, (uint8_t*)v_pool, scales, num_blocks * kPage};
-    // Few rows: a wave looks for a page at one row only, so that no wave does several after another; many, most of them of the same page as their
-    // neighbours: at 16, so that not most waves find none.
-    const int per = num_rows >= 4096 ? 16 : num_rows >= 1024 ? 4 : 1;
     const int64_t parts = ceil_div(n_q_heads, kQueryPasses * (512 / head_dim));
-    const int64_t queries = ceil_div(num_rows * parts, 4), pages = ceil_div(ceil_div(num_rows, per) * 2 * n_kv_heads, 4);
+    const int64_t queries = ceil_div(num_rows * parts, 4), pages = ceil_div(ceil_div(num_rows, kPage) * 2 * n_kv_heads, 4);
     if (queries + pages > INT32_MAX) return GLLM_E_CAPACITY;
     const dim3 grid((unsigned)(queries + pages));
-#define GLLM_STORE8(D_, T_) norm_rope_store8_kernel<D_, T_><<<grid, 256, 0, (hipStream_t)stream>>>(a, (int)queries, (int)parts, per)
+#define GLLM_STORE8(D_, T_) norm_rope_store8_kernel<D_, T_><<<grid, 256, 0, (hipStream_t)stream>>>(a, (int)queries, (int)parts)
     if (head_dim == 128 && rows_type == GLLM_ROWS_F32) GLLM_STORE8(128, float);
     else if (head_dim == 128) GLLM_STORE8(128, bf16_t);
     else if (rows_type == GLLM_ROWS_F32) GLLM_STORE8(64, float);
