@@ -248,7 +248,7 @@ __device__ __forceinline__ void norm_rotate(f32x4& lo, f32x4& hi, const bf16_t* 
 // A wave has kQueryPasses passes over query heads of a row, all asked for at one time, or the keys, or the values, of one KV head of the pages whose
 // first rows are among 16 rows: a page's largest magnitude then needs no more than a wave, and there is one pass over the projection.  The pages
 // among these that receive one row only (decode rows) are done together, D/8 lanes to each, the others one after another.
-constexpr int kQueryPasses = 4;
+constexpr int kQueryPasses = 2;
 
 // The rows of a page and their slots in it, in order of the rows.
 struct PageRows {
@@ -465,13 +465,14 @@ __global__ __launch_bounds__(256) void norm_rope_store8_kernel(Store8Args a, int
     __shared__ u32x2 lists[4][kPage];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if ((int)blockIdx.x < query_groups) {
-        const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+    const int page_groups = (int)gridDim.x - query_groups;
+    if ((int)blockIdx.x >= page_groups) {
+        const int64_t id = (int64_t)((int)blockIdx.x - page_groups) * 4 + wave;
         const int r = (int)(id / query_parts);
         if (r < a.num_rows) store_queries<D, T>(a, r, (int)(id - (int64_t)r * query_parts));
         return;
     }
-    const int64_t id = (int64_t)((int)blockIdx.x - query_groups) * 4 + wave;
+    const int64_t id = (int64_t)blockIdx.x * 4 + wave;
     const int64_t block = id / (2 * a.n_kv), r0 = block * kPage;
     const int task = (int)(id - block * (2 * a.n_kv)), h = task / 2;
     if (r0 >= a.num_rows) return;
