@@ -19,6 +19,8 @@ namespace {
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
 constexpr float kNegBig = -1.0e30f;
 constexpr int kBlock = 64;  // keys, four pages
 
@@ -585,7 +587,6 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) qf[c][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + s * 16 + h * 8));
     }
-    const bool idle = wave * CG * 32 >= ncols;
     const int wave_min = it.c + (col0 + min(wave * CG * 32, ncols - 1)) / g, wave_max = it.c + (col0 + min((wave + 1) * CG * 32, ncols) - 1) / g;
     auto partly = [&](int key0, int lo, int hi) { return key0 + kStep - 1 > lo || (a.window > 0 && key0 <= hi - a.window && key0 + kStep > a.sinks); };
 
@@ -627,90 +628,85 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 __builtin_amdgcn_global_load_lds((gptr_t)((wave < 2 ? a.k_pool : a.v_pool) + off), (lptr_t)to, 16, 0, 0);
             }
         };
-        auto store_keys = [&](int i, u32x4 x) {
+        auto put_keys = [&](int i, u32x4 lo, u32x4 hi) {
             const int q = piece % D, page = piece / D, chunk = q % (D / 4) / 4, at = (8 * (q / (D / 4)) + 4 * page + q % 4) ^ (4 * (chunk & 3));
             unsigned char* to = lds.keys[i % kKeyStages] + (2 * chunk * kStep + at) * 16;
-            *reinterpret_cast<u32x4*>(to) = widen8(x[0], x[1]);
-            *reinterpret_cast<u32x4*>(to + kStep * 16) = widen8(x[2], x[3]);
+            *reinterpret_cast<u32x4*>(to) = lo;
+            *reinterpret_cast<u32x4*>(to + kStep * 16) = hi;
         };
-        auto store_values = [&](int i, u32x4 x) {
-            const int q = piece % D, page = piece / D;
-            if (partly(key_of(min(i, steps - 1)), it.c + i0, it.c + i1)) {  // (the same for the workgroup)
-                uint32_t some = 0u;
+        // Empties this thread's values that are no numbers, where not all rows see all keys of the step.
+        auto clean_values = [&](int i, u32x4& x) {
+            if (!partly(key_of(min(i, steps - 1)), it.c + i0, it.c + i1)) return;  // (the same for the workgroup)
+            uint32_t some = 0u;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t b = no_numbers(x[w]);
-                    x[w] &= ~((b >> 7) * 0xFFu);
-                    some |= ((b >> 7 & 1) | (b >> 14 & 2) | (b >> 21 & 4) | (b >> 28 & 8)) << (4 * w);
-                }
-                if (some) atomicOr(&lds.bad[i % 4], some << (16 * page));
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t b = no_numbers(x[w]);
+                x[w] &= ~((b >> 7) * 0xFFu);
+                some |= ((b >> 7 & 1) | (b >> 14 & 2) | (b >> 21 & 4) | (b >> 28 & 8)) << (4 * w);
             }
-            unsigned char* to = lds.values[i % kValueStages] + (2 * page * D + q) * 16;
-            *reinterpret_cast<u32x4*>(to) = widen8(x[0], x[1]);
-            *reinterpret_cast<u32x4*>(to + D * 16) = widen8(x[2], x[3]);
+            if (some) atomicOr(&lds.bad[i % 4], some << (16 * (piece / D)));
         };
-        auto convert = [&](int i) {  // this thread's pieces of step i, which have come
-            const unsigned char* from = &lds.raw[i % kRaw][0][0] + threadIdx.x * 16;
-            if (D == 128) {
-                const u32x4 k = *reinterpret_cast<const u32x4*>(from), v = *reinterpret_cast<const u32x4*>(from + kStep * D);
-                store_keys(i, k);
-                store_values(i, v);
-            } else {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(from);
-                if (wave < 2) store_keys(i, x);
-                else store_values(i, x);
-            }
+        auto put_values = [&](int i, u32x4 lo, u32x4 hi) {
+            unsigned char* to = lds.values[i % kValueStages] + (2 * (piece / D) * D + piece % D) * 16;
+            *reinterpret_cast<u32x4*>(to) = lo;
+            *reinterpret_cast<u32x4*>(to + D * 16) = hi;
         };
-        auto scores = [&](int i, f32x16 (&s)[CG]) {
+        // this thread's pieces of step i, which have come
+        auto raw_keys = [&](int i) { return *reinterpret_cast<const u32x4*>(&lds.raw[i % kRaw][0][0] + threadIdx.x * 16); };
+        auto raw_values = [&](int i) { return *reinterpret_cast<const u32x4*>(&lds.raw[i % kRaw][0][0] + threadIdx.x * 16 + (D == 128 ? kStep * D : 0)); };
+        auto read_keys = [&](int i, bf16x8 (&kf)[D / 16]) {
             const unsigned char* keys = lds.keys[i % kKeyStages];
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) kf[k] = *reinterpret_cast<const bf16x8*>(keys + ((2 * k + h) * kStep + (r ^ (4 * (k & 3)))) * 16);
+        };
+        auto scores = [&](const bf16x8 (&kf)[D / 16], f32x16 (&s)[CG]) {
 #pragma unroll
             for (int c = 0; c < CG; ++c)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) s[c][v] = 0.f;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(keys + ((2 * k + h) * kStep + (r ^ (4 * (k & 3)))) * 16);
+            for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-                for (int c = 0; c < CG; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c][k], s[c], 0, 0, 0);
-            }
-#pragma unroll
-            for (int c = 0; c < CG; ++c) in_vectors(s[c]);
+                for (int c = 0; c < CG; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[c][k], s[c], 0, 0, 0);
         };
-        float factor = 0.f, log_values = 0.f, per_value = 0.f;  // of the page of this lane's keys in the step to come
-        // Masks, and the references that step i needs.
-        auto settle = [&](int i, f32x16 (&s)[CG]) {
+        struct Scale {
+            float factor, log_values, per_value;
+        };
+        auto scale_of = [&](int i) {  // of the page of this lane's keys in step i
             const int at = i - ids_base;
             const float k0 = lane_value(ps[0].keys, at), k1 = lane_value(ps[1].keys, at), l0 = lane_value(ps[0].log_values, at), l1 = lane_value(ps[1].log_values, at),
                         p0 = lane_value(ps[0].per_value, at), p1 = lane_value(ps[1].per_value, at);
-            factor = h ? k1 : k0;
-            log_values = h ? l1 : l0;
-            per_value = h ? p1 : p0;
+            return Scale{h ? k1 : k0, h ? l1 : l0, h ? p1 : p0};
+        };
+        auto largest = [&](const f32x16& s) {
+            float x = s[0];
+#pragma unroll
+            for (int v = 1; v < 16; ++v) x = fmaxf(x, s[v]);
+            return x;
+        };
+        // Masks, and the references that step i needs; top: the largest raw scores.
+        auto settle = [&](int i, f32x16 (&s)[CG], float (&top)[CG], const Scale& sc) {
             const int key0 = key_of(i);
             if (partly(key0, wave_min, wave_max)) {
                 const uint32_t bad = lds.bad[i % 4] >> (16 * h);
 #pragma unroll
-                for (int c = 0; c < CG; ++c)
+                for (int c = 0; c < CG; ++c) {
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const int key = key0 + h * kPage + v;
                         const bool hidden = (key > pos[c]) | ((key <= low[c]) & (key >= a.sinks));
                         s[c][v] = hidden ? -INFINITY : bad >> v & 1 ? NAN : s[c][v];
                     }
+                    top[c] = largest(s[c]);
+                }
             }
-            float top[CG];
             bool above = false;
 #pragma unroll
-            for (int c = 0; c < CG; ++c) {
-                float x = s[c][0];
-#pragma unroll
-                for (int v = 1; v < 16; ++v) x = fmaxf(x, s[c][v]);
-                top[c] = x * factor;
-                above |= top[c] > m[c] + kSlack;
-            }
+            for (int c = 0; c < CG; ++c) above |= top[c] * sc.factor > m[c] + kSlack;
             if (__any(above)) {
 #pragma unroll
                 for (int c = 0; c < CG; ++c) {
-                    const float up = fmaxf(m[c], fmaxf(top[c], __shfl_xor(top[c], 32))), down = __builtin_amdgcn_exp2f(m[c] - up);
+                    const float mine = top[c] * sc.factor, up = fmaxf(m[c], fmaxf(mine, __shfl_xor(mine, 32))), down = __builtin_amdgcn_exp2f(m[c] - up);
                     m[c] = up;
                     l[c] *= down;
 #pragma unroll
@@ -723,35 +719,6 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 }
             }
         };
-        auto weights = [&](f32x16 (&s)[CG], bf16x8 (&w)[CG][2]) {
-#pragma unroll
-            for (int c = 0; c < CG; ++c) {
-                const float shift = log_values - m[c];
-                float sum = 0.f;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    f32x8 p;
-#pragma unroll
-                    for (int v = 0; v < 8; ++v) {
-                        p[v] = __builtin_amdgcn_exp2f(fmaf(s[c][8 * j + v], factor, shift));
-                        sum += p[v];
-                    }
-                    w[c][j] = __builtin_convertvector(p, bf16x8);
-                }
-                l[c] += sum * per_value;
-            }
-        };
-        auto outputs = [&](int i, bf16x8 (&w)[CG][2]) {
-            const unsigned char* values = lds.values[i % kValueStages];
-#pragma unroll
-            for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const bf16x8 vf = *reinterpret_cast<const bf16x8*>(values + ((2 * h + j) * D + t * 32 + r) * 16);
-#pragma unroll
-                    for (int c = 0; c < CG; ++c) o[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, w[c][j], o[c][t], 0, 0, 0);
-                }
-        };
         if (threadIdx.x < 4) lds.bad[threadIdx.x] = 0u;
         __syncthreads();
         fetch_ids(0);
@@ -759,32 +726,109 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         for (int i = 0; i < kRaw - 1; ++i) issue(i);
         // steps 0 and 1
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 3) * LOADS) : "memory");
-        convert(0);
-        convert(1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (D == 128 || wave < 2) {
+                const u32x4 x = raw_keys(i);
+                put_keys(i, widen8(x[0], x[1]), widen8(x[2], x[3]));
+            }
+            if (D == 128 || wave >= 2) {
+                u32x4 x = raw_values(i);
+                clean_values(i, x);
+                put_values(i, widen8(x[0], x[1]), widen8(x[2], x[3]));
+            }
+        }
         lds_barrier();
         f32x16 s[CG];
-        scores(0, s);
-        settle(0, s);
+        Scale sc = scale_of(0);
+        {
+            bf16x8 kf[D / 16];
+            float top[CG];
+            read_keys(0, kf);
+            scores(kf, s);
+#pragma unroll
+            for (int c = 0; c < CG; ++c) {
+                in_vectors(s[c]);
+                top[c] = largest(s[c]);
+            }
+            settle(0, s, top, sc);
+        }
         for (int i = 0; i < steps; ++i) {
             // the codes of step i + 2 have come, and nobody reads the stages that they go to any more
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 4) * LOADS) : "memory");
+            const Scale now = sc;
             if (i + kRaw - 1 >= ids_base + 64 && i + 1 < steps) fetch_ids(i + 1);
             issue(i + kRaw - 1);
-            bf16x8 w[CG][2];
+            // A round in the order in which it is to be issued: between two matrix instructions, 32 cycles each, stand vector instructions of about as
+            // long that depend on neither.
+            constexpr int PAIRS = 8 * CG, SCORES = D / 16 * CG, OUTPUTS = D / 32 * 2 * CG, AHEAD = PAIRS / 4;
+            bf16x8 kf[D / 16], vf[D / 32][2];
+            u32x4 w[CG][2];
             f32x16 next[CG];
-            if (!idle) {
-                scores(i + 1, next);
-                weights(s, w);
-                outputs(i, w);
+            float top[CG], shift[CG], sum[CG];
+            const unsigned char *keys = lds.keys[(i + 1) % kKeyStages], *values = lds.values[i % kValueStages];
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) kf[k] = *reinterpret_cast<const bf16x8*>(keys + ((2 * k + h) * kStep + (r ^ (4 * (k & 3)))) * 16);
+            u32x4 raw = raw_keys(i + 2), raw_v = D == 128 ? raw_values(i + 2) : raw;
+            sc = scale_of(min(i + 1, steps - 1));
+#pragma unroll
+            for (int c = 0; c < CG; ++c) {
+                shift[c] = now.log_values - m[c];
+                sum[c] = 0.f;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) next[c][v] = 0.f;
             }
-            convert(i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            // Two weights of the step, their sum as they are rounded.
+            auto pair = [&](int x) {
+                const int c = x / 8, q = x % 8;
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * q], now.factor, shift[c])), p1 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * q + 1], now.factor, shift[c]));
+                const bf16x2 p = __builtin_convertvector(f32x2{p0, p1}, bf16x2);
+                w[c][q / 4][q % 4] = __builtin_bit_cast(uint32_t, p);
+                sum[c] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, p), s16x2{0x3F80, 0x3F80}, sum[c], false);
+            };
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) pair(x);  // (while the keys come from LDS)
+            if (D == 128 || wave >= 2) clean_values(i + 2, raw_v);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < SCORES; ++x) {
+                next[x % CG] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x / CG], qf[x % CG][x / CG], next[x % CG], 0, 0, 0);
+#pragma unroll
+                for (int y = AHEAD + (PAIRS - AHEAD) * x / SCORES; y < AHEAD + (PAIRS - AHEAD) * (x + 1) / SCORES; ++y) pair(y);
+                const int z = x - SCORES / 2;  // the values, in the second half
+                if (z >= 0) {
+#pragma unroll
+                    for (int y = D / 16 * z / (SCORES / 2); y < D / 16 * (z + 1) / (SCORES / 2); ++y)
+                        vf[y % (D / 32)][y / (D / 32)] = *reinterpret_cast<const bf16x8*>(values + ((2 * h + y / (D / 32)) * D + y % (D / 32) * 32 + r) * 16);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int c = 0; c < CG; ++c) l[c] += sum[c] * now.per_value;
+            u32x4 wide[4];
+#pragma unroll
+            for (int x = 0; x < OUTPUTS; ++x) {
+                const int c = x % CG, t = x / CG % (D / 32), j = x / CG / (D / 32);
+                o[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][j], __builtin_bit_cast(bf16x8, w[c][j]), o[c][t], 0, 0, 0);
+#pragma unroll
+                for (int y = 16 * CG * x / OUTPUTS; y < 16 * CG * (x + 1) / OUTPUTS; ++y) {  // the scores out of the accumulators, and the largest
+                    float z = next[y / 16][y % 16];
+                    asm("" : "+v"(z));
+                    s[y / 16][y % 16] = z;
+                    top[y / 16] = y % 16 == 0 ? z : fmaxf(top[y / 16], z);
+                }
+                if (x % (OUTPUTS / 4) == OUTPUTS / 4 - 1) {  // the codes of step i + 2
+                    const int y = x / (OUTPUTS / 4);
+                    wide[y] = y < 2 ? widen8(raw[2 * y], raw[2 * y + 1]) : widen8(raw_v[2 * y - 4], raw_v[2 * y - 3]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (D == 128 || wave < 2) put_keys(i + 2, wide[0], wide[1]);
+            if (D == 128 || wave >= 2) put_values(i + 2, wide[2], wide[3]);
             if (threadIdx.x == 0) lds.bad[(i + 3) % 4] = 0u;
             lds_barrier();
-            if (!idle && i + 1 < steps) {
-                settle(i + 1, next);
-#pragma unroll
-                for (int c = 0; c < CG; ++c) s[c] = next[c];
-            }
+            if (i + 1 < steps) settle(i + 1, s, top, sc);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no LDS fill may outlive the workgroup
     }
