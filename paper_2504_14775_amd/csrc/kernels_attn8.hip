@@ -27,8 +27,8 @@ constexpr int kBlock = 64;  // keys, four pages
 // ---- the plan --------------------------------------------------------------------------------------------------------------
 
 // Columns of a tile by the columns of a sequence.
-constexpr int kStreamCols = 16, kHalfCols = 128, kTileCols = 256;
-__host__ __device__ constexpr int tile_cols(int64_t cols) { return cols <= kStreamCols ? kStreamCols : cols <= kHalfCols ? kHalfCols : kTileCols; }
+constexpr int kStreamCols = 16, kTileCols = 256;
+__host__ __device__ constexpr int tile_cols(int64_t cols) { return cols <= kStreamCols ? kStreamCols : kTileCols; }
 
 // A unit of work: a part of the keys for the columns of one tile of a sequence.
 struct Unit {
@@ -320,11 +320,6 @@ __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d
 // A barrier that waits for this wave's reads and writes of LDS only: __syncthreads() would wait for the loads into the ring too.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Says in which half of the register file a value stands at this point: that of the matrix instructions' accumulators, or the other, where the
-// vector instructions read.
-__device__ __forceinline__ void in_accumulators(f32x16& x) { asm("" : "+a"(x)); }
-__device__ __forceinline__ void in_vectors(f32x16& x) { asm("" : "+v"(x)); }
-
 // Four codes as bf16, without rounding.
 __device__ __forceinline__ u32x2 widen(uint32_t codes) {
     return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false)),
@@ -358,14 +353,14 @@ struct Frag {
     u32x4 k[4][D / 64];  // [tile][64 dims]: row r = slot 4t + r % 4 of page r / 4, dims 16 (4p + G) ..
     u32x4 v[D / 16];     // [16 dims]: dim 16b + r of page G
 };
-template <int D>
+template <int D, int WAVES>
 struct StreamLds {
-    float o[4][16][D + 4];
-    float m[4][16], l[4][16];
+    float o[WAVES][16][D + 4];
+    float m[WAVES][16], l[WAVES][16];
 };
 
-template <int D, bool TILES>
-__device__ __forceinline__ void stream_unit(const Attn8Args& a, const Unit& it, const Parts& parts, int kvh, StreamLds<D>& join) {
+template <int D, int WAVES>
+__device__ __forceinline__ void stream_unit(const Attn8Args& a, const Unit& it, const Parts& parts, int kvh, StreamLds<D, WAVES>& join) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, G = lane >> 4, g = a.n_q / a.n_kv;
@@ -373,7 +368,7 @@ __device__ __forceinline__ void stream_unit(const Attn8Args& a, const Unit& it, 
     const Seen seen = seen_blocks(a, it.c, 0, it.n - 1);
     const int each = seen.blocks / it.parts, more = seen.blocks - each * it.parts;
     const int first = it.broken ? 0 : it.part * each + min(it.part, more), last = it.broken ? 0 : first + each + (it.part < more);
-    const int run = (last - first + 3) / 4;
+    const int run = (last - first + WAVES - 1) / WAVES;
     const int b_begin = min(first + wave * run, last), b_end = min(b_begin + run, last);
     const int last_page = max(it.c + it.n - 1, 0) / kPage;
     const int32_t* bt = a.block_tables + (int64_t)it.seq * a.table_stride;
@@ -510,14 +505,14 @@ __device__ __forceinline__ void stream_unit(const Attn8Args& a, const Unit& it, 
     for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(&join.o[wave][r][b * 16 + G * 4]) = o[b];
     __syncthreads();
     const int here = min(kStreamCols, cols - it.tile * kStreamCols);
-    for (int i = threadIdx.x; i < here * (D / 4); i += 256) {
+    for (int i = threadIdx.x; i < here * (D / 4); i += 64 * WAVES) {
         const int j = i / (D / 4), e = i % (D / 4) * 4, cc = it.tile * kStreamCols + j, rr = cc / g;
         float ms = kNegBig, ls = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) ms = fmaxf(ms, join.m[w][j]);
+        for (int w = 0; w < WAVES; ++w) ms = fmaxf(ms, join.m[w][j]);
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float x = __builtin_amdgcn_exp2f(join.m[w][j] - ms);
             const f32x4 ow = *reinterpret_cast<const f32x4*>(&join.o[w][j][e]);
 #pragma unroll
@@ -539,26 +534,32 @@ __device__ __forceinline__ void stream_unit(const Attn8Args& a, const Unit& it, 
 
 // ---- tiles of columns --------------------------------------------------------------------------------------------------------
 //
-// One workgroup of 4 waves, 32*CG columns a wave, matrix instructions of 32x32x16.  Keys come in steps of 32, two pages: their codes go from HBM
-// into a ring in LDS, each thread turns the pieces that it asked for into bf16, and all waves read these.  The row 8a + 4h + b of a score tile is
-// slot 4a + b of page h, so that the lanes of half h receive the 16 slots of page h.
-//   keys as bf16    [D / 8][32 rows][8 dims], row x of piece c at x ^ 4 (c / 2 % 4): the writes of 16 lanes hit different banks
-//   values as bf16  [2 pages][2 halves of the slots][D][8 slots]
-// In a round i the exponentials of step i run beside the scores of step i + 1 and in front of the outputs of step i.
-constexpr int kStep = 32, kRaw = 6, kKeyStages = 2, kValueStages = 3;
+// One workgroup of 8 waves, 32 columns a wave, matrix instructions of 32x32x16.  Keys come in blocks of 64, four pages: their codes go from HBM
+// into a ring in LDS, each thread turns the pieces that it asked for into bf16, and all waves read these, half a block (two pages) after the other.
+// The row 8a + 4h + b of a score tile is slot 4a + b of page h of the half, so that the lanes of half h receive the 16 slots of page h.
+//   keys as bf16    [half][D / 8][32 rows][8 dims], row x of piece c at x ^ 4 (c / 2 % 4): the writes of 16 lanes hit different banks
+//   values as bf16  [page][2 halves of the slots][D][8 slots]
+// The exponentials of a half run beside the scores of the next one and in front of its own outputs; what a phase reads from LDS is asked for in the
+// phase before.
+constexpr int kHalf = 32, kRaw = 4, kKeyStages = 2, kValueStages = 2, kWindow = 64;
+struct PageEntry {
+    int32_t id;
+    PageScale scale;
+};
 template <int D>
 struct TileLds {
-    unsigned char raw[kRaw][2][kStep * D];          // [step][keys, values]: codes as loaded
-    unsigned char keys[kKeyStages][kStep * D * 2];
-    unsigned char values[kValueStages][kStep * D * 2];
-    uint32_t bad[4];                                // of a step: bit 16h + t: slot t of page h has values that are no numbers
+    unsigned char raw[kRaw][2][kBlock * D];         // [block][keys, values]: codes as loaded; the keys of block j with the values of block j - 1
+    unsigned char keys[kKeyStages][2][kHalf * D * 2];
+    unsigned char values[kValueStages][2][kHalf * D * 2];
+    PageEntry pages[2][kWindow * 4];                // of 64 blocks and the next 64
+    uint32_t bad[4][2];                             // of a half: bit 16h + t: slot t of page h has values that are no numbers
 };
 constexpr float kSlack = 32.0f;  // a reference lags by up to this: weights stay below 2^32
 
-template <int D, int CG>
+template <int D>
 __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, const Parts& parts, int kvh, TileLds<D>& lds) {
     constexpr int PH = D * kPage;         // bytes of a page's head
-    constexpr int LOADS = D == 128 ? 2 : 1;  // of a thread and step: a piece of keys and one of values, or one of either
+    constexpr bool BOTH = D == 128;       // a thread has a piece of keys and one of values; or the lower waves keys, the upper ones values
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 31, h = lane >> 5, g = a.n_q / a.n_kv;
@@ -566,117 +567,78 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
     const int i0 = col0 / g, i1 = (col0 + ncols - 1) / g;
     const Seen seen = seen_blocks(a, it.c, i0, i1);
     const int each = seen.blocks / it.parts, more = seen.blocks - each * it.parts;
-    const int first = 2 * (it.part * each + min(it.part, more));
-    int steps = 2 * (each + (it.part < more));
-    if (it.part + 1 == it.parts && (it.c + i1) % kBlock < kStep && steps > 0) --steps;  // nobody sees the last one
-    if (it.broken) steps = 0;
+    const int first = it.part * each + min(it.part, more), blocks = it.broken ? 0 : each + (it.part < more);
     const int last_page = max(it.c + it.n - 1, 0) / kPage;
     const int32_t* bt = a.block_tables + (int64_t)it.seq * a.table_stride;
-    auto key_of = [&](int i) { return (seen.actual((first + i) >> 1) * 2 + ((first + i) & 1)) * kStep; };  // first key of step i
+    auto key_of = [&](int b) { return seen.actual(first + b) * kBlock; };  // first key of block b
 
-    bf16x8 qf[CG][D / 16];
-    int pos[CG], low[CG];
-    bool stored[CG];
+    const int tcol = wave * 32 + r, col = col0 + min(tcol, ncols - 1), row = col / g;
+    const bool idle = wave * 32 >= ncols;  // (its pieces are wanted all the same)
+    const int pos = it.c + row, low = a.window > 0 ? pos - a.window : -1;  // this column sees keys up to pos and above low, or below sinks
+    const int wave_min = it.c + (col0 + min(wave * 32, ncols - 1)) / g, wave_max = it.c + (col0 + min((wave + 1) * 32, ncols) - 1) / g;
+    auto partly = [&](int key0, int n, int lo, int hi) { return key0 + n - 1 > lo || (a.window > 0 && key0 <= hi - a.window && key0 + n > a.sinks); };
+    bf16x8 qf[D / 16];
+    const bf16_t* qrow = a.q + (int64_t)(it.row0 + row) * a.ld_q + (int64_t)(kvh * g + col - row * g) * D;
 #pragma unroll
-    for (int c = 0; c < CG; ++c) {
-        const int t = (wave * CG + c) * 32 + r, col = col0 + min(t, ncols - 1), row = col / g;
-        stored[c] = t < ncols;
-        pos[c] = it.c + row;
-        low[c] = a.window > 0 ? pos[c] - a.window : -1;
-        const bf16_t* qrow = a.q + (int64_t)(it.row0 + row) * a.ld_q + (int64_t)(kvh * g + col - row * g) * D;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[c][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + s * 16 + h * 8));
-    }
-    const int wave_min = it.c + (col0 + min(wave * CG * 32, ncols - 1)) / g, wave_max = it.c + (col0 + min((wave + 1) * CG * 32, ncols) - 1) / g;
-    auto partly = [&](int key0, int lo, int hi) { return key0 + kStep - 1 > lo || (a.window > 0 && key0 <= hi - a.window && key0 + kStep > a.sinks); };
+    for (int k = 0; k < D / 16; ++k) qf[k] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + k * 16 + h * 8));
 
-    f32x16 o[CG][D / 32];
-    float m[CG], l[CG];
+    f32x16 o[D / 32];
+    float m = kNegBig, l = 0.f;
 #pragma unroll
-    for (int c = 0; c < CG; ++c) {
-        m[c] = kNegBig;
-        l[c] = 0.f;
+    for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[c][t][v] = 0.f;
-    }
+        for (int v = 0; v < 16; ++v) o[t][v] = 0.f;
 
-    if (steps > 0) {
-        // pages of 64 steps, one per lane, both of a step, with their scales
-        int ids_base = 0, ids[2] = {0, 0};
-        PageScale ps[2];
-        auto fetch_ids = [&](int base) {
-            ids_base = base;
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                ids[p] = min(max(bt[min(key_of(min(base + lane, steps - 1)) / kPage + p, last_page)], 0), a.num_blocks - 1);
-                ps[p].of(a.scales[(int64_t)ids[p] * a.n_kv + kvh], a.scale_log2);
-            }
+    if (blocks > 0) {
+        // Page ids and scales, 64 blocks and the next 64 in LDS.
+        auto page_of = [&](int x) { return min(max(bt[min(key_of(min(x / 4, blocks - 1)) / kPage + x % 4, last_page)], 0), a.num_blocks - 1); };
+        auto entry = [&](int x, int id, f32x2 sc) {
+            PageEntry e;
+            e.id = id;
+            e.scale.of(sc, a.scale_log2);
+            lds.pages[x / (kWindow * 4) % 2][x % (kWindow * 4)] = e;
         };
-        // piece x of a step: 16 bytes of page x / D
-        const int piece = D == 128 ? threadIdx.x : threadIdx.x & 127;
-        auto issue = [&](int i) {  // every wave issues its pieces (of the last step again behind it), so that the number on their way is the same in every round
-            const int at = min(i, steps - 1) - ids_base;
-            const int page = D == 128 ? (wave < 2 ? lane_value(ids[0], at) : lane_value(ids[1], at)) : (wave % 2 == 0 ? lane_value(ids[0], at) : lane_value(ids[1], at));
-            const int64_t off = ((int64_t)page * a.n_kv + kvh) * PH + (piece % D) * 16;
-            unsigned char* to = &lds.raw[i % kRaw][0][0] + wave * 1024;
-            if (D == 128) {
-                __builtin_amdgcn_global_load_lds((gptr_t)(a.k_pool + off), (lptr_t)to, 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((gptr_t)(a.v_pool + off), (lptr_t)(to + kStep * D), 16, 0, 0);
-            } else {
-                __builtin_amdgcn_global_load_lds((gptr_t)((wave < 2 ? a.k_pool : a.v_pool) + off), (lptr_t)to, 16, 0, 0);
-            }
+        auto entry_of = [&](int b, int q) -> const PageEntry& { return lds.pages[b / kWindow % 2][b % kWindow * 4 + q]; };
+        // The pieces of a side of a block are 16 bytes, 4D of them, page after page.
+        const bool has_keys = BOTH || wave < 4, has_values = BOTH || wave >= 4;
+        const int piece = BOTH ? threadIdx.x : threadIdx.x & 255, page = piece / D, piece_at = piece % D;
+        const int64_t piece_off = (int64_t)kvh * PH + piece_at * 16, page_step = (int64_t)a.n_kv * PH;
+        // every wave issues its pieces (of the last block again behind it), so that the number on their way is the same in every round
+        auto issue = [&](int j, int id_keys, int id_values) {  // the keys of block j and the values of block j - 1
+            unsigned char* to = &lds.raw[j % kRaw][0][0] + wave * 1024;
+            if (has_keys) __builtin_amdgcn_global_load_lds((gptr_t)(a.k_pool + id_keys * page_step + piece_off), (lptr_t)to, 16, 0, 0);
+            if (has_values) __builtin_amdgcn_global_load_lds((gptr_t)(a.v_pool + id_values * page_step + piece_off), (lptr_t)(to + (BOTH ? kBlock * D : 0)), 16, 0, 0);
         };
-        auto put_keys = [&](int i, u32x4 lo, u32x4 hi) {
-            const int q = piece % D, page = piece / D, chunk = q % (D / 4) / 4, at = (8 * (q / (D / 4)) + 4 * page + q % 4) ^ (4 * (chunk & 3));
-            unsigned char* to = lds.keys[i % kKeyStages] + (2 * chunk * kStep + at) * 16;
-            *reinterpret_cast<u32x4*>(to) = lo;
-            *reinterpret_cast<u32x4*>(to + kStep * 16) = hi;
-        };
-        // Empties this thread's values that are no numbers, where not all rows see all keys of the step.
-        auto clean_values = [&](int i, u32x4& x) {
-            if (!partly(key_of(min(i, steps - 1)), it.c + i0, it.c + i1)) return;  // (the same for the workgroup)
+        auto id_of = [&](int j) { return __builtin_amdgcn_readfirstlane(entry_of(min(max(j, 0), blocks - 1), page).id); };
+        auto raw_keys = [&](int j) { return *reinterpret_cast<const u32x4*>(&lds.raw[j % kRaw][0][0] + threadIdx.x * 16); };  // which have come
+        auto raw_values = [&](int j) { return *reinterpret_cast<const u32x4*>(&lds.raw[j % kRaw][0][0] + threadIdx.x * 16 + (BOTH ? kBlock * D : 0)); };
+        // Values that are no numbers may reach the columns that see them only: where not all rows see all keys they are emptied, and the key's scores are
+        // no numbers.
+        auto clean = [&](int b, u32x4& x) {
+            if (!has_values || !partly(key_of(min(b, blocks - 1)), kBlock, it.c + i0, it.c + i1)) return;  // (the same for the wave)
             uint32_t some = 0u;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const uint32_t b = no_numbers(x[w]);
-                x[w] &= ~((b >> 7) * 0xFFu);
-                some |= ((b >> 7 & 1) | (b >> 14 & 2) | (b >> 21 & 4) | (b >> 28 & 8)) << (4 * w);
+                const uint32_t n = no_numbers(x[w]);
+                x[w] &= ~((n >> 7) * 0xFFu);
+                some |= ((n >> 7 & 1) | (n >> 14 & 2) | (n >> 21 & 4) | (n >> 28 & 8)) << (4 * w);
             }
-            if (some) atomicOr(&lds.bad[i % 4], some << (16 * (piece / D)));
+            if (some) atomicOr(&lds.bad[b % 4][page / 2], some << (16 * (page % 2)));
         };
-        auto put_values = [&](int i, u32x4 lo, u32x4 hi) {
-            unsigned char* to = lds.values[i % kValueStages] + (2 * (piece / D) * D + piece % D) * 16;
+        // where the two halves of a piece go as bf16
+        const int chunk = piece_at % (D / 4) / 4, key_row = (8 * (piece_at / (D / 4)) + 4 * (page % 2) + piece_at % 4) ^ (4 * (chunk & 3));
+        const int keys_at = (page / 2) * (kHalf * D * 2) + (2 * chunk * 32 + key_row) * 16, values_at = (2 * page * D + piece_at) * 16;
+        auto put_keys = [&](int b, u32x4 lo, u32x4 hi) {
+            if (!has_keys) return;
+            unsigned char* to = &lds.keys[b % kKeyStages][0][0] + keys_at;
+            *reinterpret_cast<u32x4*>(to) = lo;
+            *reinterpret_cast<u32x4*>(to + 32 * 16) = hi;
+        };
+        auto put_values = [&](int b, u32x4 lo, u32x4 hi) {
+            if (!has_values) return;
+            unsigned char* to = &lds.values[b % kValueStages][0][0] + values_at;
             *reinterpret_cast<u32x4*>(to) = lo;
             *reinterpret_cast<u32x4*>(to + D * 16) = hi;
-        };
-        // this thread's pieces of step i, which have come
-        auto raw_keys = [&](int i) { return *reinterpret_cast<const u32x4*>(&lds.raw[i % kRaw][0][0] + threadIdx.x * 16); };
-        auto raw_values = [&](int i) { return *reinterpret_cast<const u32x4*>(&lds.raw[i % kRaw][0][0] + threadIdx.x * 16 + (D == 128 ? kStep * D : 0)); };
-        auto read_keys = [&](int i, bf16x8 (&kf)[D / 16]) {
-            const unsigned char* keys = lds.keys[i % kKeyStages];
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) kf[k] = *reinterpret_cast<const bf16x8*>(keys + ((2 * k + h) * kStep + (r ^ (4 * (k & 3)))) * 16);
-        };
-        auto scores = [&](const bf16x8 (&kf)[D / 16], f32x16 (&s)[CG]) {
-#pragma unroll
-            for (int c = 0; c < CG; ++c)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s[c][v] = 0.f;
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-                for (int c = 0; c < CG; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[c][k], s[c], 0, 0, 0);
-        };
-        struct Scale {
-            float factor, log_values, per_value;
-        };
-        auto scale_of = [&](int i) {  // of the page of this lane's keys in step i
-            const int at = i - ids_base;
-            const float k0 = lane_value(ps[0].keys, at), k1 = lane_value(ps[1].keys, at), l0 = lane_value(ps[0].log_values, at), l1 = lane_value(ps[1].log_values, at),
-                        p0 = lane_value(ps[0].per_value, at), p1 = lane_value(ps[1].per_value, at);
-            return Scale{h ? k1 : k0, h ? l1 : l0, h ? p1 : p0};
         };
         auto largest = [&](const f32x16& s) {
             float x = s[0];
@@ -684,183 +646,189 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             for (int v = 1; v < 16; ++v) x = fmaxf(x, s[v]);
             return x;
         };
-        // Masks, and the references that step i needs; top: the largest raw scores.
-        auto settle = [&](int i, f32x16 (&s)[CG], float (&top)[CG], const Scale& sc) {
-            const int key0 = key_of(i);
-            if (partly(key0, wave_min, wave_max)) {
-                const uint32_t bad = lds.bad[i % 4] >> (16 * h);
+        // Masks, and the reference that a half needs.
+        auto settle = [&](int b, int half, f32x16& s, float top, const PageScale& sc) {
+            const int key0 = key_of(b) + half * kHalf;
+            if (partly(key0, kHalf, wave_min, wave_max)) {
+                const uint32_t bad = lds.bad[b % 4][half] >> (16 * h);
 #pragma unroll
-                for (int c = 0; c < CG; ++c) {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int key = key0 + h * kPage + v;
-                        const bool hidden = (key > pos[c]) | ((key <= low[c]) & (key >= a.sinks));
-                        s[c][v] = hidden ? -INFINITY : bad >> v & 1 ? NAN : s[c][v];
-                    }
-                    top[c] = largest(s[c]);
+                for (int v = 0; v < 16; ++v) {
+                    const int key = key0 + h * kPage + v;
+                    const bool hidden = (key > pos) | ((key <= low) & (key >= a.sinks));
+                    s[v] = hidden ? -INFINITY : bad >> v & 1 ? NAN : s[v];
                 }
+                top = largest(s);
             }
-            bool above = false;
+            top *= sc.keys;
+            if (__any(top > m + kSlack)) {
+                const float up = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), down = __builtin_amdgcn_exp2f(m - up);
+                m = up;
+                l *= down;
 #pragma unroll
-            for (int c = 0; c < CG; ++c) above |= top[c] * sc.factor > m[c] + kSlack;
-            if (__any(above)) {
+                for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-                for (int c = 0; c < CG; ++c) {
-                    const float mine = top[c] * sc.factor, up = fmaxf(m[c], fmaxf(mine, __shfl_xor(mine, 32))), down = __builtin_amdgcn_exp2f(m[c] - up);
-                    m[c] = up;
-                    l[c] *= down;
-#pragma unroll
-                    for (int t = 0; t < D / 32; ++t) {
-                        in_accumulators(o[c][t]);  // (or they are copied in front of the branch in every round)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) o[c][t][v] *= down;
-                        in_accumulators(o[c][t]);
-                    }
-                }
+                    for (int v = 0; v < 16; ++v) o[t][v] *= down;
             }
         };
-        if (threadIdx.x < 4) lds.bad[threadIdx.x] = 0u;
-        __syncthreads();
-        fetch_ids(0);
+        bf16x8 kf[D / 16], vf[D / 32][2];
+        auto read_key = [&](int b, int half, int k) { kf[k] = *reinterpret_cast<const bf16x8*>(lds.keys[b % kKeyStages][half] + ((2 * k + h) * 32 + (r ^ (4 * (k & 3)))) * 16); };
+        auto read_value = [&](int b, int half, int x) {
+            vf[x % (D / 32)][x / (D / 32)] = *reinterpret_cast<const bf16x8*>(lds.values[b % kValueStages][half] + ((2 * h + x / (D / 32)) * D + x % (D / 32) * 32 + r) * 16);
+        };
+        // One half, of block b: its weights and outputs from the scores s, and the scores of the next one, whose keys are in kf, into s; the keys of the one behind
+        // that are read into kf.  In the order in which it is to be issued: between two matrix instructions, 32 cycles each, stand vector instructions that
+        // depend on neither.  extra(x): what else goes in front of output x.
+        auto half_block = [&](int b, int half, f32x16& s, float& top, const PageScale& now, auto extra) {
+            constexpr int SCORES = D / 16, OUTPUTS = D / 32 * 2;
+            u32x4 w[2];
+            f32x16 next;
+            float sum = 0.f;
+            const float shift = now.log_values - m;
 #pragma unroll
-        for (int i = 0; i < kRaw - 1; ++i) issue(i);
-        // steps 0 and 1
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 3) * LOADS) : "memory");
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (D == 128 || wave < 2) {
-                const u32x4 x = raw_keys(i);
-                put_keys(i, widen8(x[0], x[1]), widen8(x[2], x[3]));
-            }
-            if (D == 128 || wave >= 2) {
-                u32x4 x = raw_values(i);
-                clean_values(i, x);
-                put_values(i, widen8(x[0], x[1]), widen8(x[2], x[3]));
-            }
-        }
-        lds_barrier();
-        f32x16 s[CG];
-        Scale sc = scale_of(0);
-        {
-            bf16x8 kf[D / 16];
-            float top[CG];
-            read_keys(0, kf);
-            scores(kf, s);
-#pragma unroll
-            for (int c = 0; c < CG; ++c) {
-                in_vectors(s[c]);
-                top[c] = largest(s[c]);
-            }
-            settle(0, s, top, sc);
-        }
-        for (int i = 0; i < steps; ++i) {
-            // the codes of step i + 2 have come, and nobody reads the stages that they go to any more
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 4) * LOADS) : "memory");
-            const Scale now = sc;
-            if (i + kRaw - 1 >= ids_base + 64 && i + 1 < steps) fetch_ids(i + 1);
-            issue(i + kRaw - 1);
-            // A round in the order in which it is to be issued: between two matrix instructions, 32 cycles each, stand vector instructions of about as
-            // long that depend on neither.
-            constexpr int PAIRS = 8 * CG, SCORES = D / 16 * CG, OUTPUTS = D / 32 * 2 * CG, AHEAD = PAIRS / 4;
-            bf16x8 kf[D / 16], vf[D / 32][2];
-            u32x4 w[CG][2];
-            f32x16 next[CG];
-            float top[CG], shift[CG], sum[CG];
-            const unsigned char *keys = lds.keys[(i + 1) % kKeyStages], *values = lds.values[i % kValueStages];
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) kf[k] = *reinterpret_cast<const bf16x8*>(keys + ((2 * k + h) * kStep + (r ^ (4 * (k & 3)))) * 16);
-            u32x4 raw = raw_keys(i + 2), raw_v = D == 128 ? raw_values(i + 2) : raw;
-            sc = scale_of(min(i + 1, steps - 1));
-#pragma unroll
-            for (int c = 0; c < CG; ++c) {
-                shift[c] = now.log_values - m[c];
-                sum[c] = 0.f;
-#pragma unroll
-                for (int v = 0; v < 16; ++v) next[c][v] = 0.f;
-            }
+            for (int v = 0; v < 16; ++v) next[v] = 0.f;
             __builtin_amdgcn_sched_barrier(0);
-            // Two weights of the step, their sum as they are rounded.
-            auto pair = [&](int x) {
-                const int c = x / 8, q = x % 8;
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * q], now.factor, shift[c])), p1 = __builtin_amdgcn_exp2f(fmaf(s[c][2 * q + 1], now.factor, shift[c]));
+            // Two weights, and their sum as they are rounded.
+            auto pair = [&](int q) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * q], now.keys, shift)), p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * q + 1], now.keys, shift));
                 const bf16x2 p = __builtin_convertvector(f32x2{p0, p1}, bf16x2);
-                w[c][q / 4][q % 4] = __builtin_bit_cast(uint32_t, p);
-                sum[c] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, p), s16x2{0x3F80, 0x3F80}, sum[c], false);
+                w[q / 4][q % 4] = __builtin_bit_cast(uint32_t, p);
+                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, p), s16x2{0x3F80, 0x3F80}, sum, false);
             };
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) pair(x);  // (while the keys come from LDS)
-            if (D == 128 || wave >= 2) clean_values(i + 2, raw_v);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
             for (int x = 0; x < SCORES; ++x) {
-                next[x % CG] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x / CG], qf[x % CG][x / CG], next[x % CG], 0, 0, 0);
+                next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], qf[x], next, 0, 0, 0);
+                read_value(b, half, x);
 #pragma unroll
-                for (int y = AHEAD + (PAIRS - AHEAD) * x / SCORES; y < AHEAD + (PAIRS - AHEAD) * (x + 1) / SCORES; ++y) pair(y);
-                const int z = x - SCORES / 2;  // the values, in the second half
-                if (z >= 0) {
-#pragma unroll
-                    for (int y = D / 16 * z / (SCORES / 2); y < D / 16 * (z + 1) / (SCORES / 2); ++y)
-                        vf[y % (D / 32)][y / (D / 32)] = *reinterpret_cast<const bf16x8*>(values + ((2 * h + y / (D / 32)) * D + y % (D / 32) * 32 + r) * 16);
-                }
+                for (int y = 8 * x / SCORES; y < 8 * (x + 1) / SCORES; ++y) pair(y);
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int c = 0; c < CG; ++c) l[c] += sum[c] * now.per_value;
-            u32x4 wide[4];
+            l += sum * now.per_value;
 #pragma unroll
             for (int x = 0; x < OUTPUTS; ++x) {
-                const int c = x % CG, t = x / CG % (D / 32), j = x / CG / (D / 32);
-                o[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][j], __builtin_bit_cast(bf16x8, w[c][j]), o[c][t], 0, 0, 0);
+                const int t = x % (D / 32), j = x / (D / 32);
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][j], __builtin_bit_cast(bf16x8, w[j]), o[t], 0, 0, 0);
+                read_key(b + 1, half, x);
+                extra(x);
 #pragma unroll
-                for (int y = 16 * CG * x / OUTPUTS; y < 16 * CG * (x + 1) / OUTPUTS; ++y) {  // the scores out of the accumulators, and the largest
-                    float z = next[y / 16][y % 16];
-                    asm("" : "+v"(z));
-                    s[y / 16][y % 16] = z;
-                    top[y / 16] = y % 16 == 0 ? z : fmaxf(top[y / 16], z);
-                }
-                if (x % (OUTPUTS / 4) == OUTPUTS / 4 - 1) {  // the codes of step i + 2
-                    const int y = x / (OUTPUTS / 4);
-                    wide[y] = y < 2 ? widen8(raw[2 * y], raw[2 * y + 1]) : widen8(raw_v[2 * y - 4], raw_v[2 * y - 3]);
-                }
+                for (int y = 16 * x / OUTPUTS; y < 16 * (x + 1) / OUTPUTS; ++y) top = y == 0 ? next[y] : fmaxf(top, next[y]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (D == 128 || wave < 2) put_keys(i + 2, wide[0], wide[1]);
-            if (D == 128 || wave >= 2) put_values(i + 2, wide[2], wide[3]);
-            if (threadIdx.x == 0) lds.bad[(i + 3) % 4] = 0u;
+            s = next;
+        };
+        static_assert(D / 16 == D / 32 * 2, "as many scores as outputs");
+
+        if (threadIdx.x < 8) (&lds.bad[0][0])[threadIdx.x] = 0u;
+        {
+            const int id = page_of(threadIdx.x);
+            entry(threadIdx.x, id, a.scales[(int64_t)id * a.n_kv + kvh]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kRaw; ++j) issue(j, id_of(j), id_of(j - 1));
+        // the keys of blocks 0 and 1, the values of block 0
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 2) * (BOTH ? 2 : 1)) : "memory");
+        {
+            u32x4 x = raw_keys(0);
+            put_keys(0, widen8(x[0], x[1]), widen8(x[2], x[3]));
+            x = raw_keys(1);
+            put_keys(1, widen8(x[0], x[1]), widen8(x[2], x[3]));
+            x = raw_values(1);
+            clean(0, x);
+            put_values(0, widen8(x[0], x[1]), widen8(x[2], x[3]));
+        }
+        lds_barrier();
+        int id_keys = id_of(kRaw), id_values = id_of(kRaw - 1);
+        f32x16 s;
+        float top = 0.f;
+        PageScale now = entry_of(0, h).scale;
+        if (!idle) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                read_key(0, 0, k);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[k], s, 0, 0, 0);
+            }
+            settle(0, 0, s, largest(s), now);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) read_key(0, 1, k);
+        }
+        lds_barrier();  // the keys of block 0 have been read, and those of block 2 may take their place
+        int window_id = 0;
+        f32x2 window_scale = {0.f, 0.f};
+        for (int b = 0; b < blocks; ++b) {
+            // the keys of block b + 2 and the values of block b + 1 have come, and nobody reads the stages that they go to any more
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 3) * (BOTH ? 2 : 1)) : "memory");
+            const int behind = b % kWindow;
+            if (behind <= 2 && b >= kWindow) {  // the pages of the next window but one, in three rounds
+                const int x = (b / kWindow + 1) * kWindow * 4 + (int)threadIdx.x;
+                if (threadIdx.x < kWindow * 4) {
+                    if (behind == 0) window_id = page_of(x);
+                    else if (behind == 1) window_scale = a.scales[(int64_t)window_id * a.n_kv + kvh];
+                    else entry(x, window_id, window_scale);
+                }
+            }
+            u32x4 rk = raw_keys(b + 2), rv = raw_values(b + 2);
+            const PageScale then = entry_of(b, 2 + h).scale, after = entry_of(min(b + 1, blocks - 1), h).scale;
+            clean(b + 1, rv);
+            u32x4 wide[4];
+            if (!idle) {
+                half_block(b, 0, s, top, now, [&](int x) {
+                    if (x == 1) wide[0] = widen8(rk[0], rk[1]);
+                    if (x == 3) wide[1] = widen8(rk[2], rk[3]);
+                });
+                settle(b, 1, s, top, then);
+                half_block(b, 1, s, top, then, [&](int x) {
+                    if (x == 1) wide[2] = widen8(rv[0], rv[1]);
+                    if (x == 3) wide[3] = widen8(rv[2], rv[3]);
+                });
+            } else {
+                wide[0] = widen8(rk[0], rk[1]);
+                wide[1] = widen8(rk[2], rk[3]);
+                wide[2] = widen8(rv[0], rv[1]);
+                wide[3] = widen8(rv[2], rv[3]);
+            }
+            put_keys(b + 2, wide[0], wide[1]);
+            put_values(b + 1, wide[2], wide[3]);
+            issue(b + kRaw, id_keys, id_values);
+            id_keys = id_of(b + kRaw + 1);
+            id_values = id_of(b + kRaw);
+            if (threadIdx.x < 2) lds.bad[(b + 3) % 4][threadIdx.x] = 0u;
             lds_barrier();
-            if (i + 1 < steps) settle(i + 1, s, top, sc);
+            now = after;
+            if (!idle && b + 1 < blocks) settle(b + 1, 0, s, top, now);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no LDS fill may outlive the workgroup
     }
-#pragma unroll
-    for (int c = 0; c < CG; ++c) {
-        l[c] += __shfl_xor(l[c], 32);
-        if (!stored[c]) continue;
-        const int t0 = (wave * CG + c) * 32 + r, col = col0 + t0, row = col / g;
-        if (it.parts > 1) {
-            const int64_t place = kvh * parts.places + it.place + t0;
-#pragma unroll
-            for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    *reinterpret_cast<f32x4*>(parts.o + place * D + t * 32 + b * 8 + h * 4) = f32x4{o[c][t][4 * b], o[c][t][4 * b + 1], o[c][t][4 * b + 2], o[c][t][4 * b + 3]};
-            if (h == 0) parts.ml[place] = f32x2{m[c], l[c]};
-            continue;
-        }
-        const float inv = it.broken ? 0.f : 1.0f / l[c];
-        bf16_t* orow = a.out + (int64_t)(it.row0 + row) * a.ld_o + (int64_t)(kvh * g + col - row * g) * D;
+    l += __shfl_xor(l, 32);
+    if (tcol >= ncols) return;
+    if (it.parts > 1) {
+        const int64_t place = kvh * parts.places + it.place + tcol;
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const f32x4 x = {o[c][t][4 * b] * inv, o[c][t][4 * b + 1] * inv, o[c][t][4 * b + 2] * inv, o[c][t][4 * b + 3] * inv};
-                *reinterpret_cast<bf16x4*>(orow + t * 32 + b * 8 + h * 4) = __builtin_convertvector(x, bf16x4);
-            }
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<f32x4*>(parts.o + place * D + t * 32 + b * 8 + h * 4) = f32x4{o[t][4 * b], o[t][4 * b + 1], o[t][4 * b + 2], o[t][4 * b + 3]};
+        if (h == 0) parts.ml[place] = f32x2{m, l};
+        return;
     }
+    const float inv = it.broken ? 0.f : 1.0f / l;
+    bf16_t* orow = a.out + (int64_t)(it.row0 + row) * a.ld_o + (int64_t)(kvh * g + col - row * g) * D;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 x = {o[t][4 * b] * inv, o[t][4 * b + 1] * inv, o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv};
+            *reinterpret_cast<bf16x4*>(orow + t * 32 + b * 8 + h * 4) = __builtin_convertvector(x, bf16x4);
+        }
 }
 
+// Threads of a workgroup: four waves where there are stream units only, two workgroups to a compute unit, eight with tiles.
+template <bool TILES>
+constexpr int kThreads = TILES ? 512 : 256;
+
 template <int D, bool TILES>
-__global__ __launch_bounds__(256, TILES ? 1 : 2) void attention8_kernel(Attn8Args a) {
+__global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Args a) {
     // (one LDS object: with a second one the compiler waits for all loads into the ring before it reads from it)
     extern __shared__ __attribute__((aligned(1024))) unsigned char attn8_lds[];
     const int kvh = blockIdx.x % a.n_kv;
@@ -874,9 +842,8 @@ __global__ __launch_bounds__(256, TILES ? 1 : 2) void attention8_kernel(Attn8Arg
     }
     if (it.parts > 1 && it.part == 0 && kvh == 0 && threadIdx.x == 0)
         parts.rec[it.cut_tile] = Record{it.row0, it.n, it.tile, it.width, it.place, it.step, it.parts, 0};
-    if (!TILES || it.width == kStreamCols) stream_unit<D, TILES>(a, it, parts, kvh, *reinterpret_cast<StreamLds<D>*>(attn8_lds));
-    else if (it.width == kHalfCols) tile_unit<D, 1>(a, it, parts, kvh, *reinterpret_cast<TileLds<D>*>(attn8_lds));
-    else tile_unit<D, 2>(a, it, parts, kvh, *reinterpret_cast<TileLds<D>*>(attn8_lds));
+    if (!TILES || it.width == kStreamCols) stream_unit<D, kThreads<TILES> / 64>(a, it, parts, kvh, *reinterpret_cast<StreamLds<D, kThreads<TILES> / 64>*>(attn8_lds));
+    else tile_unit<D>(a, it, parts, kvh, *reinterpret_cast<TileLds<D>*>(attn8_lds));
 }
 
 // The partial results of all tiles joined, in order of the parts: a work item is (record, KV head, 1024 / D columns), a thread per four dims
@@ -957,9 +924,9 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
     if (a.num_seqs > 64) attention8_plan_kernel<TILES><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
-    int lds = sizeof(StreamLds<D>);
+    int lds = sizeof(StreamLds<D, kThreads<TILES> / 64>);
     if (TILES) {
-        lds = sizeof(TileLds<D>) > sizeof(StreamLds<D>) ? sizeof(TileLds<D>) : sizeof(StreamLds<D>);
+        lds = sizeof(TileLds<D>) > lds ? sizeof(TileLds<D>) : lds;
         static std::atomic<uint64_t> allowed{0};  // devices on which this kernel may use the LDS that it asks for
         int dev = 0;
         hipError_t e = hipGetDevice(&dev);
@@ -970,7 +937,7 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
             if (dev < 64) allowed.fetch_or(1ull << dev);
         }
     }
-    attention8_kernel<D, TILES><<<(unsigned)(units * a.n_kv), 256, lds, stream>>>(a);
+    attention8_kernel<D, TILES><<<(unsigned)(units * a.n_kv), kThreads<TILES>, lds, stream>>>(a);
     // no sequence can be cut whose table has no more pages than the fewest blocks of a part
     if (a.table_stride > kBlock / kPage * kMinShare) attention8_merge_kernel<D, TILES><<<kMergeGroups, 256, 0, stream>>>(a);
     return hipGetLastError();
