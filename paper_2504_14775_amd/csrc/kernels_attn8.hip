@@ -609,7 +609,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             if (has_keys) __builtin_amdgcn_global_load_lds((gptr_t)(a.k_pool + id_keys * page_step + piece_off), (lptr_t)to, 16, 0, 0);
             if (has_values) __builtin_amdgcn_global_load_lds((gptr_t)(a.v_pool + id_values * page_step + piece_off), (lptr_t)(to + (BOTH ? kBlock * D : 0)), 16, 0, 0);
         };
-        auto id_of = [&](int j) { return __builtin_amdgcn_readfirstlane(entry_of(min(max(j, 0), blocks - 1), page).id); };
+        auto id_of = [&](int j) { return entry_of(min(max(j, 0), blocks - 1), page).id; };  // (the same for the wave; read a round before it is wanted)
         auto raw_keys = [&](int j) { return *reinterpret_cast<const u32x4*>(&lds.raw[j % kRaw][0][0] + threadIdx.x * 16); };  // which have come
         auto raw_values = [&](int j) { return *reinterpret_cast<const u32x4*>(&lds.raw[j % kRaw][0][0] + threadIdx.x * 16 + (BOTH ? kBlock * D : 0)); };
         // Values that are no numbers may reach the columns that see them only: where not all rows see all keys they are emptied, and the key's scores are
@@ -676,8 +676,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             vf[x % (D / 32)][x / (D / 32)] = *reinterpret_cast<const bf16x8*>(lds.values[b % kValueStages][half] + ((2 * h + x / (D / 32)) * D + x % (D / 32) * 32 + r) * 16);
         };
         // One half, of block b: its weights and outputs from the scores s, and the scores of the next one, whose keys are in kf, into s; the keys of the one behind
-        // that are read into kf.  In the order in which it is to be issued: between two matrix instructions, 32 cycles each, stand vector instructions that
-        // depend on neither.  extra(x): what else goes in front of output x.
+        // that are read into kf.  extra(x): what else goes behind output x.
         auto half_block = [&](int b, int half, f32x16& s, float& top, const PageScale& now, auto extra) {
             constexpr int SCORES = D / 16, OUTPUTS = D / 32 * 2;
             u32x4 w[2];
@@ -686,7 +685,6 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             const float shift = now.log_values - m;
 #pragma unroll
             for (int v = 0; v < 16; ++v) next[v] = 0.f;
-            __builtin_amdgcn_sched_barrier(0);
             // Two weights, and their sum as they are rounded.
             auto pair = [&](int q) {
                 const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * q], now.keys, shift)), p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * q + 1], now.keys, shift));
@@ -700,7 +698,6 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 read_value(b, half, x);
 #pragma unroll
                 for (int y = 8 * x / SCORES; y < 8 * (x + 1) / SCORES; ++y) pair(y);
-                __builtin_amdgcn_sched_barrier(0);
             }
             l += sum * now.per_value;
 #pragma unroll
@@ -711,7 +708,6 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 extra(x);
 #pragma unroll
                 for (int y = 16 * x / OUTPUTS; y < 16 * (x + 1) / OUTPUTS; ++y) top = y == 0 ? next[y] : fmaxf(top, next[y]);
-                __builtin_amdgcn_sched_barrier(0);
             }
             s = next;
         };
@@ -724,7 +720,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kRaw; ++j) issue(j, id_of(j), id_of(j - 1));
+        for (int j = 0; j < kRaw; ++j) issue(j, __builtin_amdgcn_readfirstlane(id_of(j)), __builtin_amdgcn_readfirstlane(id_of(j - 1)));
         // the keys of blocks 0 and 1, the values of block 0
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 2) * (BOTH ? 2 : 1)) : "memory");
         {
@@ -768,7 +764,11 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                     else entry(x, window_id, window_scale);
                 }
             }
+            issue(b + kRaw, __builtin_amdgcn_readfirstlane(id_keys), __builtin_amdgcn_readfirstlane(id_values));
             u32x4 rk = raw_keys(b + 2), rv = raw_values(b + 2);
+            id_keys = id_of(b + kRaw + 1);
+            id_values = id_of(b + kRaw);
+            if (threadIdx.x < 2) lds.bad[(b + 3) % 4][threadIdx.x] = 0u;
             const PageScale then = entry_of(b, 2 + h).scale, after = entry_of(min(b + 1, blocks - 1), h).scale;
             clean(b + 1, rv);
             u32x4 wide[4];
@@ -777,6 +777,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                     if (x == 1) wide[0] = widen8(rk[0], rk[1]);
                     if (x == 3) wide[1] = widen8(rk[2], rk[3]);
                 });
+                put_keys(b + 2, wide[0], wide[1]);
                 settle(b, 1, s, top, then);
                 half_block(b, 1, s, top, then, [&](int x) {
                     if (x == 1) wide[2] = widen8(rv[0], rv[1]);
@@ -788,12 +789,8 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 wide[2] = widen8(rv[0], rv[1]);
                 wide[3] = widen8(rv[2], rv[3]);
             }
-            put_keys(b + 2, wide[0], wide[1]);
+            if (idle) put_keys(b + 2, wide[0], wide[1]);
             put_values(b + 1, wide[2], wide[3]);
-            issue(b + kRaw, id_keys, id_values);
-            id_keys = id_of(b + kRaw + 1);
-            id_values = id_of(b + kRaw);
-            if (threadIdx.x < 2) lds.bad[(b + 3) % 4][threadIdx.x] = 0u;
             lds_barrier();
             now = after;
             if (!idle && b + 1 < blocks) settle(b + 1, 0, s, top, now);
