@@ -8,10 +8,11 @@
 // both in the one multiply-add that the exponential's argument takes anyway; a lane holds keys of one page only, so that its part of the sum of
 // the weights is that of p s_v times 1 / s_v.
 //
-// Up to 16 columns (decode rows) the keys are a stream from HBM: stream_unit.  More go in tiles whose keys pass through LDS: tile_unit.
-// The keys of long sequences are cut into parts, planned on the device, and the parts' results joined by a second launch.
+// Up to 16 columns (decode rows) the keys are a stream from HBM: stream_wave.  More go in tiles whose keys pass through LDS: tile_unit.
+// The keys of long sequences are shared among waves, or units, by a plan made on the device, and the parts' results joined by a second launch.
 #include "cache8.h"
 
+#include <algorithm>
 #include <atomic>
 
 namespace {
@@ -25,32 +26,34 @@ constexpr float kNegBig = -1.0e30f;
 constexpr int kBlock = 64;  // keys, four pages
 
 // ---- the plan --------------------------------------------------------------------------------------------------------------
-
-// Columns of a tile by the columns of a sequence.
+//
+// The lengths stand on the device.  Sequences of up to 16 columns are streams: their blocks of 64 keys, one sequence behind the other, are dealt in
+// equal runs to the waves of some workgroups.  The others have tiles of 256 columns, each a unit of work of its own or, where there are few of
+// them, several, which share its keys.  The stream's workgroups are the first of the launch.
 constexpr int kStreamCols = 16, kTileCols = 256;
-__host__ __device__ constexpr int tile_cols(int64_t cols) { return cols <= kStreamCols ? kStreamCols : kTileCols; }
 
-// A unit of work: a part of the keys for the columns of one tile of a sequence.
+// A unit of work of a tile: a part of its keys.
 struct Unit {
     int32_t seq, row0, n, c;
-    int32_t width;               // tile_cols()
     int32_t tile, part, parts;
-    bool broken;                 // the sequence breaks a rule: zeros
     int32_t place;               // parts > 1: of its partial results, in columns
     int32_t step;                // and from a part's to the next one's
     int32_t cut_tile;            // and of its tile among those with such units
 };
 
-constexpr int kMinShare = 6;     // fewest blocks worth a workgroup
-// Workgroups that the keys are cut into, over all KV heads.
+constexpr int kMinShare = 6;     // fewest blocks worth a unit
+constexpr int kWhole = 6;        // most blocks of a stream that is never cut
+constexpr int kGroups = 256;     // workgroups that run at one time: one on each compute unit
+constexpr int kStreamGroups = 256;
+// All of these are for each KV head.
+__host__ __device__ constexpr int per_head(int total, int n_kv) { return total / n_kv > 0 ? total / n_kv : 1; }
 template <bool TILES>
-__host__ __device__ constexpr int target_units(int n_kv) { return (TILES ? 512 : 768) / n_kv > 0 ? (TILES ? 512 : 768) / n_kv : 1; }
-// Columns of partial results, and tiles that have them.  A sequence is cut where it has more blocks than a share, into at most ceil(blocks /
+__host__ __device__ constexpr int max_workers(int n_kv) { return per_head(TILES ? kGroups : kStreamGroups, n_kv); }
+__host__ __device__ constexpr int target_units(int n_kv) { return per_head(2 * kGroups, n_kv); }
+// Tiles with partial results and columns of these.  A tile is cut where its sequence has more blocks than a share, into at most ceil(blocks /
 // share) parts; the shares of all are at least half their blocks by the target (seq_plan: twice the weight is at least the blocks).
-template <bool TILES>
-__host__ __device__ constexpr int max_cut_tiles(int n_kv) { return 2 * target_units<TILES>(n_kv); }
-template <bool TILES>
-__host__ __device__ constexpr int max_places(int n_kv) { return 4 * target_units<TILES>(n_kv) * (TILES ? kTileCols : kStreamCols); }
+__host__ __device__ constexpr int max_cut_tiles(int n_kv) { return 2 * target_units(n_kv); }
+__host__ __device__ constexpr int max_places(int n_kv) { return 4 * target_units(n_kv) * kTileCols; }
 
 // The blocks that the rows i0 .. i1 of a sequence see, counted without those between the first tokens that stay and the window.
 struct Seen {
@@ -65,31 +68,37 @@ __device__ __forceinline__ Seen seen_blocks(const Attn8Args& a, int c, int i0, i
     const int sink = min(a.sinks / kBlock + (a.sinks % kBlock > 0), low);
     return Seen{sink, low - sink, high - low + 1 + sink};
 }
+// Most blocks that `rows` rows of a sequence see of its own.
+__host__ __device__ inline int64_t most_blocks(int64_t own, int64_t rows, int window, int sinks) {
+    const int64_t near = (window + rows + kBlock - 2) / kBlock + 1 + sinks / kBlock + 1;
+    return window > 0 && near < own ? near : own;
+}
 
 struct SeqPlan {
-    int32_t row0, n, c, width, tiles, blocks;  // blocks: of the tile that sees most, at most
-    float weight;                              // tiles times about their blocks, at least half of tiles * blocks
-    bool broken, unordered;
+    int32_t row0, n, c, stream;       // stream: its blocks, or none
+    int32_t tiles, blocks;            // blocks: of the tile that sees most, at most
+    float weight;                     // tiles times about their blocks, at least half of tiles * blocks
+    bool broken, unordered;           // a rule: zeros
 };
 __device__ __forceinline__ SeqPlan seq_plan(const Attn8Args& a, int s) {
-    SeqPlan p{0, 0, 0, kStreamCols, 0, 0, 0.f, true, false};
+    SeqPlan p{0, 0, 0, 0, 0, 0, 0.f, false, false};
     if (s >= a.num_seqs) return p;
     const int r0 = a.row_start[s], r1 = a.row_start[s + 1], g = a.n_q / a.n_kv;
     p.c = a.cached_len[s];
     p.unordered = r0 < 0 || r1 < r0 || r1 > a.num_rows;
     p.row0 = r0;
     p.n = p.unordered ? 0 : r1 - r0;
+    if (p.n == 0) return p;
     p.broken = p.n > a.max_new || p.c < 0 || (int64_t)p.c + p.n > min((int64_t)a.table_stride * kPage, (int64_t)kMaxPositions);
-    p.width = (int64_t)a.max_new * g <= kStreamCols ? kStreamCols : tile_cols((int64_t)p.n * g);  // (a call of short sequences has stream units only)
-    p.tiles = (p.n * g + p.width - 1) / p.width;  // (num_rows * g fits 31 bits: the launcher)
-    if (p.broken || p.n == 0) return p;
-    const int all = (p.c + p.n - 1) / kBlock + 1;
-    p.blocks = all;
-    if (a.window > 0) {
-        const int64_t near = ((int64_t)a.window + p.width / g + 1 + kBlock - 2) / kBlock + 1 + a.sinks / kBlock + 1;
-        p.blocks = (int)min((int64_t)all, near);
+    if (p.broken) return p;
+    const int64_t cols = (int64_t)p.n * g;
+    if (cols <= kStreamCols) {
+        p.stream = seen_blocks(a, p.c, 0, p.n - 1).blocks;
+    } else {
+        p.tiles = (int)((cols + kTileCols - 1) / kTileCols);
+        p.blocks = (int)most_blocks((p.c + p.n - 1) / kBlock + 1, kTileCols / g + 2, a.window, a.sinks);
+        p.weight = (float)p.tiles * (p.tiles > 1 ? fminf((float)p.blocks, (2.f * p.c + p.n) * (0.5f / kBlock) + 2.f) : (float)p.blocks);
     }
-    p.weight = (float)p.tiles * (p.tiles > 1 ? min((float)p.blocks, (2.f * p.c + p.n) * (0.5f / kBlock) + 2.f) : (float)p.blocks);
     return p;
 }
 
@@ -107,19 +116,28 @@ __device__ __forceinline__ void scan_wave(T& x) {
     scan_step<T, 0x142, 0xa>(x);  // the last lane of a row to the next row, of both to the upper half
     scan_step<T, 0x143, 0xc>(x);
 }
-__device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-__device__ __forceinline__ float lane_value(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
+template <typename T>
+__device__ __forceinline__ T lane_value(T x, int lane) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
 
-// Blocks of a share.  (The sum is exact up to 2^24, and by 1e-4 of itself more from there on, which is more than the roundings of its additions,
-// 2^-24 of it each, take away: kMaxAttn8Seqs / 4096 of a lane and 15 over lanes and runs.)
+// What follows from the sums over all sequences.  A block of a tile takes about three times a stream's share of the memory for one.  (The sums are
+// exact up to 2^24, and by 1e-4 of themselves more from there on where that counts, in the share: more than the roundings of their additions, 2^-24 of
+// it each, take away, kMaxAttn8Seqs / 4096 of a lane and 15 over lanes and runs.)
 static_assert(kMaxAttn8Seqs / (64 * 64) + 15 < 16777216 / 10000, "the sum of all weights");
+constexpr float kTileCost = 3.f;
+constexpr int kFewBlocks = 2;    // of a wave of the stream, where there are so few
 template <bool TILES>
-__device__ __forceinline__ int share_of(float total, int n_kv) {
-    const float target = (float)target_units<TILES>(n_kv);
-    const float even = total < 16777216.f ? ceilf(total / target) : total / target * 1.0001f + 1.f;
+__device__ __forceinline__ int workers_of(float stream, float tiles, int n_kv) {
+    if (!(stream > 0.f)) return 0;
+    const int most = max_workers<TILES>(n_kv);
+    const float fair = TILES ? rintf(stream / (stream + kTileCost * tiles) * (float)most) : (float)most;
+    return (int)fmaxf(fminf(fair, ceilf(stream / (float)(kFewBlocks * (TILES ? 8 : 4)))), 1.f);
+}
+__device__ __forceinline__ int share_of(float tiles, int n_kv) {
+    const float target = (float)target_units(n_kv);
+    const float even = tiles < 16777216.f ? ceilf(tiles / target) : tiles / target * 1.0001f + 1.f;
     return (int)fminf(fmaxf(even, (float)kMinShare), 1e9f);
 }
-// The units of a sequence.  They are in order of their size, in quarters of a share, so that the last workgroups to start are short ones;
+// The units of a sequence's tiles.  They are in order of their size, in quarters of a share, so that the last workgroups to start are short ones;
 // in a quarter by sequence, part and tile, the last tiles, which see most, first.
 __device__ __forceinline__ int split_seq(const SeqPlan& q, int share, int& parts, int& quarter) {
     parts = max(1, (q.blocks - 1) / share + 1);
@@ -131,7 +149,7 @@ __device__ __forceinline__ int split_seq(const SeqPlan& q, int share, int& parts
 // at place `before`.  places, cut_tiles: those of the sequences in front, on return of these too.
 __device__ __forceinline__ bool unit_of(const SeqPlan& q, int parts, int units, int mine, int before, int place, int s0, int& places, int& cut_tiles, Unit& u) {
     const bool cut = parts > 1;
-    int cut_upto = cut ? units * q.width : 0, tiles_upto = cut ? q.tiles : 0;
+    int cut_upto = cut ? units * kTileCols : 0, tiles_upto = cut ? q.tiles : 0;
     scan_wave(cut_upto);
     scan_wave(tiles_upto);
     const int at = place - before;
@@ -142,13 +160,11 @@ __device__ __forceinline__ bool unit_of(const SeqPlan& q, int parts, int units, 
         u.row0 = lane_value(q.row0, l);
         u.n = lane_value(q.n, l);
         u.c = lane_value(q.c, l);
-        u.width = lane_value(q.width, l);
-        u.broken = lane_value((int)q.broken, l);
         u.parts = lane_value(parts, l);
         u.part = i / tiles;
         u.tile = tiles - 1 - (i - u.part * tiles);
-        u.step = tiles * u.width;
-        u.place = places + lane_value(cut_upto - (cut ? units * q.width : 0), l) + u.part * u.step + u.tile * u.width;
+        u.step = tiles * kTileCols;
+        u.place = places + lane_value(cut_upto - (cut ? units * kTileCols : 0), l) + u.part * u.step + u.tile * kTileCols;
         u.cut_tile = cut_tiles + lane_value(tiles_upto - (cut ? q.tiles : 0), l) + u.tile;
         return true;
     }
@@ -159,24 +175,42 @@ __device__ __forceinline__ bool unit_of(const SeqPlan& q, int parts, int units, 
 
 // Up to 64 sequences every wave works the plan out for itself, all of them with the same arithmetic, without LDS and barriers.  More are
 // planned by a launch of their own, which cuts them into up to 64 runs of whole waves and leaves what stands in front of each; a wave then looks
-// at the runs and at one of them.
+// at the runs and at some of their sequences.
 constexpr int kPlanRuns = 64;
 struct Plan {
-    int32_t share, units;               // units: none where the rows break their order
+    int32_t share, units, workers;      // units, workers: none where the rows break their order
+    int32_t broken;                     // whether any sequence breaks a rule
+    int64_t stream;                     // blocks of all streams
+    int64_t stream_before[kPlanRuns];   // in front of a run
     int32_t start[4];                   // place of the first unit of a quarter
     int32_t before[4][kPlanRuns];       // place of a run's first unit in a quarter
     int32_t places[kPlanRuns], cut_tiles[kPlanRuns];  // in front of a run
 };
 __host__ __device__ inline int plan_run(int num_seqs) { return (num_seqs + 64 * kPlanRuns - 1) / (64 * kPlanRuns) * 64; }  // sequences
 
-// false behind the last unit.  cut_tiles: behind it the number of tiles whose keys are cut, or -1 where the plan's launch has written it.
+// The work of a workgroup's place: a worker of the stream, a unit of a tile, or none.
+struct Job {
+    int workers;          // of the stream
+    int64_t stream;       // blocks of all streams
+    bool is_unit;
+    Unit unit;
+    int cut_tiles;        // behind the last unit: tiles whose keys are cut, or -1 where the plan's launch has written it
+    bool broken;
+    SeqPlan seqs;         // up to 64 sequences: that of this lane
+};
 template <bool TILES>
-__device__ __forceinline__ bool find_unit(const Attn8Args& a, const Plan* plan, int place, Unit& u, int& cut_tiles) {
+__device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, int place, Job& j) {
     const int lane = threadIdx.x & 63;
     int places = 0;
+    j.is_unit = false;
+    j.cut_tiles = 0;
     if (a.num_seqs > 64) {
-        cut_tiles = -1;
-        if (place >= plan->units) return false;
+        j.workers = plan->workers;
+        j.stream = plan->stream;
+        j.broken = plan->broken;
+        j.cut_tiles = -1;
+        place -= j.workers;
+        if (!TILES || place < 0 || place >= plan->units) return;
         const int share = plan->share;
         const int quarter = (place >= plan->start[1]) + (place >= plan->start[2]) + (place >= plan->start[3]);
         const int first = plan->before[quarter][lane];
@@ -189,19 +223,35 @@ __device__ __forceinline__ bool find_unit(const Attn8Args& a, const Plan* plan, 
             const int units = split_seq(q, share, parts, its), mine = its == quarter ? units : 0;
             int x = mine;
             scan_wave(x);
-            if (unit_of(q, parts, units, mine, at + x - mine, place, s0, places, cut, u)) return true;
+            if (unit_of(q, parts, units, mine, at + x - mine, place, s0, places, cut, j.unit)) {
+                j.is_unit = true;
+                return;
+            }
             at += lane_value(x, 63);
         }
-        return false;
+        return;
     }
-    const SeqPlan p = seq_plan(a, lane);
-    cut_tiles = 0;
-    if (__any(p.unordered)) return false;  // rows in no order may belong to two sequences: the launch would have no place for their units
-    float total = p.weight;
-    scan_wave(total);
-    total = lane_value(total, 63);
+    j.seqs = seq_plan(a, lane);
+    j.broken = __any(j.seqs.broken);
+    uint32_t blocks = (uint32_t)j.seqs.stream;  // (64 times 2^25 at most)
+    scan_wave(blocks);
+    j.stream = lane_value(blocks, 63);
+    float tiles = 0.f;
+    if (TILES) {
+        tiles = j.seqs.weight;
+        scan_wave(tiles);
+        tiles = lane_value(tiles, 63);
+    }
+    j.workers = workers_of<TILES>((float)j.stream, tiles, a.n_kv);
+    if (__any(j.seqs.unordered)) {  // rows in no order may belong to two sequences
+        j.workers = 0;
+        j.broken = false;
+        return;
+    }
+    place -= j.workers;
+    if (!TILES || place < 0) return;
     int parts, quarter, before = 0, start = 0;
-    const int units = split_seq(p, share_of<TILES>(total, a.n_kv), parts, quarter);
+    const int units = split_seq(j.seqs, share_of(tiles, a.n_kv), parts, quarter);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         int x = quarter == c ? units : 0;
@@ -209,58 +259,80 @@ __device__ __forceinline__ bool find_unit(const Attn8Args& a, const Plan* plan, 
         if (quarter == c) before = start + x - units;
         start += lane_value(x, 63);
     }
-    return unit_of(p, parts, units, units, before, place, 0, places, cut_tiles, u);
+    j.is_unit = unit_of(j.seqs, parts, units, units, before, place, 0, places, j.cut_tiles, j.unit);
 }
 
 // One workgroup; wave w has the runs w, w + 16, ...
 template <bool TILES>
 __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan* plan, int32_t* count) {
-    __shared__ float totals[kPlanRuns];
+    __shared__ float totals[2][kPlanRuns];
+    __shared__ int64_t stream[kPlanRuns];
     __shared__ int sums[6][kPlanRuns];  // of a run: units of each quarter, places, tiles that are cut
-    __shared__ int any_unordered;
+    __shared__ int any_unordered, any_broken;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int len = plan_run(a.num_seqs);
     if (threadIdx.x < kPlanRuns) {
-        totals[threadIdx.x] = 0.f;
+        totals[0][threadIdx.x] = totals[1][threadIdx.x] = 0.f;
+        stream[threadIdx.x] = 0;
         for (int k = 0; k < 6; ++k) sums[k][threadIdx.x] = 0;
     }
-    if (threadIdx.x == 0) any_unordered = 0;
+    if (threadIdx.x == 0) any_unordered = any_broken = 0;
     __syncthreads();
     for (int run = wave; run < kPlanRuns && run * len < a.num_seqs; run += 16) {
         float total = 0.f;
-        bool unordered = false;
+        int64_t blocks = 0;
+        bool unordered = false, broken = false;
         for (int s0 = run * len; s0 < min((run + 1) * len, a.num_seqs); s0 += 64) {
             const SeqPlan q = seq_plan(a, s0 + lane);
             total += q.weight;
+            blocks += q.stream;
             unordered |= q.unordered;
+            broken |= q.broken;
         }
         scan_wave(total);
-        if (lane == 63) totals[run] = total;
+#pragma unroll
+        for (int by = 1; by < 64; by *= 2) blocks += __shfl_xor(blocks, by);
+        if (lane == 63) {
+            totals[0][run] = total;
+            stream[run] = blocks;
+        }
         if (unordered) any_unordered = 1;
+        if (broken) any_broken = 1;
     }
     __syncthreads();
-    float total = totals[lane];
+    float total = totals[0][lane];
     scan_wave(total);
-    const int share = share_of<TILES>(lane_value(total, 63), a.n_kv);
-    for (int run = wave; run < kPlanRuns && run * len < a.num_seqs; run += 16) {
-        int sum[6] = {0, 0, 0, 0, 0, 0};
-        for (int s0 = run * len; s0 < min((run + 1) * len, a.num_seqs); s0 += 64) {
-            const SeqPlan q = seq_plan(a, s0 + lane);
-            int parts, quarter;
-            const int units = split_seq(q, share, parts, quarter);
+    total = lane_value(total, 63);
+    const int share = share_of(total, a.n_kv);
+    if (TILES) {
+        for (int run = wave; run < kPlanRuns && run * len < a.num_seqs; run += 16) {
+            int sum[6] = {0, 0, 0, 0, 0, 0};
+            for (int s0 = run * len; s0 < min((run + 1) * len, a.num_seqs); s0 += 64) {
+                const SeqPlan q = seq_plan(a, s0 + lane);
+                int parts, quarter;
+                const int units = split_seq(q, share, parts, quarter);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) sum[c] += quarter == c ? units : 0;
-            sum[4] += parts > 1 ? units * q.width : 0;
-            sum[5] += parts > 1 ? q.tiles : 0;
-        }
+                for (int c = 0; c < 4; ++c) sum[c] += quarter == c ? units : 0;
+                sum[4] += parts > 1 ? units * kTileCols : 0;
+                sum[5] += parts > 1 ? q.tiles : 0;
+            }
 #pragma unroll
-        for (int k = 0; k < 6; ++k) {
-            scan_wave(sum[k]);
-            if (lane == 63) sums[k][run] = sum[k];
+            for (int k = 0; k < 6; ++k) {
+                scan_wave(sum[k]);
+                if (lane == 63) sums[k][run] = sum[k];
+            }
         }
+        __syncthreads();
     }
-    __syncthreads();
     if (wave > 0) return;
+    int64_t blocks = stream[lane];
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) {
+        const int64_t y = __shfl_up(blocks, by);
+        if (lane >= by) blocks += y;
+    }
+    plan->stream_before[lane] = lane * len < a.num_seqs ? blocks - stream[lane] : INT64_MAX;
+    const int64_t all_blocks = __shfl(blocks, 63);
     int start = 0;
 #pragma unroll
     for (int k = 0; k < 6; ++k) {
@@ -280,39 +352,57 @@ __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan
     if (lane == 0) {
         plan->share = share;
         plan->units = any_unordered ? 0 : start;
+        plan->workers = any_unordered ? 0 : workers_of<TILES>((float)all_blocks, total, a.n_kv);
+        plan->broken = any_unordered ? 0 : any_broken;
+        plan->stream = all_blocks;
     }
 }
 
 // ---- partial results ------------------------------------------------------------------------------------------------------
 //
-// Workspace: the plan of many sequences, a record per tile whose keys are cut, then per KV head and column of a part the reference and the sum,
-// then the unnormalised outputs.
+// Workspace: the plan of many sequences; the waves of the stream; a record per tile whose keys are cut; then per KV head and column of a part the
+// reference and the sum, then the unnormalised outputs, of the stream and of the tiles.  A wave of the stream has places for two streams that
+// are not its own alone: the one that its run begins with, and the one that it ends with.
+struct StreamRecord {       // of the stream that begins in a wave's run and goes on in the next one's
+    int32_t row0, cols, waves;  // waves: that have a part of it, or none
+    int32_t place;          // of the first part, in streams; those of the others are the first ones of their waves
+};
 struct Record {
-    int32_t row0, n, tile, width;
-    int32_t place, step, parts, pad;
+    int32_t row0, n, tile;
+    int32_t place, step, parts, pad[2];
 };
 struct Parts {
-    int32_t* count;  // records
+    int32_t* count;    // records
+    int32_t* waves;    // waves of the stream
     Plan* plan;
+    StreamRecord* stream;
     Record* rec;
-    f32x2* ml;       // [n_kv][places]
-    float* o;        // [n_kv][places][d]
-    int64_t places;
+    f32x2 *stream_ml, *ml;  // [n_kv][2 * max waves][16], [n_kv][places]
+    float *stream_o, *o;    // and [d]
+    int64_t max_waves, places;
 };
 template <bool TILES>
 __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d) {
-    t.places = max_places<TILES>(n_kv);
-    const size_t cols = (size_t)t.places * n_kv;
+    t.max_waves = max_workers<TILES>(n_kv) * (TILES ? 8 : 4);
+    t.places = TILES ? max_places(n_kv) : 0;
     char* p = (char*)base;
-    t.count = (int32_t*)p;
-    t.plan = (Plan*)(p + 256);
-    constexpr size_t head = 256 + (sizeof(Plan) + 255) / 256 * 256;
-    t.rec = (Record*)(p + head);
-    size_t off = head + (max_cut_tiles<TILES>(n_kv) * sizeof(Record) + 255) / 256 * 256;
-    t.ml = (f32x2*)(p + off);
-    off += (cols * 8 + 255) / 256 * 256;
-    t.o = (float*)(p + off);
-    return off + cols * d * 4;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char* at = p + off;
+        off += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    t.count = (int32_t*)take(256);
+    t.waves = t.count + 1;
+    t.plan = (Plan*)take(sizeof(Plan));
+    t.stream = (StreamRecord*)take(t.max_waves * sizeof(StreamRecord));
+    t.rec = (Record*)take(TILES ? max_cut_tiles(n_kv) * sizeof(Record) : 0);
+    const size_t stream_cols = (size_t)n_kv * 2 * t.max_waves * kStreamCols, cols = (size_t)n_kv * t.places;
+    t.stream_ml = (f32x2*)take(stream_cols * 8);
+    t.stream_o = (float*)take(stream_cols * d * 4);
+    t.ml = (f32x2*)take(cols * 8);
+    t.o = (float*)take(cols * d * 4);
+    return off;
 }
 
 // ---- common to both kinds of units -------------------------------------------------------------------------------------
@@ -343,193 +433,291 @@ struct PageScale {
     }
 };
 
-// ---- few columns -----------------------------------------------------------------------------------------------------------
+// ---- streams ---------------------------------------------------------------------------------------------------------------
 //
-// Each wave takes a run of the unit's blocks for all columns, operands straight to registers.  Matrix instructions of 16x16x32: the row 4q + i of
-// score tile t is slot 4t + i of page q, so that a lane of group G receives the 16 slots of page G.  An instruction that loads keys takes runs of
-// 256 bytes from each of the four pages, one that loads values the 16 slots of 16 dims of each.
+// Each wave takes a run of blocks for all columns of their sequences, operands straight to registers.  Matrix instructions of 16x16x32: the row
+// 4q + i of score tile t is slot 4t + i of page q, so that a lane of group G receives the 16 slots of page G.  An instruction that loads keys takes
+// runs of 256 bytes from each of the four pages, one that loads values the 16 slots of 16 dims of each.  The keys of the next block are asked for
+// when the scores of this one are made, its values when this one's outputs are, into the same registers; so there is always half a block on its way,
+// and the waves that share a compute unit hide each other's work.
+// A value that all lanes have, for the compiler to know.
+__device__ __forceinline__ int64_t of_wave(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+// Where the run of wave w begins.
+__device__ __forceinline__ int64_t run_begin(int64_t blocks, int waves, int w) { return of_wave((int64_t)((uint64_t)blocks * (uint32_t)w / (uint32_t)waves)); }
+
 template <int D>
-struct Frag {
-    u32x4 k[4][D / 64];  // [tile][64 dims]: row r = slot 4t + r % 4 of page r / 4, dims 16 (4p + G) ..
-    u32x4 v[D / 16];     // [16 dims]: dim 16b + r of page G
-};
-template <int D, int WAVES>
-struct StreamLds {
-    float o[WAVES][16][D + 4];
-    float m[WAVES][16], l[WAVES][16];
-};
-
-template <int D, int WAVES>
-__device__ __forceinline__ void stream_unit(const Attn8Args& a, const Unit& it, const Parts& parts, int kvh, StreamLds<D, WAVES>& join) {
+__device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, const Parts& parts, int kvh, int w, int waves) {
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, G = lane >> 4, g = a.n_q / a.n_kv;
-    const int cols = it.n * g;
-    const Seen seen = seen_blocks(a, it.c, 0, it.n - 1);
-    const int each = seen.blocks / it.parts, more = seen.blocks - each * it.parts;
-    const int first = it.broken ? 0 : it.part * each + min(it.part, more), last = it.broken ? 0 : first + each + (it.part < more);
-    const int run = (last - first + WAVES - 1) / WAVES;
-    const int b_begin = min(first + wave * run, last), b_end = min(b_begin + run, last);
-    const int last_page = max(it.c + it.n - 1, 0) / kPage;
-    const int32_t* bt = a.block_tables + (int64_t)it.seq * a.table_stride;
+    // The run.  A stream of few blocks belongs to the wave in whose run its last one lies.
+    const int64_t lo = run_begin(job.stream, waves, w), hi = run_begin(job.stream, waves, w + 1);
 
-    int ids_base = b_begin, ids = 0;  // pages of 16 blocks, one per lane, with their scales
-    PageScale ps;
-    auto fetch_ids = [&](int base) {
-        ids_base = base;
-        ids = min(max(bt[min(seen.actual(base + lane / 4) * 4 + lane % 4, last_page)], 0), a.num_blocks - 1);
-        ps.of(a.scales[(int64_t)ids * a.n_kv + kvh], a.scale_log2);
+    // 64 sequences, one per lane, of which those up to lane `at` have been dealt with; `upto` blocks up to the end of this lane's, counted from all.
+    SeqPlan q;
+    int s0 = 0, at = -1;
+    int64_t before = 0;   // in front of the 64
+    uint32_t upto = 0;
+    auto look = [&]() {
+        upto = (uint32_t)q.stream;
+        scan_wave(upto);
     };
-    auto load_block = [&](Frag<D>& f, int b) {
+    if (a.num_seqs > 64) {
+        const int64_t first = parts.plan->stream_before[lane];
+        const int run = __popcll(__ballot(first <= lo)) - 1;
+        s0 = run * plan_run(a.num_seqs);
+        before = of_wave(__shfl(first, run));
+        q = seq_plan(a, s0 + lane);
+    } else {
+        q = job.seqs;
+    }
+    look();
+
+    struct Segment {      // the blocks begin .. end - 1 of a sequence's
+        int seq, row0, n, c, begin, end, blocks;
+        int64_t start;    // of the sequence in the stream
+    };
+    auto next_segment = [&](Segment& seg) -> bool {
+        for (;;) {
+            uint64_t rest = __ballot(q.stream > 0 && before + (int64_t)upto > lo);
+            if (at >= 0) rest &= at >= 63 ? 0 : ~((2ull << at) - 1);
+            if (rest) {
+                at = __builtin_ctzll(rest);
+                seg.seq = s0 + at;
+                seg.row0 = lane_value(q.row0, at);
+                seg.n = lane_value(q.n, at);
+                seg.c = lane_value(q.c, at);
+                seg.blocks = lane_value(q.stream, at);
+                const int64_t end = before + (int64_t)lane_value(upto, at);
+                seg.start = end - seg.blocks;
+                if (seg.blocks <= kWhole) {
+                    if (end > hi) return false;
+                    seg.begin = 0;
+                    seg.end = seg.blocks;
+                    return true;
+                }
+                if (seg.start >= hi) return false;
+                seg.begin = (int)(seg.start < lo ? lo - seg.start : 0);
+                seg.end = (int)((end < hi ? end : hi) - seg.start);
+                if (seg.begin < seg.end) return true;
+                continue;
+            }
+            before += (int64_t)lane_value(upto, 63);
+            s0 += 64;
+            at = -1;
+            if (s0 >= a.num_seqs || before >= hi) return false;
+            q = seq_plan(a, s0 + lane);
+            look();
+        }
+    };
+    // Page ids, of 16 blocks from `base` on, one per lane, as they stand in the table.
+    auto table_ids = [&](const Segment& s, const Seen& seen, int base) {
+        return a.block_tables[(int64_t)s.seq * a.table_stride + min(seen.actual(base + lane / 4) * 4 + lane % 4, (s.c + s.n - 1) / kPage)];
+    };
+    // operands: keys [tile][64 dims], row r = slot 4t + r % 4 of page r / 4, dims 16 (4p + G) ..; values [16 dims], dim 16b + r of page G
+    u32x4 k[4][D / 64], v[D / 16];
+    bf16x8 qf[D / 64][2], qn[D / 64][2];  // queries of this segment, and of the next one
+    f32x2 scale = {1.f, 1.f}, scale_next = {1.f, 1.f};  // of page G
+    const uint8_t* values_at = nullptr;
+    int ids = 0, ids_base = 0;
+    auto load_keys = [&](int b) {
         constexpr int PH = D * kPage;  // bytes of a page's head
-        const int at = (b - ids_base) * 4;
-        const uint8_t* k = a.k_pool + ((int64_t)__shfl(ids, at + (r >> 2)) * a.n_kv + kvh) * PH + G * 64 + (r & 3) * 16;
-        const uint8_t* v = a.v_pool + ((int64_t)__shfl(ids, at + G) * a.n_kv + kvh) * PH + r * kPage;
+        const int i = (b - ids_base) * 4;
+        const int64_t page = (int64_t)__shfl(ids, i + G) * a.n_kv + kvh;
+        const uint8_t* at = a.k_pool + ((int64_t)__shfl(ids, i + (r >> 2)) * a.n_kv + kvh) * PH + G * 64 + (r & 3) * 16;
+        values_at = a.v_pool + page * PH + r * kPage;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int p = 0; p < D / 64; ++p) f.k[t][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + t * (4 * D) + p * 256));
-#pragma unroll
-        for (int b16 = 0; b16 < D / 16; ++b16) f.v[b16] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + b16 * 256));
+            for (int p = 0; p < D / 64; ++p) k[t][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at + t * (4 * D) + p * 256));
+        scale_next = a.scales[page];
     };
-    Frag<D> fa, fb;
-    if (b_begin < b_end) {
-        fetch_ids(b_begin);
-        load_block(fa, b_begin);
-    }
-    bf16x8 qf[D / 64][2];
-    const int col = min(it.tile * kStreamCols + r, cols - 1), row = col / g;
-    const bf16_t* qrow = a.q + (int64_t)(it.row0 + row) * a.ld_q + (int64_t)(kvh * g + col - row * g) * D;
+    auto load_values = [&]() {
 #pragma unroll
-    for (int p = 0; p < D / 64; ++p)
+        for (int b = 0; b < D / 16; ++b) v[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(values_at + b * 256));
+    };
+    auto load_queries = [&](const Segment& s) {
+        const int cols = s.n * g, col = min(r, cols - 1), row = col / g;
+        const bf16_t* qrow = a.q + (int64_t)(s.row0 + row) * a.ld_q + (int64_t)(kvh * g + col - row * g) * D;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) qf[p][h] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + 64 * p + 16 * G + 8 * h));
+        for (int p = 0; p < D / 64; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) qn[p][h] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + 64 * p + 16 * G + 8 * h));
+    };
 
     f32x4 o[D / 16];
     float m = kNegBig, l = 0.f;
+    int pos = 0, low = 0, pos_min = 0, low_max = 0;  // this column sees keys up to pos and above low, or below sinks
+    auto enter = [&](const Segment& s) {
+        const int cols = s.n * g, row = min(r, cols - 1) / g;
+        pos = s.c + row;
+        low = a.window > 0 ? pos - a.window : -1;
+        pos_min = s.c;
+        low_max = a.window > 0 ? s.c + s.n - 1 - a.window : -1;
+        m = kNegBig;
+        l = 0.f;
 #pragma unroll
-    for (int b = 0; b < D / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int pos = it.c + row, low = a.window > 0 ? pos - a.window : -1;  // this column sees keys up to pos and above low, or below sinks
-    const int pos_min = it.c, low_max = a.window > 0 ? it.c + it.n - 1 - a.window : -1;
-    auto attend = [&](Frag<D>& f, int b) {
-        const int key0 = seen.actual(b) * kBlock, at = (b - ids_base) * 4 + G;
-        const float factor = __shfl(ps.keys, at), log_values = __shfl(ps.log_values, at), per_value = __shfl(ps.per_value, at);
-        f32x4 s[4];
+        for (int b = 0; b < D / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < D / 64; ++p)
 #pragma unroll
-            for (int p = 0; p < D / 64; ++p)
+            for (int h = 0; h < 2; ++h) qf[p][h] = qn[p][h];
+    };
+    StreamRecord record{0, 0, 0, 0};
+    auto finish = [&](const Segment& s) {
+        float sum = l + __shfl_xor(l, 16);
+        sum += __shfl_xor(sum, 32);
+        const int cols = s.n * g;
+        if (s.end - s.begin == s.blocks) {
+            if (r < cols) {
+                const float inv = 1.0f / sum;
+                const int row = r / g;
+                bf16_t* orow = a.out + (int64_t)(s.row0 + row) * a.ld_o + (int64_t)(kvh * g + r - row * g) * D + G * 4;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, widen8(f.k[t][p][2 * h], f.k[t][p][2 * h + 1])), qf[p][h], s[t], 0, 0, 0);
+                for (int b = 0; b < D / 16; ++b) *reinterpret_cast<bf16x4*>(orow + b * 16) = __builtin_convertvector(o[b] * inv, bf16x4);
+            }
+            return;
         }
-        if (key0 + kBlock - 1 > pos_min || (key0 <= low_max && key0 + kBlock > a.sinks)) {  // not all keys are seen by all columns
-            // values that are no numbers may reach the columns that see them only: they are emptied and the key's scores are no numbers
-            u32x4 bad = {0u, 0u, 0u, 0u};
+        const int place = 2 * w + (s.start + s.begin > lo);  // the first stream of the run, or the last
+        if (r < cols) {
+            const int64_t at = ((int64_t)kvh * 2 * parts.max_waves + place) * kStreamCols + r;
 #pragma unroll
-            for (int b16 = 0; b16 < D / 16; ++b16)
+            for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(parts.stream_o + at * D + b * 16 + G * 4) = o[b];
+            if (G == 0) parts.stream_ml[at] = f32x2{m, sum};
+        }
+        if (s.begin == 0) {  // the wave of its last block: the last one whose run does not begin behind it
+            const int last = (int)(((uint64_t)(s.start + s.blocks) * (uint32_t)waves - 1) / (uint64_t)job.stream);
+            record = StreamRecord{s.row0, cols, last - w + 1, place};
+        }
+    };
+    Segment seg{}, then{};
+    Seen seen{0, 0, 0}, seen_then{0, 0, 0};
+    int ids_then = 0, ids_ahead = 0;  // pages that the next segment begins with, of the next 16 blocks
+    auto look_ahead = [&]() -> bool {
+        if (!next_segment(then)) return false;
+        seen_then = seen_blocks(a, then.c, 0, then.n - 1);
+        ids_then = table_ids(then, seen_then, then.begin);
+        return true;
+    };
+    auto begin_next = [&]() {  // its keys
+        ids = min(max(ids_then, 0), a.num_blocks - 1);
+        ids_base = then.begin;
+        load_keys(ids_base);
+        load_queries(then);
+    };
+    bool more = look_ahead();
+    if (more) {
+        begin_next();
+        load_values();
+        seg = then;
+        seen = seen_then;
+        scale = scale_next;
+        enter(seg);
+        more = look_ahead();
+        for (int b = seg.begin;;) {
+            const bool same = b + 1 < seg.end;
+            const int key0 = seen.actual(b) * kBlock;
+            f32x4 s[4];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) bad[w] |= no_numbers(f.v[b16][w]);
-            if (__any((bad[0] | bad[1] | bad[2] | bad[3]) != 0u)) {
+            for (int t = 0; t < 4; ++t) {
+                s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int p = 0; p < D / 64; ++p)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, widen8(k[t][p][2 * h], k[t][p][2 * h + 1])), qf[p][h], s[t], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (the keys of the next block take the place of these)
+            if (same) {
+                if (b - ids_base == 12 && ids_base + 16 < seg.end) ids_ahead = table_ids(seg, seen, ids_base + 16);
+                if (b + 1 - ids_base == 16) {
+                    ids = min(max(ids_ahead, 0), a.num_blocks - 1);
+                    ids_base = b + 1;
+                }
+                load_keys(b + 1);
+            } else if (more) {
+                begin_next();
+            }
+            PageScale ps;
+            ps.of(scale, a.scale_log2);
+            if (key0 + kBlock - 1 > pos_min || (key0 <= low_max && key0 + kBlock > a.sinks)) {  // not all keys are seen by all columns
+                // values that are no numbers may reach the columns that see them only: they are emptied and the key's scores are no numbers
+                u32x4 bad = {0u, 0u, 0u, 0u};
 #pragma unroll
                 for (int b16 = 0; b16 < D / 16; ++b16)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) f.v[b16][w] &= ~((no_numbers(f.v[b16][w]) >> 7) * 0xFFu);
+                    for (int x = 0; x < 4; ++x) bad[x] |= no_numbers(v[b16][x]);
+                if (__any((bad[0] | bad[1] | bad[2] | bad[3]) != 0u)) {
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
+                    for (int b16 = 0; b16 < D / 16; ++b16)
 #pragma unroll
-                    for (int by = 1; by < 16; by *= 2) bad[w] |= (uint32_t)__shfl_xor((int)bad[w], by);
-            }
+                        for (int x = 0; x < 4; ++x) v[b16][x] &= ~((no_numbers(v[b16][x]) >> 7) * 0xFFu);
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+                    for (int x = 0; x < 4; ++x)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = key0 + G * kPage + 4 * t + i;
-                    const bool hidden = (key > pos) | ((key <= low) & (key >= a.sinks));
-                    s[t][i] = hidden ? -INFINITY : bad[t] >> (8 * i + 7) & 1 ? NAN : s[t][i];
+                        for (int by = 1; by < 16; by *= 2) bad[x] |= (uint32_t)__shfl_xor((int)bad[x], by);
                 }
-        }
-        float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
-        for (int t = 1; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
-        top *= factor;
-        if (__any(top > m)) {  // the reference moves to the running maximum, the same in the four lanes of a column
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
-            const float down = __builtin_amdgcn_exp2f(m - top);
-            m = top;
-            l *= down;
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = key0 + G * kPage + 4 * t + i;
+                        const bool hidden = (key > pos) | ((key <= low) & (key >= a.sinks));
+                        s[t][i] = hidden ? -INFINITY : bad[t] >> (8 * i + 7) & 1 ? NAN : s[t][i];
+                    }
+            }
+            float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+#pragma unroll
+            for (int t = 1; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
+            top *= ps.keys;
+            if (__any(top > m)) {  // the reference moves to the running maximum, the same in the four lanes of a column
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
+                const float down = __builtin_amdgcn_exp2f(m - top);
+                m = top;
+                l *= down;
+#pragma unroll
+                for (int b16 = 0; b16 < D / 16; ++b16)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[b16][x] *= down;
+            }
+            const float shift = ps.log_values - m;
+            float sum = 0.f;
+            bf16x8 wt[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                f32x8 p;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    p[x] = __builtin_amdgcn_exp2f(fmaf(s[2 * j + x / 4][x % 4], ps.keys, shift));
+                    sum += p[x];
+                }
+                wt[j] = __builtin_convertvector(p, bf16x8);
+            }
+            l += sum * ps.per_value;
 #pragma unroll
             for (int b16 = 0; b16 < D / 16; ++b16)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) o[b16][v] *= down;
-        }
-        const float shift = log_values - m;
-        float sum = 0.f;
-        bf16x8 w[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            f32x8 p;
-#pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                p[v] = __builtin_amdgcn_exp2f(fmaf(s[2 * j + v / 4][v % 4], factor, shift));
-                sum += p[v];
+                for (int j = 0; j < 2; ++j)
+                    o[b16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, widen8(v[b16][2 * j], v[b16][2 * j + 1])), wt[j], o[b16], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (same || more) load_values();
+            scale = scale_next;
+            if (same) {
+                ++b;
+                continue;
             }
-            w[j] = __builtin_convertvector(p, bf16x8);
-        }
-        l += sum * per_value;
-#pragma unroll
-        for (int b16 = 0; b16 < D / 16; ++b16)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                o[b16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, widen8(f.v[b16][2 * j], f.v[b16][2 * j + 1])), w[j], o[b16], 0, 0, 0);
-    };
-    for (int b = b_begin; b < b_end; b += 2) {  // (16 blocks of page ids: an even number, so that they run out in front of fa only)
-        if (b + 1 < b_end) load_block(fb, b + 1);
-        attend(fa, b);
-        if (b + 2 < b_end && b + 2 < ids_base + 16) load_block(fa, b + 2);
-        if (b + 1 < b_end) attend(fb, b + 1);
-        if (b + 2 < b_end && b + 2 >= ids_base + 16) {
-            fetch_ids(b + 2);
-            load_block(fa, b + 2);
+            finish(seg);
+            if (!more) break;
+            seg = then;
+            seen = seen_then;
+            b = seg.begin;
+            enter(seg);
+            more = look_ahead();
         }
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (G == 0) {
-        join.m[wave][r] = m;
-        join.l[wave][r] = l;
-    }
-#pragma unroll
-    for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(&join.o[wave][r][b * 16 + G * 4]) = o[b];
-    __syncthreads();
-    const int here = min(kStreamCols, cols - it.tile * kStreamCols);
-    for (int i = threadIdx.x; i < here * (D / 4); i += 64 * WAVES) {
-        const int j = i / (D / 4), e = i % (D / 4) * 4, cc = it.tile * kStreamCols + j, rr = cc / g;
-        float ms = kNegBig, ls = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) ms = fmaxf(ms, join.m[w][j]);
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float x = __builtin_amdgcn_exp2f(join.m[w][j] - ms);
-            const f32x4 ow = *reinterpret_cast<const f32x4*>(&join.o[w][j][e]);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] += ow[v] * x;
-            ls += join.l[w][j] * x;
-        }
-        if (it.parts > 1) {
-            const int64_t place = kvh * parts.places + it.place + j;
-            *reinterpret_cast<f32x4*>(parts.o + place * D + e) = acc;
-            if (e == 0) parts.ml[place] = f32x2{ms, ls};
-            continue;
-        }
-        const float inv = it.broken ? 0.f : 1.0f / ls;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[v] *= inv;
-        *reinterpret_cast<bf16x4*>(a.out + (int64_t)(it.row0 + rr) * a.ld_o + (int64_t)(kvh * g + cc - rr * g) * D + e) = __builtin_convertvector(acc, bf16x4);
-    }
+    if (kvh == 0 && lane == 0) parts.stream[w] = record;
 }
 
 // ---- tiles of columns --------------------------------------------------------------------------------------------------------
@@ -563,12 +751,12 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 31, h = lane >> 5, g = a.n_q / a.n_kv;
-    const int cols = it.n * g, col0 = it.tile * it.width, ncols = min(it.width, cols - col0);
+    const int cols = it.n * g, col0 = it.tile * kTileCols, ncols = min(kTileCols, cols - col0);
     const int i0 = col0 / g, i1 = (col0 + ncols - 1) / g;
     const Seen seen = seen_blocks(a, it.c, i0, i1);
     const int each = seen.blocks / it.parts, more = seen.blocks - each * it.parts;
-    const int first = it.part * each + min(it.part, more), blocks = it.broken ? 0 : each + (it.part < more);
-    const int last_page = max(it.c + it.n - 1, 0) / kPage;
+    const int first = it.part * each + min(it.part, more), blocks = each + (it.part < more);
+    const int last_page = (it.c + it.n - 1) / kPage;
     const int32_t* bt = a.block_tables + (int64_t)it.seq * a.table_stride;
     auto key_of = [&](int b) { return seen.actual(first + b) * kBlock; };  // first key of block b
 
@@ -809,7 +997,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         if (h == 0) parts.ml[place] = f32x2{m, l};
         return;
     }
-    const float inv = it.broken ? 0.f : 1.0f / l;
+    const float inv = 1.0f / l;
     bf16_t* orow = a.out + (int64_t)(it.row0 + row) * a.ld_o + (int64_t)(kvh * g + col - row * g) * D;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
@@ -820,7 +1008,21 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         }
 }
 
-// Threads of a workgroup: four waves where there are stream units only, two workgroups to a compute unit, eight with tiles.
+// The rows of sequences that break a rule become zeros, by one wave.
+template <int D>
+__device__ __forceinline__ void write_zeros(const Attn8Args& a, int kvh) {
+    const int lane = threadIdx.x & 63, g = a.n_q / a.n_kv;
+    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
+        const SeqPlan q = seq_plan(a, s0 + lane);
+        for (uint64_t todo = __ballot(q.broken); todo; todo &= todo - 1) {
+            const int l = __builtin_ctzll(todo), row0 = lane_value(q.row0, l), n = lane_value(q.n, l);
+            for (int i = 0; i < n; ++i)
+                for (int e = lane * 4; e < g * D; e += 256) *reinterpret_cast<u32x2*>(a.out + (int64_t)(row0 + i) * a.ld_o + (int64_t)kvh * g * D + e) = u32x2{0u, 0u};
+        }
+    }
+}
+
+// Threads of a workgroup: four waves where there are streams only, two workgroups to a compute unit, eight with tiles.
 template <bool TILES>
 constexpr int kThreads = TILES ? 512 : 256;
 
@@ -828,78 +1030,96 @@ template <int D, bool TILES>
 __global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Args a) {
     // (one LDS object: with a second one the compiler waits for all loads into the ring before it reads from it)
     extern __shared__ __attribute__((aligned(1024))) unsigned char attn8_lds[];
-    const int kvh = blockIdx.x % a.n_kv;
-    Unit it;
+    constexpr int WAVES = kThreads<TILES> / 64;
+    const int kvh = blockIdx.x % a.n_kv, place = blockIdx.x / a.n_kv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
-    int cut_tiles;
-    if (!find_unit<TILES>(a, parts.plan, blockIdx.x / a.n_kv, it, cut_tiles)) {
-        if (cut_tiles >= 0 && blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) *parts.count = cut_tiles;  // (the last workgroup is behind the last unit)
+    Job job;
+    find_job<TILES>(a, parts.plan, place, job);
+    if (blockIdx.x + a.n_kv >= gridDim.x) {  // behind the last unit
+        if (job.broken && wave == 0) write_zeros<D>(a, kvh);
+        if (kvh == 0 && threadIdx.x == 0) {
+            if (job.cut_tiles >= 0) *parts.count = job.cut_tiles;
+            *parts.waves = job.workers * WAVES;
+        }
         return;
     }
-    if (it.parts > 1 && it.part == 0 && kvh == 0 && threadIdx.x == 0)
-        parts.rec[it.cut_tile] = Record{it.row0, it.n, it.tile, it.width, it.place, it.step, it.parts, 0};
-    if (!TILES || it.width == kStreamCols) stream_unit<D, kThreads<TILES> / 64>(a, it, parts, kvh, *reinterpret_cast<StreamLds<D, kThreads<TILES> / 64>*>(attn8_lds));
-    else tile_unit<D>(a, it, parts, kvh, *reinterpret_cast<TileLds<D>*>(attn8_lds));
+    if (place < job.workers) {
+        stream_wave<D>(a, job, parts, kvh, place * WAVES + wave, job.workers * WAVES);
+        return;
+    }
+    if constexpr (TILES) {
+        if (!job.is_unit) return;
+        const Unit& it = job.unit;
+        if (it.parts > 1 && it.part == 0 && kvh == 0 && threadIdx.x == 0) parts.rec[it.cut_tile] = Record{it.row0, it.n, it.tile, it.place, it.step, it.parts, {}};
+        tile_unit<D>(a, it, parts, kvh, *reinterpret_cast<TileLds<D>*>(attn8_lds));
+    }
 }
 
-// The partial results of all tiles joined, in order of the parts: a work item is (record, KV head, 1024 / D columns), a thread per four dims
-// of a column.  The kernel is all latency: kMergeBatch parts are asked for at a time, where there are fewer the last one again.
+// The partial results of a column joined, in order of the parts, of which `at` says the places; kMergeBatch parts are asked for at a time, where there are fewer
+// the last one again.
 constexpr int kMergeBatch = 12;
-constexpr int kMergeGroups = 2048;  // workgroups
-template <int D>
-__device__ __forceinline__ void merge_columns(const Attn8Args& a, const Parts& parts, const Record& rec, int kvh, int tcol) {
-    const int g = a.n_q / a.n_kv, e = threadIdx.x % (D / 4) * 4, col = rec.tile * rec.width + tcol;
-    if (tcol >= rec.width || col >= rec.n * g) return;
-    const int64_t first = kvh * parts.places + rec.place + tcol;
+template <typename At>
+__device__ __forceinline__ bf16x4 merge_column(const f32x2* ml, const float* o, int n, int d, int e, At at) {
     float m = kNegBig, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < rec.parts; p0 += kMergeBatch) {
-        f32x2 ml[kMergeBatch];
-        f32x4 o[kMergeBatch];
+    for (int p0 = 0; p0 < n; p0 += kMergeBatch) {
+        f32x2 x[kMergeBatch];
+        f32x4 y[kMergeBatch];
 #pragma unroll
         for (int u = 0; u < kMergeBatch; ++u) {
-            const int64_t at = first + (int64_t)min(p0 + u, rec.parts - 1) * rec.step;
-            ml[u] = parts.ml[at];
-            o[u] = *reinterpret_cast<const f32x4*>(parts.o + at * D + e);
+            const int64_t place = at(min(p0 + u, n - 1));
+            x[u] = ml[place];
+            y[u] = *reinterpret_cast<const f32x4*>(o + place * d + e);
         }
         float top = m;
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) top = fmaxf(top, ml[u][0]);
+        for (int u = 0; u < kMergeBatch; ++u) top = fmaxf(top, x[u][0]);
         const float down = __builtin_amdgcn_exp2f(m - top);
         l *= down;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[v] *= down;
+        acc *= down;
         m = top;
 #pragma unroll
         for (int u = 0; u < kMergeBatch; ++u) {
-            if (p0 + u >= rec.parts) continue;
-            const float w = __builtin_amdgcn_exp2f(ml[u][0] - m);
-            l += ml[u][1] * w;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] += o[u][v] * w;
+            if (p0 + u >= n) continue;
+            const float w = __builtin_amdgcn_exp2f(x[u][0] - m);
+            l += x[u][1] * w;
+            acc += y[u] * w;
         }
     }
-    const float inv = 1.0f / l;
-#pragma unroll
-    for (int v = 0; v < 4; ++v) acc[v] *= inv;
-    *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) = __builtin_convertvector(acc, bf16x4);
+    return __builtin_convertvector(acc * (1.0f / l), bf16x4);
 }
+// All latency.  The first workgroups take a wave of the stream and a KV head each, the others 1024 / D columns of a cut tile.
 template <int D, bool TILES>
-__global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a) {
-    constexpr int COLS = 1024 / D;
+__global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int stream_groups) {
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
-    const int groups = (TILES ? kTileCols : kStreamCols) / COLS, per_record = a.n_kv * groups;
-    int work = blockIdx.x;
-    Record rec = parts.rec[min(work / per_record, max_cut_tiles<TILES>(a.n_kv) - 1)];  // (behind the last one: anything)
-    const int total = *parts.count * per_record;
-    while (work < total) {
-        const int rest = work % per_record;
-        work += gridDim.x;
-        const Record next = parts.rec[min(work / per_record, max_cut_tiles<TILES>(a.n_kv) - 1)];
-        merge_columns<D>(a, parts, rec, rest % a.n_kv, rest / a.n_kv * COLS + (int)threadIdx.x / (D / 4));
-        rec = next;
+    const int g = a.n_q / a.n_kv;
+    if ((int)blockIdx.x < stream_groups) {
+        const int w = blockIdx.x / a.n_kv, kvh = blockIdx.x % a.n_kv;
+        const StreamRecord rec = parts.stream[w];
+        if (w >= *parts.waves || rec.waves == 0) return;
+        for (int i = threadIdx.x; i < rec.cols * (D / 4); i += 256) {
+            const int col = i / (D / 4), e = i % (D / 4) * 4;
+            const int64_t first = (int64_t)kvh * 2 * parts.max_waves;
+            *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) =
+                merge_column(parts.stream_ml, parts.stream_o, rec.waves, D, e, [&](int p) { return (first + (p == 0 ? rec.place : 2 * (w + p))) * kStreamCols + col; });
+        }
+        return;
+    }
+    if constexpr (TILES) {
+        constexpr int COLS = 1024 / D, GROUPS = kTileCols / COLS;
+        const int per_record = a.n_kv * GROUPS, total = *parts.count * per_record;
+        for (int work = blockIdx.x - stream_groups; work < total; work += gridDim.x - stream_groups) {
+            const Record rec = parts.rec[work / per_record];
+            const int rest = work % per_record, kvh = rest % a.n_kv, tcol = rest / a.n_kv * COLS + (int)threadIdx.x / (D / 4), col = rec.tile * kTileCols + tcol;
+            const int e = threadIdx.x % (D / 4) * 4;
+            if (col >= rec.n * g) continue;
+            const int64_t first = kvh * parts.places + rec.place + tcol;
+            *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) =
+                merge_column(parts.ml, parts.o, rec.parts, D, e, [&](int p) { return first + (int64_t)p * rec.step; });
+        }
     }
 }
 
@@ -914,16 +1134,17 @@ size_t attention8_workspace_bytes(int n_q, int n_kv, int d, int max_new) {
 
 template <int D, bool TILES>
 static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
-    // no more tiles than whole ones in all rows and a partly filled one per sequence; cutting the keys adds no more units than twice the
-    // shares; and one place behind the last unit
-    const int64_t units = (int64_t)a.num_rows * (a.n_q / a.n_kv) / (TILES ? kTileCols : kStreamCols) + a.num_seqs + 2 * target_units<TILES>(a.n_kv) + 1;
-    if (units * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
+    // the stream's workgroups; no more tiles than whole ones in all rows and a partly filled one per sequence, and cutting the keys adds no more units
+    // than twice the target; and one place behind the last unit
+    const int g = a.n_q / a.n_kv;
+    const int64_t tiles = TILES ? (int64_t)a.num_rows * g / kTileCols + a.num_seqs : 0;
+    const int64_t places = max_workers<TILES>(a.n_kv) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
+    if (places * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
     if (a.num_seqs > 64) attention8_plan_kernel<TILES><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
-    int lds = sizeof(StreamLds<D, kThreads<TILES> / 64>);
+    const int lds = TILES ? sizeof(TileLds<D>) : 0;
     if (TILES) {
-        lds = sizeof(TileLds<D>) > lds ? sizeof(TileLds<D>) : lds;
         static std::atomic<uint64_t> allowed{0};  // devices on which this kernel may use the LDS that it asks for
         int dev = 0;
         hipError_t e = hipGetDevice(&dev);
@@ -934,9 +1155,14 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
             if (dev < 64) allowed.fetch_or(1ull << dev);
         }
     }
-    attention8_kernel<D, TILES><<<(unsigned)(units * a.n_kv), kThreads<TILES>, lds, stream>>>(a);
-    // no sequence can be cut whose table has no more pages than the fewest blocks of a part
-    if (a.table_stride > kBlock / kPage * kMinShare) attention8_merge_kernel<D, TILES><<<kMergeGroups, 256, 0, stream>>>(a);
+    attention8_kernel<D, TILES><<<(unsigned)(places * a.n_kv), kThreads<TILES>, lds, stream>>>(a);
+    // no sequence can be cut that has no more blocks than the fewest of a part
+    const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : kStreamCols / g;
+    if (most_blocks(own, rows, a.window, a.sinks) > (kWhole < kMinShare ? kWhole : kMinShare)) {
+        const int stream_groups = (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, kStreamCols / g, a.window, a.sinks) + 8) * a.n_kv;
+        const int64_t tile_groups = TILES ? std::min<int64_t>(2048, std::min<int64_t>(max_cut_tiles(a.n_kv), tiles) * a.n_kv * (kTileCols * D / 1024)) : 0;
+        attention8_merge_kernel<D, TILES><<<(unsigned)(stream_groups + tile_groups), 256, 0, stream>>>(a, stream_groups);
+    }
     return hipGetLastError();
 }
 
