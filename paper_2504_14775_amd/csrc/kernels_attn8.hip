@@ -44,12 +44,15 @@ struct Unit {
 constexpr int kMinShare = 6;     // fewest blocks worth a unit
 constexpr int kWhole = 6;        // most blocks of a stream that is never cut
 constexpr int kGroups = 256;     // workgroups that run at one time: one on each compute unit
-constexpr int kStreamGroups = 256;
 // All of these are for each KV head.
 __host__ __device__ constexpr int per_head(int total, int n_kv) { return total / n_kv > 0 ? total / n_kv : 1; }
+// Workgroups of the stream at most.
 template <bool TILES>
-__host__ __device__ constexpr int max_workers(int n_kv) { return per_head(TILES ? kGroups : kStreamGroups, n_kv); }
-__host__ __device__ constexpr int target_units(int n_kv) { return per_head(2 * kGroups, n_kv); }
+__host__ __device__ constexpr int max_workers(int n_kv, int d) { return per_head(TILES || d == 128 ? kGroups : 2 * kGroups, n_kv); }
+// Units that the keys of tiles are cut into.  Every part of a tile writes and reads partial results of (d + 2) floats a column, as much as eight blocks of
+// keys.  us at 128 / 256 / 512: a chunk of 901 behind 2011 keys (14B heads) 103 / 105 / 102, of 4096 behind none (8B) 165 / 167 / 230, 251 decode rows beside 1400
+// chunk rows (14B) 201 / 225 / 263, 100 rows behind 6000 keys 40 / 38 / 42.
+__host__ __device__ constexpr int target_units(int n_kv) { return per_head(kGroups / 2, n_kv); }
 // Tiles with partial results and columns of these.  A tile is cut where its sequence has more blocks than a share, into at most ceil(blocks /
 // share) parts; the shares of all are at least half their blocks by the target (seq_plan: twice the weight is at least the blocks).
 __host__ __device__ constexpr int max_cut_tiles(int n_kv) { return 2 * target_units(n_kv); }
@@ -119,16 +122,19 @@ __device__ __forceinline__ void scan_wave(T& x) {
 template <typename T>
 __device__ __forceinline__ T lane_value(T x, int lane) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
 
-// What follows from the sums over all sequences.  A block of a tile takes about three times a stream's share of the memory for one.  (The sums are
+// What follows from the sums over all sequences.  (The sums are
 // exact up to 2^24, and by 1e-4 of themselves more from there on where that counts, in the share: more than the roundings of their additions, 2^-24 of
 // it each, take away, kMaxAttn8Seqs / 4096 of a lane and 15 over lanes and runs.)
 static_assert(kMaxAttn8Seqs / (64 * 64) + 15 < 16777216 / 10000, "the sum of all weights");
-constexpr float kTileCost = 3.f;
-constexpr int kFewBlocks = 2;    // of a wave of the stream, where there are so few
+// A block of a tile keeps a compute unit busy for 2.2 us, one of a stream, where half of the units draw all that the memory gives, for 0.35.  us at 4 / 6 / 8:
+// 251 decode rows beside 1400 chunk rows (14B heads) 212 / 201 / 211, 256 beside 1792 (8B) 226 / 202 / 214, 32 beside 4 x 128 91 / 82 / 79.
+constexpr float kTileCost = 6.f;
+// Blocks of a wave of the stream, where there are few: us at 2 / 4 / 8, one sequence of 3000 keys (8B heads) 12.8 / 15.0 / 17.7, of 20000 18.9 / 17.9 / 21.7.
+constexpr int kFewBlocks = 2;
 template <bool TILES>
-__device__ __forceinline__ int workers_of(float stream, float tiles, int n_kv) {
+__device__ __forceinline__ int workers_of(float stream, float tiles, int n_kv, int d) {
     if (!(stream > 0.f)) return 0;
-    const int most = max_workers<TILES>(n_kv);
+    const int most = max_workers<TILES>(n_kv, d);
     const float fair = TILES ? rintf(stream / (stream + kTileCost * tiles) * (float)most) : (float)most;
     return (int)fmaxf(fminf(fair, ceilf(stream / (float)(kFewBlocks * (TILES ? 8 : 4)))), 1.f);
 }
@@ -242,7 +248,7 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
         scan_wave(tiles);
         tiles = lane_value(tiles, 63);
     }
-    j.workers = workers_of<TILES>((float)j.stream, tiles, a.n_kv);
+    j.workers = workers_of<TILES>((float)j.stream, tiles, a.n_kv, a.d);
     if (__any(j.seqs.unordered)) {  // rows in no order may belong to two sequences
         j.workers = 0;
         j.broken = false;
@@ -352,7 +358,7 @@ __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan
     if (lane == 0) {
         plan->share = share;
         plan->units = any_unordered ? 0 : start;
-        plan->workers = any_unordered ? 0 : workers_of<TILES>((float)all_blocks, total, a.n_kv);
+        plan->workers = any_unordered ? 0 : workers_of<TILES>((float)all_blocks, total, a.n_kv, a.d);
         plan->broken = any_unordered ? 0 : any_broken;
         plan->stream = all_blocks;
     }
@@ -363,9 +369,9 @@ __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan
 // Workspace: the plan of many sequences; the waves of the stream; a record per tile whose keys are cut; then per KV head and column of a part the
 // reference and the sum, then the unnormalised outputs, of the stream and of the tiles.  A wave of the stream has places for two streams that
 // are not its own alone: the one that its run begins with, and the one that it ends with.
-struct StreamRecord {       // of the stream that begins in a wave's run and goes on in the next one's
+struct StreamRecord {       // of a sequence, or, of more than 64, of the one that begins in a wave's run and goes on in the next one's
     int32_t row0, cols, waves;  // waves: that have a part of it, or none
-    int32_t place;          // of the first part, in streams; those of the others are the first ones of their waves
+    int32_t wave, place;    // of the first part, in streams; those of the others are the first ones of their waves
 };
 struct Record {
     int32_t row0, n, tile;
@@ -383,7 +389,7 @@ struct Parts {
 };
 template <bool TILES>
 __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d) {
-    t.max_waves = max_workers<TILES>(n_kv) * (TILES ? 8 : 4);
+    t.max_waves = max_workers<TILES>(n_kv, d) * (TILES ? 8 : 4);
     t.places = TILES ? max_places(n_kv) : 0;
     char* p = (char*)base;
     size_t off = 0;
@@ -395,7 +401,7 @@ __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d
     t.count = (int32_t*)take(256);
     t.waves = t.count + 1;
     t.plan = (Plan*)take(sizeof(Plan));
-    t.stream = (StreamRecord*)take(t.max_waves * sizeof(StreamRecord));
+    t.stream = (StreamRecord*)take((t.max_waves > 64 ? t.max_waves : 64) * sizeof(StreamRecord));
     t.rec = (Record*)take(TILES ? max_cut_tiles(n_kv) * sizeof(Record) : 0);
     const size_t stream_cols = (size_t)n_kv * 2 * t.max_waves * kStreamCols, cols = (size_t)n_kv * t.places;
     t.stream_ml = (f32x2*)take(stream_cols * 8);
@@ -564,12 +570,13 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 #pragma unroll
             for (int h = 0; h < 2; ++h) qf[p][h] = qn[p][h];
     };
-    StreamRecord record{0, 0, 0, 0};
+    StreamRecord record{0, 0, 0, 0, 0};
     auto finish = [&](const Segment& s) {
         float sum = l + __shfl_xor(l, 16);
         sum += __shfl_xor(sum, 32);
         const int cols = s.n * g;
-        if (s.end - s.begin == s.blocks) {
+        const bool one = s.end - s.begin == s.blocks;  // the only part
+        if (one) {
             if (r < cols) {
                 const float inv = 1.0f / sum;
                 const int row = r / g;
@@ -577,6 +584,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 #pragma unroll
                 for (int b = 0; b < D / 16; ++b) *reinterpret_cast<bf16x4*>(orow + b * 16) = __builtin_convertvector(o[b] * inv, bf16x4);
             }
+            if (a.num_seqs <= 64 && kvh == 0 && lane == 0) parts.stream[s.seq] = StreamRecord{0, 0, 0, 0, 0};
             return;
         }
         const int place = 2 * w + (s.start + s.begin > lo);  // the first stream of the run, or the last
@@ -588,7 +596,8 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
         }
         if (s.begin == 0) {  // the wave of its last block: the last one whose run does not begin behind it
             const int last = (int)(((uint64_t)(s.start + s.blocks) * (uint32_t)waves - 1) / (uint64_t)job.stream);
-            record = StreamRecord{s.row0, cols, last - w + 1, place};
+            record = StreamRecord{s.row0, cols, last - w + 1, w, place};
+            if (a.num_seqs <= 64 && kvh == 0 && lane == 0) parts.stream[s.seq] = record;
         }
     };
     Segment seg{}, then{};
@@ -717,7 +726,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
             more = look_ahead();
         }
     }
-    if (kvh == 0 && lane == 0) parts.stream[w] = record;
+    if (a.num_seqs > 64 && kvh == 0 && lane == 0) parts.stream[w] = record;
 }
 
 // ---- tiles of columns --------------------------------------------------------------------------------------------------------
@@ -1039,6 +1048,8 @@ __global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Arg
     find_job<TILES>(a, parts.plan, place, job);
     if (blockIdx.x + a.n_kv >= gridDim.x) {  // behind the last unit
         if (job.broken && wave == 0) write_zeros<D>(a, kvh);
+        if (a.num_seqs <= 64 && kvh == 0 && wave == 0 && (int)(threadIdx.x & 63) < a.num_seqs && (job.workers == 0 || job.seqs.stream == 0))
+            parts.stream[threadIdx.x & 63] = StreamRecord{0, 0, 0, 0, 0};
         if (kvh == 0 && threadIdx.x == 0) {
             if (job.cut_tiles >= 0) *parts.count = job.cut_tiles;
             *parts.waves = job.workers * WAVES;
@@ -1057,68 +1068,100 @@ __global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Arg
     }
 }
 
-// The partial results of a column joined, in order of the parts, of which `at` says the places; kMergeBatch parts are asked for at a time, where there are fewer
-// the last one again.
-constexpr int kMergeBatch = 12;
-template <typename At>
-__device__ __forceinline__ bf16x4 merge_column(const f32x2* ml, const float* o, int n, int d, int e, At at) {
-    float m = kNegBig, l = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < n; p0 += kMergeBatch) {
-        f32x2 x[kMergeBatch];
-        f32x4 y[kMergeBatch];
+// Partial results of a column joined: parts first, first + step, ... of n, of which `at` says the places; BATCH of them are asked for at a time, where
+// there are fewer the last one again.
+struct Joined {
+    float m, l;
+    f32x4 o;
+};
+template <int BATCH, typename At>
+__device__ __forceinline__ Joined join_batches(const f32x2* ml, const float* o, int first, int step, int n, int d, int e, At at) {
+    Joined j{kNegBig, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    for (int p0 = first; p0 < n; p0 += BATCH * step) {
+        f32x2 x[BATCH];
+        f32x4 y[BATCH];
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) {
-            const int64_t place = at(min(p0 + u, n - 1));
+        for (int u = 0; u < BATCH; ++u) {
+            const int64_t place = at(min(p0 + u * step, n - 1));
             x[u] = ml[place];
             y[u] = *reinterpret_cast<const f32x4*>(o + place * d + e);
         }
-        float top = m;
+        float top = j.m;
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) top = fmaxf(top, x[u][0]);
-        const float down = __builtin_amdgcn_exp2f(m - top);
-        l *= down;
-        acc *= down;
-        m = top;
+        for (int u = 0; u < BATCH; ++u) top = fmaxf(top, x[u][0]);
+        const float down = __builtin_amdgcn_exp2f(j.m - top);
+        j.l *= down;
+        j.o *= down;
+        j.m = top;
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) {
-            if (p0 + u >= n) continue;
-            const float w = __builtin_amdgcn_exp2f(x[u][0] - m);
-            l += x[u][1] * w;
-            acc += y[u] * w;
+        for (int u = 0; u < BATCH; ++u) {
+            if (p0 + u * step >= n) continue;
+            const float w = __builtin_amdgcn_exp2f(x[u][0] - j.m);
+            j.l += x[u][1] * w;
+            j.o += y[u] * w;
         }
     }
-    return __builtin_convertvector(acc * (1.0f / l), bf16x4);
+    return j;
 }
-// All latency.  The first workgroups take a wave of the stream and a KV head each, the others 1024 / D columns of a cut tile.
-template <int D, bool TILES>
-__global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int stream_groups) {
+template <typename At>
+__device__ __forceinline__ Joined join_parts(const f32x2* ml, const float* o, int first, int step, int n, int d, int e, At at) {
+    const int mine = (n - first + step - 1) / step;
+    if (mine <= 2) return join_batches<2>(ml, o, first, step, n, d, e, at);
+    if (mine <= 4) return join_batches<4>(ml, o, first, step, n, d, e, at);
+    return join_batches<12>(ml, o, first, step, n, d, e, at);
+}
+// All latency.  The first workgroups take a wave of the stream and a KV head each: D/4 threads have a column, or, where that leaves threads over, each so many of
+// its parts; the others 2048 / D columns of a cut tile.
+template <int D, bool TILES, int THREADS>
+__global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, int stream_groups) {
+    constexpr int LANES = D / 4, TEAMS = THREADS / LANES;
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
-    const int g = a.n_q / a.n_kv;
+    const int g = a.n_q / a.n_kv, team = threadIdx.x / LANES, e = threadIdx.x % LANES * 4;
+    auto out_of = [&](int row, int head) { return reinterpret_cast<bf16x4*>(a.out + (int64_t)row * a.ld_o + (int64_t)head * D + e); };
     if ((int)blockIdx.x < stream_groups) {
-        const int w = blockIdx.x / a.n_kv, kvh = blockIdx.x % a.n_kv;
-        const StreamRecord rec = parts.stream[w];
-        if (w >= *parts.waves || rec.waves == 0) return;
-        for (int i = threadIdx.x; i < rec.cols * (D / 4); i += 256) {
-            const int col = i / (D / 4), e = i % (D / 4) * 4;
-            const int64_t first = (int64_t)kvh * 2 * parts.max_waves;
-            *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) =
-                merge_column(parts.stream_ml, parts.stream_o, rec.waves, D, e, [&](int p) { return (first + (p == 0 ? rec.place : 2 * (w + p))) * kStreamCols + col; });
+        __shared__ Joined joined[TEAMS][LANES];
+        const int i = blockIdx.x / a.n_kv, kvh = blockIdx.x % a.n_kv;
+        if (a.num_seqs > 64 && i >= *parts.waves) return;
+        const StreamRecord rec = parts.stream[i];
+        if (rec.waves == 0) return;
+        const int shares = rec.cols < TEAMS ? TEAMS / rec.cols : 1, share = team % shares;
+        for (int col = team / shares; shares > 1 || col < rec.cols; col += TEAMS / shares) {
+            const bool mine = col < rec.cols;
+            Joined j{kNegBig, 0.f, {0.f, 0.f, 0.f, 0.f}};
+            if (mine)
+                j = join_parts(parts.stream_ml, parts.stream_o, share, shares, rec.waves, D, e,
+                               [&](int p) { return ((int64_t)kvh * 2 * parts.max_waves + (p == 0 ? rec.place : 2 * (rec.wave + p))) * kStreamCols + col; });
+            if (shares > 1) {
+                joined[team][threadIdx.x % LANES] = j;
+                __syncthreads();
+                if (share > 0 || !mine) return;  // (one pass)
+                float top = j.m, l = 0.f;
+                for (int x = 1; x < shares; ++x) top = fmaxf(top, joined[team + x][threadIdx.x % LANES].m);
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < shares; ++x) {
+                    const Joined& y = joined[team + x][threadIdx.x % LANES];
+                    const float by = __builtin_amdgcn_exp2f(y.m - top);
+                    l += y.l * by;
+                    o += y.o * by;
+                }
+                j = Joined{top, l, o};
+            }
+            if (mine) *out_of(rec.row0 + col / g, kvh * g + col % g) = __builtin_convertvector(j.o * (1.0f / j.l), bf16x4);
+            if (shares > 1) return;
         }
         return;
     }
     if constexpr (TILES) {
-        constexpr int COLS = 1024 / D, GROUPS = kTileCols / COLS;
+        constexpr int GROUPS = kTileCols / TEAMS;
         const int per_record = a.n_kv * GROUPS, total = *parts.count * per_record;
         for (int work = blockIdx.x - stream_groups; work < total; work += gridDim.x - stream_groups) {
             const Record rec = parts.rec[work / per_record];
-            const int rest = work % per_record, kvh = rest % a.n_kv, tcol = rest / a.n_kv * COLS + (int)threadIdx.x / (D / 4), col = rec.tile * kTileCols + tcol;
-            const int e = threadIdx.x % (D / 4) * 4;
+            const int rest = work % per_record, kvh = rest % a.n_kv, tcol = rest / a.n_kv * TEAMS + team, col = rec.tile * kTileCols + tcol;
             if (col >= rec.n * g) continue;
             const int64_t first = kvh * parts.places + rec.place + tcol;
-            *reinterpret_cast<bf16x4*>(a.out + (int64_t)(rec.row0 + col / g) * a.ld_o + (int64_t)(kvh * g + col % g) * D + e) =
-                merge_column(parts.ml, parts.o, rec.parts, D, e, [&](int p) { return first + (int64_t)p * rec.step; });
+            const Joined j = join_parts(parts.ml, parts.o, 0, 1, rec.parts, D, e, [&](int p) { return first + (int64_t)p * rec.step; });
+            *out_of(rec.row0 + col / g, kvh * g + col % g) = __builtin_convertvector(j.o * (1.0f / j.l), bf16x4);
         }
     }
 }
@@ -1138,7 +1181,7 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     // than twice the target; and one place behind the last unit
     const int g = a.n_q / a.n_kv;
     const int64_t tiles = TILES ? (int64_t)a.num_rows * g / kTileCols + a.num_seqs : 0;
-    const int64_t places = max_workers<TILES>(a.n_kv) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
+    const int64_t places = max_workers<TILES>(a.n_kv, D) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
     if (places * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
@@ -1159,9 +1202,12 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     // no sequence can be cut that has no more blocks than the fewest of a part
     const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : kStreamCols / g;
     if (most_blocks(own, rows, a.window, a.sinks) > (kWhole < kMinShare ? kWhole : kMinShare)) {
-        const int stream_groups = (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, kStreamCols / g, a.window, a.sinks) + 8) * a.n_kv;
+        const int records = a.num_seqs <= 64 ? a.num_seqs : (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, kStreamCols / g, a.window, a.sinks) + 8);
+        const int stream_groups = records * a.n_kv;
         const int64_t tile_groups = TILES ? std::min<int64_t>(2048, std::min<int64_t>(max_cut_tiles(a.n_kv), tiles) * a.n_kv * (kTileCols * D / 1024)) : 0;
-        attention8_merge_kernel<D, TILES><<<(unsigned)(stream_groups + tile_groups), 256, 0, stream>>>(a, stream_groups);
+        const dim3 grid((unsigned)(stream_groups + tile_groups));
+        if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, 512><<<grid, 512, 0, stream>>>(a, stream_groups);
+        else attention8_merge_kernel<D, TILES, 256><<<grid, 256, 0, stream>>>(a, stream_groups);
     }
     return hipGetLastError();
 }
