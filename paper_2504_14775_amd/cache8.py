@@ -107,6 +107,8 @@ def gllm_op_attention8(q, k_pool, v_pool, scales, block_tables, cached_len, row_
     if q.dim() != 2 or q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1:
         _refuse(f"{call}: shapes q {tuple(q.shape)}, out {tuple(out.shape)}, block_tables {tuple(block_tables.shape)}, cached_len {tuple(cached_len.shape)}, "
                 f"row_start {tuple(row_start.shape)}")
+    if (max_new | window | sinks) >> 31:
+        _refuse(f"{call}: max_new {max_new}, window {window}, sinks {sinks}")
     n_q = q.shape[1] // d
     lib = _lib()
     if workspace is None:

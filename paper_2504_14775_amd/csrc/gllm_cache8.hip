@@ -568,7 +568,7 @@ gllm_status gllm_op_norm_rope_store8(const void* qkv, int64_t ld_qkv, int32_t ro
                        n_q_heads, n_kv_heads, (bf16_t*)q_out, ld_q, (uint8_t*)k_pool, (uint8_t*)v_pool, scales, num_blocks * kPage};
     const int64_t parts = ceil_div(n_q_heads, kQueryPasses * (512 / head_dim));
     const int64_t queries = ceil_div(num_rows * parts, 4), pages = ceil_div(ceil_div(num_rows, kPage) * 2 * n_kv_heads, 4);
-    if (queries + pages > INT32_MAX) return GLLM_E_CAPACITY;
+    if ((queries + pages) * 256 > UINT32_MAX) return GLLM_E_CAPACITY;
     const dim3 grid((unsigned)(queries + pages));
 #define GLLM_STORE8(D_, T_) norm_rope_store8_kernel<D_, T_><<<grid, 256, 0, (hipStream_t)stream>>>(a, (int)queries, (int)parts)
     if (head_dim == 128 && rows_type == GLLM_ROWS_F32) GLLM_STORE8(128, float);

@@ -122,9 +122,9 @@ __device__ __forceinline__ void scan_wave(T& x) {
 template <typename T>
 __device__ __forceinline__ T lane_value(T x, int lane) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
 
-// What follows from the sums over all sequences.  (The sums are
-// exact up to 2^24, and by 1e-4 of themselves more from there on where that counts, in the share: more than the roundings of their additions, 2^-24 of
-// it each, take away, kMaxAttn8Seqs / 4096 of a lane and 15 over lanes and runs.)
+// What follows from the sums over all sequences.  (Weights are multiples of 1/128, and their sums exact up to 2^17.  From there on the share is by
+// 1e-4 of itself larger, which is more than the roundings of the additions, 2^-24 of the sum each, take away, kMaxAttn8Seqs / 4096 of a lane and 15
+// over lanes and runs.)
 static_assert(kMaxAttn8Seqs / (64 * 64) + 15 < 16777216 / 10000, "the sum of all weights");
 // A block of a tile keeps a compute unit busy for 2.2 us, one of a stream, where half of the units draw all that the memory gives, for 0.35.  us at 4 / 6 / 8:
 // 251 decode rows beside 1400 chunk rows (14B heads) 212 / 201 / 211, 256 beside 1792 (8B) 226 / 202 / 214, 32 beside 4 x 128 91 / 82 / 79.
@@ -140,7 +140,7 @@ __device__ __forceinline__ int workers_of(float stream, float tiles, int n_kv, i
 }
 __device__ __forceinline__ int share_of(float tiles, int n_kv) {
     const float target = (float)target_units(n_kv);
-    const float even = tiles < 16777216.f ? ceilf(tiles / target) : tiles / target * 1.0001f + 1.f;
+    const float even = tiles < 131072.f ? ceilf(tiles / target) : tiles / target * 1.0001f + 1.f;
     return (int)fminf(fmaxf(even, (float)kMinShare), 1e9f);
 }
 // The units of a sequence's tiles.  They are in order of their size, in quarters of a share, so that the last workgroups to start are short ones;
@@ -432,7 +432,8 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t codes) { return ((codes 
 struct PageScale {
     float keys, log_values, per_value;
     __device__ __forceinline__ void of(f32x2 s, float scale_log2) {
-        keys = fminf(fmaxf(s[0], kScaleMin), kScaleMax) * scale_log2;
+        // (neither 0 nor infinite: the products with hidden keys' scores and with 0 stay what they are)
+        keys = fminf(fmaxf(fminf(fmaxf(s[0], kScaleMin), kScaleMax) * scale_log2, 0x1p-126f), 0x1p127f);
         const float v = fminf(fmaxf(s[1], kScaleMin), kScaleMax);
         log_values = __builtin_amdgcn_logf(v);
         per_value = __builtin_amdgcn_rcpf(v);
@@ -457,7 +458,9 @@ template <int D>
 __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, const Parts& parts, int kvh, int w, int waves) {
     const int lane = threadIdx.x & 63;
     const int r = lane & 15, G = lane >> 4, g = a.n_q / a.n_kv;
-    // The run.  A stream of few blocks belongs to the wave in whose run its last one lies.
+    // The run.  A stream of few blocks belongs to the wave in whose run its last one lies.  (No run behind one that is not empty is empty: there are
+    // at least as many blocks as waves, or, with kFewBlocks of 2, no more than seven blocks to eight waves, of which the first has none.  A longer
+    // stream's parts are therefore those of all waves from its first to its last.)
     const int64_t lo = run_begin(job.stream, waves, w), hi = run_begin(job.stream, waves, w + 1);
 
     // 64 sequences, one per lane, of which those up to lane `at` have been dealt with; `upto` blocks up to the end of this lane's, counted from all.
@@ -1182,7 +1185,7 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     const int g = a.n_q / a.n_kv;
     const int64_t tiles = TILES ? (int64_t)a.num_rows * g / kTileCols + a.num_seqs : 0;
     const int64_t places = max_workers<TILES>(a.n_kv, D) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
-    if (places * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
+    if (places * a.n_kv * kThreads<TILES> > UINT32_MAX) return hipErrorInvalidValue;
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
     if (a.num_seqs > 64) attention8_plan_kernel<TILES><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);

@@ -74,6 +74,13 @@ def test_attention_refuses(change, status):
     assert C8._lib().gllm_op_attention8(*{**ATTENTION, **change}.values()) == status
 
 
+def test_more_work_than_a_launch_takes_is_refused():
+    for rows in (1 << 27, 1 << 30):
+        assert C8._lib().gllm_op_norm_rope_store8(*{**STORE, "rows": rows}.values()) == CAPACITY
+    large = dict(seqs=1 << 20, max_new=9, n_q=128, n_kv=64, ld_q=16384, ld_o=16384)
+    assert C8._lib().gllm_op_attention8(*{**ATTENTION, **large}.values()) == CAPACITY
+
+
 @pytest.mark.parametrize("shape", [(0, 1, 128, 1), (4, 0, 128, 1), (5, 2, 128, 1), (34, 2, 64, 1), (4, 2, 96, 1), (4, 2, 128, 0)])
 def test_no_workspace_for_what_attention_does_not_take(shape):
     assert C8.gllm_op_attention8_workspace_bytes(*shape) == 0

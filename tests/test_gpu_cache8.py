@@ -538,6 +538,105 @@ def test_strides_page_order_and_repetition():
     assert torch.equal(a.out, first)
 
 
+def spoilt_workspace(b, max_new):
+    """Of the size asked for, all bytes set: counts of -1, sums that are no numbers."""
+    return torch.full((C8.gllm_op_attention8_workspace_bytes(b.n_q, b.n_kv, b.d, max_new),), 255, dtype=torch.uint8, device=DEV)
+
+
+def test_scales_whose_product_with_the_scores_leaves_the_range():
+    print("attention8 products out of range", flush=True)
+    b = Batch((8, 2, 64), [20, 1, 3], [60, 70, 40], seed=14)
+    b.scales[:, :, 0] = 1e-30
+    b.run(scale=1e-30)
+    b.check(scale=1e-30, label="scale 1e-30 over scales of 1e-30")
+    b.scales[:, :, 0] = 1e30
+    b.q.zero_()
+    b.run(scale=2e38)
+    b.check(scale=2e38, label="queries of zeros, scale 2e38 over scales of 1e30")
+
+
+@pytest.mark.parametrize("seqs,n", [(17, 40), (70, 20)])
+def test_shared_prefix_of_more_pages_than_a_tile_holds_ids_of(seqs, n):
+    """One prefix for all sequences, whose tiles are too many to be cut."""
+    print(f"attention8 {seqs} sequences over one prefix", flush=True)
+    prefix = 562 * PAGE
+    b = Batch((8, 8, 64), [n] * seqs, [prefix] + [0] * (seqs - 1), seed=15)
+    own = -(-n // PAGE)
+    for s in range(1, seqs):
+        b.tables[s, 562:562 + own] = b.tables[s, :own]
+        b.tables[s, :562] = b.tables[0, :562]
+    b.cached = [prefix] * seqs
+    b.dev[0], b.dev[1] = dev_ints(b.tables), dev_ints(b.cached)
+    for window, sinks in ((0, 0), (8500, 100)):
+        b.run(window, sinks)
+        b.check(window, sinks, label=f"{seqs} sequences over one prefix, window {window}")
+
+
+@pytest.mark.parametrize("new,cached", [([1], [400]), ([1, 40], [400, 10]), ([2, 30], [385, 3]), ([1, 1, 20], [383, 384, 500]), ([1, 1], [100, 449])], ids=str)
+def test_streams_about_as_long_as_are_cut(new, cached):
+    print(f"attention8 streams {new} {cached}", flush=True)
+    b = Batch((16, 2, 64), new, cached, seed=16)
+    b.run(workspace=spoilt_workspace(b, max(new)))
+    b.check(label=f"streams {new} {cached}")
+
+
+@pytest.mark.parametrize("heads,most", [((16, 1, 128), 1), ((4, 2, 64), 8), ((32, 8, 128), 4), ((8, 8, 64), 1)], ids=str)
+@pytest.mark.parametrize("seqs", [40, 64, 65, 200])
+def test_streams_of_very_different_lengths(seqs, heads, most):
+    print(f"attention8 {seqs} streams, {heads}", flush=True)
+    rng = np.random.default_rng(seqs)
+    cached = [int(rng.choice([0, 1, 15, 63, 64, 320, 383, 384, 448, 1500])) for _ in range(seqs)]
+    cached[3], cached[7] = 5000, 9000
+    new = [int(rng.integers(0 if i % 3 else 1, most + 1)) for i in range(seqs)]
+    new[3] = most
+    b = Batch(heads, new, cached, seed=17)
+    ws = spoilt_workspace(b, most)
+    for window, sinks in ((0, 0), (1000, 130)):
+        ws.fill_(255)
+        b.run(window, sinks, max_new=most, workspace=ws)
+        b.check(window, sinks, max_new=most, label=f"{seqs} streams {heads} window {window}")
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64), (12, 4, 128), (16, 1, 128)], ids=str)
+@pytest.mark.parametrize("seqs", [30, 64, 65, 150])
+def test_hybrids_of_every_kind_of_sequence(seqs, heads):
+    print(f"attention8 hybrid of {seqs}, {heads}", flush=True)
+    rng = np.random.default_rng(seqs)
+    new = [int(rng.choice([0, 1, 1, 1, 2, 5, 40, 130])) for _ in range(seqs)]
+    cached = [int(rng.choice([0, 1, 16, 70, 383, 500, 1300])) for _ in range(seqs)]
+    new[2], new[5], cached[5], new[seqs - 1], cached[seqs - 1] = 300, 1, 6000, 7, 2500
+    b = Batch(heads, new, cached, seed=18, tail_rows=5)
+    ws = spoilt_workspace(b, 300)
+    for window, sinks, broken in ((0, 0, False), (200, 17, False), (0, 0, True)):
+        if broken:
+            for s in (0, 9, seqs - 2):
+                b.cached[s] = [-3, 1 << 21, 2 ** 31 - 1][s % 3]
+            b.dev[1] = dev_ints(b.cached)
+        b.out.fill_(7.0)
+        ws.fill_(255)
+        b.run(window, sinks, max_new=300, workspace=ws)
+        b.check(window, sinks, max_new=300, label=f"hybrid of {seqs} {heads} window {window}")
+    b.out.fill_(7.0)
+    ws.fill_(255)
+    starts = b.starts.copy()
+    starts[seqs // 2] += 10 ** 6
+    b.dev[2] = dev_ints(starts)
+    b.run(max_new=300, workspace=ws)
+    assert bool((b.out == 7.0).all())
+
+
+@pytest.mark.parametrize("most", [2, 12])
+def test_more_sequences_than_runs_of_64(most):
+    print("attention8 5000 sequences", flush=True)
+    rng = np.random.default_rng(19)
+    new, cached = rng.integers(0, most + 1, 5000).tolist(), rng.integers(0, 40, 5000).tolist()
+    cached[4321] = 3000
+    new[4321] = most
+    b = Batch((4, 2, 64), new, cached, seed=19)
+    b.run(workspace=spoilt_workspace(b, most))
+    b.check(label=f"5000 sequences of up to {most}")
+
+
 # ---- refusals, streams, graphs -----------------------------------------------------------------------------------------------
 
 def test_binding_refuses_what_does_not_fit():
@@ -653,3 +752,56 @@ def test_a_step_captured_and_replayed_grows_its_sequences():
         ref, weight, mass = ref[:total], weight[:total], mass[:total]
         assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2 * mass[..., None] * (d + 10) * 2.0 ** -24 + 2.0 ** -17) * weight).all(), step
         cached += new
+
+
+@pytest.mark.parametrize("seqs", [20, 100])
+def test_attention_captured_and_replayed_with_other_lengths(seqs):
+    """Streams, tiles and broken sequences change places between replays, in a workspace that something else has written to."""
+    print(f"attention8 of {seqs} from a graph", flush=True)
+    heads, most = (12, 4, 128), 200
+    rng = np.random.default_rng(seqs)
+    b = Batch(heads, [most] + [4] * (seqs - 1), [4000] + [600] * (seqs - 1), seed=20, tail_rows=1500)
+    ws = spoilt_workspace(b, most)
+    tables, cached, starts = b.dev
+
+    def call(workspace, out):
+        C8.gllm_op_attention8(b.q, b.k, b.v, b.scales, tables, cached, starts, out, most, workspace=workspace)
+
+    b.k.copy_(torch.where(b.k & 0x7F == NAN_CODE, 0x20, b.k))            # (all slots and pages hold numbers)
+    b.v.copy_(torch.where(b.v & 0x7F == NAN_CODE, 0x20, b.v))
+    b.scales.nan_to_num_(nan=0.01)
+    eager = torch.empty_like(b.out)
+    call(None, eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(ws, b.out)
+    for step in range(6):
+        new = rng.choice([0, 1, 2, 5, 30], seqs)
+        new[step] = [most, 1, 150, 4, 33, most][step]
+        c = rng.integers(0, 580, seqs)
+        c[0] = 3900 if step % 2 else 100
+        if step % 3 == 2:
+            c[step + 4] = -1
+        cached.copy_(dev_ints(c))
+        starts.copy_(dev_ints(np.concatenate([[0], np.cumsum(new)])))
+        eager.fill_(7.0)
+        b.out.fill_(7.0)
+        ws.fill_(255)
+        call(None, eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(eager, b.out), step
+        # and against the oracle
+        b.new, b.cached, b.tables = new.tolist(), c.tolist(), tables.cpu().numpy()
+        b.starts = starts.cpu().numpy()
+        b.check(max_new=most, label=f"replay {step}")
+
+
+def test_binding_refuses_lengths_that_do_not_fit_32_bits():
+    b = Batch((8, 2, 64), [2, 1], [25, 46], seed=21)
+    for change in (dict(max_new=(1 << 32) + 2), dict(window=1 << 32), dict(window=40, sinks=1 << 32), dict(window=-1), dict(max_new=-(1 << 32) + 2)):
+        with pytest.raises(B.GllmError):
+            C8.gllm_op_attention8(b.q, b.k, b.v, b.scales, *b.dev, b.out, **{"max_new": 2, **change})
+    assert bool((b.out == 7.0).all())
