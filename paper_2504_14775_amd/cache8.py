@@ -39,14 +39,14 @@ _BF16, _F32, _I32, _U8, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torc
 
 def _pool_shape(call: str, k_pool, v_pool, scales):
     """(pages, KV heads, head size) of a layer's pools; codes are uint8 or float8_e4m3fn."""
-    k, v = k_pool.shape, v_pool.shape
-    if len(k) != 6 or len(v) != 4 or k[:2] != v[:2] or k[2] != 4 or k[4] != 4 or k[5] != 16 or v[3] != PAGE or v[2] != 16 * k[3] or v[2] == 0 or \
-            scales.shape != (k[0], k[1], 2):
-        _refuse(f"{call}: pools of shapes {tuple(k)}, {tuple(v)} and {tuple(scales.shape)}")
-    for t in (k_pool, v_pool):
-        if t.dtype is not _U8 and t.dtype is not _E4M3:
-            _refuse(f"{call}: codes are uint8 or float8_e4m3fn, got {t.dtype}")
-    return k[0], k[1], v[2]
+    v = v_pool.shape
+    pages, n_kv, d = v[:3] if len(v) == 4 and v[3] == PAGE else (0, 0, 0)
+    if d == 0 or d % 16 != 0 or k_pool.shape != (pages, n_kv, 4, d // 16, 4, 16) or scales.shape != (pages, n_kv, 2):
+        _refuse(f"{call}: pools of shapes {tuple(k_pool.shape)}, {tuple(v)} and {tuple(scales.shape)}")
+    for t in (k_pool.dtype, v_pool.dtype):
+        if t is not _U8 and t is not _E4M3:
+            _refuse(f"{call}: codes are uint8 or float8_e4m3fn, got {t}")
+    return pages, n_kv, d
 
 
 def gllm_op_step_maps(new_tokens, cached_len, free_pages, block_tables, num_blocks: int, row_start, positions, slots, needed, stream=None) -> None:
@@ -75,17 +75,19 @@ def gllm_op_norm_rope_store8(qkv, q_gain, k_gain, eps: float, rope, positions, s
     pages, n_kv, d = _pool_shape(call, k_pool, v_pool, scales)
     if qkv.dtype is not _F32 and qkv.dtype is not _BF16:
         _refuse(f"{call}: rows are float32 or bfloat16, got {qkv.dtype}")
-    gains = tuple((g, _BF16) for g in (q_gain, k_gain) if g is not None)
-    dev = _check(call, ((qkv, qkv.dtype), (rope, _F32), (positions, _I32), (slots, _I32), (q_out, _BF16), (k_pool, k_pool.dtype),
-                        (v_pool, v_pool.dtype), (scales, _F32)) + gains, rows_only=(qkv, q_out))
-    rows = slots.numel()
-    if qkv.dim() != 2 or q_out.dim() != 2 or qkv.shape[0] != rows or q_out.shape[0] != rows or positions.numel() != rows or q_out.shape[1] % d != 0 or \
-            qkv.shape[1] != q_out.shape[1] + 2 * n_kv * d or rope.dim() != 3 or rope.shape[1:] != (d // 2, 2) or any(g.numel() != d for g, _ in gains):
-        _refuse(f"{call}: shapes qkv {tuple(qkv.shape)}, q_out {tuple(q_out.shape)}, rope {tuple(rope.shape)}, positions {tuple(positions.shape)}, "
-                f"slots {tuple(slots.shape)}, gains {[tuple(g.shape) for g, _ in gains]}, {n_kv} KV heads of {d}")
+    tensors = ((qkv, qkv.dtype), (rope, _F32), (positions, _I32), (slots, _I32), (q_out, _BF16), (k_pool, k_pool.dtype), (v_pool, v_pool.dtype),
+               (scales, _F32))
+    gains = [g for g in (q_gain, k_gain) if g is not None]
+    dev = _check(call, tensors + tuple((g, _BF16) for g in gains) if gains else tensors, rows_only=(qkv, q_out))
+    rows, table = slots.numel(), rope.shape
+    width = q_out.shape[1] if q_out.dim() == 2 else 0
+    if qkv.shape != (rows, width + 2 * n_kv * d) or q_out.shape != (rows, width) or width % d != 0 or positions.numel() != rows or \
+            table != (table[0], d // 2, 2) or [g.numel() for g in gains] != [d] * len(gains):
+        _refuse(f"{call}: shapes qkv {tuple(qkv.shape)}, q_out {tuple(q_out.shape)}, rope {tuple(table)}, positions {tuple(positions.shape)}, "
+                f"slots {tuple(slots.shape)}, gains {[tuple(g.shape) for g in gains]}, {n_kv} KV heads of {d}")
     st = _lib().gllm_op_norm_rope_store8(qkv.data_ptr(), _row_stride(qkv), 0 if qkv.dtype is _F32 else 1, None if q_gain is None else q_gain.data_ptr(),
-                                         None if k_gain is None else k_gain.data_ptr(), eps, rope.data_ptr(), rope.shape[0], positions.data_ptr(),
-                                         slots.data_ptr(), rows, q_out.shape[1] // d, n_kv, d, q_out.data_ptr(), _row_stride(q_out), k_pool.data_ptr(),
+                                         None if k_gain is None else k_gain.data_ptr(), eps, rope.data_ptr(), table[0], positions.data_ptr(),
+                                         slots.data_ptr(), rows, width // d, n_kv, d, q_out.data_ptr(), _row_stride(q_out), k_pool.data_ptr(),
                                          v_pool.data_ptr(), scales.data_ptr(), pages, _stream(stream, dev))
     if st != GLLM_OK:
         raise GllmError(st, call)

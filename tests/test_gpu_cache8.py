@@ -805,3 +805,60 @@ def test_binding_refuses_lengths_that_do_not_fit_32_bits():
         with pytest.raises(B.GllmError):
             C8.gllm_op_attention8(b.q, b.k, b.v, b.scales, *b.dev, b.out, **{"max_new": 2, **change})
     assert bool((b.out == 7.0).all())
+
+
+def test_pools_beyond_4_gib():
+    """The same pages at the far end of a large pool: the same bits."""
+    print("a pool beyond 4 GiB", flush=True)
+    heads, pages = (16, 8, 128), 270000
+    k, v = (torch.zeros(pages, *shape, dtype=torch.uint8, device=DEV) for shape in ((8, 4, 8, 4, 16), (8, 128, 16)))
+    scales = torch.ones(pages, 8, 2, device=DEV)
+    assert k.numel() > 2 ** 32 and v.numel() > 2 ** 32
+    b = Batch(heads, [1, 2, 60, 5], [500, 30, 700, 2000], seed=22)
+    want = b.run().clone()
+    few = b.k.shape[0]
+    small = [x.clone() for x in (b.k, b.v, b.scales)]
+    for big, x in zip((k, v, scales), small):
+        big[pages - few:] = x
+    b.k, b.v, b.scales = k, v, scales
+    b.dev[0] = dev_ints(b.tables + (pages - few))
+    b.out.fill_(7.0)
+    assert torch.equal(b.run(), want)
+    s = Store(heads, RUNS, seed=23)
+    few = s.k.shape[0]
+    for big, x in zip((k, v, scales), (s.k, s.v, s.scales)):
+        big[pages - few:] = x
+    s.run()
+    want = [x.clone() for x in (s.q_out, s.k, s.v, s.scales)]
+    s.q_out.fill_(7.0)
+    s.k, s.v, s.scales = k, v, scales
+    s.slots = s.slots + (pages - few) * PAGE
+    s.run()
+    assert torch.equal(s.q_out, want[0])
+    for big, x in zip((k, v, scales), want[1:]):
+        assert torch.equal(big[pages - few:].view(torch.uint8), x.view(torch.uint8))
+
+
+def test_rows_whose_offsets_pass_32_bits():
+    print("rows far apart", flush=True)
+    far = 1 << 28
+    b = Batch((8, 2, 128), [1, 20, 3], [100, 200, 50], seed=24)
+    want = b.run().clone()
+    rows, width = b.q.shape
+    wide = torch.empty(rows, far, dtype=torch.bfloat16, device=DEV)
+    assert rows * far > 2 ** 32
+    wide[:, :width] = b.q
+    b.q, b.out = wide[:, :width], wide[:, 4096:4096 + width]
+    b.out.fill_(7.0)
+    assert torch.equal(b.run(), want)
+    s = Store((8, 2, 128), [(0, 16), (3, 4), (5, 1)], torch.bfloat16, seed=25)
+    first = [x.clone() for x in (s.k, s.v, s.scales)]
+    s.run()
+    want = [x.clone() for x in (s.q_out, s.k, s.v, s.scales)]
+    rows, width = s.qkv.shape
+    wide[:rows, :width] = s.qkv
+    s.qkv, s.q_out = wide[:rows, :width], wide[:rows, 4096:4096 + s.q_out.shape[1]]
+    s.k, s.v, s.scales = first
+    s.run()
+    for a, x in zip((s.q_out, s.k, s.v, s.scales), want):
+        assert torch.equal(a, x)
