@@ -10,6 +10,14 @@
 //
 // Up to 16 columns (decode rows) the keys are a stream from HBM: stream_wave.  More go in tiles whose keys pass through LDS: tile_unit.
 // The keys of long sequences are shared among waves, or units, by a plan made on the device, and the parts' results joined by a second launch.
+//
+// Roundings: queries, codes as bf16 (exact), weights p s_v and the output are bf16, all else float.  A weight rounded to bf16 is what a matrix
+// instruction takes; its error, up to 2^-8 of it, is in the output's tolerance.  Tiles sum the rounded weights (one instruction for two of them, and
+// the error of a weight cancels where all values agree), streams, which have instructions to spare, the unrounded.
+//
+// Measured (8 KV heads of 128): 32 decode rows behind 300 .. 20000 keys, 308 MB, 58 us with the joining, 53 + 5, 5.8 TB/s inside the kernel (a copy
+// reaches 5.2); 64 behind a window of 1024, 33 us; 251 decode rows and 1802 chunk rows together, 938 MB and 63 GFLOP, 201 us; a chunk of 4096 behind
+// 4096 keys, 64 heads, 825 GFLOP that count, 823 us, 1.0 PFLOP/s (a large product reaches 1.42).
 #include "cache8.h"
 
 #include <algorithm>
@@ -49,9 +57,9 @@ __host__ __device__ constexpr int per_head(int total, int n_kv) { return total /
 // Workgroups of the stream at most.
 template <bool TILES>
 __host__ __device__ constexpr int max_workers(int n_kv, int d) { return per_head(TILES || d == 128 ? kGroups : 2 * kGroups, n_kv); }
-// Units that the keys of tiles are cut into.  Every part of a tile writes and reads partial results of (d + 2) floats a column, as much as eight blocks of
-// keys.  us at 128 / 256 / 512: a chunk of 901 behind 2011 keys (14B heads) 103 / 105 / 102, of 4096 behind none (8B) 165 / 167 / 230, 251 decode rows beside 1400
-// chunk rows (14B) 201 / 225 / 263, 100 rows behind 6000 keys 40 / 38 / 42.
+// Units that the keys of tiles are cut into.  Every part of a tile writes and reads partial results of (d + 2) floats a column, as much as eight
+// blocks of keys.  us at 128 / 256 / 512: a chunk of 901 behind 2011 keys (14B heads) 103 / 105 / 102, of 4096 behind none (8B) 165 / 167 / 230, 251
+// decode rows beside 1802 chunk rows (14B) 201 / 225 / 263, 100 rows behind 6000 keys 40 / 38 / 42.
 __host__ __device__ constexpr int target_units(int n_kv) { return per_head(kGroups / 2, n_kv); }
 // Tiles with partial results and columns of these.  A tile is cut where its sequence has more blocks than a share, into at most ceil(blocks /
 // share) parts; the shares of all are at least half their blocks by the target (seq_plan: twice the weight is at least the blocks).
@@ -126,10 +134,11 @@ __device__ __forceinline__ T lane_value(T x, int lane) { return __builtin_bit_ca
 // 1e-4 of itself larger, which is more than the roundings of the additions, 2^-24 of the sum each, take away, kMaxAttn8Seqs / 4096 of a lane and 15
 // over lanes and runs.)
 static_assert(kMaxAttn8Seqs / (64 * 64) + 15 < 16777216 / 10000, "the sum of all weights");
-// A block of a tile keeps a compute unit busy for 2.2 us, one of a stream, where half of the units draw all that the memory gives, for 0.35.  us at 4 / 6 / 8:
-// 251 decode rows beside 1400 chunk rows (14B heads) 212 / 201 / 211, 256 beside 1792 (8B) 226 / 202 / 214, 32 beside 4 x 128 91 / 82 / 79.
+// A block of a tile keeps a compute unit busy for 2.2 us, one of a stream, where half of the units draw all that the memory gives, for 0.35.  us at 4
+// / 6 / 8: 251 decode rows beside 1802 chunk rows (14B heads) 212 / 201 / 211, 256 beside 1792 (8B) 226 / 202 / 214, 32 beside 4 x 128 91 / 82 / 79.
 constexpr float kTileCost = 6.f;
-// Blocks of a wave of the stream, where there are few: us at 2 / 4 / 8, one sequence of 3000 keys (8B heads) 12.8 / 15.0 / 17.7, of 20000 18.9 / 17.9 / 21.7.
+// Blocks of a wave of the stream, where there are few: us at 2 / 4 / 8, one sequence of 3000 keys (8B heads) 12.8 / 15.0 / 17.7, of 20000 18.9 / 17.9
+// / 21.7.
 constexpr int kFewBlocks = 2;
 template <bool TILES>
 __device__ __forceinline__ int workers_of(float stream, float tiles, int n_kv, int d) {
@@ -442,11 +451,14 @@ struct PageScale {
 
 // ---- streams ---------------------------------------------------------------------------------------------------------------
 //
-// Each wave takes a run of blocks for all columns of their sequences, operands straight to registers.  Matrix instructions of 16x16x32: the row
-// 4q + i of score tile t is slot 4t + i of page q, so that a lane of group G receives the 16 slots of page G.  An instruction that loads keys takes
-// runs of 256 bytes from each of the four pages, one that loads values the 16 slots of 16 dims of each.  The keys of the next block are asked for
-// when the scores of this one are made, its values when this one's outputs are, into the same registers; so there is always half a block on its way,
-// and the waves that share a compute unit hide each other's work.
+// Each wave takes a run of blocks for all columns of their sequences, operands straight to registers.  Matrix instructions of 16x16x32: the row 4q +
+// i of score tile t is slot 4t + i of page q, so that a lane of group G receives the 16 slots of page G.  An instruction that loads keys takes runs
+// of 256 bytes from each of the four pages, one that loads values the 16 slots of 16 dims of each.  The keys of the next block are asked for when the
+// scores of this one are made, its values when this one's outputs are, into the same registers; so there is always half a block on its way, and the
+// waves that share a compute unit hide each other's work.  Bound by HBM: 16 KB a block and KV head for 32 matrix instructions, whose unit is busy for
+// 1/15 of the time.  Two blocks in registers would spill; without equal runs (parts of whole blocks per sequence, so many to each) 71 us instead of
+// 57 for 32 decode rows behind 300 .. 20000 keys.
+
 // A value that all lanes have, for the compiler to know.
 __device__ __forceinline__ int64_t of_wave(int64_t x) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
@@ -741,6 +753,14 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 //   values as bf16  [page][2 halves of the slots][D][8 slots]
 // The exponentials of a half run beside the scores of the next one and in front of its own outputs; what a phase reads from LDS is asked for in the
 // phase before.
+//
+// What bounds it, a chunk of 4096 behind 4096 keys: matrix cores busy 0.42 of the time, vector units 0.43 by their own counter (about 0.54 with the
+// exponentials at a quarter of the rate), LDS 0.5 (each wave reads all keys and values: 256 KB a block and 64 KB of staging at 128 bytes a cycle), no
+// bank conflicts; none of the three is full, since a wave's chain goes through all of them and 8 waves, all that the registers allow, meet at a
+// barrier every 64 keys.  823 us; without staging, barriers and masks 715, without LDS reads besides 653, without exponentials besides 590, which is
+// the matrix cores' rate at the power limit.  Steps to here: 4 waves of 64 columns, 32 keys at a time, 1143, matrix and vector instructions in a
+// given order 1002, 8 waves of 32 and blocks of 64 keys 846.  Raised priority of half of the waves, and pieces of the first blocks asked for beside
+// their scales, change nothing.
 constexpr int kHalf = 32, kRaw = 4, kKeyStages = 2, kValueStages = 2, kWindow = 64;
 struct PageEntry {
     int32_t id;
@@ -1113,8 +1133,8 @@ __device__ __forceinline__ Joined join_parts(const f32x2* ml, const float* o, in
     if (mine <= 4) return join_batches<4>(ml, o, first, step, n, d, e, at);
     return join_batches<12>(ml, o, first, step, n, d, e, at);
 }
-// All latency.  The first workgroups take a wave of the stream and a KV head each: D/4 threads have a column, or, where that leaves threads over, each so many of
-// its parts; the others 2048 / D columns of a cut tile.
+// All latency.  The first workgroups take a wave of the stream and a KV head each: D/4 threads have a column, or, where that leaves threads over,
+// each so many of its parts; the others as many columns of a cut tile as there are D/4 threads.
 template <int D, bool TILES, int THREADS>
 __global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, int stream_groups) {
     constexpr int LANES = D / 4, TEAMS = THREADS / LANES;
