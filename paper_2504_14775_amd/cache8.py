@@ -13,6 +13,7 @@ from .branch import _check, _own_workspace, _refuse, _row_stride, _stream
 EXPORTS = ["gllm_op_step_maps", "gllm_op_norm_rope_store8", "gllm_op_attention8", "gllm_op_attention8_workspace_bytes"]
 PAGE = 16
 
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
 _ready = None
 
 
@@ -37,6 +38,10 @@ def _lib():
 _BF16, _F32, _I32, _U8, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn
 
 
+# A call's tensors are checked by one expression first, which takes a microsecond less than a loop over them; where it does not hold, _check says what is
+# wrong, or that nothing is (rows with strides).
+
+
 def _pool_shape(call: str, k_pool, v_pool, scales):
     """(pages, KV heads, head size) of a layer's pools; codes are uint8 or float8_e4m3fn."""
     v = v_pool.shape
@@ -53,13 +58,19 @@ def gllm_op_step_maps(new_tokens, cached_len, free_pages, block_tables, num_bloc
     """new_tokens, cached_len: int32 [S]; free_pages: int32 [F]; block_tables: int32 [S, entries], extended; row_start: int32 [S+1],
     positions, slots: int32 [R], needed: int32 [2], written."""
     call = "gllm_op_step_maps"
-    dev = _check(call, ((new_tokens, _I32), (cached_len, _I32), (free_pages, _I32), (block_tables, _I32), (row_start, _I32), (positions, _I32),
-                        (slots, _I32), (needed, _I32)))
+    dev = new_tokens.get_device()
+    if not (dev >= 0 and cached_len.get_device() == free_pages.get_device() == block_tables.get_device() == row_start.get_device() ==
+            positions.get_device() == slots.get_device() == needed.get_device() == dev == _device() and
+            new_tokens.dtype is cached_len.dtype is free_pages.dtype is block_tables.dtype is row_start.dtype is positions.dtype is slots.dtype is needed.dtype is _I32 and
+            new_tokens.is_contiguous() and cached_len.is_contiguous() and free_pages.is_contiguous() and block_tables.is_contiguous() and
+            row_start.is_contiguous() and positions.is_contiguous() and slots.is_contiguous() and needed.is_contiguous()):
+        _check(call, ((new_tokens, _I32), (cached_len, _I32), (free_pages, _I32), (block_tables, _I32), (row_start, _I32), (positions, _I32), (slots, _I32),
+                      (needed, _I32)))
     seqs, rows = new_tokens.numel(), slots.numel()
-    if cached_len.numel() != seqs or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1 or positions.numel() != rows or \
+    if free_pages.dim() != 1 or cached_len.numel() != seqs or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1 or positions.numel() != rows or \
             needed.numel() != 2:
-        _refuse(f"{call}: shapes new_tokens {tuple(new_tokens.shape)}, cached_len {tuple(cached_len.shape)}, block_tables {tuple(block_tables.shape)}, "
-                f"row_start {tuple(row_start.shape)}, positions {tuple(positions.shape)}, slots {tuple(slots.shape)}, needed {tuple(needed.shape)}")
+        _refuse(f"{call}: shapes new_tokens {tuple(new_tokens.shape)}, cached_len {tuple(cached_len.shape)}, free_pages {tuple(free_pages.shape)}, "
+                f"block_tables {tuple(block_tables.shape)}, row_start {tuple(row_start.shape)}, positions {tuple(positions.shape)}, slots {tuple(slots.shape)}, needed {tuple(needed.shape)}")
     st = _lib().gllm_op_step_maps(new_tokens.data_ptr(), cached_len.data_ptr(), seqs, free_pages.data_ptr(), free_pages.numel(), block_tables.data_ptr(),
                                   block_tables.shape[1], num_blocks, rows, row_start.data_ptr(), positions.data_ptr(), slots.data_ptr(),
                                   needed.data_ptr(), _stream(stream, dev))
@@ -75,16 +86,24 @@ def gllm_op_norm_rope_store8(qkv, q_gain, k_gain, eps: float, rope, positions, s
     pages, n_kv, d = _pool_shape(call, k_pool, v_pool, scales)
     if qkv.dtype is not _F32 and qkv.dtype is not _BF16:
         _refuse(f"{call}: rows are float32 or bfloat16, got {qkv.dtype}")
-    tensors = ((qkv, qkv.dtype), (rope, _F32), (positions, _I32), (slots, _I32), (q_out, _BF16), (k_pool, k_pool.dtype), (v_pool, v_pool.dtype),
-               (scales, _F32))
-    gains = [g for g in (q_gain, k_gain) if g is not None]
-    dev = _check(call, tensors + tuple((g, _BF16) for g in gains) if gains else tensors, rows_only=(qkv, q_out))
+    dev = qkv.get_device()
+    if not (dev >= 0 and rope.get_device() == positions.get_device() == slots.get_device() == q_out.get_device() == k_pool.get_device() ==
+            v_pool.get_device() == scales.get_device() == dev == _device() and rope.dtype is scales.dtype is _F32 and
+            positions.dtype is slots.dtype is _I32 and q_out.dtype is _BF16 and qkv.is_contiguous() and rope.is_contiguous() and
+            positions.is_contiguous() and slots.is_contiguous() and q_out.is_contiguous() and k_pool.is_contiguous() and v_pool.is_contiguous() and
+            scales.is_contiguous()):
+        _check(call, ((qkv, qkv.dtype), (rope, _F32), (positions, _I32), (slots, _I32), (q_out, _BF16), (k_pool, k_pool.dtype), (v_pool, v_pool.dtype),
+                      (scales, _F32)), rows_only=(qkv, q_out))
+    for g in (q_gain, k_gain):
+        if g is not None and not (g.get_device() == dev and g.dtype is _BF16 and g.is_contiguous() and g.numel() == d):
+            _check(call, ((qkv, qkv.dtype), (g, _BF16)), rows_only=(qkv,))
+            _refuse(f"{call}: a gain of shape {tuple(g.shape)} for heads of {d}")
     rows, table = slots.numel(), rope.shape
     width = q_out.shape[1] if q_out.dim() == 2 else 0
     if qkv.shape != (rows, width + 2 * n_kv * d) or q_out.shape != (rows, width) or width % d != 0 or positions.numel() != rows or \
-            table != (table[0], d // 2, 2) or [g.numel() for g in gains] != [d] * len(gains):
+            rope.dim() != 3 or table[1] != d // 2 or table[2] != 2:
         _refuse(f"{call}: shapes qkv {tuple(qkv.shape)}, q_out {tuple(q_out.shape)}, rope {tuple(table)}, positions {tuple(positions.shape)}, "
-                f"slots {tuple(slots.shape)}, gains {[tuple(g.shape) for g in gains]}, {n_kv} KV heads of {d}")
+                f"slots {tuple(slots.shape)}, {n_kv} KV heads of {d}")
     st = _lib().gllm_op_norm_rope_store8(qkv.data_ptr(), _row_stride(qkv), 0 if qkv.dtype is _F32 else 1, None if q_gain is None else q_gain.data_ptr(),
                                          None if k_gain is None else k_gain.data_ptr(), eps, rope.data_ptr(), table[0], positions.data_ptr(),
                                          slots.data_ptr(), rows, width // d, n_kv, d, q_out.data_ptr(), _row_stride(q_out), k_pool.data_ptr(),
@@ -103,8 +122,14 @@ def gllm_op_attention8(q, k_pool, v_pool, scales, block_tables, cached_len, row_
     scale: 1/sqrt(d) if not given; workspace: uint8, taken from torch's allocator if not given."""
     call = "gllm_op_attention8"
     pages, n_kv, d = _pool_shape(call, k_pool, v_pool, scales)
-    dev = _check(call, ((q, _BF16), (out, _BF16), (k_pool, k_pool.dtype), (v_pool, v_pool.dtype), (scales, _F32), (block_tables, _I32), (cached_len, _I32),
-                        (row_start, _I32)), rows_only=(q, out))
+    dev = q.get_device()
+    if not (dev >= 0 and out.get_device() == k_pool.get_device() == v_pool.get_device() == scales.get_device() == block_tables.get_device() ==
+            cached_len.get_device() == row_start.get_device() == dev == _device() and q.dtype is out.dtype is _BF16 and scales.dtype is _F32 and
+            block_tables.dtype is cached_len.dtype is row_start.dtype is _I32 and q.is_contiguous() and out.is_contiguous() and k_pool.is_contiguous() and
+            v_pool.is_contiguous() and scales.is_contiguous() and block_tables.is_contiguous() and cached_len.is_contiguous() and
+            row_start.is_contiguous()):
+        _check(call, ((q, _BF16), (out, _BF16), (k_pool, k_pool.dtype), (v_pool, v_pool.dtype), (scales, _F32), (block_tables, _I32), (cached_len, _I32),
+                      (row_start, _I32)), rows_only=(q, out))
     seqs = cached_len.numel()
     if q.dim() != 2 or q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1:
         _refuse(f"{call}: shapes q {tuple(q.shape)}, out {tuple(out.shape)}, block_tables {tuple(block_tables.shape)}, cached_len {tuple(cached_len.shape)}, "
@@ -115,7 +140,8 @@ def gllm_op_attention8(q, k_pool, v_pool, scales, block_tables, cached_len, row_
     lib = _lib()
     if workspace is None:
         workspace = _own_workspace(call, int(lib.gllm_op_attention8_workspace_bytes(n_q, n_kv, d, max_new)), q, stream)
-    _check(call, ((workspace, _U8),))
+    elif workspace.get_device() != dev or workspace.dtype is not _U8 or not workspace.is_contiguous():
+        _check(call, ((q, _BF16), (workspace, _U8)), rows_only=(q,))
     st = lib.gllm_op_attention8(q.data_ptr(), _row_stride(q), k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(), pages, block_tables.data_ptr(),
                                 block_tables.shape[1], cached_len.data_ptr(), row_start.data_ptr(), seqs, q.shape[0], max_new, window, sinks, n_q, n_kv, d,
                                 1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(), _row_stride(out), workspace.data_ptr(),

@@ -862,3 +862,26 @@ def test_rows_whose_offsets_pass_32_bits():
     s.run()
     for a, x in zip((s.q_out, s.k, s.v, s.scales), want):
         assert torch.equal(a, x)
+
+
+def test_binding_looks_at_every_tensor():
+    """Each argument in turn of another type, on the CPU, with gaps or of another shape; nothing is written."""
+    b = Batch((8, 2, 64), [2, 1], [25, 46], seed=26)
+    s = Store((8, 2, 64), [(0, 3)], seed=27)
+    row, entry = dev_ints([0] * 3), dev_ints([0, 1, 2])
+    maps = [dev_ints(x) for x in ([2, 1], [25, 46], [1, 2], np.zeros((2, 3)), [0] * 3, [0] * 3, [0] * 3, [0] * 2)]
+    calls = [(lambda *t: C8.gllm_op_attention8(*t, 2), [b.q, b.k, b.v, b.scales, *b.dev, b.out]),
+             (lambda *t: C8.gllm_op_attention8(*t[:-1], 2, workspace=t[-1]), [b.q, b.k, b.v, b.scales, *b.dev, b.out, spoilt_workspace(b, 2)]),
+             (lambda qkv, g, h, *t: C8.gllm_op_norm_rope_store8(qkv, g, h, 1e-6, *t), [s.qkv, *s.gains, s.rope, row, entry, s.q_out, s.k, s.v, s.scales]),
+             (lambda *t: C8.gllm_op_step_maps(*t[:4], 9, *t[4:]), maps)]
+    for call, tensors in calls:
+        written = [t.clone() for t in tensors]
+        for i, t in enumerate(tensors):
+            gaps = torch.zeros(*t.shape, 2, dtype=t.dtype, device=DEV)[..., 0]
+            for other in (t.double(), t.cpu(), gaps, t.new_zeros(()), t.new_zeros((2, 3, 5, 7))):
+                with pytest.raises(B.GllmError):
+                    call(*tensors[:i], other, *tensors[i + 1:])
+        for t, was in zip(tensors, written):
+            assert torch.equal(t.view(torch.uint8), was.view(torch.uint8))
+        call(*tensors)
+    torch.cuda.synchronize()
