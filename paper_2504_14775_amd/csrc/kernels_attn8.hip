@@ -760,7 +760,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 // barrier every 64 keys.  823 us; without staging, barriers and masks 715, without LDS reads besides 653, without exponentials besides 590, which is
 // the matrix cores' rate at the power limit.  Steps to here: 4 waves of 64 columns, 32 keys at a time, 1143, matrix and vector instructions in a
 // given order 1002, 8 waves of 32 and blocks of 64 keys 846.  Raised priority of half of the waves, and pieces of the first blocks asked for beside
-// their scales, change nothing.
+// their scales, change nothing, nor does a fifth fewer vector instructions (a reference that moves when a sum of weights has grown).
 constexpr int kHalf = 32, kRaw = 4, kKeyStages = 2, kValueStages = 2, kWindow = 64;
 struct PageEntry {
     int32_t id;
