@@ -251,7 +251,7 @@ __device__ __forceinline__ void norm_rotate(f32x4& lo, f32x4& hi, const bf16_t* 
 // among these that receive one row only (decode rows) are done together, D/8 lanes to each, the others one after another (1024 decode rows 23 -> 17
 // us).  Bound by HBM for chunks: 8192 rows of 64 + 16 heads of 128 in float, 491 MB, 94 us, 5.2 TB/s, what a copy reaches; queries alone 75, pages
 // alone 23.  2053 rows of 40 + 16 heads, 251 of them single, 85 MB: 20 us, of which 15 for the pages alone, whose chain (slots, rows, largest
-// magnitude, kept codes, stores) is the longer one, so that they are the first workgroups (26 us behind the queries).  64 decode rows 10 us, latency.
+// magnitude, kept codes, stores) is the longer one, so that they are the first workgroups (26 us behind the queries).  64 decode rows 9 us, latency.
 // Query passes 1 / 2 / 4: 77 / 75 / 78 us for the queries of the 8192 rows.
 constexpr int kQueryPasses = 2;
 
