@@ -25,9 +25,6 @@
 
 namespace {
 
-typedef const __attribute__((address_space(1))) void* gptr_t;
-typedef __attribute__((address_space(3))) void* lptr_t;
-
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kNegBig = -1.0e30f;
@@ -422,7 +419,7 @@ __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d
 
 // ---- common to both kinds of units -------------------------------------------------------------------------------------
 
-// A barrier that waits for this wave's reads and writes of LDS only: __syncthreads() would wait for the loads into the ring too.
+// A barrier that waits for this wave's reads and writes of LDS only: __syncthreads() would wait for the loads on their way too.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Four codes as bf16, without rounding.
@@ -746,29 +743,30 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 
 // ---- tiles of columns --------------------------------------------------------------------------------------------------------
 //
-// One workgroup of 8 waves, 32 columns a wave, matrix instructions of 32x32x16.  Keys come in blocks of 64, four pages: their codes go from HBM
-// into a ring in LDS, each thread turns the pieces that it asked for into bf16, and all waves read these, half a block (two pages) after the other.
+// One workgroup of 8 waves, 32 columns a wave, matrix instructions of 32x32x16.  Keys come in blocks of 64, four pages: each thread asks for a piece
+// of their codes and of their values a block ahead, puts it into LDS as bf16 when it has come, and all waves read these, half a block (two pages)
+// after the other.  (Codes through a ring in LDS, four blocks deep, cost 4 to 5 % more: the reads and waits of what every thread had asked for itself.)
 // The row 8a + 4h + b of a score tile is slot 4a + b of page h of the half, so that the lanes of half h receive the 16 slots of page h.
 //   keys as bf16    [half][D / 8][32 rows][8 dims], row x of piece c at x ^ 4 (c / 2 % 4): the writes of 16 lanes hit different banks
 //   values as bf16  [page][2 halves of the slots][D][8 slots]
 // The exponentials of a half run beside the scores of the next one and in front of its own outputs; what a phase reads from LDS is asked for in the
 // phase before.
 //
-// What bounds it, a chunk of 4096 behind 4096 keys: matrix cores busy 0.42 of the time, vector units 0.43 by their own counter (about 0.54 with the
-// exponentials at a quarter of the rate), LDS 0.5 (each wave reads all keys and values: 256 KB a block and 64 KB of staging at 128 bytes a cycle), no
-// bank conflicts; none of the three is full, since a wave's chain goes through all of them and 8 waves, all that the registers allow, meet at a
-// barrier every 64 keys.  823 us; without staging, barriers and masks 715, without LDS reads besides 653, without exponentials besides 590, which is
-// the matrix cores' rate at the power limit.  Steps to here: 4 waves of 64 columns, 32 keys at a time, 1143, matrix and vector instructions in a
-// given order 1002, 8 waves of 32 and blocks of 64 keys 846.  Raised priority of half of the waves, and pieces of the first blocks asked for beside
-// their scales, change nothing, nor does a fifth fewer vector instructions (a reference that moves when a sum of weights has grown).
-constexpr int kHalf = 32, kRaw = 4, kKeyStages = 2, kValueStages = 2, kWindow = 64;
+// What bounds it, a chunk of 4096 behind 4096 keys: 780 us, 1.06 PFLOP/s.  Per block of 64 keys (2.0 us) the matrix cores are busy for 0.9 us, the
+// vector units for about 1.2 (32 exponentials and some 190 others a wave), LDS, which each wave reads all keys and values from, for 1.1; a wave's
+// chain goes through all three, and there are two waves on a SIMD to hide each other's waits, all that the registers allow.  What each costs, with
+// data that does not change so that the clock stays: without staging and barriers 18 % less, without exponentials 8 %, without reads of LDS nothing;
+// random data costs 5 %, by the clock.  Steps to here: 4 waves of 64 columns, 32 keys at a time, 1143 us, matrix and vector instructions in a given
+// order 1002, 8 waves of 32 and blocks of 64 keys 846, the compiler's own order 832.  No gain: raised priority of half of the waves, a reference that
+// moves when a sum of weights has grown (a fifth fewer vector instructions), instructions held in the order of the source (3 % slower).
+
+constexpr int kHalf = 32, kKeyStages = 2, kValueStages = 2, kWindow = 64;
 struct PageEntry {
     int32_t id;
     PageScale scale;
 };
 template <int D>
 struct TileLds {
-    unsigned char raw[kRaw][2][kBlock * D];         // [block][keys, values]: codes as loaded; the keys of block j with the values of block j - 1
     unsigned char keys[kKeyStages][2][kHalf * D * 2];
     unsigned char values[kValueStages][2][kHalf * D * 2];
     PageEntry pages[2][kWindow * 4];                // of 64 blocks and the next 64
@@ -823,15 +821,10 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         const bool has_keys = BOTH || wave < 4, has_values = BOTH || wave >= 4;
         const int piece = BOTH ? threadIdx.x : threadIdx.x & 255, page = piece / D, piece_at = piece % D;
         const int64_t piece_off = (int64_t)kvh * PH + piece_at * 16, page_step = (int64_t)a.n_kv * PH;
-        // every wave issues its pieces (of the last block again behind it), so that the number on their way is the same in every round
-        auto issue = [&](int j, int id_keys, int id_values) {  // the keys of block j and the values of block j - 1
-            unsigned char* to = &lds.raw[j % kRaw][0][0] + wave * 1024;
-            if (has_keys) __builtin_amdgcn_global_load_lds((gptr_t)(a.k_pool + id_keys * page_step + piece_off), (lptr_t)to, 16, 0, 0);
-            if (has_values) __builtin_amdgcn_global_load_lds((gptr_t)(a.v_pool + id_values * page_step + piece_off), (lptr_t)(to + (BOTH ? kBlock * D : 0)), 16, 0, 0);
-        };
-        auto id_of = [&](int j) { return entry_of(min(max(j, 0), blocks - 1), page).id; };  // (the same for the wave; read a round before it is wanted)
-        auto raw_keys = [&](int j) { return *reinterpret_cast<const u32x4*>(&lds.raw[j % kRaw][0][0] + threadIdx.x * 16); };  // which have come
-        auto raw_values = [&](int j) { return *reinterpret_cast<const u32x4*>(&lds.raw[j % kRaw][0][0] + threadIdx.x * 16 + (BOTH ? kBlock * D : 0)); };
+        // (behind the last block its pieces again)
+        auto load_keys = [&](int id) { return has_keys ? *reinterpret_cast<const u32x4*>(a.k_pool + id * page_step + piece_off) : u32x4{0u, 0u, 0u, 0u}; };
+        auto load_values = [&](int id) { return has_values ? *reinterpret_cast<const u32x4*>(a.v_pool + id * page_step + piece_off) : u32x4{0u, 0u, 0u, 0u}; };
+        auto id_of = [&](int j) { return entry_of(min(j, blocks - 1), page).id; };  // (the same for the wave; read a round before it is wanted)
         // Values that are no numbers may reach the columns that see them only: where not all rows see all keys they are emptied, and the key's scores are
         // no numbers.
         auto clean = [&](int b, u32x4& x) {
@@ -939,21 +932,21 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             entry(threadIdx.x, id, a.scales[(int64_t)id * a.n_kv + kvh]);
         }
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kRaw; ++j) issue(j, __builtin_amdgcn_readfirstlane(id_of(j)), __builtin_amdgcn_readfirstlane(id_of(j - 1)));
-        // the keys of blocks 0 and 1, the values of block 0
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 2) * (BOTH ? 2 : 1)) : "memory");
+        auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+        u32x4 rk, rv;  // the next pieces
         {
-            u32x4 x = raw_keys(0);
-            put_keys(0, widen8(x[0], x[1]), widen8(x[2], x[3]));
-            x = raw_keys(1);
-            put_keys(1, widen8(x[0], x[1]), widen8(x[2], x[3]));
-            x = raw_values(1);
-            clean(0, x);
-            put_values(0, widen8(x[0], x[1]), widen8(x[2], x[3]));
+            const int id0 = uniform(id_of(0)), id1 = uniform(id_of(1)), id2 = uniform(id_of(2));
+            const u32x4 k0 = load_keys(id0), k1 = load_keys(id1);
+            u32x4 v0 = load_values(id0);
+            rk = load_keys(id2);
+            rv = load_values(id1);
+            put_keys(0, widen8(k0[0], k0[1]), widen8(k0[2], k0[3]));
+            put_keys(1, widen8(k1[0], k1[1]), widen8(k1[2], k1[3]));
+            clean(0, v0);
+            put_values(0, widen8(v0[0], v0[1]), widen8(v0[2], v0[3]));
         }
         lds_barrier();
-        int id_keys = id_of(kRaw), id_values = id_of(kRaw - 1);
+        int id_keys = id_of(3), id_values = id_of(2);
         f32x16 s;
         float top = 0.f;
         PageScale now = entry_of(0, h).scale;
@@ -973,8 +966,6 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         int window_id = 0;
         f32x2 window_scale = {0.f, 0.f};
         for (int b = 0; b < blocks; ++b) {
-            // the keys of block b + 2 and the values of block b + 1 have come, and nobody reads the stages that they go to any more
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRaw - 3) * (BOTH ? 2 : 1)) : "memory");
             const int behind = b % kWindow;
             if (behind <= 2 && b >= kWindow) {  // the pages of the next window but one, in three rounds
                 const int x = (b / kWindow + 1) * kWindow * 4 + (int)threadIdx.x;
@@ -984,38 +975,44 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                     else entry(x, window_id, window_scale);
                 }
             }
-            issue(b + kRaw, __builtin_amdgcn_readfirstlane(id_keys), __builtin_amdgcn_readfirstlane(id_values));
-            u32x4 rk = raw_keys(b + 2), rv = raw_values(b + 2);
-            id_keys = id_of(b + kRaw + 1);
-            id_values = id_of(b + kRaw);
+            // (nobody reads the stages of the keys of block b + 2 and of the values of block b + 1 any more)
+            const int next_keys = uniform(id_keys), next_values = uniform(id_values);
+            id_keys = id_of(b + 4);
+            id_values = id_of(b + 3);
             if (threadIdx.x < 2) lds.bad[(b + 3) % 4][threadIdx.x] = 0u;
             const PageScale then = entry_of(b, 2 + h).scale, after = entry_of(min(b + 1, blocks - 1), h).scale;
-            clean(b + 1, rv);
             u32x4 wide[4];
             if (!idle) {
                 half_block(b, 0, s, top, now, [&](int x) {
                     if (x == 1) wide[0] = widen8(rk[0], rk[1]);
-                    if (x == 3) wide[1] = widen8(rk[2], rk[3]);
+                    if (x == 3) {
+                        wide[1] = widen8(rk[2], rk[3]);
+                        rk = load_keys(next_keys);
+                    }
                 });
                 put_keys(b + 2, wide[0], wide[1]);
                 settle(b, 1, s, top, then);
+                clean(b + 1, rv);
                 half_block(b, 1, s, top, then, [&](int x) {
                     if (x == 1) wide[2] = widen8(rv[0], rv[1]);
-                    if (x == 3) wide[3] = widen8(rv[2], rv[3]);
+                    if (x == 3) {
+                        wide[3] = widen8(rv[2], rv[3]);
+                        rv = load_values(next_values);
+                    }
                 });
             } else {
-                wide[0] = widen8(rk[0], rk[1]);
-                wide[1] = widen8(rk[2], rk[3]);
+                put_keys(b + 2, widen8(rk[0], rk[1]), widen8(rk[2], rk[3]));
+                rk = load_keys(next_keys);
+                clean(b + 1, rv);
                 wide[2] = widen8(rv[0], rv[1]);
                 wide[3] = widen8(rv[2], rv[3]);
+                rv = load_values(next_values);
             }
-            if (idle) put_keys(b + 2, wide[0], wide[1]);
             put_values(b + 1, wide[2], wide[3]);
             lds_barrier();
             now = after;
             if (!idle && b + 1 < blocks) settle(b + 1, 0, s, top, now);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no LDS fill may outlive the workgroup
     }
     l += __shfl_xor(l, 32);
     if (tcol >= ncols) return;
@@ -1060,7 +1057,6 @@ constexpr int kThreads = TILES ? 512 : 256;
 
 template <int D, bool TILES>
 __global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Args a) {
-    // (one LDS object: with a second one the compiler waits for all loads into the ring before it reads from it)
     extern __shared__ __attribute__((aligned(1024))) unsigned char attn8_lds[];
     constexpr int WAVES = kThreads<TILES> / 64;
     const int kvh = blockIdx.x % a.n_kv, place = blockIdx.x / a.n_kv;
