@@ -760,23 +760,29 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 // order 1002, 8 waves of 32 and blocks of 64 keys 846, the compiler's own order 832.  No gain: raised priority of half of the waves, a reference that
 // moves when a sum of weights has grown (a fifth fewer vector instructions), instructions held in the order of the source (3 % slower).
 
-constexpr int kHalf = 32, kKeyStages = 2, kValueStages = 2, kWindow = 64;
+// Blocks that LDS holds: with four a barrier after every second round is enough.  us with two / four: 64 dims, 14 heads on 2, a chunk of 4096 behind
+// 4096 227 / 206, 8 heads on 8, four chunks of 1024 60 / 57; 128 dims, a chunk of 4096 behind 4096 (64 heads on 8) 800 / 805, of 8191 in a window 311
+// / 316.
+template <int D>
+constexpr int kStages = D == 64 ? 4 : 2;
+constexpr int kHalf = 32, kWindow = 64;
 struct PageEntry {
     int32_t id;
     PageScale scale;
 };
 template <int D>
 struct TileLds {
-    unsigned char keys[kKeyStages][2][kHalf * D * 2];
-    unsigned char values[kValueStages][2][kHalf * D * 2];
+    unsigned char keys[kStages<D>][2][kHalf * D * 2];
+    unsigned char values[kStages<D>][2][kHalf * D * 2];
     PageEntry pages[2][kWindow * 4];                // of 64 blocks and the next 64
-    uint32_t bad[4][2];                             // of a half: bit 16h + t: slot t of page h has values that are no numbers
+    uint32_t bad[2 * kStages<D>][2];                             // of a half: bit 16h + t: slot t of page h has values that are no numbers
 };
 constexpr float kSlack = 32.0f;  // a reference lags by up to this: weights stay below 2^32
 
 template <int D>
 __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, const Parts& parts, int kvh, TileLds<D>& lds) {
     constexpr int PH = D * kPage;         // bytes of a page's head
+    constexpr int AHEAD = kStages<D> / 2; // blocks that values in LDS are ahead of the round; keys are one more
     constexpr bool BOTH = D == 128;       // a thread has a piece of keys and one of values; or the lower waves keys, the upper ones values
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -836,20 +842,20 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 x[w] &= ~((n >> 7) * 0xFFu);
                 some |= ((n >> 7 & 1) | (n >> 14 & 2) | (n >> 21 & 4) | (n >> 28 & 8)) << (4 * w);
             }
-            if (some) atomicOr(&lds.bad[b % 4][page / 2], some << (16 * (page % 2)));
+            if (some) atomicOr(&lds.bad[b % (2 * kStages<D>)][page / 2], some << (16 * (page % 2)));
         };
         // where the two halves of a piece go as bf16
         const int chunk = piece_at % (D / 4) / 4, key_row = (8 * (piece_at / (D / 4)) + 4 * (page % 2) + piece_at % 4) ^ (4 * (chunk & 3));
         const int keys_at = (page / 2) * (kHalf * D * 2) + (2 * chunk * 32 + key_row) * 16, values_at = (2 * page * D + piece_at) * 16;
         auto put_keys = [&](int b, u32x4 lo, u32x4 hi) {
             if (!has_keys) return;
-            unsigned char* to = &lds.keys[b % kKeyStages][0][0] + keys_at;
+            unsigned char* to = &lds.keys[b % kStages<D>][0][0] + keys_at;
             *reinterpret_cast<u32x4*>(to) = lo;
             *reinterpret_cast<u32x4*>(to + 32 * 16) = hi;
         };
         auto put_values = [&](int b, u32x4 lo, u32x4 hi) {
             if (!has_values) return;
-            unsigned char* to = &lds.values[b % kValueStages][0][0] + values_at;
+            unsigned char* to = &lds.values[b % kStages<D>][0][0] + values_at;
             *reinterpret_cast<u32x4*>(to) = lo;
             *reinterpret_cast<u32x4*>(to + D * 16) = hi;
         };
@@ -863,7 +869,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         auto settle = [&](int b, int half, f32x16& s, float top, const PageScale& sc) {
             const int key0 = key_of(b) + half * kHalf;
             if (partly(key0, kHalf, wave_min, wave_max)) {
-                const uint32_t bad = lds.bad[b % 4][half] >> (16 * h);
+                const uint32_t bad = lds.bad[b % (2 * kStages<D>)][half] >> (16 * h);
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int key = key0 + h * kPage + v;
@@ -884,9 +890,9 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             }
         };
         bf16x8 kf[D / 16], vf[D / 32][2];
-        auto read_key = [&](int b, int half, int k) { kf[k] = *reinterpret_cast<const bf16x8*>(lds.keys[b % kKeyStages][half] + ((2 * k + h) * 32 + (r ^ (4 * (k & 3)))) * 16); };
+        auto read_key = [&](int b, int half, int k) { kf[k] = *reinterpret_cast<const bf16x8*>(lds.keys[b % kStages<D>][half] + ((2 * k + h) * 32 + (r ^ (4 * (k & 3)))) * 16); };
         auto read_value = [&](int b, int half, int x) {
-            vf[x % (D / 32)][x / (D / 32)] = *reinterpret_cast<const bf16x8*>(lds.values[b % kValueStages][half] + ((2 * h + x / (D / 32)) * D + x % (D / 32) * 32 + r) * 16);
+            vf[x % (D / 32)][x / (D / 32)] = *reinterpret_cast<const bf16x8*>(lds.values[b % kStages<D>][half] + ((2 * h + x / (D / 32)) * D + x % (D / 32) * 32 + r) * 16);
         };
         // One half, of block b: its weights and outputs from the scores s, and the scores of the next one, whose keys are in kf, into s; the keys of the one behind
         // that are read into kf.  extra(x): what else goes behind output x.
@@ -926,7 +932,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         };
         static_assert(D / 16 == D / 32 * 2, "as many scores as outputs");
 
-        if (threadIdx.x < 8) (&lds.bad[0][0])[threadIdx.x] = 0u;
+        if (threadIdx.x < 4 * kStages<D>) (&lds.bad[0][0])[threadIdx.x] = 0u;
         {
             const int id = page_of(threadIdx.x);
             entry(threadIdx.x, id, a.scales[(int64_t)id * a.n_kv + kvh]);
@@ -935,18 +941,27 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
         u32x4 rk, rv;  // the next pieces
         {
-            const int id0 = uniform(id_of(0)), id1 = uniform(id_of(1)), id2 = uniform(id_of(2));
+            constexpr bool MORE = AHEAD == 2;
+            const int id0 = uniform(id_of(0)), id1 = uniform(id_of(1)), id2 = uniform(id_of(2)), id3 = MORE ? uniform(id_of(3)) : 0;
             const u32x4 k0 = load_keys(id0), k1 = load_keys(id1);
+            u32x4 k2{}, v1{};
+            if (MORE) k2 = load_keys(id2);
             u32x4 v0 = load_values(id0);
-            rk = load_keys(id2);
-            rv = load_values(id1);
+            if (MORE) v1 = load_values(id1);
+            rk = load_keys(MORE ? id3 : id2);
+            rv = load_values(MORE ? id2 : id1);
             put_keys(0, widen8(k0[0], k0[1]), widen8(k0[2], k0[3]));
             put_keys(1, widen8(k1[0], k1[1]), widen8(k1[2], k1[3]));
+            if (MORE) put_keys(2, widen8(k2[0], k2[1]), widen8(k2[2], k2[3]));
             clean(0, v0);
             put_values(0, widen8(v0[0], v0[1]), widen8(v0[2], v0[3]));
+            if (MORE) {
+                clean(1, v1);
+                put_values(1, widen8(v1[0], v1[1]), widen8(v1[2], v1[3]));
+            }
         }
         lds_barrier();
-        int id_keys = id_of(3), id_values = id_of(2);
+        int id_keys = id_of(AHEAD + 2), id_values = id_of(AHEAD + 1);
         f32x16 s;
         float top = 0.f;
         PageScale now = entry_of(0, h).scale;
@@ -962,7 +977,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) read_key(0, 1, k);
         }
-        lds_barrier();  // the keys of block 0 have been read, and those of block 2 may take their place
+        lds_barrier();  // the keys of block 0 have been read, and others may take their place
         int window_id = 0;
         f32x2 window_scale = {0.f, 0.f};
         for (int b = 0; b < blocks; ++b) {
@@ -975,11 +990,12 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                     else entry(x, window_id, window_scale);
                 }
             }
-            // (nobody reads the stages of the keys of block b + 2 and of the values of block b + 1 any more)
+            // A round reads the keys of block b + 1, the values of block b and the flags of b and b + 1, and writes the keys of block b + AHEAD + 1,
+            // the values and the flags of block b + AHEAD: what AHEAD rounds on is read, and AHEAD rounds ago was, as that of other blocks.
             const int next_keys = uniform(id_keys), next_values = uniform(id_values);
-            id_keys = id_of(b + 4);
-            id_values = id_of(b + 3);
-            if (threadIdx.x < 2) lds.bad[(b + 3) % 4][threadIdx.x] = 0u;
+            id_keys = id_of(b + AHEAD + 3);
+            id_values = id_of(b + AHEAD + 2);
+            if (threadIdx.x < 2) lds.bad[(b + 2 * AHEAD + (AHEAD == 1)) % (2 * kStages<D>)][threadIdx.x] = 0u;
             const PageScale then = entry_of(b, 2 + h).scale, after = entry_of(min(b + 1, blocks - 1), h).scale;
             u32x4 wide[4];
             if (!idle) {
@@ -990,9 +1006,9 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                         rk = load_keys(next_keys);
                     }
                 });
-                put_keys(b + 2, wide[0], wide[1]);
+                put_keys(b + AHEAD + 1, wide[0], wide[1]);
                 settle(b, 1, s, top, then);
-                clean(b + 1, rv);
+                clean(b + AHEAD, rv);
                 half_block(b, 1, s, top, then, [&](int x) {
                     if (x == 1) wide[2] = widen8(rv[0], rv[1]);
                     if (x == 3) {
@@ -1001,15 +1017,15 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                     }
                 });
             } else {
-                put_keys(b + 2, widen8(rk[0], rk[1]), widen8(rk[2], rk[3]));
+                put_keys(b + AHEAD + 1, widen8(rk[0], rk[1]), widen8(rk[2], rk[3]));
                 rk = load_keys(next_keys);
-                clean(b + 1, rv);
+                clean(b + AHEAD, rv);
                 wide[2] = widen8(rv[0], rv[1]);
                 wide[3] = widen8(rv[2], rv[3]);
                 rv = load_values(next_values);
             }
-            put_values(b + 1, wide[2], wide[3]);
-            lds_barrier();
+            put_values(b + AHEAD, wide[2], wide[3]);
+            if (AHEAD == 1 || b % 2 == 1) lds_barrier();
             now = after;
             if (!idle && b + 1 < blocks) settle(b + 1, 0, s, top, now);
         }
