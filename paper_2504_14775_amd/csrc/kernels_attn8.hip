@@ -17,7 +17,7 @@
 //
 // Measured (8 KV heads of 128): 32 decode rows behind 300 .. 20000 keys, 308 MB, 58 us with the joining, 53 + 5, 5.8 TB/s inside the kernel (a copy
 // reaches 5.2); 64 behind a window of 1024, 33 us; 251 decode rows and 1802 chunk rows together, 938 MB and 63 GFLOP, 201 us; a chunk of 4096 behind
-// 4096 keys, 64 heads, 825 GFLOP that count, 823 us, 1.0 PFLOP/s (a large product reaches 1.42).
+// 4096 keys, 64 heads, 825 GFLOP that count, 780 us, 1.06 PFLOP/s (a large product reaches 1.42).
 #include "cache8.h"
 
 #include <algorithm>
@@ -55,8 +55,8 @@ __host__ __device__ constexpr int per_head(int total, int n_kv) { return total /
 template <bool TILES>
 __host__ __device__ constexpr int max_workers(int n_kv, int d) { return per_head(TILES || d == 128 ? kGroups : 2 * kGroups, n_kv); }
 // Units that the keys of tiles are cut into.  Every part of a tile writes and reads partial results of (d + 2) floats a column, as much as eight
-// blocks of keys.  us at 128 / 256 / 512: a chunk of 901 behind 2011 keys (14B heads) 103 / 105 / 102, of 4096 behind none (8B) 165 / 167 / 230, 251
-// decode rows beside 1802 chunk rows (14B) 201 / 225 / 263, 100 rows behind 6000 keys 40 / 38 / 42.
+// blocks of keys.  us at 128 / 256 / 512: a chunk of 901 behind 2011 keys (14B heads) 95 / 99 / 99, of 4096 behind none (8B) 155 / 156 / 220, 251
+// decode rows beside 1802 chunk rows (14B) 201 / 224 / 262, 100 rows behind 6000 keys 41 / 39 / 43.
 __host__ __device__ constexpr int target_units(int n_kv) { return per_head(kGroups / 2, n_kv); }
 // Tiles with partial results and columns of these.  A tile is cut where its sequence has more blocks than a share, into at most ceil(blocks /
 // share) parts; the shares of all are at least half their blocks by the target (seq_plan: twice the weight is at least the blocks).
@@ -131,8 +131,8 @@ __device__ __forceinline__ T lane_value(T x, int lane) { return __builtin_bit_ca
 // 1e-4 of itself larger, which is more than the roundings of the additions, 2^-24 of the sum each, take away, kMaxAttn8Seqs / 4096 of a lane and 15
 // over lanes and runs.)
 static_assert(kMaxAttn8Seqs / (64 * 64) + 15 < 16777216 / 10000, "the sum of all weights");
-// A block of a tile keeps a compute unit busy for 2.2 us, one of a stream, where half of the units draw all that the memory gives, for 0.35.  us at 4
-// / 6 / 8: 251 decode rows beside 1802 chunk rows (14B heads) 212 / 201 / 211, 256 beside 1792 (8B) 226 / 202 / 214, 32 beside 4 x 128 91 / 82 / 79.
+// A block of a tile keeps a compute unit busy for 2.0 us, one of a stream, where half of the units draw all that the memory gives, for 0.35.  us at 4
+// / 6 / 8: 251 decode rows beside 1802 chunk rows (14B heads) 208 / 201 / 211, 256 beside 1792 (8B) 148 / 131 / 142, 32 beside 4 x 128 55 / 56 / 47.
 constexpr float kTileCost = 6.f;
 // Blocks of a wave of the stream, where there are few: us at 2 / 4 / 8, one sequence of 3000 keys (8B heads) 12.8 / 15.0 / 17.7, of 20000 18.9 / 17.9
 // / 21.7.
