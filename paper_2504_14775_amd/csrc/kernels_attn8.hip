@@ -17,7 +17,7 @@
 //
 // Measured (8 KV heads of 128): 32 decode rows behind 300 .. 20000 keys, 308 MB, 58 us with the joining, 53 + 5, 5.8 TB/s inside the kernel (a copy
 // reaches 5.2); 64 behind a window of 1024, 33 us; 251 decode rows and 1802 chunk rows together, 938 MB and 63 GFLOP, 201 us; a chunk of 4096 behind
-// 4096 keys, 64 heads, 825 GFLOP that count, 780 us, 1.06 PFLOP/s (a large product reaches 1.42).
+// 4096 keys, 64 heads, 825 GFLOP that count, 786 us, 1.05 PFLOP/s (a large product reaches 1.42).
 #include "cache8.h"
 
 #include <algorithm>
@@ -752,13 +752,13 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 // The exponentials of a half run beside the scores of the next one and in front of its own outputs; what a phase reads from LDS is asked for in the
 // phase before.
 //
-// What bounds it, a chunk of 4096 behind 4096 keys: 780 us, 1.06 PFLOP/s.  Per block of 64 keys (2.0 us) the matrix cores are busy for 0.9 us, the
-// vector units for about 1.2 (32 exponentials and some 190 others a wave), LDS, which each wave reads all keys and values from, for 1.1; a wave's
+// What bounds it, a chunk of 4096 behind 4096 keys: 786 us, 1.05 PFLOP/s.  Per block of 64 keys (2.0 us) the matrix cores are busy for 0.9 us, the
+// vector units for about 1.1 (32 exponentials and some 170 others a wave), LDS, which each wave reads all keys and values from, for 1.1; a wave's
 // chain goes through all three, and there are two waves on a SIMD to hide each other's waits, all that the registers allow.  What each costs, with
-// data that does not change so that the clock stays: without staging and barriers 18 % less, without exponentials 8 %, without reads of LDS nothing;
-// random data costs 5 %, by the clock.  Steps to here: 4 waves of 64 columns, 32 keys at a time, 1143 us, matrix and vector instructions in a given
-// order 1002, 8 waves of 32 and blocks of 64 keys 846, the compiler's own order 832.  No gain: raised priority of half of the waves, a reference that
-// moves when a sum of weights has grown (a fifth fewer vector instructions), instructions held in the order of the source (3 % slower).
+// data that does not change, so that the clock stays up (which is worth 5 to 8 % itself): staging and barriers 8 %, exponentials 8 %, reads of LDS
+// nothing.  Steps to here: 4 waves of 64 columns, 32 keys at a time, 1143 us, matrix and vector instructions in a given order 1002, 8 waves of 32 and
+// blocks of 64 keys 846, the compiler's own order 823.  No gain: raised priority of half of the waves, a reference that moves when a sum of weights
+// has grown (a fifth fewer vector instructions), instructions held in the order of the source (3 % slower).
 
 // Blocks that LDS holds: with four a barrier after every second round is enough.  us with two / four: 64 dims, 14 heads on 2, a chunk of 4096 behind
 // 4096 227 / 206, 8 heads on 8, four chunks of 1024 60 / 57; 128 dims, a chunk of 4096 behind 4096 (64 heads on 8) 800 / 805, of 8191 in a window 311
