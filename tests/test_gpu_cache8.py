@@ -324,6 +324,18 @@ def test_a_page_filled_token_by_token_is_as_one_filled_at_once_but_for_small_cod
 
 # ---- attention ---------------------------------------------------------------------------------------------------------------
 
+def bound(ref, weight, mass, d):
+    """How far an output may lie from the reference, with u = 2^-8, half a step of bf16, and weight = sum p |v|.  The weights are rounded to
+    q = p (1 + e), |e| <= u, and divided by their own sum, rounded or not.  By the rounded one:
+      |sum q v / sum q - ref| = |sum p e (v - ref)| / sum q <= u (weight + |ref|) / (1 - u),        as sum p (v - ref) = 0 and sum p = 1
+    (by the other one u weight, which is less), and the output is rounded to bf16, by u of itself:
+      u |ref| + (1 + u) u (weight + |ref|) / (1 - u) <= u |ref| + (u + 2^-15 + 2^-22) (weight + |ref|).
+    Beside that scores and exponents in float: a score of magnitude `mass` is off by (d + 10) 2^-24 of that, its weight by as much, both in
+    the weights and in their sum, and 2^-17 for what is left (exponential, scales' logarithms and reciprocals, sums)."""
+    u = 2.0 ** -8
+    return u * np.abs(ref) + (u + 2.0 ** -15 + 2.0 ** -22) * (weight + np.abs(ref)) + (2 * mass[..., None] * (d + 10) * 2.0 ** -24 + 2.0 ** -17) * weight
+
+
 class Batch:
     """Inputs of one call of attention: sequences of given new and cached lengths over a pool in which nothing but their positions holds numbers."""
 
@@ -387,7 +399,7 @@ class Batch:
         rows[list(skip_rows)] = False
         assert np.all(got[self.starts[-1]:] == 7.0)                          # rows of no sequence stay as they were
         assert np.isfinite(got[rows]).all(), label
-        tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2 * mass[..., None] * (self.d + 10) * 2.0 ** -24 + 2.0 ** -17) * weight
+        tol = bound(ref, weight, mass, self.d)
         off = np.abs(got - ref)[rows]
         print(f"[parity] attention8 {label}: max abs {off.max():.3g}, of the bound {(off / (tol[rows] + 1e-30)).max():.2f}", flush=True)
         assert (off - tol[rows]).max() <= 1e-30, label
@@ -581,7 +593,7 @@ def test_streams_about_as_long_as_are_cut(new, cached):
 
 
 @pytest.mark.parametrize("heads,most", [((16, 1, 128), 1), ((4, 2, 64), 8), ((32, 8, 128), 4), ((8, 8, 64), 1)], ids=str)
-@pytest.mark.parametrize("seqs", [40, 64, 65, 200])
+@pytest.mark.parametrize("seqs", [40, 64, 65, 200, 256, 257])
 def test_streams_of_very_different_lengths(seqs, heads, most):
     print(f"attention8 {seqs} streams, {heads}", flush=True)
     rng = np.random.default_rng(seqs)
@@ -598,7 +610,7 @@ def test_streams_of_very_different_lengths(seqs, heads, most):
 
 
 @pytest.mark.parametrize("heads", [(8, 2, 64), (12, 4, 128), (16, 1, 128)], ids=str)
-@pytest.mark.parametrize("seqs", [30, 64, 65, 150])
+@pytest.mark.parametrize("seqs", [30, 64, 65, 150, 256, 257, 400])
 def test_hybrids_of_every_kind_of_sequence(seqs, heads):
     print(f"attention8 hybrid of {seqs}, {heads}", flush=True)
     rng = np.random.default_rng(seqs)
@@ -750,7 +762,7 @@ def test_a_step_captured_and_replayed_grows_its_sequences():
         ref, weight, mass = O.attention(q, k, v, eager.tables.cpu().numpy(), cached, eager.maps[0].cpu().numpy(), d ** -0.5, 40, 3)
         got = f64(eager.out).reshape(ref.shape)[:total]
         ref, weight, mass = ref[:total], weight[:total], mass[:total]
-        assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2 * mass[..., None] * (d + 10) * 2.0 ** -24 + 2.0 ** -17) * weight).all(), step
+        assert (np.abs(got - ref) <= bound(ref, weight, mass, d)).all(), step
         cached += new
 
 
