@@ -185,9 +185,14 @@ __device__ __forceinline__ bool unit_of(const SeqPlan& q, int parts, int units, 
     return false;
 }
 
-// Up to 64 sequences every wave works the plan out for itself, all of them with the same arithmetic, without LDS and barriers.  More are
-// planned by a launch of their own, which cuts them into up to 64 runs of whole waves and leaves what stands in front of each; a wave then looks
-// at the runs and at some of their sequences.
+// Up to 64 sequences, 256 where there are streams only, every wave works the plan out for itself, all of them with the same arithmetic, without LDS
+// and barriers.  More are planned by a launch of their own, which cuts them into up to 64 runs of whole waves and leaves what stands in front of
+// each.  Above 64 a wave then looks at the runs and at some of their sequences.  (us with that launch and without, decode rows behind 300 .. 700 keys
+// (8B heads): 128 38.2 / 35.1, 256 59.1 / 57.4; 65 behind 64 .. 300 15.9 / 12.5.  With tiles there are many workgroups without work, and each would
+// plan first: 253 sequences, 2 of them chunks, 201 / 227.)
+constexpr int kOwnRuns = 4;
+template <bool TILES>
+__host__ __device__ constexpr bool plans_alone(int num_seqs) { return num_seqs <= (TILES ? 64 : 64 * kOwnRuns); }
 constexpr int kPlanRuns = 64;
 struct Plan {
     int32_t share, units, workers;      // units, workers: none where the rows break their order
@@ -209,6 +214,7 @@ struct Job {
     int cut_tiles;        // behind the last unit: tiles whose keys are cut, or -1 where the plan's launch has written it
     bool broken;
     SeqPlan seqs;         // up to 64 sequences: that of this lane
+    int64_t before;       // more, and planned here: blocks of the streams in front of run `lane`
 };
 template <bool TILES>
 __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, int place, Job& j) {
@@ -216,6 +222,27 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
     int places = 0;
     j.is_unit = false;
     j.cut_tiles = 0;
+    if (!TILES && a.num_seqs > 64 && plans_alone<TILES>(a.num_seqs)) {
+        SeqPlan q[kOwnRuns];
+        bool unordered = false, broken = false;
+        j.stream = 0;
+        j.before = INT64_MAX;
+#pragma unroll
+        for (int r = 0; r < kOwnRuns; ++r) q[r] = seq_plan(a, 64 * r + lane);
+#pragma unroll
+        for (int r = 0; r < kOwnRuns; ++r) {
+            unordered |= q[r].unordered;
+            broken |= q[r].broken;
+            uint32_t blocks = (uint32_t)q[r].stream;
+            scan_wave(blocks);
+            if (lane == r && 64 * r < a.num_seqs) j.before = j.stream;
+            j.stream += lane_value(blocks, 63);
+        }
+        const bool none = __any(unordered);
+        j.broken = !none && __any(broken);
+        j.workers = none ? 0 : workers_of<TILES>((float)j.stream, 0.f, a.n_kv, a.d);
+        return;
+    }
     if (a.num_seqs > 64) {
         j.workers = plan->workers;
         j.stream = plan->stream;
@@ -463,7 +490,7 @@ __device__ __forceinline__ int64_t of_wave(int64_t x) {
 // Where the run of wave w begins.
 __device__ __forceinline__ int64_t run_begin(int64_t blocks, int waves, int w) { return of_wave((int64_t)((uint64_t)blocks * (uint32_t)w / (uint32_t)waves)); }
 
-template <int D>
+template <int D, bool TILES>
 __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, const Parts& parts, int kvh, int w, int waves) {
     const int lane = threadIdx.x & 63;
     const int r = lane & 15, G = lane >> 4, g = a.n_q / a.n_kv;
@@ -482,7 +509,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
         scan_wave(upto);
     };
     if (a.num_seqs > 64) {
-        const int64_t first = parts.plan->stream_before[lane];
+        const int64_t first = plans_alone<TILES>(a.num_seqs) ? job.before : parts.plan->stream_before[lane];
         const int run = __popcll(__ballot(first <= lo)) - 1;
         s0 = run * plan_run(a.num_seqs);
         before = of_wave(__shfl(first, run));
@@ -1092,7 +1119,7 @@ __global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Arg
         return;
     }
     if (place < job.workers) {
-        stream_wave<D>(a, job, parts, kvh, place * WAVES + wave, job.workers * WAVES);
+        stream_wave<D, TILES>(a, job, parts, kvh, place * WAVES + wave, job.workers * WAVES);
         return;
     }
     if constexpr (TILES) {
@@ -1220,7 +1247,7 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     if (places * a.n_kv * kThreads<TILES> > UINT32_MAX) return hipErrorInvalidValue;
     Parts parts;
     parts_in<TILES>(parts, a.workspace, a.n_kv, D);
-    if (a.num_seqs > 64) attention8_plan_kernel<TILES><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
+    if (!plans_alone<TILES>(a.num_seqs)) attention8_plan_kernel<TILES><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
     const int lds = TILES ? sizeof(TileLds<D>) : 0;
     if (TILES) {
         static std::atomic<uint64_t> allowed{0};  // devices on which this kernel may use the LDS that it asks for
