@@ -46,7 +46,9 @@ struct Unit {
     int32_t cut_tile;            // and of its tile among those with such units
 };
 
-constexpr int kMinShare = 6;     // fewest blocks worth a unit
+// Fewest blocks worth a unit.  us at 2 / 3 / 6 / 10 (8B heads): a chunk of 64 behind 1000 keys 20.6 / 20.8 / 23.8 / 28.7, of 512 behind none 26.7 /
+// 26.7 / 28.9 / 29.3, of 32 behind 4000 21.1 / 21.1 / 21.4 / 25.3, 4 of 128 behind up to 700 28.2 / 28.3 / 30.7 / 35.5.
+constexpr int kMinShare = 2;
 constexpr int kWhole = 6;        // most blocks of a stream that is never cut
 constexpr int kGroups = 256;     // workgroups that run at one time: one on each compute unit
 // All of these are for each KV head.
@@ -1261,9 +1263,9 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
         }
     }
     attention8_kernel<D, TILES><<<(unsigned)(places * a.n_kv), kThreads<TILES>, lds, stream>>>(a);
-    // no sequence can be cut that has no more blocks than the fewest of a part
+    // no sequence can be cut that has no more blocks than these
     const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : kStreamCols / g;
-    if (most_blocks(own, rows, a.window, a.sinks) > (kWhole < kMinShare ? kWhole : kMinShare)) {
+    if (most_blocks(own, rows, a.window, a.sinks) > (TILES && kMinShare < kWhole ? kMinShare : kWhole)) {
         const int records = a.num_seqs <= 64 ? a.num_seqs : (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, kStreamCols / g, a.window, a.sinks) + 8);
         const int stream_groups = records * a.n_kv;
         const int64_t tile_groups = TILES ? std::min<int64_t>(2048, std::min<int64_t>(max_cut_tiles(a.n_kv), tiles) * a.n_kv * (kTileCols * D / 1024)) : 0;
