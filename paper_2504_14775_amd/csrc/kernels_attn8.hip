@@ -35,7 +35,7 @@ constexpr int kBlock = 64;  // keys, four pages
 // The lengths stand on the device.  Sequences of up to 16 columns are streams: their blocks of 64 keys, one sequence behind the other, are dealt in
 // equal runs to the waves of some workgroups.  The others have tiles of 256 columns, each a unit of work of its own or, where there are few of
 // them, several, which share its keys.  The stream's workgroups are the first of the launch.
-constexpr int kStreamCols = 16, kTileCols = 256;
+constexpr int kStreamCols = 16, kWideCols = 32, kTileCols = 256;
 
 // A unit of work of a tile: a part of its keys.
 struct Unit {
@@ -54,8 +54,8 @@ constexpr int kGroups = 256;     // workgroups that run at one time: one on each
 // All of these are for each KV head.
 __host__ __device__ constexpr int per_head(int total, int n_kv) { return total / n_kv > 0 ? total / n_kv : 1; }
 // Workgroups of the stream at most.
-template <bool TILES>
-__host__ __device__ constexpr int max_workers(int n_kv, int d) { return per_head(TILES || d == 128 ? kGroups : 2 * kGroups, n_kv); }
+template <bool TILES, int COLS>
+__host__ __device__ constexpr int max_workers(int n_kv, int d) { return per_head(TILES || d == 128 || COLS > kStreamCols ? kGroups : 2 * kGroups, n_kv); }
 // Units that the keys of tiles are cut into.  Every part of a tile writes and reads partial results of (d + 2) floats a column, as much as eight
 // blocks of keys.  us at 128 / 256 / 512: a chunk of 901 behind 2011 keys (14B heads) 95 / 99 / 99, of 4096 behind none (8B) 155 / 156 / 220, 251
 // decode rows beside 1802 chunk rows (14B) 201 / 224 / 262, 100 rows behind 6000 keys 41 / 39 / 43.
@@ -90,6 +90,7 @@ struct SeqPlan {
     float weight;                     // tiles times about their blocks, at least half of tiles * blocks
     bool broken, unordered;           // a rule: zeros
 };
+template <int COLS>
 __device__ __forceinline__ SeqPlan seq_plan(const Attn8Args& a, int s) {
     SeqPlan p{0, 0, 0, 0, 0, 0, 0.f, false, false};
     if (s >= a.num_seqs) return p;
@@ -102,7 +103,7 @@ __device__ __forceinline__ SeqPlan seq_plan(const Attn8Args& a, int s) {
     p.broken = p.n > a.max_new || p.c < 0 || (int64_t)p.c + p.n > min((int64_t)a.table_stride * kPage, (int64_t)kMaxPositions);
     if (p.broken) return p;
     const int64_t cols = (int64_t)p.n * g;
-    if (cols <= kStreamCols) {
+    if (cols <= COLS) {
         p.stream = seen_blocks(a, p.c, 0, p.n - 1).blocks;
     } else {
         p.tiles = (int)((cols + kTileCols - 1) / kTileCols);
@@ -139,10 +140,10 @@ constexpr float kTileCost = 6.f;
 // Blocks of a wave of the stream, where there are few: us at 2 / 4 / 8, one sequence of 3000 keys (8B heads) 12.8 / 15.0 / 17.7, of 20000 18.9 / 17.9
 // / 21.7.
 constexpr int kFewBlocks = 2;
-template <bool TILES>
+template <bool TILES, int COLS>
 __device__ __forceinline__ int workers_of(float stream, float tiles, int n_kv, int d) {
     if (!(stream > 0.f)) return 0;
-    const int most = max_workers<TILES>(n_kv, d);
+    const int most = max_workers<TILES, COLS>(n_kv, d);
     const float fair = TILES ? rintf(stream / (stream + kTileCost * tiles) * (float)most) : (float)most;
     return (int)fmaxf(fminf(fair, ceilf(stream / (float)(kFewBlocks * (TILES ? 8 : 4)))), 1.f);
 }
@@ -218,7 +219,7 @@ struct Job {
     SeqPlan seqs;         // up to 64 sequences: that of this lane
     int64_t before;       // more, and planned here: blocks of the streams in front of run `lane`
 };
-template <bool TILES>
+template <bool TILES, int COLS>
 __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, int place, Job& j) {
     const int lane = threadIdx.x & 63;
     int places = 0;
@@ -230,7 +231,7 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
         j.stream = 0;
         j.before = INT64_MAX;
 #pragma unroll
-        for (int r = 0; r < kOwnRuns; ++r) q[r] = seq_plan(a, 64 * r + lane);
+        for (int r = 0; r < kOwnRuns; ++r) q[r] = seq_plan<COLS>(a, 64 * r + lane);
 #pragma unroll
         for (int r = 0; r < kOwnRuns; ++r) {
             unordered |= q[r].unordered;
@@ -242,7 +243,7 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
         }
         const bool none = __any(unordered);
         j.broken = !none && __any(broken);
-        j.workers = none ? 0 : workers_of<TILES>((float)j.stream, 0.f, a.n_kv, a.d);
+        j.workers = none ? 0 : workers_of<TILES, COLS>((float)j.stream, 0.f, a.n_kv, a.d);
         return;
     }
     if (a.num_seqs > 64) {
@@ -259,7 +260,7 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
         int at = lane_value(first, run), cut = plan->cut_tiles[run];
         places = plan->places[run];
         for (int s0 = begin; s0 < end; s0 += 64) {
-            const SeqPlan q = seq_plan(a, s0 + lane);
+            const SeqPlan q = seq_plan<COLS>(a, s0 + lane);
             int parts, its;
             const int units = split_seq(q, share, parts, its), mine = its == quarter ? units : 0;
             int x = mine;
@@ -272,7 +273,7 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
         }
         return;
     }
-    j.seqs = seq_plan(a, lane);
+    j.seqs = seq_plan<COLS>(a, lane);
     j.broken = __any(j.seqs.broken);
     uint32_t blocks = (uint32_t)j.seqs.stream;  // (64 times 2^25 at most)
     scan_wave(blocks);
@@ -283,7 +284,7 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
         scan_wave(tiles);
         tiles = lane_value(tiles, 63);
     }
-    j.workers = workers_of<TILES>((float)j.stream, tiles, a.n_kv, a.d);
+    j.workers = workers_of<TILES, COLS>((float)j.stream, tiles, a.n_kv, a.d);
     if (__any(j.seqs.unordered)) {  // rows in no order may belong to two sequences
         j.workers = 0;
         j.broken = false;
@@ -304,7 +305,7 @@ __device__ __forceinline__ void find_job(const Attn8Args& a, const Plan* plan, i
 }
 
 // One workgroup; wave w has the runs w, w + 16, ...
-template <bool TILES>
+template <bool TILES, int COLS>
 __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan* plan, int32_t* count) {
     __shared__ float totals[2][kPlanRuns];
     __shared__ int64_t stream[kPlanRuns];
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan
         int64_t blocks = 0;
         bool unordered = false, broken = false;
         for (int s0 = run * len; s0 < min((run + 1) * len, a.num_seqs); s0 += 64) {
-            const SeqPlan q = seq_plan(a, s0 + lane);
+            const SeqPlan q = seq_plan<COLS>(a, s0 + lane);
             total += q.weight;
             blocks += q.stream;
             unordered |= q.unordered;
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan
         for (int run = wave; run < kPlanRuns && run * len < a.num_seqs; run += 16) {
             int sum[6] = {0, 0, 0, 0, 0, 0};
             for (int s0 = run * len; s0 < min((run + 1) * len, a.num_seqs); s0 += 64) {
-                const SeqPlan q = seq_plan(a, s0 + lane);
+                const SeqPlan q = seq_plan<COLS>(a, s0 + lane);
                 int parts, quarter;
                 const int units = split_seq(q, share, parts, quarter);
 #pragma unroll
@@ -393,7 +394,7 @@ __global__ __launch_bounds__(1024) void attention8_plan_kernel(Attn8Args a, Plan
     if (lane == 0) {
         plan->share = share;
         plan->units = any_unordered ? 0 : start;
-        plan->workers = any_unordered ? 0 : workers_of<TILES>((float)all_blocks, total, a.n_kv, a.d);
+        plan->workers = any_unordered ? 0 : workers_of<TILES, COLS>((float)all_blocks, total, a.n_kv, a.d);
         plan->broken = any_unordered ? 0 : any_broken;
         plan->stream = all_blocks;
     }
@@ -418,13 +419,13 @@ struct Parts {
     Plan* plan;
     StreamRecord* stream;
     Record* rec;
-    f32x2 *stream_ml, *ml;  // [n_kv][2 * max waves][16], [n_kv][places]
+    f32x2 *stream_ml, *ml;  // [n_kv][2 * max waves][columns of a stream], [n_kv][places]
     float *stream_o, *o;    // and [d]
     int64_t max_waves, places;
 };
-template <bool TILES>
+template <bool TILES, int COLS>
 __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d) {
-    t.max_waves = max_workers<TILES>(n_kv, d) * (TILES ? 8 : 4);
+    t.max_waves = max_workers<TILES, COLS>(n_kv, d) * (TILES ? 8 : 4);
     t.places = TILES ? max_places(n_kv) : 0;
     char* p = (char*)base;
     size_t off = 0;
@@ -438,7 +439,7 @@ __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d
     t.plan = (Plan*)take(sizeof(Plan));
     t.stream = (StreamRecord*)take((t.max_waves > 64 ? t.max_waves : 64) * sizeof(StreamRecord));
     t.rec = (Record*)take(TILES ? max_cut_tiles(n_kv) * sizeof(Record) : 0);
-    const size_t stream_cols = (size_t)n_kv * 2 * t.max_waves * kStreamCols, cols = (size_t)n_kv * t.places;
+    const size_t stream_cols = (size_t)n_kv * 2 * t.max_waves * COLS, cols = (size_t)n_kv * t.places;
     t.stream_ml = (f32x2*)take(stream_cols * 8);
     t.stream_o = (float*)take(stream_cols * d * 4);
     t.ml = (f32x2*)take(cols * 8);
@@ -492,8 +493,9 @@ __device__ __forceinline__ int64_t of_wave(int64_t x) {
 // Where the run of wave w begins.
 __device__ __forceinline__ int64_t run_begin(int64_t blocks, int waves, int w) { return of_wave((int64_t)((uint64_t)blocks * (uint32_t)w / (uint32_t)waves)); }
 
-template <int D, bool TILES>
+template <int D, bool TILES, int COLS>
 __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, const Parts& parts, int kvh, int w, int waves) {
+    constexpr int SETS = COLS / 16;  // of 16 columns, which share the keys and values
     const int lane = threadIdx.x & 63;
     const int r = lane & 15, G = lane >> 4, g = a.n_q / a.n_kv;
     // The run.  A stream of few blocks belongs to the wave in whose run its last one lies.  (No run behind one that is not empty is empty: there are
@@ -515,7 +517,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
         const int run = __popcll(__ballot(first <= lo)) - 1;
         s0 = run * plan_run(a.num_seqs);
         before = of_wave(__shfl(first, run));
-        q = seq_plan(a, s0 + lane);
+        q = seq_plan<COLS>(a, s0 + lane);
     } else {
         q = job.seqs;
     }
@@ -554,7 +556,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
             s0 += 64;
             at = -1;
             if (s0 >= a.num_seqs || before >= hi) return false;
-            q = seq_plan(a, s0 + lane);
+            q = seq_plan<COLS>(a, s0 + lane);
             look();
         }
     };
@@ -564,7 +566,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
     };
     // operands: keys [tile][64 dims], row r = slot 4t + r % 4 of page r / 4, dims 16 (4p + G) ..; values [16 dims], dim 16b + r of page G
     u32x4 k[4][D / 64], v[D / 16];
-    bf16x8 qf[D / 64][2], qn[D / 64][2];  // queries of this segment, and of the next one
+    bf16x8 qf[SETS][D / 64][2], qn[SETS][D / 64][2];  // queries of this segment, and of the next one
     f32x2 scale = {1.f, 1.f}, scale_next = {1.f, 1.f};  // of page G
     const uint8_t* values_at = nullptr;
     int ids = 0, ids_base = 0;
@@ -585,55 +587,66 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
         for (int b = 0; b < D / 16; ++b) v[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(values_at + b * 256));
     };
     auto load_queries = [&](const Segment& s) {
-        const int cols = s.n * g, col = min(r, cols - 1), row = col / g;
-        const bf16_t* qrow = a.q + (int64_t)(s.row0 + row) * a.ld_q + (int64_t)(kvh * g + col - row * g) * D;
+        const int cols = s.n * g;
 #pragma unroll
-        for (int p = 0; p < D / 64; ++p)
+        for (int c = 0; c < SETS; ++c) {
+            const int col = min(16 * c + r, cols - 1), row = col / g;
+            const bf16_t* qrow = a.q + (int64_t)(s.row0 + row) * a.ld_q + (int64_t)(kvh * g + col - row * g) * D;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) qn[p][h] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + 64 * p + 16 * G + 8 * h));
+            for (int p = 0; p < D / 64; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) qn[c][p][h] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + 64 * p + 16 * G + 8 * h));
+        }
     };
 
-    f32x4 o[D / 16];
-    float m = kNegBig, l = 0.f;
-    int pos = 0, low = 0, pos_min = 0, low_max = 0;  // this column sees keys up to pos and above low, or below sinks
+    f32x4 o[SETS][D / 16];
+    float m[SETS], l[SETS];
+    int pos[SETS], low[SETS], pos_min = 0, low_max = 0;  // a column sees keys up to pos and above low, or below sinks
     auto enter = [&](const Segment& s) {
-        const int cols = s.n * g, row = min(r, cols - 1) / g;
-        pos = s.c + row;
-        low = a.window > 0 ? pos - a.window : -1;
+        const int cols = s.n * g;
         pos_min = s.c;
         low_max = a.window > 0 ? s.c + s.n - 1 - a.window : -1;
-        m = kNegBig;
-        l = 0.f;
 #pragma unroll
-        for (int b = 0; b < D / 16; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < SETS; ++c) {
+            pos[c] = s.c + min(16 * c + r, cols - 1) / g;
+            low[c] = a.window > 0 ? pos[c] - a.window : -1;
+            m[c] = kNegBig;
+            l[c] = 0.f;
 #pragma unroll
-        for (int p = 0; p < D / 64; ++p)
+            for (int b = 0; b < D / 16; ++b) o[c][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) qf[p][h] = qn[p][h];
+            for (int p = 0; p < D / 64; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) qf[c][p][h] = qn[c][p][h];
+        }
     };
     StreamRecord record{0, 0, 0, 0, 0};
     auto finish = [&](const Segment& s) {
-        float sum = l + __shfl_xor(l, 16);
-        sum += __shfl_xor(sum, 32);
         const int cols = s.n * g;
         const bool one = s.end - s.begin == s.blocks;  // the only part
-        if (one) {
-            if (r < cols) {
-                const float inv = 1.0f / sum;
-                const int row = r / g;
-                bf16_t* orow = a.out + (int64_t)(s.row0 + row) * a.ld_o + (int64_t)(kvh * g + r - row * g) * D + G * 4;
+        const int place = 2 * w + (s.start + s.begin > lo);  // the first stream of the run, or the last
 #pragma unroll
-                for (int b = 0; b < D / 16; ++b) *reinterpret_cast<bf16x4*>(orow + b * 16) = __builtin_convertvector(o[b] * inv, bf16x4);
+        for (int c = 0; c < SETS; ++c) {
+            float sum = l[c] + __shfl_xor(l[c], 16);
+            sum += __shfl_xor(sum, 32);
+            const int col = 16 * c + r;
+            if (col >= cols) continue;
+            if (one) {
+                const float inv = 1.0f / sum;
+                const int row = col / g;
+                bf16_t* orow = a.out + (int64_t)(s.row0 + row) * a.ld_o + (int64_t)(kvh * g + col - row * g) * D + G * 4;
+#pragma unroll
+                for (int b = 0; b < D / 16; ++b) *reinterpret_cast<bf16x4*>(orow + b * 16) = __builtin_convertvector(o[c][b] * inv, bf16x4);
+            } else {
+                const int64_t at = ((int64_t)kvh * 2 * parts.max_waves + place) * COLS + col;
+#pragma unroll
+                for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(parts.stream_o + at * D + b * 16 + G * 4) = o[c][b];
+                if (G == 0) parts.stream_ml[at] = f32x2{m[c], sum};
             }
+        }
+        if (one) {
             if (a.num_seqs <= 64 && kvh == 0 && lane == 0) parts.stream[s.seq] = StreamRecord{0, 0, 0, 0, 0};
             return;
-        }
-        const int place = 2 * w + (s.start + s.begin > lo);  // the first stream of the run, or the last
-        if (r < cols) {
-            const int64_t at = ((int64_t)kvh * 2 * parts.max_waves + place) * kStreamCols + r;
-#pragma unroll
-            for (int b = 0; b < D / 16; ++b) *reinterpret_cast<f32x4*>(parts.stream_o + at * D + b * 16 + G * 4) = o[b];
-            if (G == 0) parts.stream_ml[at] = f32x2{m, sum};
         }
         if (s.begin == 0) {  // the wave of its last block: the last one whose run does not begin behind it
             const int last = (int)(((uint64_t)(s.start + s.blocks) * (uint32_t)waves - 1) / (uint64_t)job.stream);
@@ -668,15 +681,19 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
         for (int b = seg.begin;;) {
             const bool same = b + 1 < seg.end;
             const int key0 = seen.actual(b) * kBlock;
-            f32x4 s[4];
+            f32x4 s[SETS][4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < SETS; ++c) s[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int p = 0; p < D / 64; ++p)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, widen8(k[t][p][2 * h], k[t][p][2 * h + 1])), qf[p][h], s[t], 0, 0, 0);
+                    for (int h = 0; h < 2; ++h) {
+                        const bf16x8 kf = __builtin_bit_cast(bf16x8, widen8(k[t][p][2 * h], k[t][p][2 * h + 1]));
+#pragma unroll
+                        for (int c = 0; c < SETS; ++c) s[c][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][p][h], s[c][t], 0, 0, 0);
+                    }
             }
             __builtin_amdgcn_sched_barrier(0);  // (the keys of the next block take the place of these)
             if (same) {
@@ -713,44 +730,53 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int key = key0 + G * kPage + 4 * t + i;
-                        const bool hidden = (key > pos) | ((key <= low) & (key >= a.sinks));
-                        s[t][i] = hidden ? -INFINITY : bad[t] >> (8 * i + 7) & 1 ? NAN : s[t][i];
+#pragma unroll
+                        for (int c = 0; c < SETS; ++c) {
+                            const bool hidden = (key > pos[c]) | ((key <= low[c]) & (key >= a.sinks));
+                            s[c][t][i] = hidden ? -INFINITY : bad[t] >> (8 * i + 7) & 1 ? NAN : s[c][t][i];
+                        }
                     }
             }
-            float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+            bf16x8 wt[SETS][2];
 #pragma unroll
-            for (int t = 1; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
-            top *= ps.keys;
-            if (__any(top > m)) {  // the reference moves to the running maximum, the same in the four lanes of a column
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
-                const float down = __builtin_amdgcn_exp2f(m - top);
-                m = top;
-                l *= down;
+            for (int c = 0; c < SETS; ++c) {
+                float top = fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3]));
 #pragma unroll
-                for (int b16 = 0; b16 < D / 16; ++b16)
+                for (int t = 1; t < 4; ++t) top = fmaxf(top, fmaxf(fmaxf(s[c][t][0], s[c][t][1]), fmaxf(s[c][t][2], s[c][t][3])));
+                top *= ps.keys;
+                if (__any(top > m[c])) {  // the reference moves to the running maximum, the same in the four lanes of a column
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m[c]);
+                    const float down = __builtin_amdgcn_exp2f(m[c] - top);
+                    m[c] = top;
+                    l[c] *= down;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) o[b16][x] *= down;
-            }
-            const float shift = ps.log_values - m;
-            float sum = 0.f;
-            bf16x8 wt[2];
+                    for (int b16 = 0; b16 < D / 16; ++b16)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                f32x8 p;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    p[x] = __builtin_amdgcn_exp2f(fmaf(s[2 * j + x / 4][x % 4], ps.keys, shift));
-                    sum += p[x];
+                        for (int x = 0; x < 4; ++x) o[c][b16][x] *= down;
                 }
-                wt[j] = __builtin_convertvector(p, bf16x8);
+                const float shift = ps.log_values - m[c];
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    f32x8 p;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        p[x] = __builtin_amdgcn_exp2f(fmaf(s[c][2 * j + x / 4][x % 4], ps.keys, shift));
+                        sum += p[x];
+                    }
+                    wt[c][j] = __builtin_convertvector(p, bf16x8);
+                }
+                l[c] += sum * ps.per_value;
             }
-            l += sum * ps.per_value;
 #pragma unroll
             for (int b16 = 0; b16 < D / 16; ++b16)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    o[b16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, widen8(v[b16][2 * j], v[b16][2 * j + 1])), wt[j], o[b16], 0, 0, 0);
+                for (int j = 0; j < 2; ++j) {
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, widen8(v[b16][2 * j], v[b16][2 * j + 1]));
+#pragma unroll
+                    for (int c = 0; c < SETS; ++c) o[c][b16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, wt[c][j], o[c][b16], 0, 0, 0);
+                }
             __builtin_amdgcn_sched_barrier(0);
             if (same || more) load_values();
             scale = scale_next;
@@ -1083,11 +1109,11 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
 }
 
 // The rows of sequences that break a rule become zeros, by one wave.
-template <int D>
+template <int D, int COLS>
 __device__ __forceinline__ void write_zeros(const Attn8Args& a, int kvh) {
     const int lane = threadIdx.x & 63, g = a.n_q / a.n_kv;
     for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
-        const SeqPlan q = seq_plan(a, s0 + lane);
+        const SeqPlan q = seq_plan<COLS>(a, s0 + lane);
         for (uint64_t todo = __ballot(q.broken); todo; todo &= todo - 1) {
             const int l = __builtin_ctzll(todo), row0 = lane_value(q.row0, l), n = lane_value(q.n, l);
             for (int i = 0; i < n; ++i)
@@ -1100,18 +1126,18 @@ __device__ __forceinline__ void write_zeros(const Attn8Args& a, int kvh) {
 template <bool TILES>
 constexpr int kThreads = TILES ? 512 : 256;
 
-template <int D, bool TILES>
-__global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Args a) {
+template <int D, bool TILES, int COLS>
+__global__ __launch_bounds__(kThreads<TILES>, COLS > kStreamCols ? 1 : 2) void attention8_kernel(Attn8Args a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char attn8_lds[];
     constexpr int WAVES = kThreads<TILES> / 64;
     const int kvh = blockIdx.x % a.n_kv, place = blockIdx.x / a.n_kv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Parts parts;
-    parts_in<TILES>(parts, a.workspace, a.n_kv, D);
+    parts_in<TILES, COLS>(parts, a.workspace, a.n_kv, D);
     Job job;
-    find_job<TILES>(a, parts.plan, place, job);
+    find_job<TILES, COLS>(a, parts.plan, place, job);
     if (blockIdx.x + a.n_kv >= gridDim.x) {  // behind the last unit
-        if (job.broken && wave == 0) write_zeros<D>(a, kvh);
+        if (job.broken && wave == 0) write_zeros<D, COLS>(a, kvh);
         if (a.num_seqs <= 64 && kvh == 0 && wave == 0 && (int)(threadIdx.x & 63) < a.num_seqs && (job.workers == 0 || job.seqs.stream == 0))
             parts.stream[threadIdx.x & 63] = StreamRecord{0, 0, 0, 0, 0};
         if (kvh == 0 && threadIdx.x == 0) {
@@ -1121,7 +1147,7 @@ __global__ __launch_bounds__(kThreads<TILES>, 2) void attention8_kernel(Attn8Arg
         return;
     }
     if (place < job.workers) {
-        stream_wave<D, TILES>(a, job, parts, kvh, place * WAVES + wave, job.workers * WAVES);
+        stream_wave<D, TILES, COLS>(a, job, parts, kvh, place * WAVES + wave, job.workers * WAVES);
         return;
     }
     if constexpr (TILES) {
@@ -1176,11 +1202,11 @@ __device__ __forceinline__ Joined join_parts(const f32x2* ml, const float* o, in
 }
 // All latency.  The first workgroups take a wave of the stream and a KV head each: D/4 threads have a column, or, where that leaves threads over,
 // each so many of its parts; the others as many columns of a cut tile as there are D/4 threads.
-template <int D, bool TILES, int THREADS>
+template <int D, bool TILES, int COLS, int THREADS>
 __global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, int stream_groups) {
     constexpr int LANES = D / 4, TEAMS = THREADS / LANES;
     Parts parts;
-    parts_in<TILES>(parts, a.workspace, a.n_kv, D);
+    parts_in<TILES, COLS>(parts, a.workspace, a.n_kv, D);
     const int g = a.n_q / a.n_kv, team = threadIdx.x / LANES, e = threadIdx.x % LANES * 4;
     auto out_of = [&](int row, int head) { return reinterpret_cast<bf16x4*>(a.out + (int64_t)row * a.ld_o + (int64_t)head * D + e); };
     if ((int)blockIdx.x < stream_groups) {
@@ -1195,7 +1221,7 @@ __global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, 
             Joined j{kNegBig, 0.f, {0.f, 0.f, 0.f, 0.f}};
             if (mine)
                 j = join_parts(parts.stream_ml, parts.stream_o, share, shares, rec.waves, D, e,
-                               [&](int p) { return ((int64_t)kvh * 2 * parts.max_waves + (p == 0 ? rec.place : 2 * (rec.wave + p))) * kStreamCols + col; });
+                               [&](int p) { return ((int64_t)kvh * 2 * parts.max_waves + (p == 0 ? rec.place : 2 * (rec.wave + p))) * COLS + col; });
             if (shares > 1) {
                 joined[team][threadIdx.x % LANES] = j;
                 __syncthreads();
@@ -1232,24 +1258,27 @@ __global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, 
 
 }  // namespace
 
-static bool has_tiles(int n_q, int n_kv, int max_new) { return (int64_t)max_new * (n_q / n_kv) > kStreamCols; }
+// The most columns that a sequence of a call can have.
+static int64_t most_cols(int n_q, int n_kv, int max_new) { return (int64_t)max_new * (n_q / n_kv); }
 
 size_t attention8_workspace_bytes(int n_q, int n_kv, int d, int max_new) {
     Parts t;
-    return has_tiles(n_q, n_kv, max_new) ? parts_in<true>(t, nullptr, n_kv, d) : parts_in<false>(t, nullptr, n_kv, d);
+    const int64_t cols = most_cols(n_q, n_kv, max_new);
+    return cols <= kStreamCols ? parts_in<false, kStreamCols>(t, nullptr, n_kv, d) : cols <= kWideCols ? parts_in<false, kWideCols>(t, nullptr, n_kv, d)
+                                                                                                       : parts_in<true, kStreamCols>(t, nullptr, n_kv, d);
 }
 
-template <int D, bool TILES>
+template <int D, bool TILES, int COLS>
 static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     // the stream's workgroups; no more tiles than whole ones in all rows and a partly filled one per sequence, and cutting the keys adds no more units
     // than twice the target; and one place behind the last unit
     const int g = a.n_q / a.n_kv;
     const int64_t tiles = TILES ? (int64_t)a.num_rows * g / kTileCols + a.num_seqs : 0;
-    const int64_t places = max_workers<TILES>(a.n_kv, D) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
+    const int64_t places = max_workers<TILES, COLS>(a.n_kv, D) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
     if (places * a.n_kv * kThreads<TILES> > UINT32_MAX) return hipErrorInvalidValue;
     Parts parts;
-    parts_in<TILES>(parts, a.workspace, a.n_kv, D);
-    if (!plans_alone<TILES>(a.num_seqs)) attention8_plan_kernel<TILES><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
+    parts_in<TILES, COLS>(parts, a.workspace, a.n_kv, D);
+    if (!plans_alone<TILES>(a.num_seqs)) attention8_plan_kernel<TILES, COLS><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
     const int lds = TILES ? sizeof(TileLds<D>) : 0;
     if (TILES) {
         static std::atomic<uint64_t> allowed{0};  // devices on which this kernel may use the LDS that it asks for
@@ -1257,21 +1286,21 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
         hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
         if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(attention8_kernel<D, TILES>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(attention8_kernel<D, TILES, COLS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
             if (e != hipSuccess) return e;
             if (dev < 64) allowed.fetch_or(1ull << dev);
         }
     }
-    attention8_kernel<D, TILES><<<(unsigned)(places * a.n_kv), kThreads<TILES>, lds, stream>>>(a);
+    attention8_kernel<D, TILES, COLS><<<(unsigned)(places * a.n_kv), kThreads<TILES>, lds, stream>>>(a);
     // no sequence can be cut that has no more blocks than these
-    const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : kStreamCols / g;
+    const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : COLS / g;
     if (most_blocks(own, rows, a.window, a.sinks) > (TILES && kMinShare < kWhole ? kMinShare : kWhole)) {
-        const int records = a.num_seqs <= 64 ? a.num_seqs : (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, kStreamCols / g, a.window, a.sinks) + 8);
+        const int records = a.num_seqs <= 64 ? a.num_seqs : (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, COLS / g, a.window, a.sinks) + 8);
         const int stream_groups = records * a.n_kv;
         const int64_t tile_groups = TILES ? std::min<int64_t>(2048, std::min<int64_t>(max_cut_tiles(a.n_kv), tiles) * a.n_kv * (kTileCols * D / 1024)) : 0;
         const dim3 grid((unsigned)(stream_groups + tile_groups));
-        if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, 512><<<grid, 512, 0, stream>>>(a, stream_groups);
-        else attention8_merge_kernel<D, TILES, 256><<<grid, 256, 0, stream>>>(a, stream_groups);
+        if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, COLS, 512><<<grid, 512, 0, stream>>>(a, stream_groups);
+        else attention8_merge_kernel<D, TILES, COLS, 256><<<grid, 256, 0, stream>>>(a, stream_groups);
     }
     return hipGetLastError();
 }
@@ -1279,8 +1308,8 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
 hipError_t launch_attention8(const Attn8Args& a, hipStream_t stream) {
     if (a.num_seqs <= 0 || a.num_rows <= 0) return hipSuccess;
     if (a.num_seqs > kMaxAttn8Seqs || (int64_t)a.num_rows * (a.n_q / a.n_kv) > INT32_MAX) return hipErrorInvalidValue;
-    const bool tiles = has_tiles(a.n_q, a.n_kv, a.max_new);
-    if (a.d == 128) return tiles ? launch<128, true>(a, stream) : launch<128, false>(a, stream);
-    if (a.d == 64) return tiles ? launch<64, true>(a, stream) : launch<64, false>(a, stream);
+    const int64_t cols = most_cols(a.n_q, a.n_kv, a.max_new);
+    if (a.d == 128) return cols <= kStreamCols ? launch<128, false, kStreamCols>(a, stream) : cols <= kWideCols ? launch<128, false, kWideCols>(a, stream) : launch<128, true, kStreamCols>(a, stream);
+    if (a.d == 64) return cols <= kStreamCols ? launch<64, false, kStreamCols>(a, stream) : cols <= kWideCols ? launch<64, false, kWideCols>(a, stream) : launch<64, true, kStreamCols>(a, stream);
     return hipErrorInvalidValue;
 }

@@ -609,6 +609,49 @@ def test_streams_of_very_different_lengths(seqs, heads, most):
         b.check(window, sinks, max_new=most, label=f"{seqs} streams {heads} window {window}")
 
 
+@pytest.mark.parametrize("heads,most", [((32, 8, 128), 8), ((40, 8, 128), 6), ((16, 1, 128), 2), ((8, 8, 128), 32), ((7, 1, 64), 4), ((4, 2, 64), 16), ((8, 8, 64), 17)], ids=str)
+@pytest.mark.parametrize("seqs", [1, 12, 65, 256, 257])
+def test_a_few_rows_of_each_sequence(seqs, heads, most):
+    """Between 17 and 32 columns."""
+    print(f"attention8 {seqs} sequences of up to {most} rows, {heads}", flush=True)
+    rng = np.random.default_rng(seqs)
+    cached = [int(rng.choice([0, 1, 15, 48, 63, 320, 383, 384, 900])) for _ in range(seqs)]
+    new = [int(rng.integers(1, most + 1)) for _ in range(seqs)]
+    cached[0], new[0] = 7000, most
+    b = Batch(heads, new, cached, seed=28, tail_rows=3)
+    ws = spoilt_workspace(b, most)
+    for window, sinks, broken in ((0, 0, False), (70, 10, False), (900, 130, True)):
+        if broken and seqs > 4:
+            b.cached[3] = -1
+            b.dev[1] = dev_ints(b.cached)
+        b.out.fill_(7.0)
+        ws.fill_(255)
+        b.run(window, sinks, workspace=ws)
+        b.check(window, sinks, max_new=most, label=f"{seqs} of up to {most} rows {heads} window {window}")
+    want = b.out.clone()
+    b.run(900, 130, workspace=ws)
+    assert torch.equal(b.out, want)
+
+
+@pytest.mark.parametrize("heads,new", [((8, 2, 128), [8, 3, 5]), ((8, 2, 64), [7, 1, 8]), ((16, 1, 64), [2, 1, 2])], ids=str)
+def test_no_numbers_among_a_few_rows(heads, new):
+    print(f"attention8: NaN codes, {new} {heads}", flush=True)
+    window, sinks = 48, 5
+    b = Batch(heads, new, [45, 100, 200], seed=29)
+    where = [(0, 0, 45 + new[0] // 2), (0, 1, 40), (1, 1, 100), (2, 0, 201), (2, 1, 3), (1, 0, 60)]
+    for s, side, pos in where:
+        b.put(side, s, pos, NAN_CODE)
+    b.run(window, sinks)
+    spoilt = [int(b.starts[s]) + i for s, (n, c) in enumerate(zip(new, b.cached)) for i in range(n)
+              if any(t == s and pos <= c + i and (pos > c + i - window or pos < sinks) for t, _, pos in where)]
+    got = f64(b.out)
+    assert np.isnan(got[spoilt]).all(1).all()
+    rest = [r for r in range(len(got)) if r not in spoilt]
+    assert np.isfinite(got[rest]).all()
+    if rest:
+        b.check(window, sinks, label="rows beside", skip_rows=spoilt)
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 64), (12, 4, 128), (16, 1, 128)], ids=str)
 @pytest.mark.parametrize("seqs", [30, 64, 65, 150, 256, 257, 400])
 def test_hybrids_of_every_kind_of_sequence(seqs, heads):
