@@ -1203,7 +1203,7 @@ __device__ __forceinline__ Joined join_parts(const f32x2* ml, const float* o, in
 // All latency.  The first workgroups take a wave of the stream and a KV head each: D/4 threads have a column, or, where that leaves threads over,
 // each so many of its parts; the others as many columns of a cut tile as there are D/4 threads.
 template <int D, bool TILES, int COLS, int THREADS>
-__global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, int stream_groups) {
+__global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, int stream_groups, int split) {
     constexpr int LANES = D / 4, TEAMS = THREADS / LANES;
     Parts parts;
     parts_in<TILES, COLS>(parts, a.workspace, a.n_kv, D);
@@ -1211,13 +1211,15 @@ __global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, 
     auto out_of = [&](int row, int head) { return reinterpret_cast<bf16x4*>(a.out + (int64_t)row * a.ld_o + (int64_t)head * D + e); };
     if ((int)blockIdx.x < stream_groups) {
         __shared__ Joined joined[TEAMS][LANES];
-        const int i = blockIdx.x / a.n_kv, kvh = blockIdx.x % a.n_kv;
+        const int kvh = blockIdx.x % a.n_kv, i = blockIdx.x / a.n_kv / split, each = (COLS + split - 1) / split, col0 = blockIdx.x / a.n_kv % split * each;
         if (a.num_seqs > 64 && i >= *parts.waves) return;
         const StreamRecord rec = parts.stream[i];
-        if (rec.waves == 0) return;
-        const int shares = rec.cols < TEAMS ? TEAMS / rec.cols : 1, share = team % shares;
-        for (int col = team / shares; shares > 1 || col < rec.cols; col += TEAMS / shares) {
-            const bool mine = col < rec.cols;
+        const int cols = min(rec.cols - col0, each);
+        if (rec.waves == 0 || cols <= 0) return;
+        const int shares = cols < TEAMS ? TEAMS / cols : 1, share = team % shares;
+        for (int c = team / shares; shares > 1 || c < cols; c += TEAMS / shares) {
+            const bool mine = c < cols;
+            const int col = col0 + c;
             Joined j{kNegBig, 0.f, {0.f, 0.f, 0.f, 0.f}};
             if (mine)
                 j = join_parts(parts.stream_ml, parts.stream_o, share, shares, rec.waves, D, e,
@@ -1296,11 +1298,12 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : COLS / g;
     if (most_blocks(own, rows, a.window, a.sinks) > (TILES && kMinShare < kWhole ? kMinShare : kWhole)) {
         const int records = a.num_seqs <= 64 ? a.num_seqs : (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, COLS / g, a.window, a.sinks) + 8);
-        const int stream_groups = records * a.n_kv;
+        // columns of few streams are spread over workgroups
+        const int split = std::max(1, std::min(COLS / 4, kGroups / std::max(1, records * a.n_kv))), stream_groups = records * a.n_kv * split;
         const int64_t tile_groups = TILES ? std::min<int64_t>(2048, std::min<int64_t>(max_cut_tiles(a.n_kv), tiles) * a.n_kv * (kTileCols * D / 1024)) : 0;
         const dim3 grid((unsigned)(stream_groups + tile_groups));
-        if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, COLS, 512><<<grid, 512, 0, stream>>>(a, stream_groups);
-        else attention8_merge_kernel<D, TILES, COLS, 256><<<grid, 256, 0, stream>>>(a, stream_groups);
+        if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, COLS, 512><<<grid, 512, 0, stream>>>(a, stream_groups, split);
+        else attention8_merge_kernel<D, TILES, COLS, 256><<<grid, 256, 0, stream>>>(a, stream_groups, split);
     }
     return hipGetLastError();
 }
