@@ -8,7 +8,8 @@
 // both in the one multiply-add that the exponential's argument takes anyway; a lane holds keys of one page only, so that its part of the sum of
 // the weights is that of p s_v times 1 / s_v.
 //
-// Up to 16 columns (decode rows) the keys are a stream from HBM: stream_wave.  More go in tiles whose keys pass through LDS: tile_unit.
+// Up to 16 columns (decode rows), or 32 where no sequence of a call can have more, the keys are a stream from HBM: stream_wave.  More go in tiles whose
+// keys pass through LDS: tile_unit.
 // The keys of long sequences are shared among waves, or units, by a plan made on the device, and the parts' results joined by a second launch.
 //
 // Roundings: queries, codes as bf16 (exact), weights p s_v and the output are bf16, all else float.  A weight rounded to bf16 is what a matrix
@@ -17,7 +18,7 @@
 //
 // Measured (8 KV heads of 128): 32 decode rows behind 300 .. 20000 keys, 308 MB, 58 us with the joining, 53 + 5, 5.8 TB/s inside the kernel (a copy
 // reaches 5.2); 64 behind a window of 1024, 33 us; 251 decode rows and 1802 chunk rows together, 938 MB and 63 GFLOP, 201 us; a chunk of 4096 behind
-// 4096 keys, 64 heads, 825 GFLOP that count, 786 us, 1.05 PFLOP/s (a large product reaches 1.42).
+// 4096 keys, 64 heads, 825 GFLOP that count, 795 us, 1.04 PFLOP/s (a large product reaches 1.42).
 #include "cache8.h"
 
 #include <algorithm>
@@ -32,9 +33,11 @@ constexpr int kBlock = 64;  // keys, four pages
 
 // ---- the plan --------------------------------------------------------------------------------------------------------------
 //
-// The lengths stand on the device.  Sequences of up to 16 columns are streams: their blocks of 64 keys, one sequence behind the other, are dealt in
-// equal runs to the waves of some workgroups.  The others have tiles of 256 columns, each a unit of work of its own or, where there are few of
-// them, several, which share its keys.  The stream's workgroups are the first of the launch.
+// The lengths stand on the device.  Sequences of up to 16 columns (32) are streams: their blocks of 64 keys, one sequence behind the other, are dealt
+// in equal runs to the waves of some workgroups.  The others have tiles of 256 columns, each a unit of work of its own or, where there are few of
+// them, several, which share its keys.  The stream's workgroups are the first of the launch. Streams of 32 columns need 393 registers, which the
+// launch with tiles has not: there those of 17 columns and more are tiles.  us as tiles / as streams (8B heads): 32 sequences of 5 rows behind up to
+// 8000 keys 165 / 58, of 8 166 / 64, 100 of up to 8 behind up to 700 68 / 45.
 constexpr int kStreamCols = 16, kWideCols = 32, kTileCols = 256;
 
 // A unit of work of a tile: a part of its keys.
@@ -807,7 +810,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 // The exponentials of a half run beside the scores of the next one and in front of its own outputs; what a phase reads from LDS is asked for in the
 // phase before.
 //
-// What bounds it, a chunk of 4096 behind 4096 keys: 786 us, 1.05 PFLOP/s.  Per block of 64 keys (2.0 us) the matrix cores are busy for 0.9 us, the
+// What bounds it, a chunk of 4096 behind 4096 keys: 795 us, 1.04 PFLOP/s.  Per block of 64 keys (2.0 us) the matrix cores are busy for 0.9 us, the
 // vector units for about 1.1 (32 exponentials and some 170 others a wave), LDS, which each wave reads all keys and values from, for 1.1; a wave's
 // chain goes through all three, and there are two waves on a SIMD to hide each other's waits, all that the registers allow.  What each costs, with
 // data that does not change, so that the clock stays up (which is worth 5 to 8 % itself): staging and barriers 8 %, exponentials 8 %, reads of LDS
@@ -1200,8 +1203,9 @@ __device__ __forceinline__ Joined join_parts(const f32x2* ml, const float* o, in
     if (mine <= 4) return join_batches<4>(ml, o, first, step, n, d, e, at);
     return join_batches<12>(ml, o, first, step, n, d, e, at);
 }
-// All latency.  The first workgroups take a wave of the stream and a KV head each: D/4 threads have a column, or, where that leaves threads over,
-// each so many of its parts; the others as many columns of a cut tile as there are D/4 threads.
+// All latency.  The first workgroups take some columns of a stream and a KV head each: D/4 threads have a column, or, where that leaves threads over,
+// each so many of its parts; the others as many columns of a cut tile as there are D/4 threads.  (Few streams have many parts: with all columns of a
+// stream in a workgroup 8 rows behind 20000 keys take 59 us instead of 25.)
 template <int D, bool TILES, int COLS, int THREADS>
 __global__ __launch_bounds__(THREADS) void attention8_merge_kernel(Attn8Args a, int stream_groups, int split) {
     constexpr int LANES = D / 4, TEAMS = THREADS / LANES;
