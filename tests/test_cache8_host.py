@@ -77,7 +77,7 @@ def test_attention_refuses(change, status):
 def test_more_work_than_a_launch_takes_is_refused():
     for rows in (1 << 27, 1 << 30):
         assert C8._lib().gllm_op_norm_rope_store8(*{**STORE, "rows": rows}.values()) == CAPACITY
-    large = dict(seqs=1 << 20, max_new=9, n_q=128, n_kv=64, ld_q=16384, ld_o=16384)
+    large = dict(seqs=1 << 20, max_new=17, n_q=128, n_kv=64, ld_q=16384, ld_o=16384)
     assert C8._lib().gllm_op_attention8(*{**ATTENTION, **large}.values()) == CAPACITY
 
 
