@@ -61,16 +61,18 @@ def gllm_op_step_maps(new_tokens, cached_len, free_pages, block_tables, num_bloc
     dev = new_tokens.get_device()
     if not (dev >= 0 and cached_len.get_device() == free_pages.get_device() == block_tables.get_device() == row_start.get_device() ==
             positions.get_device() == slots.get_device() == needed.get_device() == dev == _device() and
-            new_tokens.dtype is cached_len.dtype is free_pages.dtype is block_tables.dtype is row_start.dtype is positions.dtype is slots.dtype is needed.dtype is _I32 and
+            new_tokens.dtype is cached_len.dtype is free_pages.dtype is block_tables.dtype is _I32 and
+            row_start.dtype is positions.dtype is slots.dtype is needed.dtype is _I32 and
             new_tokens.is_contiguous() and cached_len.is_contiguous() and free_pages.is_contiguous() and block_tables.is_contiguous() and
             row_start.is_contiguous() and positions.is_contiguous() and slots.is_contiguous() and needed.is_contiguous()):
         _check(call, ((new_tokens, _I32), (cached_len, _I32), (free_pages, _I32), (block_tables, _I32), (row_start, _I32), (positions, _I32), (slots, _I32),
                       (needed, _I32)))
     seqs, rows = new_tokens.numel(), slots.numel()
-    if free_pages.dim() != 1 or cached_len.numel() != seqs or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1 or positions.numel() != rows or \
-            needed.numel() != 2:
-        _refuse(f"{call}: shapes new_tokens {tuple(new_tokens.shape)}, cached_len {tuple(cached_len.shape)}, free_pages {tuple(free_pages.shape)}, "
-                f"block_tables {tuple(block_tables.shape)}, row_start {tuple(row_start.shape)}, positions {tuple(positions.shape)}, slots {tuple(slots.shape)}, needed {tuple(needed.shape)}")
+    if free_pages.dim() != 1 or cached_len.numel() != seqs or block_tables.dim() != 2 or block_tables.shape[0] != seqs or \
+            row_start.numel() != seqs + 1 or positions.numel() != rows or needed.numel() != 2:
+        _refuse(f"{call}: shapes new_tokens {tuple(new_tokens.shape)}, cached_len {tuple(cached_len.shape)}, "
+                f"free_pages {tuple(free_pages.shape)}, block_tables {tuple(block_tables.shape)}, "
+                f"row_start {tuple(row_start.shape)}, positions {tuple(positions.shape)}, slots {tuple(slots.shape)}, needed {tuple(needed.shape)}")
     st = _lib().gllm_op_step_maps(new_tokens.data_ptr(), cached_len.data_ptr(), seqs, free_pages.data_ptr(), free_pages.numel(), block_tables.data_ptr(),
                                   block_tables.shape[1], num_blocks, rows, row_start.data_ptr(), positions.data_ptr(), slots.data_ptr(),
                                   needed.data_ptr(), _stream(stream, dev))

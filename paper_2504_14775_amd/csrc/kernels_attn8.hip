@@ -1125,7 +1125,7 @@ __device__ __forceinline__ void write_zeros(const Attn8Args& a, int kvh) {
     }
 }
 
-// Threads of a workgroup: four waves where there are streams only, two workgroups to a compute unit, eight with tiles.
+// Threads of a workgroup: four waves where there are streams only (of 64 dims and 16 columns two workgroups to a compute unit), eight with tiles.
 template <bool TILES>
 constexpr int kThreads = TILES ? 512 : 256;
 
@@ -1270,8 +1270,8 @@ static int64_t most_cols(int n_q, int n_kv, int max_new) { return (int64_t)max_n
 size_t attention8_workspace_bytes(int n_q, int n_kv, int d, int max_new) {
     Parts t;
     const int64_t cols = most_cols(n_q, n_kv, max_new);
-    return cols <= kStreamCols ? parts_in<false, kStreamCols>(t, nullptr, n_kv, d) : cols <= kWideCols ? parts_in<false, kWideCols>(t, nullptr, n_kv, d)
-                                                                                                       : parts_in<true, kStreamCols>(t, nullptr, n_kv, d);
+    if (cols <= kStreamCols) return parts_in<false, kStreamCols>(t, nullptr, n_kv, d);
+    return cols <= kWideCols ? parts_in<false, kWideCols>(t, nullptr, n_kv, d) : parts_in<true, kStreamCols>(t, nullptr, n_kv, d);
 }
 
 template <int D, bool TILES, int COLS>
@@ -1312,11 +1312,17 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+template <int D>
+static hipError_t launch_for(const Attn8Args& a, hipStream_t stream) {
+    const int64_t cols = most_cols(a.n_q, a.n_kv, a.max_new);
+    if (cols <= kStreamCols) return launch<D, false, kStreamCols>(a, stream);
+    return cols <= kWideCols ? launch<D, false, kWideCols>(a, stream) : launch<D, true, kStreamCols>(a, stream);
+}
+
 hipError_t launch_attention8(const Attn8Args& a, hipStream_t stream) {
     if (a.num_seqs <= 0 || a.num_rows <= 0) return hipSuccess;
     if (a.num_seqs > kMaxAttn8Seqs || (int64_t)a.num_rows * (a.n_q / a.n_kv) > INT32_MAX) return hipErrorInvalidValue;
-    const int64_t cols = most_cols(a.n_q, a.n_kv, a.max_new);
-    if (a.d == 128) return cols <= kStreamCols ? launch<128, false, kStreamCols>(a, stream) : cols <= kWideCols ? launch<128, false, kWideCols>(a, stream) : launch<128, true, kStreamCols>(a, stream);
-    if (a.d == 64) return cols <= kStreamCols ? launch<64, false, kStreamCols>(a, stream) : cols <= kWideCols ? launch<64, false, kWideCols>(a, stream) : launch<64, true, kStreamCols>(a, stream);
+    if (a.d == 128) return launch_for<128>(a, stream);
+    if (a.d == 64) return launch_for<64>(a, stream);
     return hipErrorInvalidValue;
 }
