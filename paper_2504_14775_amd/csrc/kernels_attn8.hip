@@ -889,10 +889,11 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         auto load_keys = [&](int id) { return has_keys ? *reinterpret_cast<const u32x4*>(a.k_pool + id * page_step + piece_off) : u32x4{0u, 0u, 0u, 0u}; };
         auto load_values = [&](int id) { return has_values ? *reinterpret_cast<const u32x4*>(a.v_pool + id * page_step + piece_off) : u32x4{0u, 0u, 0u, 0u}; };
         auto id_of = [&](int j) { return entry_of(min(j, blocks - 1), page).id; };  // (the same for the wave; read a round before it is wanted)
-        // Values that are no numbers may reach the columns that see them only: where not all rows see all keys they are emptied, and the key's scores are
-        // no numbers.
+        // Values that are no numbers may reach the columns that see them only: where not all rows of the tile see all keys of a block they are emptied, and
+        // the key's scores are no numbers, in all waves: also in one that sees all keys itself.
+        auto emptied = [&](int b) { return partly(key_of(b), kBlock, it.c + i0, it.c + i1); };  // (the same for all waves)
         auto clean = [&](int b, u32x4& x) {
-            if (!has_values || !partly(key_of(min(b, blocks - 1)), kBlock, it.c + i0, it.c + i1)) return;  // (the same for the wave)
+            if (!has_values || !emptied(min(b, blocks - 1))) return;
             uint32_t some = 0u;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -926,15 +927,18 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         // Masks, and the reference that a half needs.
         auto settle = [&](int b, int half, f32x16& s, float top, const PageScale& sc) {
             const int key0 = key_of(b) + half * kHalf;
-            if (partly(key0, kHalf, wave_min, wave_max)) {
-                const uint32_t bad = lds.bad[b % (2 * kStages<D>)][half] >> (16 * h);
+            if (emptied(b)) {  // (wherever a wave does not see a half whole, the tile does not see the block whole)
+                const uint32_t flags = __builtin_amdgcn_readfirstlane(lds.bad[b % (2 * kStages<D>)][half]);
+                if (flags || partly(key0, kHalf, wave_min, wave_max)) {
+                    const uint32_t bad = flags >> (16 * h);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int key = key0 + h * kPage + v;
-                    const bool hidden = (key > pos) | ((key <= low) & (key >= a.sinks));
-                    s[v] = hidden ? -INFINITY : bad >> v & 1 ? NAN : s[v];
+                    for (int v = 0; v < 16; ++v) {
+                        const int key = key0 + h * kPage + v;
+                        const bool hidden = (key > pos) | ((key <= low) & (key >= a.sinks));
+                        s[v] = hidden ? -INFINITY : bad >> v & 1 ? NAN : s[v];
+                    }
+                    top = largest(s);
                 }
-                top = largest(s);
             }
             top *= sc.keys;
             if (__any(top > m + kSlack)) {

@@ -536,6 +536,33 @@ def test_codes_that_are_no_numbers_spoil_the_rows_that_see_them_only(new, heads)
     b.check(window, sinks, label="rows beside", skip_rows=spoilt)
 
 
+def spoilt_by(b, s, pos, window, sinks):
+    """The rows that see a position of sequence s."""
+    c = b.cached[s]
+    return [int(b.starts[s]) + i for i in range(b.new[s]) if pos <= c + i and (window == 0 or pos > c + i - window or pos < sinks)]
+
+
+@pytest.mark.parametrize("side", [0, 1], ids=["key", "value"])
+@pytest.mark.parametrize("heads", [(16, 4, 64), (16, 2, 128), (4, 2, 128), (6, 6, 64)], ids=str)
+@pytest.mark.parametrize("new,cached,window,sinks,at", [
+    ([64], [0], 0, 0, (5, 0, 31, 32, 63)), ([64], [1000], 0, 0, (970, 999, 1000, 1031, 1063)), ([130], [0], 0, 0, (10, 63, 64, 100, 129)),
+    ([600, 3], [40, 7], 0, 0, (20, 90, 320, 600)), ([200], [300], 100, 0, (201, 230, 260, 300, 390)), ([150], [500], 64, 20, (0, 15, 19, 437, 455, 500, 600)),
+    ([64] + [24] * 59, [330] + [300] * 59, 0, 0, (5, 320, 335, 350, 380)), ([70] + [24] * 80, [330] + [300] * 80, 90, 70, (66, 242, 280, 335, 399))], ids=str)
+def test_one_code_that_is_no_number_spoils_all_rows_of_a_tile_that_see_it(new, cached, window, sinks, at, heads, side):
+    """One position at a time, in blocks that some rows of a tile see and others do not: tiles that are cut, and (many sequences) tiles that are not."""
+    print(f"attention8: one NaN {'value' if side else 'key'}, {len(new)} sequences, {new[0]} behind {cached[0]} {heads}", flush=True)
+    b = Batch(heads, new, cached, seed=30)
+    for pos in at:
+        b.put(side, 0, pos, NAN_CODE)
+        b.run(window, sinks)
+        spoilt = spoilt_by(b, 0, pos, window, sinks)
+        bad = np.isnan(f64(b.out))
+        b.put(side, 0, pos, 0x30)                            # (what it is does not reach the other rows)
+        assert np.nonzero(bad.any(1))[0].tolist() == spoilt and bad[spoilt].all(), pos
+        if pos == at[-1]:
+            b.check(window, sinks, label=f"rows beside position {pos}", skip_rows=spoilt)
+
+
 def test_strides_page_order_and_repetition():
     print("attention8: strided rows, other page orders", flush=True)
     a = Batch((12, 4, 128), NEW, CACHED, seed=9, q_pad=24, tail_rows=2)
