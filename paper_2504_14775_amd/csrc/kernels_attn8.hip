@@ -3,16 +3,17 @@
 // Per KV head the n rows of a sequence times the g query heads of the group are n*g columns over one stream of keys, column j being head
 // j % g of row j / g:  S^T = K.Q^T, softmax down the columns with a running reference, O^T += V^T.P^T, in transposed form so that the
 // scores a lane receives are the operand that it supplies (kernels_attn.hip).  A code times its page's scale is a value: codes become bf16
-// without rounding (4 bits of mantissa), the key scale s_k of a page multiplies its scores and the value scale s_v its weights,
-//     p s_v = 2^(s c s_k - m + log2 s_v),   c = scale * log2(e),
-// both in the one multiply-add that the exponential's argument takes anyway; a lane holds keys of one page only, so that its part of the sum of
-// the weights is that of p s_v times 1 / s_v.
+// without rounding (4 bits of mantissa).  The key scale s_k of a page multiplies its scores.  Its value scale s_v = 2^e f, 1 <= f < 2, is shared out: the
+// codes take 2^e as they become bf16, which has the exponents for it (2^-109 .. 2^109), and the weights f,
+//     p f = 2^(s c s_k - m + log2 f),   c = scale * log2(e),
+// in the one multiply-add that the exponential's argument takes anyway; a lane holds keys of one page only, so that its part of the sum of
+// the weights is that of p f times 1 / f.  (Weights of p s_v would leave float's range under small scales, and be missing from the sum of the weights.)
 //
 // Up to 16 columns (decode rows), or 32 where no sequence of a call can have more, the keys are a stream from HBM: stream_wave.  More go in tiles whose
 // keys pass through LDS: tile_unit.
 // The keys of long sequences are shared among waves, or units, by a plan made on the device, and the parts' results joined by a second launch.
 //
-// Roundings: queries, codes as bf16 (exact), weights p s_v and the output are bf16, all else float.  A weight rounded to bf16 is what a matrix
+// Roundings: queries, codes as bf16 (exact), weights p f and the output are bf16, all else float.  A weight rounded to bf16 is what a matrix
 // instruction takes; its error, up to 2^-8 of it, is in the output's tolerance.  Tiles sum the rounded weights (one instruction for two of them, and
 // the error of a weight cancels where all values agree), streams, which have instructions to spare, the unrounded.
 //
@@ -455,27 +456,30 @@ __host__ __device__ inline size_t parts_in(Parts& t, void* base, int n_kv, int d
 // A barrier that waits for this wave's reads and writes of LDS only: __syncthreads() would wait for the loads on their way too.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Four codes as bf16, without rounding.
-__device__ __forceinline__ u32x2 widen(uint32_t codes) {
-    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, true))};
+// Four codes times a power of two as bf16, without rounding.
+__device__ __forceinline__ u32x2 widen(uint32_t codes, float power) {
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, true))};
 }
-__device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi) {
-    const u32x2 a = widen(lo), b = widen(hi);
+__device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi, float power = 1.0f) {
+    const u32x2 a = widen(lo, power), b = widen(hi, power);
     return u32x4{a[0], a[1], b[0], b[1]};
 }
 // Bit 7 of every byte that is no number.
 __device__ __forceinline__ uint32_t no_numbers(uint32_t codes) { return ((codes & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
-// What a page's scales come to: the factor of its scores, log2 of that of its weights, and one over that.
+// What a page's scales come to: the factor of its scores, log2 of that of its weights, and one over that; and the power of two that its values take.
 struct PageScale {
     float keys, log_values, per_value;
-    __device__ __forceinline__ void of(f32x2 s, float scale_log2) {
+    // Returns the power of two.
+    __device__ __forceinline__ float of(f32x2 s, float scale_log2) {
         // (neither 0 nor infinite: the products with hidden keys' scores and with 0 stay what they are)
         keys = fminf(fmaxf(fminf(fmaxf(s[0], kScaleMin), kScaleMax) * scale_log2, 0x1p-126f), 0x1p127f);
-        const float v = fminf(fmaxf(s[1], kScaleMin), kScaleMax);
-        log_values = __builtin_amdgcn_logf(v);
-        per_value = __builtin_amdgcn_rcpf(v);
+        const uint32_t v = __builtin_bit_cast(uint32_t, fminf(fmaxf(s[1], kScaleMin), kScaleMax));
+        const float f = __builtin_bit_cast(float, (v & 0x007FFFFFu) | 0x3F800000u);
+        log_values = __builtin_amdgcn_logf(f);
+        per_value = __builtin_amdgcn_rcpf(f);
+        return __builtin_bit_cast(float, v & 0x7F800000u);
     }
 };
 
@@ -710,7 +714,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
                 begin_next();
             }
             PageScale ps;
-            ps.of(scale, a.scale_log2);
+            const float power = ps.of(scale, a.scale_log2);
             if (key0 + kBlock - 1 > pos_min || (key0 <= low_max && key0 + kBlock > a.sinks)) {  // not all keys are seen by all columns
                 // values that are no numbers may reach the columns that see them only: they are emptied and the key's scores are no numbers
                 u32x4 bad = {0u, 0u, 0u, 0u};
@@ -776,7 +780,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
             for (int b16 = 0; b16 < D / 16; ++b16)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const bf16x8 vf = __builtin_bit_cast(bf16x8, widen8(v[b16][2 * j], v[b16][2 * j + 1]));
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, widen8(v[b16][2 * j], v[b16][2 * j + 1], power));
 #pragma unroll
                     for (int c = 0; c < SETS; ++c) o[c][b16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, wt[c][j], o[c][b16], 0, 0, 0);
                 }
@@ -826,6 +830,7 @@ constexpr int kStages = D == 64 ? 4 : 2;
 constexpr int kHalf = 32, kWindow = 64;
 struct PageEntry {
     int32_t id;
+    float power;
     PageScale scale;
 };
 template <int D>
@@ -835,7 +840,7 @@ struct TileLds {
     PageEntry pages[2][kWindow * 4];                // of 64 blocks and the next 64
     uint32_t bad[2 * kStages<D>][2];                             // of a half: bit 16h + t: slot t of page h has values that are no numbers
 };
-constexpr float kSlack = 32.0f;  // a reference lags by up to this: weights stay below 2^32
+constexpr float kSlack = 32.0f;  // a reference lags by up to this: weights stay below 2^33
 
 template <int D>
 __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, const Parts& parts, int kvh, TileLds<D>& lds) {
@@ -877,7 +882,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         auto entry = [&](int x, int id, f32x2 sc) {
             PageEntry e;
             e.id = id;
-            e.scale.of(sc, a.scale_log2);
+            e.power = e.scale.of(sc, a.scale_log2);
             lds.pages[x / (kWindow * 4) % 2][x % (kWindow * 4)] = e;
         };
         auto entry_of = [&](int b, int q) -> const PageEntry& { return lds.pages[b / kWindow % 2][b % kWindow * 4 + q]; };
@@ -889,6 +894,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
         auto load_keys = [&](int id) { return has_keys ? *reinterpret_cast<const u32x4*>(a.k_pool + id * page_step + piece_off) : u32x4{0u, 0u, 0u, 0u}; };
         auto load_values = [&](int id) { return has_values ? *reinterpret_cast<const u32x4*>(a.v_pool + id * page_step + piece_off) : u32x4{0u, 0u, 0u, 0u}; };
         auto id_of = [&](int j) { return entry_of(min(j, blocks - 1), page).id; };  // (the same for the wave; read a round before it is wanted)
+        auto power_of = [&](int j) { return entry_of(min(j, blocks - 1), page).power; };
         // Values that are no numbers may reach the columns that see them only: where not all rows of the tile see all keys of a block they are emptied, and
         // the key's scores are no numbers, in all waves: also in one that sees all keys itself.
         auto emptied = [&](int b) { return partly(key_of(b), kBlock, it.c + i0, it.c + i1); };  // (the same for all waves)
@@ -1016,10 +1022,10 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             put_keys(1, widen8(k1[0], k1[1]), widen8(k1[2], k1[3]));
             if (MORE) put_keys(2, widen8(k2[0], k2[1]), widen8(k2[2], k2[3]));
             clean(0, v0);
-            put_values(0, widen8(v0[0], v0[1]), widen8(v0[2], v0[3]));
+            put_values(0, widen8(v0[0], v0[1], power_of(0)), widen8(v0[2], v0[3], power_of(0)));
             if (MORE) {
                 clean(1, v1);
-                put_values(1, widen8(v1[0], v1[1]), widen8(v1[2], v1[3]));
+                put_values(1, widen8(v1[0], v1[1], power_of(1)), widen8(v1[2], v1[3], power_of(1)));
             }
         }
         lds_barrier();
@@ -1057,6 +1063,7 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
             const int next_keys = uniform(id_keys), next_values = uniform(id_values);
             id_keys = id_of(b + AHEAD + 3);
             id_values = id_of(b + AHEAD + 2);
+            const float power = power_of(b + AHEAD);  // of the values in rv
             if (threadIdx.x < 2) lds.bad[(b + 2 * AHEAD + (AHEAD == 1)) % (2 * kStages<D>)][threadIdx.x] = 0u;
             const PageScale then = entry_of(b, 2 + h).scale, after = entry_of(min(b + 1, blocks - 1), h).scale;
             u32x4 wide[4];
@@ -1072,9 +1079,9 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 settle(b, 1, s, top, then);
                 clean(b + AHEAD, rv);
                 half_block(b, 1, s, top, then, [&](int x) {
-                    if (x == 1) wide[2] = widen8(rv[0], rv[1]);
+                    if (x == 1) wide[2] = widen8(rv[0], rv[1], power);
                     if (x == 3) {
-                        wide[3] = widen8(rv[2], rv[3]);
+                        wide[3] = widen8(rv[2], rv[3], power);
                         rv = load_values(next_values);
                     }
                 });
@@ -1082,8 +1089,8 @@ __device__ __forceinline__ void tile_unit(const Attn8Args& a, const Unit& it, co
                 put_keys(b + AHEAD + 1, widen8(rk[0], rk[1]), widen8(rk[2], rk[3]));
                 rk = load_keys(next_keys);
                 clean(b + AHEAD, rv);
-                wide[2] = widen8(rv[0], rv[1]);
-                wide[3] = widen8(rv[2], rv[3]);
+                wide[2] = widen8(rv[0], rv[1], power);
+                wide[3] = widen8(rv[2], rv[3], power);
                 rv = load_values(next_values);
             }
             put_values(b + AHEAD, wide[2], wide[3]);

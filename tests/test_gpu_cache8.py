@@ -594,6 +594,52 @@ def test_scales_whose_product_with_the_scores_leaves_the_range():
     b.check(scale=2e38, label="queries of zeros, scale 2e38 over scales of 1e30")
 
 
+@pytest.mark.parametrize("n", [1, 20, 40])
+def test_keys_of_low_weight_whose_values_are_all_zeros_count_in_the_sum(n):
+    """One key of a score 27 above (in base 2) the 2^24 behind it, whose pages of zeros have the least scale: in the sum of the weights they are an
+    eighth (and 16 of them, a lane's in a block, 2^-23, what float adds to 1 without rounding).  As many KV heads as compute units, so that the keys are
+    cut into few parts; 1 column, 20, and a tile of 40."""
+    print(f"attention8: 2^24 keys of zeros, {n} rows", flush=True)
+    heads, keys = 256, 1 << 24
+    b = Batch((heads, heads, 64), [n], [32], seed=31)
+    first, rest = b.tables[0, 0], b.tables[0, 1]
+    b.tables = np.full((1, keys // PAGE + 4), rest, dtype=np.int32)
+    b.tables[0, 0] = first
+    b.cached = [keys]
+    b.dev[0], b.dev[1] = dev_ints(b.tables), dev_ints(b.cached)
+    b.k.zero_()
+    b.v.zero_()
+    b.put(0, 0, 0, 0x38)                                     # code of 1
+    b.put(1, 0, 0, 0x38)
+    b.scales.fill_(1.0)
+    b.scales[int(rest), :, 1] = O.LEAST
+    b.q.fill_(1.0)
+    above = 27.0
+    b.run(scale=above * np.log(2) / 64)
+    total = 1 + (keys + np.arange(n)) * 2.0 ** -above
+    want = np.broadcast_to((1 / total)[:, None], (n, heads * 64))
+    tol = bound(want, want, np.full(n, above * np.log(2)), 64)
+    off = np.abs(f64(b.out) - want)
+    print(f"[parity] attention8 keys of zeros: max abs {off.max():.3g}, of the bound {(off / tol).max():.2f}", flush=True)
+    assert (off <= tol).all()
+
+
+@pytest.mark.parametrize("heads", [(16, 4, 64), (8, 1, 128)], ids=str)
+@pytest.mark.parametrize("new", [1, 3, 100])
+def test_pages_of_zeros_under_large_scales(new, heads):
+    """Keys of large scores whose values are zeros: their scale does not matter, and they count as any others."""
+    print(f"attention8: zeros under scales of 2^100, {new} rows {heads}", flush=True)
+    b = Batch(heads, [new], [300], seed=32)
+    b.q.mul_(7.0)
+    for page in range(18):
+        b.scales[b.tables[0, page], :, 0] = 0.01 if page >= 4 else 1e-5
+        if page >= 4:
+            b.v[b.tables[0, page]] = 0
+            b.scales[b.tables[0, page], :, 1] = float("inf") if page % 2 else 2.0 ** 100
+    b.run()
+    b.check(label=f"zeros under scales of 2^100 {heads}")
+
+
 @pytest.mark.parametrize("seqs,n", [(17, 40), (70, 20)])
 def test_shared_prefix_of_more_pages_than_a_tile_holds_ids_of(seqs, n):
     """One prefix for all sequences, whose tiles are too many to be cut."""
