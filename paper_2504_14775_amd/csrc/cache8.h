@@ -1,5 +1,6 @@
 // Internal declarations of the operators over a KV cache in 8 bits (include/gllm_cache8.h).
 #pragma once
+#include "../../include/gllm_stage.h"
 #include "common.h"
 
 constexpr float kCodeMax = 448.0f;                 // the largest e4m3 value
@@ -26,4 +27,5 @@ struct Attn8Args {
 };
 constexpr int kMaxAttn8Seqs = 1 << 20;
 size_t attention8_workspace_bytes(int n_q, int n_kv, int d, int max_new);
-hipError_t launch_attention8(const Attn8Args& a, hipStream_t stream);
+// GLLM_E_CAPACITY, with nothing enqueued, for more work than a launch takes; GLLM_E_HIP for errors of the runtime.
+gllm_status launch_attention8(const Attn8Args& a, hipStream_t stream);

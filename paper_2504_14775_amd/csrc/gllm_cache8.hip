@@ -615,6 +615,5 @@ gllm_status gllm_op_attention8(const void* q, int64_t ld_q, const void* k_pool, 
     a.n_q = n_q_heads; a.n_kv = n_kv_heads; a.d = head_dim;
     a.scale_log2 = base2(scale);
     a.workspace = workspace;
-    const hipError_t e = launch_attention8(a, (hipStream_t)stream);
-    return e == hipSuccess ? GLLM_OK : e == hipErrorInvalidValue ? GLLM_E_CAPACITY : GLLM_E_HIP;
+    return launch_attention8(a, (hipStream_t)stream);
 }

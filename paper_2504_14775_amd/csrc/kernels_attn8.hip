@@ -1286,13 +1286,13 @@ size_t attention8_workspace_bytes(int n_q, int n_kv, int d, int max_new) {
 }
 
 template <int D, bool TILES, int COLS>
-static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
+static gllm_status launch(const Attn8Args& a, hipStream_t stream) {
     // the stream's workgroups; no more tiles than whole ones in all rows and a partly filled one per sequence, and cutting the keys adds no more units
     // than twice the target; and one place behind the last unit
     const int g = a.n_q / a.n_kv;
     const int64_t tiles = TILES ? (int64_t)a.num_rows * g / kTileCols + a.num_seqs : 0;
     const int64_t places = max_workers<TILES, COLS>(a.n_kv, D) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
-    if (places * a.n_kv * kThreads<TILES> > UINT32_MAX) return hipErrorInvalidValue;
+    if (places * a.n_kv * kThreads<TILES> > UINT32_MAX) return GLLM_E_CAPACITY;
     Parts parts;
     parts_in<TILES, COLS>(parts, a.workspace, a.n_kv, D);
     if (!plans_alone<TILES>(a.num_seqs)) attention8_plan_kernel<TILES, COLS><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
@@ -1300,11 +1300,10 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
     if (TILES) {
         static std::atomic<uint64_t> allowed{0};  // devices on which this kernel may use the LDS that it asks for
         int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
-        if (e != hipSuccess) return e;
+        if (hipGetDevice(&dev) != hipSuccess) return GLLM_E_HIP;
         if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(attention8_kernel<D, TILES, COLS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-            if (e != hipSuccess) return e;
+            if (hipFuncSetAttribute(reinterpret_cast<const void*>(attention8_kernel<D, TILES, COLS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+                return GLLM_E_HIP;
             if (dev < 64) allowed.fetch_or(1ull << dev);
         }
     }
@@ -1320,20 +1319,20 @@ static hipError_t launch(const Attn8Args& a, hipStream_t stream) {
         if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, COLS, 512><<<grid, 512, 0, stream>>>(a, stream_groups, split);
         else attention8_merge_kernel<D, TILES, COLS, 256><<<grid, 256, 0, stream>>>(a, stream_groups, split);
     }
-    return hipGetLastError();
+    return hipGetLastError() == hipSuccess ? GLLM_OK : GLLM_E_HIP;
 }
 
 template <int D>
-static hipError_t launch_for(const Attn8Args& a, hipStream_t stream) {
+static gllm_status launch_for(const Attn8Args& a, hipStream_t stream) {
     const int64_t cols = most_cols(a.n_q, a.n_kv, a.max_new);
     if (cols <= kStreamCols) return launch<D, false, kStreamCols>(a, stream);
     return cols <= kWideCols ? launch<D, false, kWideCols>(a, stream) : launch<D, true, kStreamCols>(a, stream);
 }
 
-hipError_t launch_attention8(const Attn8Args& a, hipStream_t stream) {
-    if (a.num_seqs <= 0 || a.num_rows <= 0) return hipSuccess;
-    if (a.num_seqs > kMaxAttn8Seqs || (int64_t)a.num_rows * (a.n_q / a.n_kv) > INT32_MAX) return hipErrorInvalidValue;
+gllm_status launch_attention8(const Attn8Args& a, hipStream_t stream) {
+    if (a.num_seqs <= 0 || a.num_rows <= 0) return GLLM_OK;
+    if (a.num_seqs > kMaxAttn8Seqs || (int64_t)a.num_rows * (a.n_q / a.n_kv) > INT32_MAX) return GLLM_E_CAPACITY;
     if (a.d == 128) return launch_for<128>(a, stream);
     if (a.d == 64) return launch_for<64>(a, stream);
-    return hipErrorInvalidValue;
+    return GLLM_E_UNSUPPORTED;
 }

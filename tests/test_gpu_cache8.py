@@ -10,6 +10,8 @@ Attention: the weights of the softmax, times the scale of the value's page, and 
 of the type), the scores summed in float32.  With A = sum p|v| and M the largest sum |q_i k_i| * scale of a row, an output is off by at
 most 2^-8 |out| + (2^-8 + 2 M (d + 10) 2^-24 + 2^-17) A: the middle term is what an error of a score does to p and to its sum (d products
 and sums of 2^-24 each, the scales, twice: numerator and denominator), the last the exponentials, the logarithm of a scale and the sums over keys."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -22,6 +24,7 @@ from gpu_util import DEV
 pytestmark = pytest.mark.gpu
 PAGE = 16
 NAN_CODE = 0x7F
+HIP, INVALID_VALUE = -6, 1     # gllm_status, hipError_t
 HEADS = [(4, 2, 64), (32, 8, 128), (10, 2, 128), (16, 1, 128), (8, 8, 64), (12, 4, 128), (7, 1, 64)]
 
 
@@ -788,6 +791,26 @@ def test_binding_refuses_what_does_not_fit():
     i = dev_ints([1, 2])
     with pytest.raises(B.GllmError):
         C8.gllm_op_step_maps(i, i, i, i.view(2, 1), 5, i, i, i, i)
+
+
+@pytest.mark.parametrize("max_new", [1, 8, 40])
+def test_errors_of_the_runtime_are_no_lack_of_capacity(max_new):
+    """An error of the runtime that nobody has read yet is returned by the next call that reads it, as one of the runtime."""
+    b = Batch((8, 2, 64), [1, 1], [25, 46], seed=33)
+    ws = spoilt_workspace(b, max_new)
+    torch.cuda.synchronize()
+    hip = C8._lib()
+    hip.hipGetDeviceCount.argtypes = [C.c_void_p]
+    hip.hipPeekAtLastError.argtypes = hip.hipGetLastError.argtypes = []
+    try:
+        assert hip.hipGetDeviceCount(None) == INVALID_VALUE and hip.hipPeekAtLastError() == INVALID_VALUE
+        with pytest.raises(B.GllmError) as e:
+            C8.gllm_op_attention8(b.q, b.k, b.v, b.scales, *b.dev, b.out, max_new, workspace=ws)
+        assert e.value.status == HIP
+    finally:
+        hip.hipGetLastError()
+    b.run(max_new=max_new)
+    b.check(max_new=max_new, label="behind an error")
 
 
 def test_codes_may_be_given_as_float8():
