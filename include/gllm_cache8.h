@@ -96,8 +96,8 @@ gllm_status gllm_op_norm_rope_store8(const void* qkv, int64_t ld_qkv, int32_t ro
  * Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads with at most 16 query heads per KV head, at most
  * GLLM_CACHE8_MAX_BLOCKS blocks (else GLLM_E_UNSUPPORTED); scale > 0 and at most 2.3e38 (else GLLM_E_INVALID), |q . k * scale| at most 1e8
  * and the values' magnitude at most 1e15 (beyond these, results are not).
- * GLLM_E_CAPACITY for a workspace that is too small, for more than 2^20 sequences and for more work than a launch takes (there is none too
- * much up to (num_rows * n_q_heads / n_kv_heads / 256 + num_seqs) * n_kv_heads = 2^22). */
+ * GLLM_E_CAPACITY, with nothing enqueued, for a workspace that is too small, for more than 2^20 sequences and for more work than a launch takes
+ * (there is none too much up to (num_rows * n_q_heads / n_kv_heads / 256 + num_seqs) * n_kv_heads = 2^22 and below 2^20 KV heads). */
 gllm_status gllm_op_attention8(const void* q, int64_t ld_q, const void* k_pool, const void* v_pool, const float* scales, int64_t num_blocks,
                                const int32_t* block_tables, int32_t block_table_stride, const int32_t* cached_len,
                                const int32_t* row_start, int32_t num_seqs, int32_t num_rows, int32_t max_new, int32_t window, int32_t sinks,

@@ -1292,9 +1292,17 @@ static gllm_status launch(const Attn8Args& a, hipStream_t stream) {
     const int g = a.n_q / a.n_kv;
     const int64_t tiles = TILES ? (int64_t)a.num_rows * g / kTileCols + a.num_seqs : 0;
     const int64_t places = max_workers<TILES, COLS>(a.n_kv, D) + tiles + (TILES ? 2 * target_units(a.n_kv) : 0) + 1;
-    if (places * a.n_kv * kThreads<TILES> > UINT32_MAX) return GLLM_E_CAPACITY;
     Parts parts;
     parts_in<TILES, COLS>(parts, a.workspace, a.n_kv, D);
+    // the joining: no sequence can be cut that has no more blocks than these
+    const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : COLS / g;
+    const bool joined = most_blocks(own, rows, a.window, a.sinks) > (TILES && kMinShare < kWhole ? kMinShare : kWhole);
+    const int64_t records = a.num_seqs <= 64 ? a.num_seqs : std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, COLS / g, a.window, a.sinks) + 8);
+    // columns of few streams are spread over workgroups
+    const int64_t split = std::max<int64_t>(1, std::min<int64_t>(COLS / 4, kGroups / (records * a.n_kv))), stream_groups = records * a.n_kv * split;
+    const int64_t tile_groups = TILES ? std::min<int64_t>(2048, std::min<int64_t>(max_cut_tiles(a.n_kv), tiles) * a.n_kv * (kTileCols * D / 1024)) : 0;
+    const int join_threads = a.num_seqs <= 64 ? 512 : 256;
+    if (places * a.n_kv * kThreads<TILES> > UINT32_MAX || (joined && (stream_groups + tile_groups) * join_threads > UINT32_MAX)) return GLLM_E_CAPACITY;
     if (!plans_alone<TILES>(a.num_seqs)) attention8_plan_kernel<TILES, COLS><<<1, 1024, 0, stream>>>(a, parts.plan, parts.count);
     const int lds = TILES ? sizeof(TileLds<D>) : 0;
     if (TILES) {
@@ -1308,16 +1316,10 @@ static gllm_status launch(const Attn8Args& a, hipStream_t stream) {
         }
     }
     attention8_kernel<D, TILES, COLS><<<(unsigned)(places * a.n_kv), kThreads<TILES>, lds, stream>>>(a);
-    // no sequence can be cut that has no more blocks than these
-    const int64_t own = ceil_div(a.table_stride, kBlock / kPage), rows = TILES ? kTileCols / g + 2 : COLS / g;
-    if (most_blocks(own, rows, a.window, a.sinks) > (TILES && kMinShare < kWhole ? kMinShare : kWhole)) {
-        const int records = a.num_seqs <= 64 ? a.num_seqs : (int)std::min<int64_t>(parts.max_waves, (int64_t)a.num_seqs * most_blocks(own, COLS / g, a.window, a.sinks) + 8);
-        // columns of few streams are spread over workgroups
-        const int split = std::max(1, std::min(COLS / 4, kGroups / std::max(1, records * a.n_kv))), stream_groups = records * a.n_kv * split;
-        const int64_t tile_groups = TILES ? std::min<int64_t>(2048, std::min<int64_t>(max_cut_tiles(a.n_kv), tiles) * a.n_kv * (kTileCols * D / 1024)) : 0;
+    if (joined) {
         const dim3 grid((unsigned)(stream_groups + tile_groups));
-        if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, COLS, 512><<<grid, 512, 0, stream>>>(a, stream_groups, split);
-        else attention8_merge_kernel<D, TILES, COLS, 256><<<grid, 256, 0, stream>>>(a, stream_groups, split);
+        if (a.num_seqs <= 64) attention8_merge_kernel<D, TILES, COLS, 512><<<grid, 512, 0, stream>>>(a, (int)stream_groups, (int)split);
+        else attention8_merge_kernel<D, TILES, COLS, 256><<<grid, 256, 0, stream>>>(a, (int)stream_groups, (int)split);
     }
     return hipGetLastError() == hipSuccess ? GLLM_OK : GLLM_E_HIP;
 }

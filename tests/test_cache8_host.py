@@ -81,6 +81,14 @@ def test_more_work_than_a_launch_takes_is_refused():
     assert C8._lib().gllm_op_attention8(*{**ATTENTION, **large}.values()) == CAPACITY
 
 
+@pytest.mark.parametrize("max_new", [1, 17])
+def test_more_work_than_the_joining_takes_is_refused(max_new):
+    """64 sequences and 2^18 KV heads: the first launch takes them, the joining would not (before anything is enqueued, or the outputs would be half done)."""
+    heads = 1 << 18
+    much = dict(seqs=64, rows=64, stride=100, max_new=max_new, n_q=heads, n_kv=heads, d=64, ld_q=64 * heads, ld_o=64 * heads)
+    assert C8._lib().gllm_op_attention8(*{**ATTENTION, **much}.values()) == CAPACITY
+
+
 @pytest.mark.parametrize("shape", [(0, 1, 128, 1), (4, 0, 128, 1), (5, 2, 128, 1), (34, 2, 64, 1), (4, 2, 96, 1), (4, 2, 128, 0)])
 def test_no_workspace_for_what_attention_does_not_take(shape):
     assert C8.gllm_op_attention8_workspace_bytes(*shape) == 0
