@@ -59,6 +59,7 @@ gllm_status gllm_op_step_maps(const int32_t* new_tokens, const int32_t* cached_l
  *   qkv       DEVICE float or bf16 (rows_type) [num_rows][ld_qkv]: query heads, key heads, value heads (ld_qkv a multiple of 4, 16-byte
  *             aligned, bf16 8-byte)
  *   q_gain, k_gain  DEVICE bf16 [head_dim], 8-byte aligned, or NULL: heads as they are
+ *   eps       0, or positive and inside float's range (else GLLM_E_INVALID)
  *   rope      DEVICE float [max_position][head_dim/2][2]: cosine and sine, 16-byte aligned; a position outside [0, max_position) is read
  *             as the nearest one inside
  *   positions, slots  DEVICE int32 [num_rows], as gllm_op_step_maps writes them.  Nothing is written for a row with a slot outside
@@ -69,8 +70,9 @@ gllm_status gllm_op_step_maps(const int32_t* new_tokens, const int32_t* cached_l
  * (at least 1) with which m / 448 fits, and the kept codes are divided by it and rounded; a scale that is not positive and finite counts as
  * 2^-100 there.  All other slots are left as they are.  A value that is not finite becomes the code that is not a number.
  * Supported: head_dim 64 or 128, any head counts with n_q_heads + 2 * n_kv_heads <= 65535 (else GLLM_E_UNSUPPORTED), at most
- * GLLM_CACHE8_MAX_BLOCKS blocks.  The mean of squares is held in float: magnitudes up to 1e17 with a gain.  GLLM_E_CAPACITY for more rows than
- * a launch takes (there are none too many up to num_rows * (n_q_heads + 2 * n_kv_heads) = 2^25). */
+ * GLLM_CACHE8_MAX_BLOCKS blocks.  The mean of squares is held in float: with a gain, magnitudes up to 1e17, and sqrt(mean(h^2) + eps) from 1e-18 on
+ * or 0 (then a head of zeros becomes 0 / 0).  GLLM_E_CAPACITY for more rows than a launch takes (there are none too many up to
+ * num_rows * (n_q_heads + 2 * n_kv_heads) = 2^25). */
 gllm_status gllm_op_norm_rope_store8(const void* qkv, int64_t ld_qkv, int32_t rows_type, const void* q_gain, const void* k_gain, double eps,
                                      const float* rope, int32_t max_position, const int32_t* positions, const int32_t* slots,
                                      int32_t num_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void* q_out, int64_t ld_q,

@@ -557,8 +557,8 @@ gllm_status gllm_op_norm_rope_store8(const void* qkv, int64_t ld_qkv, int32_t ro
                                      const float* rope, int32_t max_position, const int32_t* positions, const int32_t* slots,
                                      int32_t num_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void* q_out, int64_t ld_q,
                                      void* k_pool, void* v_pool, float* scales, int64_t num_blocks, void* stream) {
-    if (num_rows < 0 || n_q_heads < 1 || n_kv_heads < 1 || max_position < 1 || num_blocks < 1 || !(eps >= 0.0) || !std::isfinite(eps) ||
-        (rows_type != GLLM_ROWS_F32 && rows_type != GLLM_ROWS_BF16))
+    if (num_rows < 0 || n_q_heads < 1 || n_kv_heads < 1 || max_position < 1 || num_blocks < 1 || !(eps >= 0.0) || !std::isfinite((float)eps) ||
+        (eps > 0.0 && (float)eps == 0.f) || (rows_type != GLLM_ROWS_F32 && rows_type != GLLM_ROWS_BF16))
         return GLLM_E_INVALID;
     if ((head_dim != 64 && head_dim != 128) || (int64_t)n_q_heads + 2 * (int64_t)n_kv_heads > 65535 || num_blocks > GLLM_CACHE8_MAX_BLOCKS)
         return GLLM_E_UNSUPPORTED;

@@ -55,6 +55,13 @@ def test_norm_rope_store_refuses(change, status):
     assert C8._lib().gllm_op_norm_rope_store8(*{**STORE, **change}.values()) == status
 
 
+@pytest.mark.parametrize("eps", [1e-60, 2.0 ** -150, 3.5e38, 1e300])
+def test_norm_rope_store_refuses_an_eps_that_float_does_not_hold(eps):
+    """Rounded to 0 it would make heads of zeros no numbers, rounded to infinity every head zeros."""
+    assert C8._lib().gllm_op_norm_rope_store8(*{**STORE, "eps": eps}.values()) == INVALID
+    assert C8._lib().gllm_op_norm_rope_store8(*{**STORE, "eps": eps, "rows": 0}.values()) == INVALID
+
+
 ATTENTION = dict(q=P, ld_q=512, k=P, v=P, scales=P, num_blocks=9, tables=P, stride=4, cached=P, starts=P, seqs=2, rows=5, max_new=8, window=0, sinks=0,
                  n_q=4, n_kv=2, d=128, scale=0.1, out=P, ld_o=512, ws=P, ws_bytes=1 << 40, stream=None)
 
