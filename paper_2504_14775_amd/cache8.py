@@ -73,6 +73,8 @@ def gllm_op_step_maps(new_tokens, cached_len, free_pages, block_tables, num_bloc
         _refuse(f"{call}: shapes new_tokens {tuple(new_tokens.shape)}, cached_len {tuple(cached_len.shape)}, "
                 f"free_pages {tuple(free_pages.shape)}, block_tables {tuple(block_tables.shape)}, "
                 f"row_start {tuple(row_start.shape)}, positions {tuple(positions.shape)}, slots {tuple(slots.shape)}, needed {tuple(needed.shape)}")
+    if (seqs | rows | free_pages.numel() | block_tables.shape[1]) >> 31:
+        _refuse(f"{call}: {seqs} sequences, {rows} rows, {free_pages.numel()} pages or tables of {block_tables.shape[1]} entries")
     st = _lib().gllm_op_step_maps(new_tokens.data_ptr(), cached_len.data_ptr(), seqs, free_pages.data_ptr(), free_pages.numel(), block_tables.data_ptr(),
                                   block_tables.shape[1], num_blocks, rows, row_start.data_ptr(), positions.data_ptr(), slots.data_ptr(),
                                   needed.data_ptr(), _stream(stream, dev))
@@ -136,8 +138,8 @@ def gllm_op_attention8(q, k_pool, v_pool, scales, block_tables, cached_len, row_
     if q.dim() != 2 or q.shape[1] % d != 0 or out.shape != q.shape or block_tables.dim() != 2 or block_tables.shape[0] != seqs or row_start.numel() != seqs + 1:
         _refuse(f"{call}: shapes q {tuple(q.shape)}, out {tuple(out.shape)}, block_tables {tuple(block_tables.shape)}, cached_len {tuple(cached_len.shape)}, "
                 f"row_start {tuple(row_start.shape)}")
-    if (max_new | window | sinks) >> 31:
-        _refuse(f"{call}: max_new {max_new}, window {window}, sinks {sinks}")
+    if (max_new | window | sinks | seqs | block_tables.shape[1]) >> 31:
+        _refuse(f"{call}: max_new {max_new}, window {window}, sinks {sinks}, {seqs} sequences, tables of {block_tables.shape[1]} entries")
     n_q = q.shape[1] // d
     lib = _lib()
     if workspace is None:

@@ -958,6 +958,27 @@ def test_binding_refuses_lengths_that_do_not_fit_32_bits():
     assert bool((b.out == 7.0).all())
 
 
+def test_binding_refuses_arrays_that_do_not_fit_32_bits():
+    """Arrays of 2^32 and a few entries (not looked at), whose lengths have as many as a few in their lower half."""
+    print("arrays beyond 32 bits", flush=True)
+    far = torch.empty((1 << 32) + 48, dtype=torch.int32, device=DEV)
+    few = far[:(1 << 32) + 2]
+    one, two = dev_ints([1]), dev_ints([7, 7])
+    out = [torch.full((n,), -99, dtype=torch.int32, device=DEV) for n in (2, 5, 5, 2)]
+    tables = torch.full((1, 4), -5, dtype=torch.int32, device=DEV)
+    with pytest.raises(B.GllmError):
+        C8.gllm_op_step_maps(one, one, few, tables, 9, *out)
+    with pytest.raises(B.GllmError):
+        C8.gllm_op_step_maps(one, one, two, far.view(1, -1), 9, *out)
+    with pytest.raises(B.GllmError):
+        C8.gllm_op_step_maps(one, one, two, tables, 9, out[0], few, few, out[3])
+    b = Batch((8, 2, 64), [2], [25], seed=35)
+    with pytest.raises(B.GllmError):
+        C8.gllm_op_attention8(b.q, b.k, b.v, b.scales, far.view(1, -1), *b.dev[1:], b.out, 2)
+    torch.cuda.synchronize()
+    assert all(bool((t == -99).all()) for t in out) and bool((b.out == 7.0).all())
+
+
 def test_pools_beyond_4_gib():
     """The same pages at the far end of a large pool: the same bits."""
     print("a pool beyond 4 GiB", flush=True)
