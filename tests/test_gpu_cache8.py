@@ -660,6 +660,21 @@ def test_shared_prefix_of_more_pages_than_a_tile_holds_ids_of(seqs, n):
         b.check(window, sinks, label=f"{seqs} sequences over one prefix, window {window}")
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (8500, 100)])
+def test_tiles_of_128_dims_over_more_pages_than_they_hold_ids_of(window, sinks):
+    """One prefix for all sequences, whose tiles are too many to be cut: units of 142 blocks and, with a window, of 137."""
+    print(f"attention8 one prefix, 128 dims, window {window}", flush=True)
+    seqs, n, prefix = 34, 40, 562 * PAGE
+    b = Batch((8, 8, 128), [n] * seqs, [prefix] + [0] * (seqs - 1), seed=34)
+    for s in range(1, seqs):
+        b.tables[s, 562:565] = b.tables[s, :3]
+        b.tables[s, :562] = b.tables[0, :562]
+    b.cached = [prefix] * seqs
+    b.dev[0], b.dev[1] = dev_ints(b.tables), dev_ints(b.cached)
+    b.run(window, sinks)
+    b.check(window, sinks, label=f"one prefix, 128 dims, window {window}")
+
+
 @pytest.mark.parametrize("new,cached", [([1], [400]), ([1, 40], [400, 10]), ([2, 30], [385, 3]), ([1, 1, 20], [383, 384, 500]), ([1, 1], [100, 449])], ids=str)
 def test_streams_about_as_long_as_are_cut(new, cached):
     print(f"attention8 streams {new} {cached}", flush=True)
