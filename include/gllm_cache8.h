@@ -83,7 +83,8 @@ gllm_status gllm_op_norm_rope_store8(const void* qkv, int64_t ld_qkv, int32_t ro
  * where window is 0.
  *   q             DEVICE bf16 [num_rows][ld_q], rotated queries, head h in columns h*head_dim .. (ld_q a multiple of 8, 16-byte aligned)
  *   block_tables  DEVICE int32 [num_seqs][block_table_stride]; a page id outside [0, num_blocks) is read as the nearest one inside.  Entries
- *                 of pages that no row of the sequence sees any position of are not followed: their pages may have been given back
+ *                 of blocks of four pages that no row of the sequence sees any position of are not followed; of other pages that no row sees
+ *                 any position of, memory may be read, but what it holds reaches no result.  Both may have been given back
  *   cached_len    DEVICE int32 [num_seqs]: positions in front of the call's rows.  The keys and values of the rows themselves are in the
  *                 pool already
  *   row_start     DEVICE int32 [num_seqs + 1], ascending, from 0 up to at most num_rows (otherwise no row is written)

@@ -19,7 +19,7 @@
 //
 // Measured (8 KV heads of 128): 32 decode rows behind 300 .. 20000 keys, 308 MB, 58 us with the joining, 53 + 5, 5.8 TB/s inside the kernel (a copy
 // reaches 5.2); 64 behind a window of 1024, 33 us; 251 decode rows and 1802 chunk rows together, 938 MB and 63 GFLOP, 201 us; a chunk of 4096 behind
-// 4096 keys, 64 heads, 825 GFLOP that count, 795 us, 1.04 PFLOP/s (a large product reaches 1.42).
+// 4096 keys, 64 heads, 825 GFLOP that count, 796 us, 1.04 PFLOP/s (a large product reaches 1.42).
 #include "cache8.h"
 
 #include <algorithm>
@@ -505,9 +505,9 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
     constexpr int SETS = COLS / 16;  // of 16 columns, which share the keys and values
     const int lane = threadIdx.x & 63;
     const int r = lane & 15, G = lane >> 4, g = a.n_q / a.n_kv;
-    // The run.  A stream of few blocks belongs to the wave in whose run its last one lies.  (No run behind one that is not empty is empty: there are
-    // at least as many blocks as waves, or, with kFewBlocks of 2, no more than seven blocks to eight waves, of which the first has none.  A longer
-    // stream's parts are therefore those of all waves from its first to its last.)
+    // The run.  A stream of few blocks, up to kWhole, belongs to the wave in whose run its last one lies.  The parts of a longer one are those of all waves
+    // from its first to its last: with more than kWhole blocks in a call no run behind one that is not empty is empty.  (With kFewBlocks of 2 there are
+    // at least as many blocks as waves, or seven blocks to eight waves, of which the first has none.)
     const int64_t lo = run_begin(job.stream, waves, w), hi = run_begin(job.stream, waves, w + 1);
 
     // 64 sequences, one per lane, of which those up to lane `at` have been dealt with; `upto` blocks up to the end of this lane's, counted from all.
@@ -814,7 +814,7 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 // The exponentials of a half run beside the scores of the next one and in front of its own outputs; what a phase reads from LDS is asked for in the
 // phase before.
 //
-// What bounds it, a chunk of 4096 behind 4096 keys: 795 us, 1.04 PFLOP/s.  Per block of 64 keys (2.0 us) the matrix cores are busy for 0.9 us, the
+// What bounds it, a chunk of 4096 behind 4096 keys: 796 us, 1.04 PFLOP/s.  Per block of 64 keys (2.0 us) the matrix cores are busy for 0.9 us, the
 // vector units for about 1.1 (32 exponentials and some 170 others a wave), LDS, which each wave reads all keys and values from, for 1.1; a wave's
 // chain goes through all three, and there are two waves on a SIMD to hide each other's waits, all that the registers allow.  What each costs, with
 // data that does not change, so that the clock stays up (which is worth 5 to 8 % itself): staging and barriers 8 %, exponentials 8 %, reads of LDS
@@ -823,8 +823,8 @@ __device__ __forceinline__ void stream_wave(const Attn8Args& a, const Job& job, 
 // has grown (a fifth fewer vector instructions), instructions held in the order of the source (3 % slower).
 
 // Blocks that LDS holds: with four a barrier after every second round is enough.  us with two / four: 64 dims, 14 heads on 2, a chunk of 4096 behind
-// 4096 227 / 206, 8 heads on 8, four chunks of 1024 60 / 57; 128 dims, a chunk of 4096 behind 4096 (64 heads on 8) 800 / 805, of 8191 in a window 311
-// / 316.
+// 4096 228 / 212, 8 heads on 8, four chunks of 1024 behind up to 4096 87 / 84; 128 dims, a chunk of 4096 behind 4096 (64 heads on 8) 829 / 827, of 8191
+// in a window 317 / 320 (these four on one card, on which the chunk of 4096 takes 4 % more than stands above).
 template <int D>
 constexpr int kStages = D == 64 ? 4 : 2;
 constexpr int kHalf = 32, kWindow = 64;
